@@ -15,6 +15,10 @@
  *   adt_tree_accept   greedy / speculative-sampling walk: accepted path,
  *                     its length and the bonus token.
  *   adt_kv_compact    copy the accepted nodes' K/V into the cache.
+ *   adt_rope_qkv      rotate the projections' rows to their positions, as they
+ *                     enter attention and cache.
+ *   adt_kv_score      add up the attention weight that each cached row got.
+ *   adt_kv_evict      cut the cache down to the rows with the most of it.
  *   adt_ctrl_*        host-side depth / width controller (Sec. 4.1, 4.2).
  *
  * Conventions shared by every entry point
@@ -411,6 +415,144 @@ adt_status adt_kv_compact_inplace(adt_bf16* k_cache, adt_bf16* v_cache, const in
                                   int32_t B, int32_t Hkv, int32_t D, int32_t num_layers,
                                   int32_t max_kv, int64_t cache_layer_stride,
                                   int64_t cache_stride_b, int64_t cache_stride_h, void* stream);
+
+/* ------------------------------------------------------------------------
+ * adt_rope_qkv - rotary positions of the rows that a Q/K/V projection made,
+ * written as adt_tree_attn takes them (bf16 q, k_tree, v_tree).
+ *
+ * The paper's models take their positions this way and it prints no formula;
+ * this is the usual rotation.  Head row x of node n at position t =
+ * positions[n]: for each pair p < rotary_dim/2, with angle t * inv_freq[p]
+ * (formed in 64 bits) and c, s = magnitude * cos, magnitude * sin of it,
+ *     (a, b) <- (a c - b s, b c + a s)        in fp32, rounded once to bf16
+ *   ADT_ROPE_HALF:        a = x[p],   b = x[p + rotary_dim/2]
+ *   ADT_ROPE_INTERLEAVED: a = x[2 p], b = x[2 p + 1]
+ * and elements rotary_dim .. D-1 are copied.  q and k are rotated, v is copied
+ * (rounded to bf16).
+ *
+ * q, k, v [device] rows of in_type (bf16 or fp32): head h, element d of node n
+ *         at n*ld + h*D + d; one packed projection is three pointers into the
+ *         same rows.  ld >= heads*D (in elements, any).  Any of the three may
+ *         be NULL together with its output.
+ * positions [device] int32 [N], any value (a negative one turns back).
+ * inv_freq  [device] fp64 [rotary_dim/2], radians a position (adt_rope_freqs
+ *         makes the usual ones); may be NULL when rotary_dim is 0.
+ * N >= 0 (of 0 rows no pointer is read and nothing launched); 1 <= D <= 4096; 0 <= rotary_dim <= D, even, at
+ *         most 1024; magnitude finite.
+ * q_out [device] bf16 [N][H][D]; k_out, v_out bf16 [N][Hkv][D].  An output may
+ *         be its own input (bf16, ld = heads*D); otherwise outputs overlap
+ *         neither inputs nor each other (ADT_ERR_INVALID_ARG).
+ * Pointers need their type's alignment only; rows and heads that are multiples
+ * of 16 bytes on 16-byte boundaries, with rotary_dim a multiple of 16, are
+ * moved as vectors.
+ * ------------------------------------------------------------------------ */
+typedef enum adt_dtype { ADT_TYPE_BF16 = 0, ADT_TYPE_F32 = 1 } adt_dtype;
+typedef enum adt_rope_layout { ADT_ROPE_HALF = 0, ADT_ROPE_INTERLEAVED = 1 } adt_rope_layout;
+enum { ADT_ROPE_NONE = 0, ADT_ROPE_LINEAR = 1, ADT_ROPE_NTK = 2, ADT_ROPE_BY_PARTS = 3 };
+
+typedef struct adt_rope_params {
+  double theta;       /* base, >= 1 */
+  double factor;      /* context extension s >= 1 (not read without scaling) */
+  double orig_len;    /* BY_PARTS: positions the model was trained on */
+  double turns_lo;    /* BY_PARTS: pairs that turn at most so often in them are divided by s, */
+  double turns_hi;    /*           those that turn at least so often are kept */
+  int32_t rotary_dim; /* even, 2 .. 1024 */
+  int32_t scaling;    /* ADT_ROPE_NONE .. ADT_ROPE_BY_PARTS */
+} adt_rope_params;
+
+/* Host only: inv_freq[p] = theta^(-2p/rotary_dim) for p < rotary_dim/2, scaled
+ * for contexts `factor` times the trained one:
+ *   LINEAR    inv_freq / s (positions interpolated);
+ *   NTK       theta * s^(rotary_dim/(rotary_dim-2)) for theta (rotary_dim > 2);
+ *   BY_PARTS  inv_freq * (r + (1 - r)/s), r the pair's turns in orig_len
+ *             positions mapped from [turns_lo, turns_hi] to [0, 1], clamped
+ *             (the usual bounds are 1 and 32); magnitude 0.1 ln s + 1.
+ * *magnitude is 1 otherwise.  The caller copies inv_freq to the device. */
+adt_status adt_rope_freqs(const adt_rope_params* params, double* inv_freq, float* magnitude);
+
+adt_status adt_rope_qkv(const void* q, int64_t ld_q, const void* k, int64_t ld_k, const void* v, int64_t ld_v,
+                        adt_dtype in_type, const int32_t* positions, const double* inv_freq, float magnitude,
+                        adt_rope_layout layout, int32_t N, int32_t H, int32_t Hkv, int32_t D, int32_t rotary_dim,
+                        adt_bf16* q_out, adt_bf16* k_out, adt_bf16* v_out, void* stream);
+
+/* ------------------------------------------------------------------------
+ * adt_kv_score - the attention weight that every cached row got from the
+ * tokens just committed, added to a running score, all layers in one launch
+ * (no counterpart in the paper; what adt_kv_evict goes by).
+ *
+ * Called after the commit: tree b's accepted path nodes i = 0 .. a, a =
+ * accept_len[b], sit in cache rows kv_len[b] + i, with kv_len the length
+ * before the commit, and path node i sees rows 0 .. kv_len[b] + i.  For every
+ * layer l, tree b, kv head g and row j <= kv_len[b] + a:
+ *   score_out[l][b][g][j] = (j < kv_len[b] ? decay * score_in[l][b][g][j] : 0)
+ *     + sum over i with kv_len[b] + i >= j, heads h of group g of
+ *       exp(softmax_scale * q[l][n_i][h] . k_cache[l][b][g][j] - lse[l][n_i][h])
+ * with n_i = node_offsets[b] + path[b][i].  Sums in fp32 in a fixed order:
+ * equal calls give equal bits.  Rows behind kv_len[b] + a are left as they
+ * were.  A committed single token is a path of one node; a prompt a chain.
+ *
+ * q       [device] bf16, element (l, n, h, d) at l*q_layer_stride + (n*H + h)*D + d,
+ *         as given to adt_tree_attn.
+ * lse     [device] fp32, element (l, n, h) at l*lse_layer_stride + n*H + h, as
+ *         adt_tree_attn returned it; a query with lse = -inf adds nothing.
+ * k_cache [device] bf16, strides as for adt_kv_compact; kv_len [device] int32 [B].
+ * node_offsets [device] int32 [B+1]; path [device] int32 [B][max_path];
+ *         accept_len [device] int32 [B].
+ * score_in, score_out [device] fp32, element (l, b, g, j) at l*score_layer_stride
+ *         + b*score_stride_b + g*score_stride_h + j (any strides that keep
+ *         slices of max_kv apart).  They may be the same; otherwise they do not
+ *         overlap.  With decay = 0 score_in is not read.
+ * D in {64, 128}; 1 <= max_path <= 2^20; 1 <= max_kv < 2^30; 0 <= decay <= 1;
+ * num_layers * B * Hkv <= 2^22.
+ * accept_len[b] outside [0, max_path) or kv_len[b] + accept_len[b] + 1 > max_kv
+ * sets ADT_DEVERR_KV_RANGE and skips tree b; a path entry outside the tree
+ * sets ADT_DEVERR_BAD_PATH and adds nothing.
+ * ------------------------------------------------------------------------ */
+adt_status adt_kv_score(const adt_bf16* q, const float* lse, const adt_bf16* k_cache, const int32_t* kv_len,
+                        const int32_t* node_offsets, const int32_t* path, int32_t max_path, const int32_t* accept_len,
+                        int32_t B, int32_t H, int32_t Hkv, int32_t D, int32_t num_layers, int32_t max_kv,
+                        int64_t q_layer_stride, int64_t lse_layer_stride, int64_t cache_layer_stride,
+                        int64_t cache_stride_b, int64_t cache_stride_h, float softmax_scale, float decay,
+                        const float* score_in, float* score_out, int64_t score_layer_stride, int64_t score_stride_b,
+                        int64_t score_stride_h, void* stream);
+
+/* ------------------------------------------------------------------------
+ * adt_kv_evict - cuts the cache down to a budget, all layers in one launch (no
+ * counterpart in the paper: it bounds the cache that a long sequence fills).
+ *
+ * For every layer l, tree b and kv head g, n = min(kv_len[b], budget) of the
+ * rows 0 .. kv_len[b]-1 are kept: all of them where kv_len[b] <= budget,
+ * otherwise the first n_sink, the last n_recent, and of the rows between the
+ * budget - n_sink - n_recent with the highest score (ties to the lowest row; a
+ * NaN ranks above every number, and -0 equals +0).  In ascending order they become rows
+ * 0 .. n-1 of the destination: K, V and, unless score_out is NULL, the scores.
+ * Each head keeps rows of its own; keys carry their rotated positions with
+ * them, so positions of later tokens must not be taken from the cache's length
+ * any more.  Destination rows n and up are left as they were.
+ *
+ * k_src, v_src [device] bf16 and k_dst, v_dst: strides as for adt_kv_compact.
+ *         In place (the same pointers and strides for both caches), or into
+ *         caches that overlap neither source.  A destination slice holds
+ *         min(max_kv, budget) rows.
+ * score   [device] fp32, as adt_kv_score writes it; score_out: a buffer with
+ *         strides of its own, the same buffer (with the same strides), or NULL.
+ * kv_len  [device] int32 [B], <= max_kv; kv_len_out [device] int32 [B] or NULL
+ *         receives n (not the same buffer as kv_len).
+ * keep_idx [device] int32 [num_layers][B][Hkv][budget] or NULL: the kept rows,
+ *         padded with -1.
+ * D in {64, 128}; budget >= 1; n_sink, n_recent >= 0, n_sink + n_recent <=
+ * budget; max_kv <= 2^20 (ADT_ERR_UNSUPPORTED above).
+ * kv_len[b] outside [0, max_kv] sets ADT_DEVERR_KV_RANGE and skips tree b
+ * (kv_len_out[b] = kv_len[b]; its keep_idx is not written).
+ * ------------------------------------------------------------------------ */
+adt_status adt_kv_evict(const adt_bf16* k_src, const adt_bf16* v_src, int64_t src_layer_stride, int64_t src_stride_b,
+                        int64_t src_stride_h, const float* score, int64_t score_layer_stride, int64_t score_stride_b,
+                        int64_t score_stride_h, const int32_t* kv_len, int32_t* kv_len_out, adt_bf16* k_dst,
+                        adt_bf16* v_dst, int64_t dst_layer_stride, int64_t dst_stride_b, int64_t dst_stride_h,
+                        float* score_out, int64_t score_out_layer_stride, int64_t score_out_stride_b,
+                        int64_t score_out_stride_h, int32_t* keep_idx, int32_t B, int32_t Hkv, int32_t D,
+                        int32_t num_layers, int32_t max_kv, int32_t budget, int32_t n_sink, int32_t n_recent,
+                        void* stream);
 
 /* ------------------------------------------------------------------------
  * Depth / width controller (host only, no GPU).  Sec. 4.1 adjacent

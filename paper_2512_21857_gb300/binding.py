@@ -21,6 +21,8 @@ STATUS_NAMES = {0: "ADT_OK", 1: "ADT_ERR_INVALID_ARG", 2: "ADT_ERR_UNSUPPORTED",
                 4: "ADT_ERR_TIMEOUT", 5: "ADT_ERR_WORKSPACE", 6: "ADT_ERR_DEVICE"}
 ACCEPT_GREEDY, ACCEPT_SPEC, ACCEPT_SPEC_DET = 0, 1, 2
 INIT_HORIZONTAL, INIT_VERTICAL, INIT_RANDOM, INIT_TOKENFLOCK = 0, 1, 2, 3
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_NONE, ROPE_LINEAR, ROPE_NTK, ROPE_BY_PARTS = 0, 1, 2, 3
 DEVERR_BAD_TREE, DEVERR_KV_RANGE, DEVERR_BAD_PATH, DEVERR_TIMEOUT, DEVERR_BAD_INDEX = 1, 2, 4, 8, 16
 
 EXPORTED = [
@@ -31,6 +33,7 @@ EXPORTED = [
     "adt_tree_rerank_workspace_size", "adt_tree_rerank",
     "adt_tree_accept_workspace_size", "adt_tree_accept", "adt_tree_accept_cfg",
     "adt_kv_compact", "adt_kv_compact_inplace",
+    "adt_rope_freqs", "adt_rope_qkv", "adt_kv_score", "adt_kv_evict",
     "adt_ctrl_create", "adt_ctrl_destroy", "adt_ctrl_next", "adt_ctrl_update", "adt_ctrl_get",
     "adt_ctrl_state_size", "adt_ctrl_save", "adt_ctrl_load",
 ]
@@ -49,6 +52,12 @@ class CtrlParams(ctypes.Structure):
                 ("k0", ctypes.c_int32), ("clamp_k_always", ctypes.c_int32), ("k_cap", ctypes.c_int32),
                 ("fix_d", ctypes.c_int32), ("fix_k", ctypes.c_int32), ("seed", ctypes.c_uint64),
                 ("flock_delta", ctypes.c_int32)]
+
+
+class RopeParams(ctypes.Structure):
+    _fields_ = [("theta", ctypes.c_double), ("factor", ctypes.c_double), ("orig_len", ctypes.c_double),
+                ("turns_lo", ctypes.c_double), ("turns_hi", ctypes.c_double), ("rotary_dim", ctypes.c_int32),
+                ("scaling", ctypes.c_int32)]
 
 
 _P, _I32, _I64, _F32, _SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
@@ -81,6 +90,13 @@ _SIGS = {
                         _I64, _I64, _P], _I32),
     "adt_kv_compact_inplace": ([_P, _P, _P, _P, _P, _P, _I32, _P, _I32, _I32, _I32, _I32, _I32, _I64, _I64, _I64,
                                 _P], _I32),
+    "adt_rope_freqs": ([ctypes.POINTER(RopeParams), _P, ctypes.POINTER(_F32)], _I32),
+    "adt_rope_qkv": ([_P, _I64, _P, _I64, _P, _I64, _I32, _P, _P, _F32, _I32, _I32, _I32, _I32, _I32, _I32, _P, _P, _P,
+                      _P], _I32),
+    "adt_kv_score": ([_P, _P, _P, _P, _P, _P, _I32, _P, _I32, _I32, _I32, _I32, _I32, _I32, _I64, _I64, _I64, _I64,
+                      _I64, _F32, _F32, _P, _P, _I64, _I64, _I64, _P], _I32),
+    "adt_kv_evict": ([_P, _P, _I64, _I64, _I64, _P, _I64, _I64, _I64, _P, _P, _P, _P, _I64, _I64, _I64, _P, _I64, _I64,
+                      _I64, _P, _I32, _I32, _I32, _I32, _I32, _I32, _I32, _I32, _P], _I32),
     "adt_ctrl_create": ([ctypes.POINTER(CtrlParams), _I32, _I32, ctypes.POINTER(_P)], _I32),
     "adt_ctrl_destroy": ([_P], None),
     "adt_ctrl_state_size": ([_P], _SZ),
@@ -324,6 +340,152 @@ def adt_kv_compact_inplace(k_cache, v_cache, kv_len, kv_len_out, node_offsets, p
                                       num_layers, max_kv, cache_layer_stride, cache_stride_b, cache_stride_h,
                                       _stream(stream))
     _check(st, "adt_kv_compact_inplace")
+
+
+# ----------------------------------------------------------------------------- positions and a bounded cache
+
+_TYPES = {torch.bfloat16: 0, torch.float32: 1}
+
+
+def _here(*tensors):
+    """Raises unless the tensors given (None: absent) are on the current CUDA device, which the launch goes to."""
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.get_device() != torch.cuda.current_device()):
+            raise ValueError(f"expected a tensor on the current CUDA device, got one on {t.device}")
+
+
+def adt_rope_freqs(rotary_dim, *, theta=10000.0, scaling=ROPE_NONE, factor=1.0, orig_len=0.0, turns_lo=1.0,
+                   turns_hi=32.0):
+    """(inv_freq, magnitude): fp64 [rotary_dim / 2] on the CPU, radians a position, to be copied to the device once."""
+    p = RopeParams(theta, factor, orig_len, turns_lo, turns_hi, rotary_dim, scaling)
+    inv = torch.empty(max(rotary_dim // 2, 1), dtype=torch.float64)
+    mag = _F32()
+    _check(lib().adt_rope_freqs(ctypes.byref(p), inv.data_ptr(), ctypes.byref(mag)), "adt_rope_freqs")
+    return inv, mag.value
+
+
+def _rope_rows(t, heads, D, N, name):
+    """Row stride of [N, heads * D] rows or [N, heads, D] heads (contiguous within a row)."""
+    if t.dim() == 3 and t.shape == (N, heads, D) and t.stride(2) == 1 and (t.stride(1) == D or heads == 1):
+        pass
+    elif not (t.dim() == 2 and t.shape == (N, heads * D) and t.stride(1) == 1):
+        raise ValueError(f"{name}: expected rows [{N}, {heads * D}] or [{N}, {heads}, {D}], contiguous within a row")
+    return t.stride(0) if N > 1 else heads * D
+
+
+def adt_rope_qkv(q, k, v, positions, inv_freq, *, H, Hkv, D, layout=ROPE_HALF, magnitude=1.0, q_out=None, k_out=None,
+                 v_out=None, stream=None) -> None:
+    """q [N, H * D], k and v [N, Hkv * D] rows (bf16 or fp32, any row stride; None: absent) to bf16 [N, heads, D]
+    outputs: q and k rotated by positions * inv_freq, v copied.  rotary_dim = 2 * len(inv_freq)."""
+    _here(q, k, v, positions, inv_freq, q_out, k_out, v_out)
+    _expect(positions, torch.int32, "positions")
+    _expect(inv_freq, torch.float64, "inv_freq")
+    N = positions.numel()
+    types, lds = set(), []
+    for name, t, o, heads in (("q", q, q_out, H), ("k", k, k_out, Hkv), ("v", v, v_out, Hkv)):
+        if (t is None) != (o is None):
+            raise ValueError(f"{name} and {name}_out: both or neither")
+        if t is None:
+            lds.append(0)
+            continue
+        lds.append(_rope_rows(t, heads, D, N, name))
+        types.add(t.dtype)
+        _expect(o, torch.bfloat16, name + "_out")
+        if o.numel() != N * heads * D:
+            raise ValueError(f"{name}_out: expected [{N}, {heads}, {D}]")
+    if len(types) != 1 or not types <= _TYPES.keys():
+        raise TypeError("q, k, v: bf16 or fp32, all the same")
+    st = lib().adt_rope_qkv(_ptr(q), lds[0], _ptr(k), lds[1], _ptr(v), lds[2], _TYPES[types.pop()], _ptr(positions),
+                            _ptr(inv_freq), float(magnitude), layout, N, H, Hkv, D, 2 * inv_freq.numel(), _ptr(q_out),
+                            _ptr(k_out), _ptr(v_out), _stream(stream))
+    _check(st, "adt_rope_qkv")
+
+
+def _strides3(t, shape, name, inner):
+    """Strides of the first three dimensions of [layers, B, Hkv, rows, ...]; the rows have `inner` elements, packed."""
+    if t.dim() != len(shape) or t.shape[:3] != shape[:3] or t.shape[3] < shape[3] or t.shape[4:] != shape[4:]:
+        raise ValueError(f"{name}: expected {list(shape)} or more rows, got {list(t.shape)}")
+    if (t.shape[3] > 1 and t.stride(3) != inner) or (inner > 1 and t.stride(4) != 1):
+        raise ValueError(f"{name}: expected packed rows")
+    return t.stride()[:3]
+
+
+def _rows3(t, shape, dtype, name):
+    """Stride of the first dimension of [layers, ...], the rest contiguous and at least `shape`."""
+    if t.dtype != dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    if t.dim() != len(shape) + 1 or t.shape[2:] != shape[1:]:
+        raise ValueError(f"{name}: expected [layers, nodes, {', '.join(map(str, shape[1:]))}]")
+    if not t[0].is_contiguous():
+        raise ValueError(f"{name}: expected each layer contiguous")
+    return t.stride(0)
+
+
+def adt_kv_score(q, lse, k_cache, kv_len, node_offsets, path, max_path, accept_len, score, *, score_out=None, B, H, Hkv,
+                 D, num_layers, max_kv, softmax_scale, decay=1.0, stream=None) -> None:
+    """q [layers, nodes, H, D] bf16, lse [layers, nodes, H], k_cache [layers, B, Hkv, rows >= max_kv, D] and score
+    [layers, B, Hkv, rows >= max_kv] fp32, updated in place unless score_out (the same strides) is given."""
+    score_out = score if score_out is None else score_out
+    _here(q, lse, k_cache, kv_len, node_offsets, path, accept_len, score, score_out)
+    for t, name in ((kv_len, "kv_len"), (node_offsets, "node_offsets"), (path, "path"), (accept_len, "accept_len")):
+        _expect(t, torch.int32, name)
+    if kv_len.numel() < B or accept_len.numel() < B or node_offsets.numel() < B + 1 or path.numel() < B * max_path:
+        raise ValueError("kv_len, accept_len [B], node_offsets [B + 1], path [B, max_path]")
+    if k_cache.dtype != torch.bfloat16 or score.dtype != torch.float32 or score_out.dtype != torch.float32:
+        raise TypeError("k_cache: bf16, score: fp32")
+    if score_out is not score and score_out.stride() != score.stride():
+        raise ValueError("score and score_out must share strides")
+    qs, ls = _rows3(q, (0, H, D), torch.bfloat16, "q"), _rows3(lse, (0, H), torch.float32, "lse")
+    if q.shape[0] < num_layers or lse.shape[0] < num_layers or lse.shape[1] != q.shape[1]:
+        raise ValueError("q and lse: [layers, nodes, ...]")
+    cs = _strides3(k_cache, (num_layers, B, Hkv, max_kv, D), "k_cache", D)
+    ss = _strides3(score, (num_layers, B, Hkv, max_kv), "score", 1)
+    _strides3(score_out, (num_layers, B, Hkv, max_kv), "score_out", 1)
+    st = lib().adt_kv_score(_ptr(q), _ptr(lse), _ptr(k_cache), _ptr(kv_len), _ptr(node_offsets), _ptr(path),
+                            int(max_path), _ptr(accept_len), B, H, Hkv, D, num_layers, max_kv, qs, ls, *cs,
+                            float(softmax_scale), float(decay), _ptr(score), _ptr(score_out), *ss, _stream(stream))
+    _check(st, "adt_kv_score")
+
+
+def adt_kv_evict(k_cache, v_cache, score, kv_len, kv_len_out=None, *, k_out=None, v_out=None, score_out=None,
+                 move_scores=True, keep_idx=None, B, Hkv, D, num_layers, max_kv, budget, n_sink=0, n_recent=0,
+                 stream=None) -> None:
+    """Caches [layers, B, Hkv, rows >= max_kv, D] bf16 and score [layers, B, Hkv, rows >= max_kv] fp32 cut down to
+    `budget` rows: in place, or into k_out, v_out.  The scores go to score_out, by default to where the rows went (in
+    place: the same buffer); with move_scores=False they stay as they are."""
+    if (k_out is None) != (v_out is None):
+        raise ValueError("k_out and v_out: both or neither")
+    in_place = k_out is None
+    k_out, v_out = (k_cache, v_cache) if in_place else (k_out, v_out)
+    if not move_scores:
+        if score_out is not None:
+            raise ValueError("score_out without moving scores")
+    elif score_out is None:
+        if not in_place:
+            raise ValueError("score_out: needed where the rows go to another cache")
+        score_out = score
+    _here(k_cache, v_cache, score, kv_len, kv_len_out, k_out, v_out, score_out, keep_idx)
+    for t, name in ((kv_len, "kv_len"), (kv_len_out, "kv_len_out"), (keep_idx, "keep_idx")):
+        if t is not None:
+            _expect(t, torch.int32, name)
+    if kv_len.numel() < B or (kv_len_out is not None and kv_len_out.numel() < B):
+        raise ValueError("kv_len, kv_len_out: [B]")
+    if keep_idx is not None and keep_idx.numel() < num_layers * B * Hkv * budget:
+        raise ValueError("keep_idx: [layers, B, Hkv, budget]")
+    if any(t.dtype != torch.bfloat16 for t in (k_cache, v_cache, k_out, v_out)):
+        raise TypeError("caches: bf16")
+    if score.dtype != torch.float32 or (score_out is not None and score_out.dtype != torch.float32):
+        raise TypeError("score: fp32")
+    shape, kept = (num_layers, B, Hkv, max_kv, D), (num_layers, B, Hkv, min(max_kv, budget), D)
+    ks, ko = _strides3(k_cache, shape, "k_cache", D), _strides3(k_out, kept, "k_out", D)
+    if _strides3(v_cache, shape, "v_cache", D) != ks or _strides3(v_out, kept, "v_out", D) != ko:
+        raise ValueError("K and V must share strides")
+    cs = _strides3(score, shape[:4], "score", 1)
+    co = (0, 0, 0) if score_out is None else _strides3(score_out, kept[:4], "score_out", 1)
+    st = lib().adt_kv_evict(_ptr(k_cache), _ptr(v_cache), *ks, _ptr(score), *cs, _ptr(kv_len), _ptr(kv_len_out),
+                            _ptr(k_out), _ptr(v_out), *ko, _ptr(score_out), *co, _ptr(keep_idx), B, Hkv, D, num_layers,
+                            max_kv, budget, n_sink, n_recent, _stream(stream))
+    _check(st, "adt_kv_evict")
 
 
 # ----------------------------------------------------------------------------- controller

@@ -1,0 +1,183 @@
+// adt_rope_freqs, adt_rope_qkv: rotary positions.
+//
+// Pair p of a head at position t turns by t * inv_freq[p] radians:
+//   (a, b) -> (a c - b s, b c + a s),  c = m cos(t f), s = m sin(t f).
+// The angle is formed in 64 bits as a number of turns, t * f / (2 pi), and only
+// its fraction goes on to fp32: at t = 10^6 the angle of a pair with f = 1 has
+// 20 bits before the point, so that in fp32 the cosine would be off by 0.03.
+//
+// A CTA takes one token (and, where there are few tokens, a share of its
+// heads): one thread a pair makes the cosines and sines once, in shared memory,
+// and every head of the token uses them.
+#include <math.h>
+
+#include "adt_common.cuh"
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kMaxRotary = 1024;  // cosines and sines of a token: 4 KB of shared memory
+constexpr double kTwoPi = 6.283185307179586476925286766559;
+
+struct RopeParams {
+  const void* in[3];        // rows of q, k, v
+  int64_t ld[3];            // row strides in elements
+  __nv_bfloat16* out[3];    // [N][heads][D]
+  int heads[3];
+  const int32_t* pos;
+  const double* inv_freq;
+  float magnitude;
+  int D, rot, interleaved;
+};
+
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
+
+// Cosines and sines of the CTA's token, m included.
+__device__ __forceinline__ void token_angles(const RopeParams& p, int n, float2* cs) {
+  const double t = static_cast<double>(p.pos[n]) * (1.0 / kTwoPi);
+  for (int i = threadIdx.x; i < p.rot / 2; i += kThreads) {
+    double turns = t * p.inv_freq[i];
+    turns -= rint(turns);
+    float s, c;
+    sincospif(2.f * static_cast<float>(turns), &s, &c);
+    cs[i] = make_float2(c * p.magnitude, s * p.magnitude);
+  }
+  __syncthreads();
+}
+
+// One pair or one copied element at a time: any even rotary_dim, any head
+// size, row stride and alignment.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) rope_scalar_kernel(const RopeParams p) {
+  __shared__ float2 cs[kMaxRotary / 2];
+  adt::pdl_wait_then_release();
+  const int n = blockIdx.x;
+  token_angles(p, n, cs);
+  const int half = p.rot / 2, units = p.D - half;
+  for (int x = 0; x < 3; ++x) {
+    const T* in = static_cast<const T*>(p.in[x]) + n * p.ld[x];
+    __nv_bfloat16* out = p.out[x] + static_cast<int64_t>(n) * p.heads[x] * p.D;
+    const int count = p.heads[x] * (x < 2 ? units : p.D);
+    for (int i = blockIdx.y * kThreads + threadIdx.x; i < count; i += gridDim.y * kThreads) {
+      if (x == 2) {
+        out[i] = __float2bfloat16(to_f32(in[i]));
+        continue;
+      }
+      const int h = i / units, u = i - h * units;
+      const T* row = in + h * p.D;
+      __nv_bfloat16* dst = out + h * p.D;
+      if (u >= half) {
+        dst[u + half] = __float2bfloat16(to_f32(row[u + half]));
+        continue;
+      }
+      const int ia = p.interleaved ? 2 * u : u, ib = p.interleaved ? 2 * u + 1 : u + half;
+      const float a = to_f32(row[ia]), b = to_f32(row[ib]), c = cs[u].x, s = cs[u].y;
+      dst[ia] = __float2bfloat16(a * c - b * s);
+      dst[ib] = __float2bfloat16(b * c + a * s);
+    }
+  }
+}
+
+bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + nb && y < x + na;
+}
+
+}  // namespace
+
+extern "C" {
+
+adt_status adt_rope_freqs(const adt_rope_params* params, double* inv_freq, float* magnitude) {
+  ADT_REQUIRE(params && inv_freq && magnitude);
+  const adt_rope_params& r = *params;
+  ADT_REQUIRE(r.rotary_dim >= 2 && r.rotary_dim % 2 == 0 && r.rotary_dim <= kMaxRotary);
+  ADT_REQUIRE(isfinite(r.theta) && r.theta >= 1.0);
+  ADT_REQUIRE(r.scaling >= ADT_ROPE_NONE && r.scaling <= ADT_ROPE_BY_PARTS);
+  const bool scaled = r.scaling != ADT_ROPE_NONE;
+  ADT_REQUIRE(!scaled || (isfinite(r.factor) && r.factor >= 1.0));
+  ADT_REQUIRE(r.scaling != ADT_ROPE_NTK || r.rotary_dim > 2);
+  ADT_REQUIRE(r.scaling != ADT_ROPE_BY_PARTS ||
+              (r.orig_len >= 1 && r.turns_lo >= 0.0 && r.turns_hi > r.turns_lo && isfinite(r.turns_hi)));
+  const int R = r.rotary_dim;
+  const double theta = r.scaling == ADT_ROPE_NTK ? r.theta * pow(r.factor, static_cast<double>(R) / (R - 2)) : r.theta;
+  for (int i = 0; i < R / 2; ++i) {
+    double f = pow(theta, -2.0 * i / R);
+    if (r.scaling == ADT_ROPE_LINEAR) f /= r.factor;
+    if (r.scaling == ADT_ROPE_BY_PARTS) {
+      const double turns = r.orig_len * f / kTwoPi;
+      const double keep = fmin(1.0, fmax(0.0, (turns - r.turns_lo) / (r.turns_hi - r.turns_lo)));
+      f *= keep + (1.0 - keep) / r.factor;
+    }
+    inv_freq[i] = f;
+  }
+  *magnitude = r.scaling == ADT_ROPE_BY_PARTS ? static_cast<float>(0.1 * log(r.factor) + 1.0) : 1.f;
+  return ADT_OK;
+}
+
+adt_status adt_rope_qkv(const void* q, int64_t ld_q, const void* k, int64_t ld_k, const void* v, int64_t ld_v,
+                        adt_dtype in_type, const int32_t* positions, const double* inv_freq, float magnitude,
+                        adt_rope_layout layout, int32_t N, int32_t H, int32_t Hkv, int32_t D, int32_t rotary_dim,
+                        adt_bf16* q_out, adt_bf16* k_out, adt_bf16* v_out, void* stream) {
+  adt::TraceRange trace_("adt_rope_qkv");
+  ADT_REQUIRE(in_type == ADT_TYPE_BF16 || in_type == ADT_TYPE_F32);
+  ADT_REQUIRE(layout == ADT_ROPE_HALF || layout == ADT_ROPE_INTERLEAVED);
+  ADT_REQUIRE(N >= 0 && D >= 1 && D <= 4096 && rotary_dim >= 0 && rotary_dim % 2 == 0 && rotary_dim <= D);
+  if (rotary_dim > kMaxRotary) return ADT_ERR_UNSUPPORTED;
+  ADT_REQUIRE(isfinite(magnitude));
+  if (N == 0) return ADT_OK;
+  ADT_REQUIRE((q != nullptr) == (q_out != nullptr) && (k != nullptr) == (k_out != nullptr) &&
+              (v != nullptr) == (v_out != nullptr));
+  ADT_REQUIRE(q || k || v);
+  ADT_REQUIRE((!q || (H >= 1 && H <= 65535)) && ((!k && !v) || (Hkv >= 1 && Hkv <= 65535)));
+  ADT_REQUIRE(positions && (inv_freq || rotary_dim == 0));
+  RopeParams p{};
+  const void* in[3] = {q, k, v};
+  adt_bf16* out[3] = {q_out, k_out, v_out};
+  const int64_t ld[3] = {ld_q, ld_k, ld_v};
+  const int esize = in_type == ADT_TYPE_BF16 ? 2 : 4;
+  int64_t in_bytes[3], out_bytes[3];
+  for (int x = 0; x < 3; ++x) {
+    p.heads[x] = !in[x] ? 0 : x == 0 ? H : Hkv;
+    const int64_t width = static_cast<int64_t>(p.heads[x]) * D;
+    ADT_REQUIRE(!in[x] || (ld[x] >= width && ld[x] <= (int64_t{1} << 40)));
+    ADT_REQUIRE(reinterpret_cast<uintptr_t>(in[x]) % esize == 0 && reinterpret_cast<uintptr_t>(out[x]) % 2 == 0);
+    in_bytes[x] = in[x] ? ((N - 1) * ld[x] + width) * esize : 0;
+    out_bytes[x] = in[x] ? N * width * 2 : 0;
+    p.in[x] = in[x];
+    p.ld[x] = ld[x];
+    p.out[x] = reinterpret_cast<__nv_bfloat16*>(out[x]);
+  }
+  // An output may be its own input (every thread reads what it overwrites
+  // first); nothing else may overlap.
+  for (int x = 0; x < 3; ++x) {
+    for (int y = 0; y < 3; ++y) {
+      if (overlap(out[x], out_bytes[x], in[y], in_bytes[y]))
+        ADT_REQUIRE(x == y && out[x] == in[x] && esize == 2 && ld[x] == static_cast<int64_t>(p.heads[x]) * D);
+      ADT_REQUIRE(x == y || !overlap(out[x], out_bytes[x], out[y], out_bytes[y]));
+    }
+  }
+  p.pos = positions;
+  p.inv_freq = inv_freq;
+  p.magnitude = magnitude;
+  p.D = D;
+  p.rot = rotary_dim;
+  p.interleaved = layout == ADT_ROPE_INTERLEAVED;
+  adt::DeviceInfo info;
+  adt_status st = adt::device_info(&info);
+  if (st != ADT_OK) return st;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(N), 1, 1);
+  cfg.blockDim = dim3(kThreads, 1, 1);
+  cfg.stream = adt::as_stream(stream);
+  cudaLaunchAttribute attr[1] = {adt::pdl_attribute()};
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  if (esize == 2)
+    ADT_CUDA_TRY(cudaLaunchKernelEx(&cfg, rope_scalar_kernel<__nv_bfloat16>, p));
+  else
+    ADT_CUDA_TRY(cudaLaunchKernelEx(&cfg, rope_scalar_kernel<float>, p));
+  return adt::launch_status();
+}
+
+}  // extern "C"
