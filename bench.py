@@ -55,7 +55,7 @@ WORKLOADS = {
 HOST_MARKER = b"// ---------------------------------------------------------------- host side"
 NCU_TRAFFIC = {
     # dram__bytes_read.sum + dram__bytes_write.sum = 41,496,064 + 0
-    "ef93466f747266b8": 41496064,
+    "ff8e57f5063e1bca": 41496064,
 }
 
 

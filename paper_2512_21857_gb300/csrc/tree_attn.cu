@@ -79,6 +79,18 @@ namespace cg = cooperative_groups;
 
 namespace {
 
+using sm100::add_f32x2;
+using sm100::cp_async16;
+using sm100::ex2_approx;
+using sm100::fma_f32x2;
+using sm100::pack_f32x2;
+using sm100::pack_u32x2;
+using sm100::sw128_off;
+using sm100::tmem_ld_32;
+using sm100::tmem_wait_ld_into;
+using sm100::unpack_f32x2;
+using sm100::wait_bar;
+
 constexpr int kUnit = 64;               // keys per split unit; the tree unit
 constexpr int kChunk = 128;             // keys per pipeline chunk
 constexpr int kMaxNodes = 64;           // query rows per CTA: one tile of a tree's nodes
@@ -161,16 +173,6 @@ struct TcParams {
   uint32_t wait_limit;  // polls before a pipeline wait gives up (kWaitLimit unless a test lowers it)
 };
 
-// Byte offset of 16-byte chunk `ch` (0 .. D/8-1) of row `row` in a tile of
-// 128-byte column blocks of `block_rows` rows with the 128-byte swizzle (the
-// layout TMA writes).
-__device__ __forceinline__ uint32_t sw128_off(int row, int ch, int block_rows) {
-  return static_cast<uint32_t>((ch >> 3) * block_rows * 128 + row * 128 + (((ch & 7) ^ (row & 7)) << 4));
-}
-
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int src_bytes) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src), "r"(src_bytes) : "memory");
-}
 __device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4;\n" ::"r"(dst), "l"(src) : "memory");
 }
@@ -182,13 +184,6 @@ __device__ __forceinline__ void softmax_warps_sync() { asm volatile("bar.sync 1,
 __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
   __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<uint32_t*>(&v);
-}
-
-// 2^x with the hardware approximation (flush-to-zero); 2^-inf = 0.
-__device__ __forceinline__ float ex2_approx(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
-  return y;
 }
 
 // Four 8x8 bf16 tiles to shared memory; thread l supplies the address of row
@@ -317,21 +312,6 @@ struct Barriers {
   uint64_t drain[2];               // abort path: every MMA a thread issued finished
   uint64_t recv;                   // cluster merge: every split's rows for this owner landed
 };
-
-// Bounded wait of the pipeline that also gives up when another role has
-// aborted.  (The waits that let in-flight copies and products land before a
-// CTA leaves always keep the full kWaitLimit.)
-__device__ __forceinline__ bool wait_bar(uint64_t* bar, uint32_t parity, volatile int* abort_flag,
-                                         unsigned* err, uint32_t limit) {
-  const uint32_t a = sm100::smem_addr(bar);
-  for (uint32_t i = 0; i < limit; ++i) {
-    if (sm100::mbar_try_wait(a, parity)) return true;
-    if ((i & 255u) == 255u && *abort_flag) return false;
-  }
-  *abort_flag = 1;
-  adt::raise_error(err, ADT_DEVERR_TIMEOUT);
-  return false;
-}
 
 // The tree of a launch slot.  With several trees (up to 32) the launch slots
 // go to the trees by decreasing prefix length (ties: lower index): the CTAs
@@ -1369,29 +1349,13 @@ WsLayout ws_layout(int B, int H, int D, int splits) {
   return w;
 }
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-std::once_flag g_encode_once;
-EncodeTiledFn g_encode = nullptr;
-
-void load_encode() {
-  void* fn = nullptr;
-  cudaDriverEntryPointQueryResult q;
-  if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &q) ==
-          cudaSuccess &&
-      q == cudaDriverEntryPointSuccess)
-    g_encode = reinterpret_cast<EncodeTiledFn>(fn);
-}
-
 // 4-D map of a cache (d, pos, kv head, tree) with the 128-byte swizzle and
 // boxes of 64 columns x box_keys positions; positions at or past max_kv read
 // as zero.
 adt_status make_cache_map(CUtensorMap* map, const void* base, int D, int max_kv, int Hkv, int B, int64_t sh,
                           int64_t sb, int box_keys = kChunk) {
-  std::call_once(g_encode_once, load_encode);
-  if (!g_encode) return ADT_ERR_CUDA;
+  const adt::EncodeTiledFn encode = adt::encode_tiled();
+  if (!encode) return ADT_ERR_CUDA;
   const int64_t span = static_cast<int64_t>(max_kv > 0 ? max_kv : 1);
   cuuint64_t dims[4] = {static_cast<cuuint64_t>(D), static_cast<cuuint64_t>(span), static_cast<cuuint64_t>(Hkv),
                         static_cast<cuuint64_t>(B)};
@@ -1399,7 +1363,7 @@ adt_status make_cache_map(CUtensorMap* map, const void* base, int D, int max_kv,
                            static_cast<cuuint64_t>(sb > 0 ? sb : span * D * Hkv) * 2};
   cuuint32_t box[4] = {64, static_cast<cuuint32_t>(box_keys), 1, 1};
   cuuint32_t estr[4] = {1, 1, 1, 1};
-  CUresult r = g_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr,
+  CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr,
                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? ADT_OK : ADT_ERR_INVALID_ARG;
@@ -1410,13 +1374,13 @@ adt_status make_cache_map(CUtensorMap* map, const void* base, int D, int max_kv,
 // The node extent is nominal: the kernel only requests boxes that lie inside
 // the node_offsets[B] rows the caller's buffer holds.
 adt_status make_rows_map(CUtensorMap* map, const void* base, int D, int heads) {
-  std::call_once(g_encode_once, load_encode);
-  if (!g_encode) return ADT_ERR_CUDA;
+  const adt::EncodeTiledFn encode = adt::encode_tiled();
+  if (!encode) return ADT_ERR_CUDA;
   cuuint64_t dims[3] = {static_cast<cuuint64_t>(D), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(kTmaRows)};
   cuuint64_t strides[2] = {static_cast<cuuint64_t>(D) * 2, static_cast<cuuint64_t>(heads) * D * 2};
   cuuint32_t box[3] = {64, 1, kUnit};
   cuuint32_t estr[3] = {1, 1, 1};
-  CUresult r = g_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
+  CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? ADT_OK : ADT_ERR_INVALID_ARG;
