@@ -346,12 +346,32 @@ def adt_kv_compact_inplace(k_cache, v_cache, kv_len, kv_len_out, node_offsets, p
 
 _TYPES = {torch.bfloat16: 0, torch.float32: 1}
 
+# These calls are made from Python one at a time as often as in a graph, and take 9 to 18 tensors: each is looked at
+# once (device, type and address; shape and strides as whole tuples), which halves what a call costs the host.
 
-def _here(*tensors):
-    """Raises unless the tensors given (None: absent) are on the current CUDA device, which the launch goes to."""
-    for t in tensors:
-        if t is not None and (not t.is_cuda or t.get_device() != torch.cuda.current_device()):
-            raise ValueError(f"expected a tensor on the current CUDA device, got one on {t.device}")
+
+def _addr(t, dtype, dev, name):
+    """The address of a tensor of that type on CUDA device dev, the current one, which the launch goes to; None for None."""
+    if t is None:
+        return None
+    if t.get_device() != dev:
+        raise ValueError(f"{name}: expected a tensor on the current CUDA device, got one on {t.device}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    return t.data_ptr()
+
+
+def _vec(t, dtype, dev, count, name):
+    """The address of a contiguous tensor of at least `count` elements; None for None."""
+    a = _addr(t, dtype, dev, name)
+    if t is not None and (t.numel() < count or not t.is_contiguous()):
+        raise ValueError(f"{name}: expected {count} elements, contiguous")
+    return a
+
+
+def _device():
+    return _get_device() if _get_device is not None and torch.cuda.is_initialized() else \
+        torch.cuda.current_device() if torch.cuda.is_available() else 0
 
 
 def adt_rope_freqs(rotary_dim, *, theta=10000.0, scaling=ROPE_NONE, factor=1.0, orig_len=0.0, turns_lo=1.0,
@@ -364,86 +384,77 @@ def adt_rope_freqs(rotary_dim, *, theta=10000.0, scaling=ROPE_NONE, factor=1.0, 
     return inv, mag.value
 
 
-def _rope_rows(t, heads, D, N, name):
-    """Row stride of [N, heads * D] rows or [N, heads, D] heads (contiguous within a row)."""
-    if t.dim() == 3 and t.shape == (N, heads, D) and t.stride(2) == 1 and (t.stride(1) == D or heads == 1):
-        pass
-    elif not (t.dim() == 2 and t.shape == (N, heads * D) and t.stride(1) == 1):
-        raise ValueError(f"{name}: expected rows [{N}, {heads * D}] or [{N}, {heads}, {D}], contiguous within a row")
-    return t.stride(0) if N > 1 else heads * D
+def _rope_pair(t, out, dtype, dev, heads, D, N, name):
+    """(address, row stride, output address) of [N, heads * D] rows or [N, heads, D] heads, contiguous within a row."""
+    if t is None or out is None:
+        if t is not out:
+            raise ValueError(f"{name} and {name}_out: both or neither")
+        return None, 0, None
+    shape, strides, width = t.shape, t.stride(), heads * D
+    if not (shape == (N, width) and strides[1] == 1 or
+            shape == (N, heads, D) and strides[2] == 1 and (strides[1] == D or heads == 1)):
+        raise ValueError(f"{name}: expected rows [{N}, {width}] or [{N}, {heads}, {D}], contiguous within a row")
+    if out.numel() != N * width:
+        raise ValueError(f"{name}_out: expected [{N}, {heads}, {D}]")
+    return (_addr(t, dtype, dev, name), strides[0] if N > 1 else width,
+            _vec(out, torch.bfloat16, dev, 0, name + "_out"))
 
 
 def adt_rope_qkv(q, k, v, positions, inv_freq, *, H, Hkv, D, layout=ROPE_HALF, magnitude=1.0, q_out=None, k_out=None,
                  v_out=None, stream=None) -> None:
     """q [N, H * D], k and v [N, Hkv * D] rows (bf16 or fp32, any row stride; None: absent) to bf16 [N, heads, D]
     outputs: q and k rotated by positions * inv_freq, v copied.  rotary_dim = 2 * len(inv_freq)."""
-    _here(q, k, v, positions, inv_freq, q_out, k_out, v_out)
-    _expect(positions, torch.int32, "positions")
-    _expect(inv_freq, torch.float64, "inv_freq")
-    N = positions.numel()
-    types, lds = set(), []
-    for name, t, o, heads in (("q", q, q_out, H), ("k", k, k_out, Hkv), ("v", v, v_out, Hkv)):
-        if (t is None) != (o is None):
-            raise ValueError(f"{name} and {name}_out: both or neither")
-        if t is None:
-            lds.append(0)
-            continue
-        lds.append(_rope_rows(t, heads, D, N, name))
-        types.add(t.dtype)
-        _expect(o, torch.bfloat16, name + "_out")
-        if o.numel() != N * heads * D:
-            raise ValueError(f"{name}_out: expected [{N}, {heads}, {D}]")
-    if len(types) != 1 or not types <= _TYPES.keys():
+    dev, N = _device(), positions.numel()
+    first = q if q is not None else k if k is not None else v
+    if first is None or first.dtype not in _TYPES:
         raise TypeError("q, k, v: bf16 or fp32, all the same")
-    st = lib().adt_rope_qkv(_ptr(q), lds[0], _ptr(k), lds[1], _ptr(v), lds[2], _TYPES[types.pop()], _ptr(positions),
-                            _ptr(inv_freq), float(magnitude), layout, N, H, Hkv, D, 2 * inv_freq.numel(), _ptr(q_out),
-                            _ptr(k_out), _ptr(v_out), _stream(stream))
+    dtype = first.dtype
+    qa, ldq, qo = _rope_pair(q, q_out, dtype, dev, H, D, N, "q")
+    ka, ldk, ko = _rope_pair(k, k_out, dtype, dev, Hkv, D, N, "k")
+    va, ldv, vo = _rope_pair(v, v_out, dtype, dev, Hkv, D, N, "v")
+    st = lib().adt_rope_qkv(qa, ldq, ka, ldk, va, ldv, _TYPES[dtype], _vec(positions, torch.int32, dev, N, "positions"),
+                            _vec(inv_freq, torch.float64, dev, 0, "inv_freq"), magnitude, layout, N, H, Hkv, D,
+                            2 * inv_freq.numel(), qo, ko, vo, _stream(stream))
     _check(st, "adt_rope_qkv")
 
 
-def _strides3(t, shape, name, inner):
-    """Strides of the first three dimensions of [layers, B, Hkv, rows, ...]; the rows have `inner` elements, packed."""
-    if t.dim() != len(shape) or t.shape[:3] != shape[:3] or t.shape[3] < shape[3] or t.shape[4:] != shape[4:]:
-        raise ValueError(f"{name}: expected {list(shape)} or more rows, got {list(t.shape)}")
-    if (t.shape[3] > 1 and t.stride(3) != inner) or (inner > 1 and t.stride(4) != 1):
+def _strides3(t, layers, B, Hkv, rows, D, name):
+    """Strides of the first three dimensions of [layers, B, Hkv, rows or more, D] (D = 0: of [layers, B, Hkv, rows or
+    more]); the rows are packed."""
+    shape, strides = t.shape, t.stride()
+    want = 5 if D else 4
+    if len(shape) != want or shape[0] != layers or shape[1] != B or shape[2] != Hkv or shape[3] < rows or \
+            (D and shape[4] != D):
+        raise ValueError(f"{name}: expected {[layers, B, Hkv, rows, D][:want]} or more rows, got {list(shape)}")
+    if (strides[3] != (D or 1) and shape[3] > 1) or (D and strides[4] != 1):
         raise ValueError(f"{name}: expected packed rows")
-    return t.stride()[:3]
-
-
-def _rows3(t, shape, dtype, name):
-    """Stride of the first dimension of [layers, ...], the rest contiguous and at least `shape`."""
-    if t.dtype != dtype:
-        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
-    if t.dim() != len(shape) + 1 or t.shape[2:] != shape[1:]:
-        raise ValueError(f"{name}: expected [layers, nodes, {', '.join(map(str, shape[1:]))}]")
-    if not t[0].is_contiguous():
-        raise ValueError(f"{name}: expected each layer contiguous")
-    return t.stride(0)
+    return strides[:3]
 
 
 def adt_kv_score(q, lse, k_cache, kv_len, node_offsets, path, max_path, accept_len, score, *, score_out=None, B, H, Hkv,
                  D, num_layers, max_kv, softmax_scale, decay=1.0, stream=None) -> None:
     """q [layers, nodes, H, D] bf16, lse [layers, nodes, H], k_cache [layers, B, Hkv, rows >= max_kv, D] and score
     [layers, B, Hkv, rows >= max_kv] fp32, updated in place unless score_out (the same strides) is given."""
-    score_out = score if score_out is None else score_out
-    _here(q, lse, k_cache, kv_len, node_offsets, path, accept_len, score, score_out)
-    for t, name in ((kv_len, "kv_len"), (node_offsets, "node_offsets"), (path, "path"), (accept_len, "accept_len")):
-        _expect(t, torch.int32, name)
-    if kv_len.numel() < B or accept_len.numel() < B or node_offsets.numel() < B + 1 or path.numel() < B * max_path:
-        raise ValueError("kv_len, accept_len [B], node_offsets [B + 1], path [B, max_path]")
-    if k_cache.dtype != torch.bfloat16 or score.dtype != torch.float32 or score_out.dtype != torch.float32:
-        raise TypeError("k_cache: bf16, score: fp32")
-    if score_out is not score and score_out.stride() != score.stride():
-        raise ValueError("score and score_out must share strides")
-    qs, ls = _rows3(q, (0, H, D), torch.bfloat16, "q"), _rows3(lse, (0, H), torch.float32, "lse")
-    if q.shape[0] < num_layers or lse.shape[0] < num_layers or lse.shape[1] != q.shape[1]:
-        raise ValueError("q and lse: [layers, nodes, ...]")
-    cs = _strides3(k_cache, (num_layers, B, Hkv, max_kv, D), "k_cache", D)
-    ss = _strides3(score, (num_layers, B, Hkv, max_kv), "score", 1)
-    _strides3(score_out, (num_layers, B, Hkv, max_kv), "score_out", 1)
-    st = lib().adt_kv_score(_ptr(q), _ptr(lse), _ptr(k_cache), _ptr(kv_len), _ptr(node_offsets), _ptr(path),
-                            int(max_path), _ptr(accept_len), B, H, Hkv, D, num_layers, max_kv, qs, ls, *cs,
-                            float(softmax_scale), float(decay), _ptr(score), _ptr(score_out), *ss, _stream(stream))
+    dev, f32, i32, bf16 = _device(), torch.float32, torch.int32, torch.bfloat16
+    qs, ls, nodes = q.stride(), lse.stride(), q.shape[1]
+    if q.shape[2:] != (H, D) or q.shape[0] < num_layers or qs[1:] != (H * D, D, 1):
+        raise ValueError(f"q: expected [{num_layers}, nodes, {H}, {D}], each layer contiguous")
+    if lse.shape[1:] != (nodes, H) or lse.shape[0] < num_layers or ls[1:] != (H, 1):
+        raise ValueError(f"lse: expected [{num_layers}, {nodes}, {H}], each layer contiguous")
+    cs = _strides3(k_cache, num_layers, B, Hkv, max_kv, D, "k_cache")
+    ss = _strides3(score, num_layers, B, Hkv, max_kv, 0, "score")
+    sa = _addr(score, f32, dev, "score")
+    if score_out is None:
+        so = sa
+    else:
+        so = _addr(score_out, f32, dev, "score_out")
+        if _strides3(score_out, num_layers, B, Hkv, max_kv, 0, "score_out") != ss:
+            raise ValueError("score and score_out must share strides")
+    st = lib().adt_kv_score(_addr(q, bf16, dev, "q"), _addr(lse, f32, dev, "lse"), _addr(k_cache, bf16, dev, "k_cache"),
+                            _vec(kv_len, i32, dev, B, "kv_len"), _vec(node_offsets, i32, dev, B + 1, "node_offsets"),
+                            _vec(path, i32, dev, B * max_path, "path"), max_path,
+                            _vec(accept_len, i32, dev, B, "accept_len"), B, H, Hkv, D, num_layers, max_kv, qs[0], ls[0], *cs,
+                            softmax_scale, decay, sa, so, *ss, _stream(stream))
     _check(st, "adt_kv_score")
 
 
@@ -453,37 +464,32 @@ def adt_kv_evict(k_cache, v_cache, score, kv_len, kv_len_out=None, *, k_out=None
     """Caches [layers, B, Hkv, rows >= max_kv, D] bf16 and score [layers, B, Hkv, rows >= max_kv] fp32 cut down to
     `budget` rows: in place, or into k_out, v_out.  The scores go to score_out, by default to where the rows went (in
     place: the same buffer); with move_scores=False they stay as they are."""
+    dev, f32, i32, bf16 = _device(), torch.float32, torch.int32, torch.bfloat16
     if (k_out is None) != (v_out is None):
         raise ValueError("k_out and v_out: both or neither")
-    in_place = k_out is None
-    k_out, v_out = (k_cache, v_cache) if in_place else (k_out, v_out)
-    if not move_scores:
-        if score_out is not None:
-            raise ValueError("score_out without moving scores")
-    elif score_out is None:
-        if not in_place:
-            raise ValueError("score_out: needed where the rows go to another cache")
-        score_out = score
-    _here(k_cache, v_cache, score, kv_len, kv_len_out, k_out, v_out, score_out, keep_idx)
-    for t, name in ((kv_len, "kv_len"), (kv_len_out, "kv_len_out"), (keep_idx, "keep_idx")):
-        if t is not None:
-            _expect(t, torch.int32, name)
-    if kv_len.numel() < B or (kv_len_out is not None and kv_len_out.numel() < B):
-        raise ValueError("kv_len, kv_len_out: [B]")
-    if keep_idx is not None and keep_idx.numel() < num_layers * B * Hkv * budget:
-        raise ValueError("keep_idx: [layers, B, Hkv, budget]")
-    if any(t.dtype != torch.bfloat16 for t in (k_cache, v_cache, k_out, v_out)):
-        raise TypeError("caches: bf16")
-    if score.dtype != torch.float32 or (score_out is not None and score_out.dtype != torch.float32):
-        raise TypeError("score: fp32")
-    shape, kept = (num_layers, B, Hkv, max_kv, D), (num_layers, B, Hkv, min(max_kv, budget), D)
-    ks, ko = _strides3(k_cache, shape, "k_cache", D), _strides3(k_out, kept, "k_out", D)
-    if _strides3(v_cache, shape, "v_cache", D) != ks or _strides3(v_out, kept, "v_out", D) != ko:
+    if score_out is not None and not move_scores:
+        raise ValueError("score_out without moving scores")
+    if score_out is None and move_scores and k_out is not None:
+        raise ValueError("score_out: needed where the rows go to another cache")
+    ks = _strides3(k_cache, num_layers, B, Hkv, max_kv, D, "k_cache")
+    cs = co = _strides3(score, num_layers, B, Hkv, max_kv, 0, "score")
+    same = _strides3(v_cache, num_layers, B, Hkv, max_kv, D, "v_cache") == ks
+    ka, va, sa = _addr(k_cache, bf16, dev, "k_cache"), _addr(v_cache, bf16, dev, "v_cache"), _addr(score, f32, dev, "score")
+    ko, vo, so, os = ka, va, sa if move_scores else None, ks
+    rows = min(max_kv, budget)
+    if k_out is not None and k_out is not k_cache:
+        os = _strides3(k_out, num_layers, B, Hkv, rows, D, "k_out")
+        ko = _addr(k_out, bf16, dev, "k_out")
+    if v_out is not None and v_out is not v_cache:
+        same = same and _strides3(v_out, num_layers, B, Hkv, rows, D, "v_out") == os
+        vo = _addr(v_out, bf16, dev, "v_out")
+    if not same:
         raise ValueError("K and V must share strides")
-    cs = _strides3(score, shape[:4], "score", 1)
-    co = (0, 0, 0) if score_out is None else _strides3(score_out, kept[:4], "score_out", 1)
-    st = lib().adt_kv_evict(_ptr(k_cache), _ptr(v_cache), *ks, _ptr(score), *cs, _ptr(kv_len), _ptr(kv_len_out),
-                            _ptr(k_out), _ptr(v_out), *ko, _ptr(score_out), *co, _ptr(keep_idx), B, Hkv, D, num_layers,
+    if score_out is not None:
+        co, so = _strides3(score_out, num_layers, B, Hkv, rows, 0, "score_out"), _addr(score_out, f32, dev, "score_out")
+    st = lib().adt_kv_evict(ka, va, *ks, sa, *cs, _vec(kv_len, i32, dev, B, "kv_len"),
+                            _vec(kv_len_out, i32, dev, B, "kv_len_out"), ko, vo, *os, so, *co,
+                            _vec(keep_idx, i32, dev, num_layers * B * Hkv * budget, "keep_idx"), B, Hkv, D, num_layers,
                             max_kv, budget, n_sink, n_recent, _stream(stream))
     _check(st, "adt_kv_evict")
 

@@ -6,9 +6,9 @@
 // its fraction goes on to fp32: at t = 10^6 the angle of a pair with f = 1 has
 // 20 bits before the point, so that in fp32 the cosine would be off by 0.03.
 //
-// A CTA takes one token (and, where there are few tokens, a share of its
-// heads): one thread a pair makes the cosines and sines once, in shared memory,
-// and every head of the token uses them.
+// A CTA takes one token or a few (and, where there are few tokens, a share of
+// their heads): one thread a pair makes the cosines and sines once, in shared
+// memory, and every head of the token uses them.
 #include <math.h>
 
 #include "adt_common.cuh"
@@ -33,17 +33,158 @@ struct RopeParams {
 __device__ __forceinline__ float to_f32(float x) { return x; }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
 
-// Cosines and sines of the CTA's token, m included.
-__device__ __forceinline__ void token_angles(const RopeParams& p, int n, float2* cs) {
-  const double t = static_cast<double>(p.pos[n]) * (1.0 / kTwoPi);
-  for (int i = threadIdx.x; i < p.rot / 2; i += kThreads) {
-    double turns = t * p.inv_freq[i];
+// Cosines and sines of `tokens` tokens from n0 on, m included.
+__device__ __forceinline__ void token_angles(const RopeParams& p, int n0, int tokens, float2* cs) {
+  const int half = p.rot / 2;
+  for (int i = threadIdx.x; i < half * tokens; i += kThreads) {
+    const int t = tokens == 1 ? 0 : i / half;
+    double turns = static_cast<double>(p.pos[n0 + t]) * (1.0 / kTwoPi) * p.inv_freq[i - t * half];
     turns -= rint(turns);
     float s, c;
     sincospif(2.f * static_cast<float>(turns), &s, &c);
     cs[i] = make_float2(c * p.magnitude, s * p.magnitude);
   }
   __syncthreads();
+}
+
+// Eight consecutive elements of a row.
+template <typename T>
+struct Eight {
+  uint4 v[sizeof(T) / 2];
+  __device__ __forceinline__ void load(const T* src) {
+#pragma unroll
+    for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) v[i] = reinterpret_cast<const uint4*>(src)[i];
+  }
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+    if constexpr (sizeof(T) == 2) {
+      const uint32_t w[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(w[i] << 16);
+        x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        x[4 * i] = __uint_as_float(v[i].x);
+        x[4 * i + 1] = __uint_as_float(v[i].y);
+        x[4 * i + 2] = __uint_as_float(v[i].z);
+        x[4 * i + 3] = __uint_as_float(v[i].w);
+      }
+    }
+  }
+};
+
+__device__ __forceinline__ void put(__nv_bfloat16* dst, const float (&x)[8]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+    w[i] = *reinterpret_cast<const uint32_t*>(&b);
+  }
+  *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Moves 16-byte vectors.  A unit is what a thread rotates at a time: eight
+// pairs of a half layout (two vectors of its row), four pairs side by side
+// (one), or eight copied elements.  A thread keeps its place within the heads,
+// so that its cosines and sines are read once, and its first units are on
+// their way while the angles are made.
+template <typename T, bool kInterleaved>
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3)
+    rope_vec_kernel(const RopeParams p, int N, int tokens, int lanes, int units) {
+  extern __shared__ float2 cs[];
+  constexpr int kBatch = 2;
+  constexpr int kVecs = kInterleaved ? 1 : 2;
+  adt::pdl_wait_then_release();
+  const int n0 = blockIdx.x * tokens, here = min(tokens, N - n0);
+  const int tok = threadIdx.x / lanes, lane = threadIdx.x - tok * lanes;
+  const bool active = tok < here;
+  const int64_t n = n0 + (active ? tok : 0);
+  const int half = p.rot / 2;
+  const int per_pass = lanes / units, hl = lane / units, u = lane - hl * units;
+  const bool turned = kInterleaved ? u * 8 < p.rot : u * 16 < p.rot;
+  // First element of the unit, and of its second vector.
+  const int e0 = kInterleaved || turned ? u * 8 : p.rot + (u - p.rot / 16) * 8, e1 = e0 + half;
+  const int heads = p.heads[0] + p.heads[1];
+  const int h0 = static_cast<int>(blockIdx.y) * per_pass + hl, hstep = static_cast<int>(gridDim.y) * per_pass;
+  const int v0 = static_cast<int>(blockIdx.y) * lanes + lane, vstep = static_cast<int>(gridDim.y) * lanes;
+  const int vectors = active ? p.heads[2] * p.D / 8 : 0;
+  const int most = active && hl < per_pass ? heads : 0;
+
+  Eight<T> x[kBatch][kVecs], v[kBatch];
+  auto at = [&](int h, const T** src, __nv_bfloat16** dst) {
+    const bool q = h < p.heads[0];
+    const int hh = q ? h : h - p.heads[0];
+    *src = static_cast<const T*>(q ? p.in[0] : p.in[1]) + n * (q ? p.ld[0] : p.ld[1]) + hh * p.D;
+    *dst = (q ? p.out[0] : p.out[1]) + (n * (q ? p.heads[0] : p.heads[1]) + hh) * p.D;
+  };
+  auto fetch = [&](int h, int vi) {
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const T* src;
+      __nv_bfloat16* dst;
+      if (h + k * hstep < most) {
+        at(h + k * hstep, &src, &dst);
+        x[k][0].load(src + e0);
+        if (!kInterleaved && turned) x[k][kVecs - 1].load(src + e1);
+      }
+      if (vi + k * vstep < vectors)
+        v[k].load(static_cast<const T*>(p.in[2]) + n * p.ld[2] + static_cast<int64_t>(vi + k * vstep) * 8);
+    }
+  };
+  fetch(h0, v0);
+  token_angles(p, n0, here, cs);
+  constexpr int kPairs = kInterleaved ? 4 : 8;
+  float c[kPairs], s[kPairs];
+  if (turned && active) {
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) {
+      const float2 z = cs[tok * half + u * kPairs + i];
+      c[i] = z.x;
+      s[i] = z.y;
+    }
+  }
+  int h = h0, vi = v0;
+  while (h < most || vi < vectors) {
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      if (h + k * hstep < most) {
+        const T* src;
+        __nv_bfloat16* dst;
+        at(h + k * hstep, &src, &dst);
+        float a[8], b[8], y[8], z[8];
+        x[k][0].get(a);
+        if (!turned) {
+          put(dst + e0, a);
+        } else if constexpr (kInterleaved) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            y[2 * i] = a[2 * i] * c[i] - a[2 * i + 1] * s[i];
+            y[2 * i + 1] = a[2 * i + 1] * c[i] + a[2 * i] * s[i];
+          }
+          put(dst + e0, y);
+        } else {
+          x[k][1].get(b);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            y[i] = a[i] * c[i] - b[i] * s[i];
+            z[i] = b[i] * c[i] + a[i] * s[i];
+          }
+          put(dst + e0, y);
+          put(dst + e1, z);
+        }
+      }
+      if (vi + k * vstep < vectors) {
+        float a[8];
+        v[k].get(a);
+        put(p.out[2] + n * p.heads[2] * p.D + static_cast<int64_t>(vi + k * vstep) * 8, a);
+      }
+    }
+    h += kBatch * hstep;
+    vi += kBatch * vstep;
+    fetch(h, vi);
+  }
 }
 
 // One pair or one copied element at a time: any even rotary_dim, any head
@@ -53,7 +194,7 @@ __global__ void __launch_bounds__(kThreads) rope_scalar_kernel(const RopeParams 
   __shared__ float2 cs[kMaxRotary / 2];
   adt::pdl_wait_then_release();
   const int n = blockIdx.x;
-  token_angles(p, n, cs);
+  token_angles(p, n, 1, cs);
   const int half = p.rot / 2, units = p.D - half;
   for (int x = 0; x < 3; ++x) {
     const T* in = static_cast<const T*>(p.in[x]) + n * p.ld[x];
@@ -167,12 +308,46 @@ adt_status adt_rope_qkv(const void* q, int64_t ld_q, const void* k, int64_t ld_k
   adt_status st = adt::device_info(&info);
   if (st != ADT_OK) return st;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(N), 1, 1);
   cfg.blockDim = dim3(kThreads, 1, 1);
   cfg.stream = adt::as_stream(stream);
   cudaLaunchAttribute attr[1] = {adt::pdl_attribute()};
   cfg.attrs = attr;
   cfg.numAttrs = 1;
+  // Vectors where everything lies on 16-byte boundaries and a vector never
+  // holds both turned and copied elements, or parts of both halves.
+  const int units = p.interleaved ? D / 8 : D / 8 - rotary_dim / 16;
+  bool vec = D % 8 == 0 && rotary_dim % (p.interleaved ? 8 : 16) == 0 && units <= kThreads;
+  for (int x = 0; x < 3; ++x)
+    vec = vec && (!in[x] || (adt::aligned16(in[x]) && adt::aligned16(out[x]) && ld[x] * esize % 16 == 0));
+  const int heads = p.heads[0] + p.heads[1];
+  if (vec) {
+    // Threads of a token: a power of two that takes its heads, or its values' vectors, in one pass; tokens fill the CTA.
+    const int64_t want = static_cast<int64_t>(heads) * units > p.heads[2] * (D / 8) ? static_cast<int64_t>(heads) * units
+                                                                                    : p.heads[2] * (D / 8);
+    int lanes = 32;
+    while (lanes < kThreads && (lanes < want || lanes < units)) lanes *= 2;
+    const int tokens = kThreads / lanes;
+    const int passes = static_cast<int>((want + lanes - 1) / lanes);
+    const int groups = (N + tokens - 1) / tokens;
+    // Few tokens: their heads over several CTAs, up to two an SM.
+    int split = 2 * info.sm_count / groups;
+    split = split < 1 ? 1 : split > passes ? passes : split;
+    cfg.gridDim = dim3(static_cast<unsigned>(groups), static_cast<unsigned>(split), 1);
+    cfg.dynamicSmemBytes = static_cast<size_t>(tokens) * (rotary_dim / 2) * sizeof(float2);
+    if (esize == 2)
+      ADT_CUDA_TRY(p.interleaved
+                       ? cudaLaunchKernelEx(&cfg, rope_vec_kernel<__nv_bfloat16, true>, p, N, tokens, lanes, units)
+                       : cudaLaunchKernelEx(&cfg, rope_vec_kernel<__nv_bfloat16, false>, p, N, tokens, lanes, units));
+    else
+      ADT_CUDA_TRY(p.interleaved ? cudaLaunchKernelEx(&cfg, rope_vec_kernel<float, true>, p, N, tokens, lanes, units)
+                                 : cudaLaunchKernelEx(&cfg, rope_vec_kernel<float, false>, p, N, tokens, lanes, units));
+    return adt::launch_status();
+  }
+  const int64_t most = static_cast<int64_t>(heads > p.heads[2] ? heads : p.heads[2]) * D;
+  int64_t split = 2 * info.sm_count / N;
+  const int64_t passes = (most + kThreads - 1) / kThreads;
+  split = split < 1 ? 1 : split > passes ? passes : split;
+  cfg.gridDim = dim3(static_cast<unsigned>(N), static_cast<unsigned>(split), 1);
   if (esize == 2)
     ADT_CUDA_TRY(cudaLaunchKernelEx(&cfg, rope_scalar_kernel<__nv_bfloat16>, p));
   else

@@ -143,7 +143,7 @@ def test_bindings_refuse_cpu_tensors_and_wrong_types(lib):
     with pytest.raises(ValueError, match="CUDA"):
         B.adt_kv_evict(cache, cache, score, i32, B=1, Hkv=1, D=64, num_layers=1, max_kv=4, budget=2)
     with pytest.raises(ValueError, match="CUDA"):
-        B.adt_kv_score(bf.view(1, 2, 1, 64), f32[None, :, :1], cache, i32, i32, i32, 1, i32, score, B=1, H=1, Hkv=1, D=64,
+        B.adt_kv_score(bf.view(1, 2, 1, 64), torch.zeros(1, 2, 1), cache, i32, i32, i32, 1, i32, score, B=1, H=1, Hkv=1, D=64,
                        num_layers=1, max_kv=4, softmax_scale=1.0)
     with pytest.raises(ValueError, match="both or neither"):
         B.adt_kv_evict(cache, cache, score, i32, k_out=cache, B=1, Hkv=1, D=64, num_layers=1, max_kv=4, budget=2)
