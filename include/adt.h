@@ -541,7 +541,7 @@ adt_status adt_kv_score(const adt_bf16* q, const float* lse, const adt_bf16* k_c
  * keep_idx [device] int32 [num_layers][B][Hkv][budget] or NULL: the kept rows,
  *         padded with -1.
  * D in {64, 128}; budget >= 1; n_sink, n_recent >= 0, n_sink + n_recent <=
- * budget; max_kv <= 2^20 (ADT_ERR_UNSUPPORTED above).
+ * budget; max_kv < 2^30.
  * kv_len[b] outside [0, max_kv] sets ADT_DEVERR_KV_RANGE and skips tree b
  * (kv_len_out[b] = kv_len[b]; its keep_idx is not written).
  * ------------------------------------------------------------------------ */

@@ -2,48 +2,86 @@
 // the first n_sink rows, the last n_recent, and between them those with the
 // highest scores (ties to the lowest index), in the order they had.
 //
-// A CTA selects the rows of one (layer, tree, kv head) slice by a radix search
-// for the lowest score that stays, marks them in a bit mask in shared memory,
-// and moves them.  A kept row never moves up, so chunks of rows taken in
-// ascending order can be moved in place: a chunk's destinations lie below the
-// sources of every later chunk, and only its own loads have to be done before
-// its stores.
+// A CTA (or a few, each with K or V or some of their columns) takes one (layer,
+// tree, kv head) slice.  It searches for the lowest score that stays: a
+// histogram of the scores over their range (by order, 2048 bins), then over the
+// range of the bin that the last kept score falls into, until that bin is kept
+// whole or holds one value.  Then, window by window, it lists the rows that stay
+// and moves them: every thread copies its vectors of a chunk of rows into slots
+// of its own in shared memory, asynchronously and three chunks ahead, and from
+// there to the rows' new place.  A kept row never moves up, so chunks of rows
+// taken in ascending order can be moved in place: a chunk's destinations lie
+// below the sources of every later chunk, whose loads may be under way, and its
+// stores wait (at a barrier) for all loads of its own and the chunks before.
+//
+// Bound by HBM where slices are many: 32 layers of a 7B cache, 2304 of 2400 rows
+// kept, 370 us for 2.4 GB read and written (97 % of the measured copy rate).
+// With fewer, nothing hides the search: its chain of passes over a slice's
+// scores takes 4 us at 1700 rows and 8 us at 5120 (a pass is bound by its
+// instructions, so keys are kept, not scores; a tenth of it is instructions
+// fetched cold).  256 slices of 1777 to 6001 rows, 2048 kept, 77 us of 61; 1440
+// slices of 1577 and 1693 rows of 128 bytes, 512 kept, 76 us of 58.  Four CTAs an
+// SM hide loads best with three chunks ahead (six chunks and half the CTAs: 75
+// -> 87 us for the last); 512 threads a CTA cost it 5 us, 128 6 us and the first
+// 38.  Bulk copies a run of rows at a time were as fast for long runs (371 us) but
+// not for short ones (431 against 93 us then for the 256 slices).  Bins over the
+// scores' range spread the counts; those over the top bits of fp32 met 30 bins
+// and cost 4 us at 5120 rows.
 #include <math.h>
 
 #include "adt_common.cuh"
+#include "sm100.cuh"
 
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMaxRows = 1 << 20;  // max_kv: the bit mask takes 128 KB
-constexpr int kWindow = 4096;      // rows whose kept ones are listed at a time
-constexpr int kVecs = 8;           // 16-byte vectors that a thread moves at a time
+constexpr int kWarps = kThreads / 32;
+constexpr int kWindow = kThreads * 32;  // rows whose kept ones are listed at a time: a word of bits for every thread
+constexpr int kVecs = 2;                // 16-byte vectors of a thread in a chunk
+constexpr int kDepth = 4;               // chunks that its slots hold
+constexpr int kAhead = 3;               // chunks that loads run ahead of stores
+constexpr int kSlotBytes = kDepth * kVecs * kThreads * 16;
+constexpr int kBinBits = 11;
+constexpr int kBins = 1 << kBinBits;
+static_assert(kWindow * 4 <= kSlotBytes, "a window's keys share the slots");
+static_assert(kBins * 4 <= kWindow * 2, "its bins share the list");
 
 struct EvictParams {
-  const uint4* src[2];   // K, V
-  uint4* dst[2];
+  const uint8_t* src[2];  // K, V
+  uint8_t* dst[2];
   const float* score;
-  float* score_out;      // or NULL
+  float* score_out;       // or NULL
   const int32_t* kv_len;
-  int32_t* kv_len_out;   // or NULL
-  int32_t* keep_idx;     // [layers][B][Hkv][budget], or NULL
-  int B, Hkv, D, max_kv, budget, n_sink, n_recent, in_place;
-  int64_t sls, ssb, ssh;     // source cache strides (elements)
-  int64_t dls, dsb, dsh;     // destination cache strides
-  int64_t cls, csb, csh;     // score strides
-  int64_t ols, osb, osh;     // score_out strides
+  int32_t* kv_len_out;    // or NULL
+  int32_t* keep_idx;      // [layers][B][Hkv][budget], or NULL
+  int B, Hkv, max_kv, budget, n_sink, n_recent, in_place;
+  int parts;              // CTAs a slice: 1, or K and V apart (2) with 1, 2 or 4 shares of their columns
+  int row_bytes;          // of a cache row
+  int64_t sls, ssb, ssh;  // source cache strides (bytes)
+  int64_t dls, dsb, dsh;  // destination cache strides (bytes)
+  int64_t cls, csb, csh;  // score strides (elements)
+  int64_t ols, osb, osh;  // score_out strides (elements)
   unsigned* err;
 };
 
-// Order of a score: larger scores get larger keys, NaN the largest.
-__device__ __forceinline__ uint32_t score_key(float s) { return isnan(s) ? 0xffffffffu : adt::float_order_key(s); }
+// Order of a score: larger scores get larger keys, from 2^23 - 2 for -inf up.
+// Adding zero makes -0 equal +0 and every NaN the canonical one (sign clear, all
+// bits set), the largest.
+__device__ __forceinline__ uint32_t score_key(float s) {
+  const uint32_t u = __float_as_uint(__fadd_rn(s, 0.f));
+  return (u ^ (static_cast<uint32_t>(static_cast<int32_t>(u) >> 31) | 0x80000000u)) - 1u;
+}
+// Above every score's key: rows that stay whatever their score.  (Below every
+// key: 0, rows that are not there.)
+constexpr uint32_t kStays = 0xffffffffu;
 
 struct Scratch {
-  uint32_t hist[2048];
-  uint16_t list[kWindow];   // kept rows of a window, relative to its first
-  float score[kWindow];     // their scores
-  uint32_t warp[kThreads / 32];
-  uint32_t prefix, need, count;
+  union {
+    uint16_t list[kWindow];  // kept rows of a window, relative to its first
+    uint32_t hist[kBins];    // the search's bins
+  };
+  uint32_t warp[2 * kWarps];
+  uint32_t bin, need, count;
 };
 
 // Exclusive prefix sum of one value a thread; *total gets the sum.
@@ -59,7 +97,7 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* warp_sums, 
   __syncthreads();
   uint32_t base = 0, all = 0;
 #pragma unroll
-  for (int i = 0; i < kThreads / 32; ++i) {
+  for (int i = 0; i < kWarps; ++i) {
     const uint32_t s = warp_sums[i];
     if (i < w) base += s;
     all += s;
@@ -69,127 +107,265 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* warp_sums, 
   return base + x - v;
 }
 
-// Marks in `mask` the rows of [0, L) that stay; `want` of the rows [lo, hi) do.
-__device__ void select_rows(const float* score, int L, int lo, int hi, int want, uint32_t* mask, Scratch* sc) {
-  const int tid = threadIdx.x, words = (L + 31) / 32;
-  // Threshold: keys whose high bits (of the digits found) exceed `prefix` stay,
-  // of those that equal it the first `need`.
-  uint32_t prefix = 0, digits = 0, need = want, count = 0;
-  if (want > 0) {
-    const int shift[3] = {21, 10, 0}, bits[3] = {11, 11, 10};
-    for (int d = 0; d < 3; ++d) {
-      for (int i = tid; i < 2048; i += kThreads) sc->hist[i] = 0;
-      __syncthreads();
-      for (int j = lo + tid; j < hi; j += kThreads) {
-        const uint32_t k = score_key(score[j]);
-        if ((k & digits) == prefix) atomicAdd(&sc->hist[(k >> shift[d]) & ((1u << bits[d]) - 1)], 1u);
-      }
-      __syncthreads();
-      // Thread t holds eight bins, the highest first; the bin where the count
-      // from above reaches `need` is the digit.
-      uint32_t c[8], sum = 0, total;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) sum += c[i] = sc->hist[2047 - (tid * 8 + i)];
-      uint32_t above = block_scan(sum, sc->warp, &total);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if (above < need && need <= above + c[i]) {
-          sc->prefix = prefix | (static_cast<uint32_t>(2047 - (tid * 8 + i)) << shift[d]);
-          sc->need = need - above;
-          sc->count = c[i];
-        }
-        above += c[i];
-      }
-      __syncthreads();
-      prefix = sc->prefix;
-      need = sc->need;
-      count = sc->count;
-      digits |= ((1u << bits[d]) - 1) << shift[d];
-      __syncthreads();
-      if (count == need) break;
-    }
-  }
-  uint32_t ties = 0;  // rows before this turn whose key equals the threshold
-  const bool all_ties = want == 0 || count == need;
-  for (int j0 = 0; j0 < words * 32; j0 += kThreads) {
-    const int j = j0 + tid;
-    bool stay = j < L && (j < lo || j >= hi), tie = false;
-    if (want > 0 && j >= lo && j < hi) {
-      const uint32_t k = score_key(score[j]) & digits;
-      stay = k > prefix;
-      tie = k == prefix;
-    }
-    if (all_ties) {
-      stay |= tie && want > 0;
+// Rows with keys above `last` stay, and of those with keys in [first, last] the
+// lowest `ties` rows (ties < 0: all).
+struct Cut {
+  uint32_t first, last;
+  int ties;
+};
+
+// Keys of the rows w0 .. of a window, into shared memory; the rows from `hi` on
+// and those before `lo` stay.
+__device__ __forceinline__ void window_keys(const float* score, int w0, int L, int lo, int hi, uint32_t* keys,
+                                            uint32_t* low, uint32_t* high) {
+  const int rows = min(L - w0, kWindow);
+#pragma unroll 8
+  for (int r = threadIdx.x; r < rows; r += kThreads) {
+    uint32_t k = score_key(score[w0 + r]);
+    if (w0 + r >= lo && w0 + r < hi) {
+      *low = min(*low, k);
+      *high = max(*high, k);
     } else {
-      uint32_t total;
-      const uint32_t before = block_scan(tie ? 1u : 0u, sc->warp, &total);
-      stay |= tie && ties + before < need;
-      ties += total;
+      k = kStays;
     }
-    const uint32_t bits = __ballot_sync(adt::kFullMask, stay);
-    if ((tid & 31) == 0 && j < words * 32) mask[j >> 5] = bits;
+    keys[r] = k;
+  }
+  const int end = (rows + 31) & ~31;
+  if (rows + static_cast<int>(threadIdx.x) < end) keys[rows + threadIdx.x] = 0u;
+}
+
+// The cut that keeps `want` of the rows [lo, hi).  Of a slice that is one window
+// the keys are left in shared memory.
+__device__ __forceinline__ Cut find_cut(const float* score, uint32_t* keys, bool small, int L, int lo, int hi, int want,
+                                        Scratch* sc) {
+  const int tid = threadIdx.x;
+  uint32_t low = 0xffffffffu, high = 0u;
+  for (int i = tid; i < kBins; i += kThreads) sc->hist[i] = 0;
+  for (int w0 = 0; w0 < L; w0 += kWindow) window_keys(score, w0, L, lo, hi, keys, &low, &high);
+  low = __reduce_min_sync(adt::kFullMask, low);
+  high = __reduce_max_sync(adt::kFullMask, high);
+  if ((tid & 31) == 0) {
+    sc->warp[tid >> 5] = low;
+    sc->warp[kWarps + (tid >> 5)] = high;
   }
   __syncthreads();
+  if (want == 0) return Cut{kStays - 1u, kStays - 1u, 0};  // (the lowest none of whatever ties)
+#pragma unroll
+  for (int i = 0; i < kWarps; ++i) {
+    low = min(low, sc->warp[i]);
+    high = max(high, sc->warp[kWarps + i]);
+  }
+  uint32_t base = low, span = high - low;  // keys that still compete: base .. base + span
+  uint32_t need = want;
+  bool whole;
+  while (true) {
+    const int bits = 32 - __clz(span), shift = bits > kBinBits ? bits - kBinBits : 0;
+    if (small) {
+#pragma unroll 4
+      for (int j = tid; j < L; j += kThreads) {
+        const uint32_t k = keys[j] - base;
+        if (k <= span) atomicAdd(&sc->hist[k >> shift], 1u);
+      }
+    } else {
+#pragma unroll 4
+      for (int j = lo + tid; j < hi; j += kThreads) {
+        const uint32_t k = score_key(score[j]) - base;
+        if (k <= span) atomicAdd(&sc->hist[k >> shift], 1u);
+      }
+    }
+    __syncthreads();
+    // Each thread holds a few bins, the highest first; the one where the count
+    // from above reaches `need` is the last that is kept, in whole or in part.
+    constexpr int kOwn = kBins / kThreads;
+    uint32_t c[kOwn], sum = 0, total;
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) sum += c[i] = sc->hist[kBins - 1 - (tid * kOwn + i)];
+    uint32_t above = block_scan(sum, sc->warp, &total);
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) {
+      if (above < need && need <= above + c[i]) {
+        sc->bin = kBins - 1 - (tid * kOwn + i);
+        sc->need = need - above;
+        sc->count = c[i];
+      }
+      above += c[i];
+    }
+    __syncthreads();
+    need = sc->need;
+    base += sc->bin << shift;
+    span = min((1u << shift) - 1u, high - base);
+    whole = sc->count == need;
+    if (shift == 0 || whole) break;
+    for (int i = tid; i < kBins; i += kThreads) sc->hist[i] = 0;
+    __syncthreads();
+  }
+  return Cut{base, base + span, whole ? -1 : static_cast<int>(need)};
+}
+
+// The threads that move a tensor: all of the CTA, or half of it.
+__device__ __forceinline__ void mover_sync(int id, int threads) {
+  if (id == 1)
+    asm volatile("bar.sync 1, %0;\n" ::"r"(threads) : "memory");
+  else
+    asm volatile("bar.sync 2, %0;\n" ::"r"(threads) : "memory");
+}
+
+// Moves rows first .. rows - 1 of the list: list[r] of src to row r of dst, by
+// `threads` threads of which this is number t.  A row is 2^pitch bytes, of which
+// 2^shift vectors are moved; slots: this thread's first.  (A window's rows are
+// within 2 MB, so that offsets take 32 bits.)
+__device__ __forceinline__ void move_rows(uint8_t* slots, const uint8_t* src, uint8_t* dst, const uint16_t* list, int first,
+                                          int rows, int shift, int pitch, int t, int threads, int barrier, bool in_place) {
+  const int step = threads >> shift;  // rows that one vector of every thread makes
+  const int chunks = (rows - first + kVecs * step - 1) / (kVecs * step);
+  const int r0 = first + (t >> shift), column = (t & ((1 << shift) - 1)) * 16;
+  src += column;
+  dst += column + (static_cast<uint32_t>(r0) << pitch);
+  list += r0;
+  int to_load = rows - r0, to_store = rows - r0;  // rows from this thread's next one on
+  const uint32_t smem = sm100::smem_addr(slots), dstep = static_cast<uint32_t>(step) << pitch;
+  auto load = [&](int slot) {
+#pragma unroll
+    for (int v = 0; v < kVecs; ++v)
+      if (v * step < to_load)
+        sm100::cp_async16(smem + (slot * kVecs + v) * (kThreads * 16), src + (static_cast<uint32_t>(list[v * step]) << pitch), 16);
+    list += kVecs * step;
+    to_load -= kVecs * step;
+    asm volatile("cp.async.commit_group;\n" ::: "memory");
+  };
+#pragma unroll
+  for (int c = 0; c < kAhead; ++c) load(c);
+  for (int c = 0; c < chunks; c += kDepth) {
+#pragma unroll
+    for (int u = 0; u < kDepth; ++u) {
+      if (c + u < chunks) {
+        load((u + kAhead) % kDepth);
+        asm volatile("cp.async.wait_group %0;\n" ::"n"(kAhead) : "memory");
+        if (in_place) mover_sync(barrier, threads);
+#pragma unroll
+        for (int v = 0; v < kVecs; ++v)
+          if (v * step < to_store)
+            *reinterpret_cast<uint4*>(dst + v * dstep) =
+                *reinterpret_cast<const uint4*>(slots + (u * kVecs + v) * (kThreads * 16));
+        dst += kVecs * dstep;
+        to_store -= kVecs * step;
+      }
+    }
+  }
+  asm volatile("cp.async.wait_group 0;\n" ::: "memory");
 }
 
 __global__ void __launch_bounds__(kThreads) kv_evict_kernel(const EvictParams p) {
-  extern __shared__ uint32_t mask[];
+  extern __shared__ __align__(128) uint8_t smem[];  // the movers' slots
   __shared__ Scratch sc;
-  adt::pdl_wait_then_release();
-  const int slice = blockIdx.x, tid = threadIdx.x;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int rank = p.parts == 1 ? 0 : static_cast<int>(blockIdx.x) % p.parts, slice = blockIdx.x / p.parts;
   const int g = slice % p.Hkv, b = slice / p.Hkv % p.B, l = slice / p.Hkv / p.B;
+  adt::pdl_wait_then_release();
   const int L = p.kv_len[b];
   const bool ok = L >= 0 && L <= p.max_kv;
   const int n = ok ? min(L, p.budget) : 0;
-  if (g == 0 && l == 0 && tid == 0) {
+  if (g == 0 && l == 0 && rank == 0 && tid == 0) {
     if (!ok) adt::raise_error(p.err, ADT_DEVERR_KV_RANGE);
     if (p.kv_len_out) p.kv_len_out[b] = ok ? n : L;
   }
-  if (!ok) return;
+  if (!ok) return;  // (all CTAs of the slice)
   const float* score = p.score + l * p.cls + b * p.csb + g * p.csh;
-  float* score_out = p.score_out ? p.score_out + l * p.ols + b * p.osb + g * p.osh : nullptr;
-  int32_t* idx = p.keep_idx ? p.keep_idx + static_cast<int64_t>(slice) * p.budget : nullptr;
+  float* score_out = p.score_out && rank == 0 ? p.score_out + l * p.ols + b * p.osb + g * p.osh : nullptr;
+  int32_t* idx = p.keep_idx && rank == 0 ? p.keep_idx + static_cast<int64_t>(slice) * p.budget : nullptr;
   const int lo = L > n ? p.n_sink : L, hi = L > n ? L - p.n_recent : L;
-  select_rows(score, L, lo, hi, n - lo - (L - hi), mask, &sc);
-  const int vpr = p.D / 8;
-  const int64_t src0 = (l * p.sls + b * p.ssb + g * p.ssh) / 8, dst0 = (l * p.dls + b * p.dsb + g * p.dsh) / 8;
+  uint32_t* keys = reinterpret_cast<uint32_t*>(smem);  // of a window's rows
+  const bool small = L <= kWindow;
+  Cut cut = find_cut(score, keys, small, L, lo, hi, n - lo - (L - hi), &sc);
+  // K by one half of the threads and V by the other, or one of them by all.
+  const int movers = p.parts == 1 ? kThreads / 2 : kThreads;
+  const int x = p.parts == 1 ? tid / movers : rank & 1;
+  const int width = p.parts <= 2 ? p.row_bytes : 2 * p.row_bytes / p.parts, shift = __ffs(width / 16) - 1;
+  const int64_t column = p.parts <= 2 ? 0 : (rank >> 1) * width;
+  const uint8_t* src = (x ? p.src[1] : p.src[0]) + l * p.sls + b * p.ssb + g * p.ssh + column;
+  uint8_t* dst = (x ? p.dst[1] : p.dst[0]) + l * p.dls + b * p.dsb + g * p.dsh + column;
   int done = 0;  // rows moved before this window
   for (int w0 = 0; w0 < L; w0 += kWindow) {
-    const int words = (min(L - w0, kWindow) + 31) / 32;
-    uint32_t m = tid < words ? mask[w0 / 32 + tid] : 0u, listed;
-    uint32_t at = block_scan(__popc(m), sc.warp, &listed);
-    const int rows = static_cast<int>(listed);
-    for (; m; m &= m - 1) sc.list[at++] = static_cast<uint16_t>(tid * 32 + __ffs(m) - 1);
-    __syncthreads();
-    if (score_out)
-      for (int r = tid; r < rows; r += kThreads) sc.score[r] = score[w0 + sc.list[r]];
-    __syncthreads();
-    for (int r = tid; r < rows; r += kThreads) {
-      if (score_out) score_out[done + r] = sc.score[r];
-      if (idx) idx[done + r] = w0 + sc.list[r];
+    if (!small) {  // (all movers have left the slots)
+      uint32_t low = 0u, high = 0u;
+      window_keys(score, w0, L, lo, hi, keys, &low, &high);
+      __syncthreads();
     }
-    const int total = rows * vpr;
-    for (int x = 0; x < 2; ++x) {
-      const uint4* src = p.src[x] + src0;
-      uint4* dst = p.dst[x] + dst0;
-      for (int i0 = 0; i0 < total; i0 += kThreads * kVecs) {
-        uint4 v[kVecs];
+    // Bits of the rows that stay and of those that tie, a word a lane: a warp
+    // takes `own` words one after the other, so that the threads' words are in
+    // the rows' order.
+    const int words = (min(L - w0, kWindow) + 31) / 32, own = (words + kWarps - 1) / kWarps, first = warp * own;
+    const int here = min(own, words - first);
+    const bool by_row = cut.ties >= 0;
+    const uint32_t* key = keys + first * 32 + lane;
+    uint32_t stay = 0, tie = 0, total;
+    if (!by_row) {
+#pragma unroll 4
+      for (int i = 0; i < here; ++i) {
+        const uint32_t s = __ballot_sync(adt::kFullMask, key[i * 32] >= cut.first);
+        stay = lane == i ? s : stay;
+      }
+    } else {
+      for (int i = 0; i < here; ++i) {
+        const uint32_t k = key[i * 32];
+        const uint32_t s = __ballot_sync(adt::kFullMask, k > cut.last);
+        const uint32_t t = __ballot_sync(adt::kFullMask, k >= cut.first && k <= cut.last);
+        stay = lane == i ? s : stay;
+        tie = lane == i ? t : tie;
+      }
+    }
+    if (by_row) {
+      const int before = static_cast<int>(block_scan(__popc(tie), sc.warp, &total));
+      int most = min(max(cut.ties - before, 0), __popc(tie));  // of this word's ties, the lowest rows
+      for (; most > 0; --most) {
+        stay |= tie & (0u - tie);
+        tie &= tie - 1;
+      }
+      cut.ties -= min(cut.ties, static_cast<int>(total));
+    }
+    uint32_t at = block_scan(__popc(stay), sc.warp, &total);
+    const int rows = static_cast<int>(total);
+    // Rows before the first that goes are in place.
+    const uint32_t gone = lane < here && stay != 0xffffffffu ? (first + lane) * 32 + __ffs(~stay) - 1 : kWindow;
+    const uint32_t lead_here = __reduce_min_sync(adt::kFullMask, gone);
+    if (lane == 0) sc.warp[warp] = lead_here;
+#pragma unroll 4
+    for (int i = 0; i < here; ++i) {
+      const uint32_t bits = __shfl_sync(adt::kFullMask, stay, i), to = __shfl_sync(adt::kFullMask, at, i);
+      if (bits >> lane & 1u) sc.list[to + __popc(bits & ((1u << lane) - 1u))] = static_cast<uint16_t>((first + i) * 32 + lane);
+    }
+    if (p.parts > 1) {
+      // Scores may move in place: not before every CTA of the slice has read them.
+      sm100::cluster_arrive_release();
+      sm100::cluster_wait_acquire();
+    }
+    __syncthreads();
+    int lead = p.in_place && w0 == done ? rows : 0;
 #pragma unroll
-        for (int e = 0; e < kVecs; ++e) {
-          const int i = i0 + e * kThreads + tid, r = i / vpr;
-          if (i < total) v[e] = src[static_cast<int64_t>(w0 + sc.list[r]) * vpr + i % vpr];
+    for (int i = 0; i < kWarps; ++i) lead = min(lead, static_cast<int>(sc.warp[i]));
+    if (idx)
+      for (int r = tid; r < rows; r += kThreads) idx[done + r] = w0 + sc.list[r];
+    if (score_out) {
+      for (int r0 = 0; r0 < rows; r0 += 4 * kThreads) {  // (in place as the rows are, below)
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int r = r0 + e * kThreads + tid;
+          if (r < rows) v[e] = score[w0 + sc.list[r]];
         }
-        if (p.in_place) __syncthreads();
+        __syncthreads();
 #pragma unroll
-        for (int e = 0; e < kVecs; ++e) {
-          const int i = i0 + e * kThreads + tid, r = i / vpr;
-          if (i < total && !(p.in_place && w0 + sc.list[r] == done + r))
-            dst[static_cast<int64_t>(done + r) * vpr + i % vpr] = v[e];
+        for (int e = 0; e < 4; ++e) {
+          const int r = r0 + e * kThreads + tid;
+          if (r < rows) score_out[done + r] = v[e];
         }
       }
     }
-    __syncthreads();
+    __syncthreads();  // the slots take the place of the keys
+    move_rows(smem + tid * 16, src + static_cast<int64_t>(w0) * p.row_bytes, dst + static_cast<int64_t>(done) * p.row_bytes,
+              sc.list, lead, rows, shift, __ffs(p.row_bytes) - 1, p.parts == 1 ? tid - x * movers : tid, movers, 1 + x,
+              p.in_place != 0);
+    __syncthreads();  // the list is read
     done += rows;
   }
   if (idx)
@@ -217,11 +393,10 @@ adt_status adt_kv_evict(const adt_bf16* k_src, const adt_bf16* v_src, int64_t sr
   adt::TraceRange trace_("adt_kv_evict");
   ADT_REQUIRE(k_src && v_src && score && kv_len && k_dst && v_dst);
   ADT_REQUIRE(B >= 1 && B <= 65535 && Hkv >= 1 && Hkv <= 65535 && num_layers >= 1 && num_layers <= 65535);
-  ADT_REQUIRE(max_kv >= 1 && budget >= 1 && n_sink >= 0 && n_recent >= 0 &&
+  ADT_REQUIRE(max_kv >= 1 && max_kv < (1 << 30) && budget >= 1 && n_sink >= 0 && n_recent >= 0 &&
               static_cast<int64_t>(n_sink) + n_recent <= budget);
   ADT_REQUIRE(kv_len_out != kv_len);
   if (D != 64 && D != 128) return ADT_ERR_UNSUPPORTED;
-  if (max_kv > kMaxRows) return ADT_ERR_UNSUPPORTED;
   const int64_t keep = max_kv < budget ? max_kv : budget;  // rows that a destination slice holds
   const int64_t counts[3] = {num_layers, B, Hkv};
   const int64_t ss[3] = {src_layer_stride, src_stride_b, src_stride_h};
@@ -258,10 +433,10 @@ adt_status adt_kv_evict(const adt_bf16* k_src, const adt_bf16* v_src, int64_t sr
   adt_status st = adt::device_info(&info);
   if (st != ADT_OK) return st;
   EvictParams p{};
-  p.src[0] = reinterpret_cast<const uint4*>(k_src);
-  p.src[1] = reinterpret_cast<const uint4*>(v_src);
-  p.dst[0] = reinterpret_cast<uint4*>(k_dst);
-  p.dst[1] = reinterpret_cast<uint4*>(v_dst);
+  p.src[0] = reinterpret_cast<const uint8_t*>(k_src);
+  p.src[1] = reinterpret_cast<const uint8_t*>(v_src);
+  p.dst[0] = reinterpret_cast<uint8_t*>(k_dst);
+  p.dst[1] = reinterpret_cast<uint8_t*>(v_dst);
   p.score = score;
   p.score_out = score_out;
   p.kv_len = kv_len;
@@ -269,35 +444,45 @@ adt_status adt_kv_evict(const adt_bf16* k_src, const adt_bf16* v_src, int64_t sr
   p.keep_idx = keep_idx;
   p.B = B;
   p.Hkv = Hkv;
-  p.D = D;
   p.max_kv = max_kv;
   p.budget = budget;
   p.n_sink = n_sink;
   p.n_recent = n_recent;
   p.in_place = in_place;
-  p.sls = ss[0], p.ssb = ss[1], p.ssh = ss[2];
-  p.dls = ds[0], p.dsb = ds[1], p.dsh = ds[2];
+  p.sls = 2 * ss[0], p.ssb = 2 * ss[1], p.ssh = 2 * ss[2];
+  p.dls = 2 * ds[0], p.dsb = 2 * ds[1], p.dsh = 2 * ds[2];
   p.cls = cs[0], p.csb = cs[1], p.csh = cs[2];
   p.ols = os[0], p.osb = os[1], p.osh = os[2];
   p.err = info.error_word;
-  const size_t smem = static_cast<size_t>((max_kv + 31) / 32) * 4;
-  if (smem > 8 * 1024) {  // with the static part, past what needs no opt-in
-    static unsigned configured[2] = {0u, 0u};  // bit per device (< 64)
-    const unsigned bit = 1u << (info.device & 31);
-    unsigned& word = configured[(info.device >> 5) & 1];
-    if (!(__atomic_load_n(&word, __ATOMIC_ACQUIRE) & bit)) {
-      ADT_CUDA_TRY(cudaFuncSetAttribute(kv_evict_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxRows / 8));
-      __atomic_fetch_or(&word, bit, __ATOMIC_ACQ_REL);
-    }
+  p.row_bytes = D * 2;
+  // Few slices: K and V, then shares of their columns (32 bytes of a row at
+  // least) by CTAs of their own, until every SM has one.  Each selects the rows
+  // anew, and rows in pieces cost the memory more, so not beyond.  us with this
+  // rule, with one CTA a slice, and with a CTA more an SM: 8 heads, 576 rows of
+  // 64 6.0, 7.6, 5.9; 8 heads, 2400 rows of 128 9.4, 19.0, 9.4; 128 slices 33.2,
+  // 37.4, 36.5; 256 slices 77.2, 77.2, 87.2.
+  p.parts = 1;
+  while (p.parts < 8 && slices * p.parts < info.sm_count) p.parts *= 2;
+  static unsigned configured[2] = {0u, 0u};  // bit per device (< 64)
+  const unsigned bit = 1u << (info.device & 31);
+  unsigned& word = configured[(info.device >> 5) & 1];
+  if (!(__atomic_load_n(&word, __ATOMIC_ACQUIRE) & bit)) {  // 48.1 KB with the static part
+    ADT_CUDA_TRY(cudaFuncSetAttribute(kv_evict_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSlotBytes));
+    __atomic_fetch_or(&word, bit, __ATOMIC_ACQ_REL);
   }
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(slices), 1, 1);
+  cfg.gridDim = dim3(static_cast<unsigned>(slices * p.parts), 1, 1);
   cfg.blockDim = dim3(kThreads, 1, 1);
-  cfg.dynamicSmemBytes = smem;
+  cfg.dynamicSmemBytes = kSlotBytes;
   cfg.stream = adt::as_stream(stream);
-  cudaLaunchAttribute attr[1] = {adt::pdl_attribute()};
+  cudaLaunchAttribute attr[2];
+  attr[0] = adt::pdl_attribute();
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = static_cast<unsigned>(p.parts);
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = p.parts > 1 ? 2 : 1;
   ADT_CUDA_TRY(cudaLaunchKernelEx(&cfg, kv_evict_kernel, p));
   return adt::launch_status();
 }

@@ -120,7 +120,7 @@ def _evict_args():
     (dict(Hkv=0), INVALID), (dict(layers=0), INVALID), (dict(max_kv=0), INVALID), (dict(budget=0), INVALID),
     (dict(sink=-1), INVALID), (dict(recent=-1), INVALID), (dict(sink=30, recent=21), INVALID),
     (dict(sink=2 ** 31 - 1, recent=2 ** 31 - 1), INVALID), (dict(D=80), UNSUPPORTED),
-    (dict(max_kv=(1 << 20) + 1, budget=50), UNSUPPORTED), (dict(ssh=6399), INVALID), (dict(ssh=6300), INVALID),
+    (dict(max_kv=1 << 30, budget=50), INVALID), (dict(ssh=6399), INVALID), (dict(ssh=6300), INVALID),
     (dict(csh=99), INVALID), (dict(ko=P[6], vo=P[7], dsh=3199), INVALID), (dict(ko=P[6], vo=P[7], osh=49), INVALID),
     (dict(k=ctypes.c_void_p(8)), INVALID),
     (dict(ko=P[6]), INVALID),                              # K elsewhere, V in place
