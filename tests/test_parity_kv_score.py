@@ -215,3 +215,28 @@ def test_score_in_a_graph_on_another_stream():
     for _ in range(2):
         graph.replay()
         assert torch.equal(replayed, out)
+
+
+@pytest.mark.parametrize("D,paths", [(64, [[0, 1], [0]]), (128, [chain(130), chain(40)])])
+def test_score_wait_that_runs_out_is_reported(D, paths):
+    """Waits limited to one poll give up, the kernel leaves in order, and the next call is right."""
+    c = Case(6, 4, 2, D, [700, 1300], paths, 140, seed=17)
+    args = c.args()
+    B.adt_get_device_error()
+    B.adt_testing_set_wait_limit(1)
+    try:
+        B.adt_kv_score(*args, **c.kw())
+        assert B.adt_get_device_error() & B.DEVERR_TIMEOUT
+    finally:
+        B.adt_testing_set_wait_limit(0)
+    c.check(c.run())
+    assert B.adt_get_device_error() == 0
+
+
+@pytest.mark.parametrize("kv,paths", [
+    ([0, 2000, 1, 5, 900, 0, 129, 40], [chain(n) for n in (1, 3, 1, 130, 2, 1, 1, 9)]),    # short trees beside long ones
+    ([37] * 70, [chain(1 + b % 4) for b in range(70)]),                                    # more trees than a warp has lanes
+])
+def test_score_deals_uneven_trees(kv, paths):
+    c = Case(3, 4, 2, 64, kv, paths, 140, seed=18)
+    c.check(c.run())
