@@ -6,6 +6,11 @@
 // its fraction goes on to fp32: at t = 10^6 the angle of a pair with f = 1 has
 // 20 bits before the point, so that in fp32 the cosine would be off by 0.03.
 //
+// Bound by HBM where there are many tokens: 16384 of 32 / 32 heads x 128 124 us
+// for 805 MB (119 at the measured copy rate); 4096 of 32 / 8 heads 20.4 us for 101
+// MB (14.9; the angles' 64-bit chain is a fifth of a CTA's time there), 26.2 with
+// one unit a thread; and by a launch (2 us) up to about 300.
+//
 // A CTA takes one token or a few (and, where there are few tokens, a share of
 // their heads): one thread a pair makes the cosines and sines once, in shared
 // memory, and every head of the token uses them.
@@ -36,7 +41,7 @@ __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162flo
 // Cosines and sines of `tokens` tokens from n0 on, m included.
 __device__ __forceinline__ void token_angles(const RopeParams& p, int n0, int tokens, float2* cs) {
   const int half = p.rot / 2;
-  for (int i = threadIdx.x; i < half * tokens; i += kThreads) {
+  for (int i = threadIdx.x; i < half * tokens; i += blockDim.x) {
     const int t = tokens == 1 ? 0 : i / half;
     double turns = static_cast<double>(p.pos[n0 + t]) * (1.0 / kTwoPi) * p.inv_freq[i - t * half];
     turns -= rint(turns);
@@ -187,8 +192,88 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3)
   }
 }
 
+// Rotary sizes whose vectors would hold parts of both halves, or turned and
+// copied elements: heads go through shared memory in fp32, loaded as vectors, and
+// a thread takes two neighbouring elements with their partners, wherever they
+// lie, at a time (4-byte stores of a warp are a row's 128 bytes).  Straight from
+// global memory one element at a time 4096 tokens of 32 / 8 heads x 128 with 50
+// turned took 56 us, so 36.
+constexpr int kStaged = 4096;  // elements: 16 KB
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads) rope_staged_kernel(const RopeParams p, int group) {
+  extern __shared__ float2 shared[];
+  constexpr int kBatch = 4;
+  float2* cs = shared;
+  float* rows = reinterpret_cast<float*>(shared + ((p.rot / 2 + 1) & ~1));
+  adt::pdl_wait_then_release();
+  const int64_t n = blockIdx.x;
+  const int half = p.rot / 2, heads = p.heads[0] + p.heads[1], vpr = p.D / 8;
+  const T* q = static_cast<const T*>(p.in[0]) + n * p.ld[0];
+  const T* k = static_cast<const T*>(p.in[1]) + n * p.ld[1];
+  auto head = [&](int h) { return h < p.heads[0] ? q + h * p.D : k + (h - p.heads[0]) * p.D; };
+  // Place within a head: of the vectors loaded, and of the elements turned.
+  const int lh = threadIdx.x / vpr, lv = threadIdx.x - lh * vpr, lstep = kThreads / vpr;
+  const int twos = p.D / 2, th = threadIdx.x / twos, e = 2 * (threadIdx.x - th * twos), tstep = kThreads / twos;
+  float c[2], s[2];  // y = x c + partner s
+  int partner[2];
+  for (int h0 = blockIdx.y * group; h0 < heads; h0 += gridDim.y * group) {
+    const int here = min(group, heads - h0);
+    for (int h = lh < lstep ? lh : here; h < here; h += kBatch * lstep) {
+      Eight<T> v[kBatch];
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k)
+        if (h + k * lstep < here) v[k].load(head(h0 + h + k * lstep) + lv * 8);
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        if (h + k * lstep >= here) break;
+        float x[8];
+        v[k].get(x);
+        float4* to = reinterpret_cast<float4*>(rows + (h + k * lstep) * p.D + lv * 8);
+        to[0] = make_float4(x[0], x[1], x[2], x[3]);
+        to[1] = make_float4(x[4], x[5], x[6], x[7]);
+      }
+    }
+    if (h0 == static_cast<int>(blockIdx.y) * group) {
+      token_angles(p, blockIdx.x, 1, cs);  // (ends with a barrier)
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        const int at = e + w, pair = p.interleaved ? at >> 1 : at < half ? at : at - half;
+        const bool turned = at < p.rot, first = p.interleaved ? w == 0 : at < half;
+        const float2 z = turned ? cs[pair] : make_float2(1.f, 0.f);
+        c[w] = z.x;
+        s[w] = first ? -z.y : z.y;
+        partner[w] = !turned ? at : p.interleaved ? at ^ 1 : first ? at + half : at - half;
+      }
+    } else {
+      __syncthreads();
+    }
+    for (int h = th < tstep ? th : here; h < here; h += tstep) {
+      const float* row = rows + h * p.D;
+      const float2 x = *reinterpret_cast<const float2*>(row + e);
+      // (A copied element is its own partner: not multiplied, it may be infinite.)
+      const float y0 = partner[0] == e ? x.x : x.x * c[0] + row[partner[0]] * s[0];
+      const float y1 = partner[1] == e + 1 ? x.y : x.y * c[1] + row[partner[1]] * s[1];
+      const int hh = h0 + h;
+      __nv_bfloat16* dst = hh < p.heads[0] ? p.out[0] + (n * p.heads[0] + hh) * p.D
+                                           : p.out[1] + (n * p.heads[1] + hh - p.heads[0]) * p.D;
+      *reinterpret_cast<__nv_bfloat162*>(dst + e) = __floats2bfloat162_rn(y0, y1);
+    }
+    __syncthreads();  // before the rows are overwritten
+  }
+  const T* in = static_cast<const T*>(p.in[2]) + n * p.ld[2];
+  __nv_bfloat16* out = p.out[2] + n * p.heads[2] * p.D;
+  for (int i = blockIdx.y * kThreads + threadIdx.x; i < p.heads[2] * vpr; i += gridDim.y * kThreads) {
+    Eight<T> v;
+    float x[8];
+    v.load(in + i * 8);
+    v.get(x);
+    put(out + i * 8, x);
+  }
+}
+
 // One pair or one copied element at a time: any even rotary_dim, any head
-// size, row stride and alignment.
+// size, row stride and alignment (the vectors' kernels are 2 to 3 times as fast).
 template <typename T>
 __global__ void __launch_bounds__(kThreads) rope_scalar_kernel(const RopeParams p) {
   __shared__ float2 cs[kMaxRotary / 2];
@@ -316,23 +401,31 @@ adt_status adt_rope_qkv(const void* q, int64_t ld_q, const void* k, int64_t ld_k
   // Vectors where everything lies on 16-byte boundaries and a vector never
   // holds both turned and copied elements, or parts of both halves.
   const int units = p.interleaved ? D / 8 : D / 8 - rotary_dim / 16;
-  bool vec = D % 8 == 0 && rotary_dim % (p.interleaved ? 8 : 16) == 0 && units <= kThreads;
+  bool aligned = D % 8 == 0;
   for (int x = 0; x < 3; ++x)
-    vec = vec && (!in[x] || (adt::aligned16(in[x]) && adt::aligned16(out[x]) && ld[x] * esize % 16 == 0));
+    aligned = aligned && (!in[x] || (adt::aligned16(in[x]) && adt::aligned16(out[x]) && ld[x] * esize % 16 == 0));
+  const bool vec = aligned && rotary_dim % (p.interleaved ? 8 : 16) == 0 && units <= kThreads;
   const int heads = p.heads[0] + p.heads[1];
   if (vec) {
-    // Threads of a token: a power of two that takes its heads, or its values' vectors, in one pass; tokens fill the CTA.
-    const int64_t want = static_cast<int64_t>(heads) * units > p.heads[2] * (D / 8) ? static_cast<int64_t>(heads) * units
-                                                                                    : p.heads[2] * (D / 8);
-    int lanes = 32;
-    while (lanes < kThreads && (lanes < want || lanes < units)) lanes *= 2;
+    // Threads of a token: enough for one unit of its heads and one vector of its
+    // values each, or where there are many tokens for two of each (what a thread
+    // has in flight at a time); tokens fill the CTA.
+    const int qk = heads * units, vs = p.heads[2] * (D / 8), want = qk > vs ? qk : vs;
+    auto lanes_of = [&](int each) {
+      int l = ((want + each - 1) / each + 31) / 32 * 32;
+      l = l < units ? (units + 31) / 32 * 32 : l;
+      return l < kThreads ? l : kThreads;
+    };
+    const bool many = static_cast<int64_t>(N) * lanes_of(2) >= int64_t{4} * kThreads * info.sm_count;
+    const int lanes = lanes_of(many ? 2 : 1);
     const int tokens = kThreads / lanes;
-    const int passes = static_cast<int>((want + lanes - 1) / lanes);
+    const int passes = (want + lanes - 1) / lanes;
     const int groups = (N + tokens - 1) / tokens;
     // Few tokens: their heads over several CTAs, up to two an SM.
     int split = 2 * info.sm_count / groups;
     split = split < 1 ? 1 : split > passes ? passes : split;
     cfg.gridDim = dim3(static_cast<unsigned>(groups), static_cast<unsigned>(split), 1);
+    cfg.blockDim = dim3(static_cast<unsigned>(lanes * tokens), 1, 1);
     cfg.dynamicSmemBytes = static_cast<size_t>(tokens) * (rotary_dim / 2) * sizeof(float2);
     if (esize == 2)
       ADT_CUDA_TRY(p.interleaved
@@ -341,6 +434,21 @@ adt_status adt_rope_qkv(const void* q, int64_t ld_q, const void* k, int64_t ld_k
     else
       ADT_CUDA_TRY(p.interleaved ? cudaLaunchKernelEx(&cfg, rope_vec_kernel<float, true>, p, N, tokens, lanes, units)
                                  : cudaLaunchKernelEx(&cfg, rope_vec_kernel<float, false>, p, N, tokens, lanes, units));
+    return adt::launch_status();
+  }
+  if (aligned && D <= 2 * kThreads) {
+    // Heads staged at a time: few enough that few tokens fill the SMs.
+    int group = kStaged / D;
+    while (group > 1 && static_cast<int64_t>(N) * ((heads + group - 1) / group) < info.sm_count) group = (group + 1) / 2;
+    int split = 2 * info.sm_count / N;
+    const int most = heads > 0 ? (heads + group - 1) / group : 1;
+    split = split < 1 ? 1 : split > most ? most : split;
+    cfg.gridDim = dim3(static_cast<unsigned>(N), static_cast<unsigned>(split), 1);
+    cfg.dynamicSmemBytes = ((rotary_dim / 2 + 1) & ~1) * sizeof(float2) + static_cast<size_t>(group < heads ? group : heads) * D * 4;
+    if (esize == 2)
+      ADT_CUDA_TRY(cudaLaunchKernelEx(&cfg, rope_staged_kernel<__nv_bfloat16>, p, group));
+    else
+      ADT_CUDA_TRY(cudaLaunchKernelEx(&cfg, rope_staged_kernel<float>, p, group));
     return adt::launch_status();
   }
   const int64_t most = static_cast<int64_t>(heads > p.heads[2] ? heads : p.heads[2]) * D;
