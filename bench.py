@@ -577,14 +577,16 @@ def cpu_sample_main(args):
 
 # ------------------------------------------------------------------ main
 
-def decode_measure(batch, grid, fp32=False, graphs=True):
+def decode_measure(batch, grid, fp32=False, graphs=True, kv_budget=0):
     """The end-to-end synthetic decode loop (random-init 7B-shape target and
     a one-layer EAGLE-style draft head, ADT-Tree trees every step) over a
     grid x grid image-token grid, timed as a whole, next to vanilla greedy
     decoding of the same target in plain torch (no library call; bf16
     scaled_dot_product_attention), teacher-forced with the tree decoder's
     tokens so that every emitted token is compared with the target's greedy
-    choice.  Returns a dict of the measurements."""
+    choice.  With a kv_budget the tree decoder's cache is bounded (the greedy
+    reference's is not, so that the tokens differ by what was evicted).
+    Returns a dict of the measurements."""
     import torch
     from paper_2512_21857_gb300 import binding as B
     from paper_2512_21857_gb300 import build
@@ -594,7 +596,7 @@ def decode_measure(batch, grid, fp32=False, graphs=True):
     shape = ModelShape(dtype=torch.float32) if fp32 else ModelShape()
     g = grid
     prompt = [int(x) for x in torch.randint(0, shape.vocab, (16,), generator=torch.Generator().manual_seed(7))]
-    dec = Decoder(shape, batch=batch, grid=(g, g), prompt_len=16, seed=2025, graphs=graphs)
+    dec = Decoder(shape, batch=batch, grid=(g, g), prompt_len=16, seed=2025, graphs=graphs, kv_budget=kv_budget)
     # warm-up: the same grid once (cuBLAS plans, library set-up, the CUDA
     # graph of every tree size the run meets), then the timed run
     dec.generate(prompt)
@@ -607,7 +609,8 @@ def decode_measure(batch, grid, fp32=False, graphs=True):
                                     attn_dtype=torch.bfloat16, forced=out)
     diff = [(b, i) for b in range(batch) for i in range(n) if out[b][i] != choice[b][i]]
     attn = decode_verify_attention(dec, prompt_len=16, n=n)
-    return {"tokens_per_s": st.tokens / st.seconds, "tau": st.tau, "accepted_draft_tokens": st.accepted,
+    extra = {"kv_budget": kv_budget, "target_cache_rows": dec.target.lmax} if kv_budget else {}
+    return extra | {"tokens_per_s": st.tokens / st.seconds, "tau": st.tau, "accepted_draft_tokens": st.accepted,
             "accepted_length_histogram": {str(k): v for k, v in sorted(st.accept_hist.items())},
             "verify_steps": st.steps, "mean_depth": st.mean_depth, "seconds": st.seconds,
             "vanilla_greedy_tokens_per_s": batch * n / t_van,
@@ -632,7 +635,7 @@ def decode_verify_attention(dec, prompt_len, n, reps=50):
     from paper_2512_21857_gb300 import synth
     tm, s = dec.target, dec.s
     Bn, N = dec.batch, 64
-    L = prompt_len + n
+    L = min(prompt_len + n, tm.lmax)
     tb = synth.tree_batch([N] * Bn, s.vocab, 2026)
     dev = tm.device
     g = torch.Generator(device=dev)
@@ -684,7 +687,7 @@ def decode_verify_attention(dec, prompt_len, n, reps=50):
 
 def run_decode(args):
     """bench.py --decode: one JSON line for the decode loop alone."""
-    d = decode_measure(args.decode_batch, args.decode_grid, args.decode_fp32, not args.decode_eager)
+    d = decode_measure(args.decode_batch, args.decode_grid, args.decode_fp32, not args.decode_eager, args.decode_budget)
     line = {"metric": "synthetic end-to-end decode tokens/s", "value": d.pop("tokens_per_s"), "unit": "tokens/s",
             "n_gpus": 1, "higher_is_better": True, "dtype": "bf16", "data": "synthetic (random-init weights)",
             "config": {"workload": d.pop("workload"), "batch": args.decode_batch, "dense_dtype": d.pop("dense_dtype"),
@@ -714,6 +717,7 @@ def main():
     ap.add_argument("--decode-batch", type=int, default=1)
     ap.add_argument("--decode-grid", type=int, default=48)
     ap.add_argument("--decode-fp32", action="store_true", help="fp32 weights and residual stream in the harness")
+    ap.add_argument("--decode-budget", type=int, default=0, help="rows of the target's cache to keep (0: all)")
     ap.add_argument("--decode-eager", action="store_true", help="no CUDA graphs in the decode loop")
     ap.add_argument("--no-decode", action="store_true", help="skip the decode-loop measurement of the default run")
     ap.add_argument("--bench-decode-grid", type=int, default=16,

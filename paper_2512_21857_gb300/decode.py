@@ -10,7 +10,15 @@ walk (`adt_tree_accept`), the K/V commits (`adt_kv_compact`) and the depth /
 width controller (`adt_ctrl_*`).  The dense parts of the two networks
 (embeddings, RMSNorm, the Q/K/V/O and SwiGLU projections, rotary position
 embedding, the LM head) are plain torch around it: the model, not the
-method.
+method.  With `ModelShape.rope` the library rotates instead (`adt_rope_qkv`:
+either pair layout, part of a head, frequencies scaled for long contexts), from
+the projection straight into attention's layout.
+
+With a `kv_budget` the target's cache is bounded: every commit adds the attention
+that its tokens paid to each cached row (`adt_kv_score`), and once a cache is
+`kv_slack` rows over the budget it is cut down to it (`adt_kv_evict`: the first
+rows, the last ones and those with the most attention).  A token's position is
+counted apart from the cache's length then.
 
 Draft head (EAGLE's feature-level draft): node u with token x_u and parent
 feature f (the target's last hidden state before the final norm for the
@@ -36,6 +44,16 @@ from . import binding as B
 
 
 @dataclass
+class RopeShape:
+    """Rotary positions by the library.  base: ModelShape.rope_theta."""
+    rotary_dim: int = 0        # elements of a head that are turned (0: all)
+    interleaved: bool = False  # pairs (2p, 2p + 1) instead of (p, p + rotary_dim / 2)
+    scaling: int = B.ROPE_NONE
+    factor: float = 1.0
+    orig_len: float = 0.0
+
+
+@dataclass
 class ModelShape:
     layers: int = 32
     hidden: int = 4096
@@ -49,6 +67,7 @@ class ModelShape:
     init_std: float = 0.02
     lm_std: float = 0.0        # LM head init std (0: init_std)
     dtype: torch.dtype = torch.bfloat16  # weights and residual stream (the caches and attention stay bf16)
+    rope: RopeShape | None = None        # None: rotate-half over the whole head, in torch
 
 
 def _rms_norm(x, w, eps):
@@ -65,6 +84,26 @@ def _rope(x, pos, theta):
     xf = x.float()
     x1, x2 = xf[..., : D // 2], xf[..., D // 2:]
     return torch.cat([x1 * cos - x2 * sin, x2 * cos + x1 * sin], -1).to(x.dtype)
+
+
+def _rope_table(shape: ModelShape, device):
+    """(inv_freq fp64 on the device, magnitude) of shape.rope."""
+    r = shape.rope
+    inv, magnitude = B.adt_rope_freqs(r.rotary_dim or shape.head_dim, theta=shape.rope_theta, scaling=r.scaling,
+                                      factor=r.factor, orig_len=r.orig_len)
+    return inv.to(device), magnitude
+
+
+def _rope_plain(x, pos, inv, magnitude, interleaved):
+    """shape.rope's rotation of x [N, heads, D] in torch, angles in fp64 (the reference model's)."""
+    R = 2 * inv.numel()
+    ang = pos.double()[:, None] * inv
+    cos, sin = (torch.cos(ang) * magnitude).float()[:, None], (torch.sin(ang) * magnitude).float()[:, None]
+    xf = x.float()
+    x1, x2 = (xf[..., 0:R:2], xf[..., 1:R:2]) if interleaved else (xf[..., :R // 2], xf[..., R // 2:R])
+    y1, y2 = x1 * cos - x2 * sin, x2 * cos + x1 * sin
+    y = torch.stack([y1, y2], -1).flatten(-2) if interleaved else torch.cat([y1, y2], -1)
+    return torch.cat([y, xf[..., R:]], -1).to(x.dtype)
 
 
 class DecoderWeights:
@@ -106,7 +145,7 @@ class TreeModel:
     attention through adt_tree_attn over each image's cache and tree."""
 
     def __init__(self, shape: ModelShape, weights: DecoderWeights, batch: int, lmax: int, max_nodes: int,
-                 device):
+                 device, keep_scores=False):
         s = self.s = shape
         self.w = weights
         self.lmax = lmax
@@ -118,6 +157,9 @@ class TreeModel:
         self.ws = B.zeroed_workspace(B.adt_tree_attn_workspace_size(batch, s.heads, s.head_dim, max_nodes, lmax),
                                      device)
         self.device = device
+        self.rope = _rope_table(s, device) if s.rope else None
+        # attention that each cached row got so far (keep_scores: forward() also returns what scores() needs)
+        self.score = torch.zeros((L, batch, s.kv_heads, lmax), dtype=torch.float32, device=device) if keep_scores else None
         self.graphs_enabled = False
         self._graphs = {}
 
@@ -125,10 +167,16 @@ class TreeModel:
         """x [N, hidden] (bf16) for the nodes of `batch` trees (of image
         `image` alone when given: its cache slice, batch 1); returns the final
         hidden states [N, hidden] and each layer's tree K/V ([layers, N,
-        kv_heads, D]) for the commit."""
+        kv_heads, D]) for the commit; with keep_scores also every layer's
+        queries and their lse."""
         s = self.s
         N = x.shape[0]
         L = len(self.w.layers)
+        keep = self.score is not None
+        qs = None
+        if keep or self.rope is not None:
+            qs = torch.empty((L if keep else 1, N, s.heads, s.head_dim), dtype=torch.bfloat16, device=self.device)
+        lse = torch.empty((L, N, s.heads), dtype=torch.float32, device=self.device) if keep else None
         k_tree = torch.empty((L, N, s.kv_heads, s.head_dim), dtype=torch.bfloat16, device=self.device)
         v_tree = torch.empty_like(k_tree)
         out = torch.empty((N, s.heads, s.head_dim), dtype=torch.bfloat16, device=self.device)
@@ -137,19 +185,28 @@ class TreeModel:
         for li, lw in enumerate(self.w.layers):
             h = _rms_norm(x, lw["ln1"], s.eps)
             qkv = h @ lw["wqkv"]
-            q = _rope(qkv[:, :hq].view(N, s.heads, s.head_dim), pos, s.rope_theta).to(torch.bfloat16).contiguous()
-            k_tree[li] = _rope(qkv[:, hq:hq + hk].view(N, s.kv_heads, s.head_dim), pos, s.rope_theta)
-            v_tree[li] = qkv[:, hq + hk:].view(N, s.kv_heads, s.head_dim)
+            if self.rope is None:
+                q = _rope(qkv[:, :hq].view(N, s.heads, s.head_dim), pos, s.rope_theta).to(torch.bfloat16).contiguous()
+                k_tree[li] = _rope(qkv[:, hq:hq + hk].view(N, s.kv_heads, s.head_dim), pos, s.rope_theta)
+                v_tree[li] = qkv[:, hq + hk:].view(N, s.kv_heads, s.head_dim)
+                if keep:
+                    qs[li] = q
+            else:
+                q = qs[li if keep else 0]
+                B.adt_rope_qkv(qkv[:, :hq], qkv[:, hq:hq + hk], qkv[:, hq + hk:], pos, self.rope[0], H=s.heads,
+                               Hkv=s.kv_heads, D=s.head_dim,
+                               layout=B.ROPE_INTERLEAVED if s.rope.interleaved else B.ROPE_HALF,
+                               magnitude=self.rope[1], q_out=q, k_out=k_tree[li], v_out=v_tree[li])
             B.adt_tree_attn(q, self.k_cache[li, sl], self.v_cache[li, sl], kv_len, k_tree[li], v_tree[li], parents,
                             node_offsets, B=batch, H=s.heads, Hkv=s.kv_heads, D=s.head_dim,
                             max_nodes=self.max_nodes, max_kv=self.lmax, softmax_scale=s.head_dim ** -0.5, out=out,
-                            workspace=self.ws, cache_stride_b=self.k_cache.stride(1),
+                            lse=lse[li] if keep else None, workspace=self.ws, cache_stride_b=self.k_cache.stride(1),
                             cache_stride_h=self.k_cache.stride(2))
             x = x + out.view(N, hq).to(x.dtype) @ lw["wo"]
             h = _rms_norm(x, lw["ln2"], s.eps)
             gu = h @ lw["wgu"]
             x = x + (torch.nn.functional.silu(gu[:, : s.ffn].float()) * gu[:, s.ffn:].float()).to(x.dtype) @ lw["wd"]
-        return x, k_tree, v_tree
+        return (x, k_tree, v_tree, qs, lse) if keep else (x, k_tree, v_tree)
 
     def run(self, x, pos, parents, node_offsets, kv_len, batch, image=None):
         """forward() through a CUDA graph captured once per (nodes, batch,
@@ -184,6 +241,17 @@ class TreeModel:
                          cache_layer_stride=self.k_cache.stride(0), cache_stride_b=self.k_cache.stride(1),
                          cache_stride_h=self.k_cache.stride(2), tree_layer_stride=k_tree.stride(0))
 
+    def scores(self, qs, lse, kv_len, node_offsets, path, max_path, accept_len, batch):
+        """Adds the attention of the tokens just committed (kv_len: before them) to the rows' scores."""
+        B.adt_kv_score(qs, lse, self.k_cache, kv_len, node_offsets, path, max_path, accept_len, self.score, B=batch,
+                       H=self.s.heads, Hkv=self.s.kv_heads, D=self.s.head_dim, num_layers=len(self.w.layers),
+                       max_kv=self.lmax, softmax_scale=self.s.head_dim ** -0.5)
+
+    def evict(self, kv_len, kv_len_out, batch, budget, n_sink, n_recent):
+        """Cuts every image's cache down to `budget` rows, in place."""
+        B.adt_kv_evict(self.k_cache, self.v_cache, self.score, kv_len, kv_len_out, B=batch, Hkv=self.s.kv_heads,
+                       D=self.s.head_dim, num_layers=len(self.w.layers), max_kv=self.lmax, budget=budget, n_sink=n_sink,
+                       n_recent=n_recent)
 
     def commit_one(self, b, k_tree, v_tree, kv_len, kv_len_out, offs, path, max_path, accept_len):
         B.adt_kv_compact(self.k_cache[:, b:b + 1], self.v_cache[:, b:b + 1], kv_len, kv_len_out, k_tree, v_tree, offs,
@@ -222,16 +290,28 @@ class Decoder:
     tokens after a prompt (the same prompt for every image)."""
 
     def __init__(self, shape: ModelShape, *, batch=1, grid=(48, 48), prompt_len=16, seed=2025, device="cuda",
-                 max_nodes=64, ctrl_params=None, draft_equals_target=False, target=None, graphs=False):
+                 max_nodes=64, ctrl_params=None, draft_equals_target=False, target=None, graphs=False, kv_budget=0,
+                 kv_slack=64, kv_sink=4, kv_recent=64):
         s = self.s = shape
         self.batch, self.grid, self.prompt_len = batch, grid, prompt_len
         self.device = device
         self.max_nodes = max_nodes
         n_img = grid[0] * grid[1]
         self.lmax = prompt_len + n_img + 16
+        self.ctrl_params = dict(ctrl_params or {})
+        self.ctrl_params.setdefault("d_lo", 1)
+        self.ctrl_params.setdefault("d_hi", 9)
+        self.kv_budget, self.kv_slack = kv_budget, kv_slack
+        self.kv_keep = dict(n_sink=min(kv_sink, kv_budget // 2), n_recent=min(kv_recent, kv_budget // 2))
+        target_rows = self.lmax
+        if kv_budget:  # the target's cache holds the budget, the slack and one step's path
+            if kv_budget < 1 or kv_slack < 0:
+                raise ValueError("kv_budget >= 1 and kv_slack >= 0")
+            self.d_most = max(self.ctrl_params["d_hi"], self.ctrl_params.get("fix_d", 0))
+            target_rows = min(self.lmax, max(prompt_len, kv_budget + kv_slack) + self.d_most + 1)
         tw = target if target is not None else DecoderWeights(s, s.layers, seed, device)
         self.target_w = tw
-        self.target = TreeModel(s, tw, batch, self.lmax, max_nodes, device)
+        self.target = TreeModel(s, tw, batch, target_rows, max_nodes, device, keep_scores=kv_budget > 0)
         # draft head: fc + one layer, sharing the target's embedding, norm and LM head
         if draft_equals_target:
             # a draft that reproduces a one-layer target exactly: fc passes the
@@ -245,9 +325,6 @@ class Decoder:
         self.draft_w = dw
         self.draft = TreeModel(s, dw, batch, self.lmax, 256, device)
         self.target.graphs_enabled = self.draft.graphs_enabled = graphs
-        self.ctrl_params = dict(ctrl_params or {})
-        self.ctrl_params.setdefault("d_lo", 1)
-        self.ctrl_params.setdefault("d_hi", 9)
         self.k_max = self.ctrl_params.get("k_hi", 13)
         self.ws_expand = B.zeroed_workspace(B.adt_tree_expand_workspace_size(self.k_max, s.vocab, self.k_max), device)
         self.ws_rerank = B.zeroed_workspace(B.adt_tree_rerank_workspace_size(self._pool_cap()), device)
@@ -280,18 +357,23 @@ class Decoder:
         offs = self._i32([b * n for b in range(Bn + 1)])
         zero = self._i32([0] * Bn)
         pos = torch.arange(n, device=dev, dtype=torch.int32).repeat(Bn)
-        h, kt, vt = self.target.run(self._embed(tok), pos, par, offs, zero, Bn)
+        if self.target.score is not None:
+            self.target.score.zero_()
+        h, kt, vt, *seen = self.target.run(self._embed(tok), pos, par, offs, zero, Bn)
         path = torch.arange(n, dtype=torch.int32, device=dev).repeat(Bn, 1).contiguous()
         alen = self._i32([n - 1] * Bn)
         kv_out = torch.empty(Bn, dtype=torch.int32, device=dev)
         self.target.commit(kt, vt, zero, kv_out, offs, path, n, alen, Bn)
+        if seen:
+            self.target.scores(*seen, zero, offs, path, n, alen, Bn)
         feats = h.view(Bn, n, s.hidden)
         zf = torch.zeros(s.hidden, dtype=s.dtype, device=dev)
         state = []
         for b in range(Bn):
             # the draft catches up on prompt[:-1]: parent features f_{t-1} (zeros for t = 0)
             pf = torch.cat([zf[None], feats[b, :-1]], 0)
-            state.append(dict(kv=n, dkv=0, root=int(prompt[-1]), root_pf=feats[b, -1].clone(),
+            # kv: rows of the target's cache; seq: tokens committed, the next one's position
+            state.append(dict(kv=n, seq=n, dkv=0, root=int(prompt[-1]), root_pf=feats[b, -1].clone(),
                               catch_tok=list(prompt[:-1]),
                               catch_pf=pf, pos=0))
         return state
@@ -384,8 +466,8 @@ class Decoder:
         tok = torch.cat([t["tokens"] for t in trees])
         par = torch.cat([t["parents"] for t in trees])
         kv = self._i32([st["kv"] for st in state])
-        pos = torch.cat([t["depth"] + st["kv"] for t, st in zip(trees, state)])
-        h, kt, vt = self.target.run(self._embed(tok), pos, par, offs, kv, Bn)
+        pos = torch.cat([t["depth"] + st["seq"] for t, st in zip(trees, state)])
+        h, kt, vt, *seen = self.target.run(self._embed(tok), pos, par, offs, kv, Bn)
         logits = self._logits(h).contiguous()
         max_path = max(d for d, _ in dk) + 1
         path = torch.full((Bn, max_path), -1, dtype=torch.int32, device=dev)
@@ -395,6 +477,8 @@ class Decoder:
                           mode=B.ACCEPT_GREEDY, path=path, max_path=max_path, accept_len=alen, bonus_token=bonus)
         kv_out = torch.empty(Bn, dtype=torch.int32, device=dev)
         self.target.commit(kt, vt, kv, kv_out, offs, path, max_path, alen, Bn)
+        if seen:
+            self.target.scores(*seen, kv, offs, path, max_path, alen, Bn)
         # one host read per step: the path decides the next trees
         path_h, alen_h, bonus_h = path.cpu().tolist(), alen.cpu().tolist(), bonus.cpu().tolist()
         emitted = []
@@ -415,7 +499,12 @@ class Decoder:
             st["root"] = bonus_h[b]
             st["root_pf"] = h[idx[-1]].clone()
             st["kv"] += a + 1
+            st["seq"] += a + 1
             st["pos"] += len(new)
+        if seen and any(st["kv"] > self.kv_budget + self.kv_slack for st in state):
+            self.target.evict(kv_out, None, Bn, self.kv_budget, **self.kv_keep)
+            for st in state:
+                st["kv"] = min(st["kv"], self.kv_budget)
         return emitted, dk, alen_h
 
     def generate(self, prompt, ctrl_params=None):
@@ -425,6 +514,8 @@ class Decoder:
         params = dict(self.ctrl_params)
         if ctrl_params:
             params.update(ctrl_params)
+        if self.kv_budget and max(params["d_hi"], params.get("fix_d", 0)) > self.d_most:
+            raise ValueError("with a kv_budget the deepest tree is fixed by the Decoder's ctrl_params")
         ctrls = [B.Controller(*self.grid, **dict(params, seed=params.get("seed", 0) + b)) for b in range(self.batch)]
         torch.cuda.synchronize()
         t0 = time.perf_counter()
@@ -469,6 +560,7 @@ class DenseModel:
         self.v_cache = torch.zeros((L, batch, s.kv_heads, lmax, s.head_dim), **bf)
         self.keys = torch.arange(lmax, device=device)
         self.device = device
+        self.rope = _rope_table(shape, device) if shape.rope else None
 
     def forward(self, x, start):
         """x [batch, n, hidden]: n new tokens per image at positions start ..
@@ -481,11 +573,15 @@ class DenseModel:
         rows = pos.repeat(Bn)
         visible = self.keys[None, :] <= pos[:, None]          # [n, lmax]: causal over the cache
         group = s.heads // s.kv_heads
+
+        def turn(y):
+            return _rope(y, rows, s.rope_theta) if self.rope is None else _rope_plain(y, rows, *self.rope, s.rope.interleaved)
+
         for li, lw in enumerate(self.w.layers):
             h = _rms_norm(x, lw["ln1"], s.eps).view(Bn * n, -1)
             qkv = h @ lw["wqkv"]
-            q = _rope(qkv[:, :hq].view(Bn * n, s.heads, s.head_dim), rows, s.rope_theta).to(torch.bfloat16)
-            k = _rope(qkv[:, hq:hq + hk].view(Bn * n, s.kv_heads, s.head_dim), rows, s.rope_theta).to(torch.bfloat16)
+            q = turn(qkv[:, :hq].view(Bn * n, s.heads, s.head_dim)).to(torch.bfloat16)
+            k = turn(qkv[:, hq:hq + hk].view(Bn * n, s.kv_heads, s.head_dim)).to(torch.bfloat16)
             v = qkv[:, hq + hk:].view(Bn * n, s.kv_heads, s.head_dim).to(torch.bfloat16)
             self.k_cache[li].index_copy_(2, pos, k.view(Bn, n, s.kv_heads, s.head_dim).transpose(1, 2))
             self.v_cache[li].index_copy_(2, pos, v.view(Bn, n, s.kv_heads, s.head_dim).transpose(1, 2))

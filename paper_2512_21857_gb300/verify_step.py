@@ -8,7 +8,10 @@ A step, for each image b of a batch (Sec. 3.1, Fig. 5, Eq. 4):
   3. for every transformer layer, adt_tree_attn attends the n_b nodes over
      the prefix KV cache and their ancestors;
   4. adt_tree_accept walks each tree (greedy or speculative sampling);
-  5. adt_kv_compact commits the accepted path's K/V for all layers.
+  5. adt_kv_compact commits the accepted path's K/V for all layers;
+  6. with a kv_budget, adt_kv_score adds up the attention that the committed
+     tokens paid to each cached row, and adt_kv_evict cuts caches over the
+     budget down to it.
 Tree shapes (d_b, k_b) are host decisions (the controller, Sec. 4), so all
 launch shapes are known on the host and the whole step can be captured in a
 CUDA graph.  The images' draft phases (1-2) are independent chains of small,
@@ -41,6 +44,9 @@ class StepShape:
     lmax: int = 0         # cache capacity per image (default: max kv_len + max_nodes)
     mode: int = B.ACCEPT_GREEDY
     temperature: float = 1.0
+    kv_budget: int = 0    # rows that a cache keeps (0: all); the first kv_sink and the last kv_recent among them
+    kv_sink: int = 0
+    kv_recent: int = 0
 
     @property
     def batch(self):
@@ -117,6 +123,10 @@ class TreeVerifyStep:
         self.accept_len = torch.zeros(Bn, **i32)
         self.bonus = torch.zeros(Bn, **i32)
         self.kv_len_out = torch.zeros(Bn, **i32)
+        if s.kv_budget:
+            self.lse = torch.zeros((s.layers, self.ntot, s.H), **f32)
+            self.score = torch.zeros((s.layers, Bn, s.Hkv, self.lmax), **f32)
+            self.kv_len_kept = torch.zeros(Bn, **i32)  # rows after the eviction
         # workspaces (zero-filled once; the library leaves its counters at
         # zero); one expand and one rerank workspace per image's draft chain
         self.ws_expand = [B.zeroed_workspace(max(B.adt_tree_expand_workspace_size(kmax, s.V, kmax), 16), dev)
@@ -198,7 +208,8 @@ class TreeVerifyStep:
         B.adt_tree_attn(self.q[layer], kc, self.v_cache[layer], self.kv_len, self.k_tree[layer],
                         self.v_tree[layer], self.parents, self.node_offsets, B=s.batch, H=s.H, Hkv=s.Hkv,
                         D=s.D, max_nodes=s.max_nodes, max_kv=self.lmax, softmax_scale=s.D ** -0.5,
-                        out=self.attn_out[layer if self.keep_layer_outputs else 0], lse=None,
+                        out=self.attn_out[layer if self.keep_layer_outputs else 0],
+                        lse=self.lse[layer] if s.kv_budget else None,
                         workspace=self.ws_attn, stream=stream)
 
     def launch_verify(self, stream=None):
@@ -214,12 +225,24 @@ class TreeVerifyStep:
                          cache_stride_h=self.k_cache.stride(2), tree_layer_stride=self.k_tree.stride(0),
                          stream=stream)
 
+    def launch_evict(self, stream=None):
+        """Scores of the committed tokens' attention, then the eviction down to the budget (kv_len_kept rows)."""
+        s = self.shape
+        B.adt_kv_score(self.q, self.lse, self.k_cache, self.kv_len, self.node_offsets, self.path, self.max_path,
+                       self.accept_len, self.score, B=s.batch, H=s.H, Hkv=s.Hkv, D=s.D, num_layers=s.layers,
+                       max_kv=self.lmax, softmax_scale=s.D ** -0.5, stream=stream)
+        B.adt_kv_evict(self.k_cache, self.v_cache, self.score, self.kv_len_out, self.kv_len_kept, B=s.batch, Hkv=s.Hkv,
+                       D=s.D, num_layers=s.layers, max_kv=self.lmax, budget=s.kv_budget, n_sink=s.kv_sink,
+                       n_recent=s.kv_recent, stream=stream)
+
     def launch(self, stream=None):
-        """The whole step: draft growth, attention over every layer, accept, commit."""
+        """The whole step: draft growth, attention over every layer, accept, commit, eviction."""
         self.launch_draft(stream)
         for layer in range(self.shape.layers):
             self.launch_attention(layer, stream)
         self.launch_verify(stream)
+        if self.shape.kv_budget:
+            self.launch_evict(stream)
 
     def load_inputs(self, inp):
         """Copies a dict of host inputs (see synth.step_inputs) into the step's
@@ -234,7 +257,7 @@ class TreeVerifyStep:
 
     def kernel_launches_per_step(self):
         s = self.shape
-        return sum(s.depth) + s.batch + s.layers + 2
+        return sum(s.depth) + s.batch + s.layers + 2 + (2 if s.kv_budget else 0)
 
     def algorithmic_bytes(self):
         """Bytes the step must move at minimum (reads + writes)."""
