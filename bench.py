@@ -577,7 +577,7 @@ def cpu_sample_main(args):
 
 # ------------------------------------------------------------------ main
 
-def decode_measure(batch, grid, fp32=False, graphs=True, kv_budget=0):
+def decode_measure(batch, grid, fp32=False, graphs=True, kv_budget=0, library_rope=False):
     """The end-to-end synthetic decode loop (random-init 7B-shape target and
     a one-layer EAGLE-style draft head, ADT-Tree trees every step) over a
     grid x grid image-token grid, timed as a whole, next to vanilla greedy
@@ -585,15 +585,16 @@ def decode_measure(batch, grid, fp32=False, graphs=True, kv_budget=0):
     scaled_dot_product_attention), teacher-forced with the tree decoder's
     tokens so that every emitted token is compared with the target's greedy
     choice.  With a kv_budget the tree decoder's cache is bounded (the greedy
-    reference's is not, so that the tokens differ by what was evicted).
+    reference's is not, so that the tokens differ by what was evicted); with
+    library_rope the library rotates.
     Returns a dict of the measurements."""
     import torch
     from paper_2512_21857_gb300 import binding as B
     from paper_2512_21857_gb300 import build
-    from paper_2512_21857_gb300.decode import Decoder, ModelShape, greedy_decode
+    from paper_2512_21857_gb300.decode import Decoder, ModelShape, RopeShape, greedy_decode
     build.build()
     B.lib()
-    shape = ModelShape(dtype=torch.float32) if fp32 else ModelShape()
+    shape = ModelShape(dtype=torch.float32 if fp32 else torch.bfloat16, rope=RopeShape() if library_rope else None)
     g = grid
     prompt = [int(x) for x in torch.randint(0, shape.vocab, (16,), generator=torch.Generator().manual_seed(7))]
     dec = Decoder(shape, batch=batch, grid=(g, g), prompt_len=16, seed=2025, graphs=graphs, kv_budget=kv_budget)
@@ -610,6 +611,7 @@ def decode_measure(batch, grid, fp32=False, graphs=True, kv_budget=0):
     diff = [(b, i) for b in range(batch) for i in range(n) if out[b][i] != choice[b][i]]
     attn = decode_verify_attention(dec, prompt_len=16, n=n)
     extra = {"kv_budget": kv_budget, "target_cache_rows": dec.target.lmax} if kv_budget else {}
+    extra |= {"rotation": "library"} if library_rope else {}
     return extra | {"tokens_per_s": st.tokens / st.seconds, "tau": st.tau, "accepted_draft_tokens": st.accepted,
             "accepted_length_histogram": {str(k): v for k, v in sorted(st.accept_hist.items())},
             "verify_steps": st.steps, "mean_depth": st.mean_depth, "seconds": st.seconds,
@@ -687,7 +689,8 @@ def decode_verify_attention(dec, prompt_len, n, reps=50):
 
 def run_decode(args):
     """bench.py --decode: one JSON line for the decode loop alone."""
-    d = decode_measure(args.decode_batch, args.decode_grid, args.decode_fp32, not args.decode_eager, args.decode_budget)
+    d = decode_measure(args.decode_batch, args.decode_grid, args.decode_fp32, not args.decode_eager, args.decode_budget,
+                       args.decode_rope)
     line = {"metric": "synthetic end-to-end decode tokens/s", "value": d.pop("tokens_per_s"), "unit": "tokens/s",
             "n_gpus": 1, "higher_is_better": True, "dtype": "bf16", "data": "synthetic (random-init weights)",
             "config": {"workload": d.pop("workload"), "batch": args.decode_batch, "dense_dtype": d.pop("dense_dtype"),
@@ -718,6 +721,7 @@ def main():
     ap.add_argument("--decode-grid", type=int, default=48)
     ap.add_argument("--decode-fp32", action="store_true", help="fp32 weights and residual stream in the harness")
     ap.add_argument("--decode-budget", type=int, default=0, help="rows of the target's cache to keep (0: all)")
+    ap.add_argument("--decode-rope", action="store_true", help="rotary positions by the library in the decode loop")
     ap.add_argument("--decode-eager", action="store_true", help="no CUDA graphs in the decode loop")
     ap.add_argument("--no-decode", action="store_true", help="skip the decode-loop measurement of the default run")
     ap.add_argument("--bench-decode-grid", type=int, default=16,
