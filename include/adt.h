@@ -108,14 +108,14 @@ adt_status adt_get_device_error(void* stream, uint32_t* bits);
 const char* adt_status_string(adt_status s);
 
 /* Testing hook, not for production use.  Every wait of adt_tree_attn's
- * pipeline (a CTA waiting for its loads, products or softmax stages) and of
- * adt_tree_accept's sampling walks (a CTA waiting for its cluster's values)
- * is bounded: after `polls` unsuccessful polls it gives up, sets
+ * pipeline (a CTA waiting for its loads, products or softmax stages), of
+ * adt_kv_score's, and of adt_tree_accept's sampling walks (a CTA waiting for its
+ * cluster's values) is bounded: after `polls` unsuccessful polls it gives up, sets
  * ADT_DEVERR_TIMEOUT in the device error word and the kernel leaves cleanly
  * (the copies and tensor-core products it already issued, and the stores to
  * it that are on their way, are waited for first, so the device stays usable;
  * the outputs of that call are unspecified).  This sets the bound for the
- * launches that follow in this process; 0 restores the defaults (2^20 and
+ * launches that follow in this process; 0 restores the defaults (2^20, 2^24 and
  * 2^22 polls), 1 makes every wait of a sampling walk give up.  It lets a
  * test make a bounded wait run out without any fault; it is not synchronised
  * with calls on other threads. */
@@ -500,8 +500,8 @@ adt_status adt_rope_qkv(const void* q, int64_t ld_q, const void* k, int64_t ld_k
  *         accept_len [device] int32 [B].
  * score_in, score_out [device] fp32, element (l, b, g, j) at l*score_layer_stride
  *         + b*score_stride_b + g*score_stride_h + j (any strides that keep
- *         slices of max_kv apart).  They may be the same; otherwise they do not
- *         overlap.  With decay = 0 score_in is not read.
+ *         slices of max_kv apart, up to 2^40).  They may be the same; otherwise
+ *         the memory that they span does not overlap.  With decay = 0 score_in is not read.
  * D in {64, 128}; 1 <= max_path <= 2^20; 1 <= max_kv < 2^30; 0 <= decay <= 1;
  * num_layers * B * Hkv <= 2^22.
  * accept_len[b] outside [0, max_path) or kv_len[b] + accept_len[b] + 1 > max_kv
@@ -532,7 +532,8 @@ adt_status adt_kv_score(const adt_bf16* q, const float* lse, const adt_bf16* k_c
  *
  * k_src, v_src [device] bf16 and k_dst, v_dst: strides as for adt_kv_compact.
  *         In place (the same pointers and strides for both caches), or into
- *         caches that overlap neither source.  A destination slice holds
+ *         caches that overlap neither source (compared as the ranges of memory
+ *         that they span).  A destination slice holds
  *         min(max_kv, budget) rows.
  * score   [device] fp32, as adt_kv_score writes it; score_out: a buffer with
  *         strides of its own, the same buffer (with the same strides), or NULL.
@@ -540,8 +541,8 @@ adt_status adt_kv_score(const adt_bf16* q, const float* lse, const adt_bf16* k_c
  *         receives n (not the same buffer as kv_len).
  * keep_idx [device] int32 [num_layers][B][Hkv][budget] or NULL: the kept rows,
  *         padded with -1.
- * D in {64, 128}; budget >= 1; n_sink, n_recent >= 0, n_sink + n_recent <=
- * budget; max_kv < 2^30.
+ * D in {64, 128}; 1 <= budget < 2^30; n_sink, n_recent >= 0, n_sink + n_recent
+ * <= budget; max_kv < 2^30; strides at most 2^40 elements.
  * kv_len[b] outside [0, max_kv] sets ADT_DEVERR_KV_RANGE and skips tree b
  * (kv_len_out[b] = kv_len[b]; its keep_idx is not written).
  * ------------------------------------------------------------------------ */

@@ -369,9 +369,14 @@ def _vec(t, dtype, dev, count, name):
     return a
 
 
-def _device():
-    return _get_device() if _get_device is not None and torch.cuda.is_initialized() else \
-        torch.cuda.current_device() if torch.cuda.is_available() else 0
+def _launch_on(t, stream, name):
+    """(current CUDA device, handle of the stream) of a call whose tensor t has to be on that device."""
+    dev = t.get_device()
+    if dev < 0 or dev != (_get_device() if _get_device is not None else torch.cuda.current_device()):
+        raise ValueError(f"{name}: expected a tensor on the current CUDA device, got one on {t.device}")
+    if stream is not None:
+        return dev, stream.cuda_stream
+    return dev, _raw_stream(dev) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
 
 
 def adt_rope_freqs(rotary_dim, *, theta=10000.0, scaling=ROPE_NONE, factor=1.0, orig_len=0.0, turns_lo=1.0,
@@ -404,7 +409,8 @@ def adt_rope_qkv(q, k, v, positions, inv_freq, *, H, Hkv, D, layout=ROPE_HALF, m
                  v_out=None, stream=None) -> None:
     """q [N, H * D], k and v [N, Hkv * D] rows (bf16 or fp32, any row stride; None: absent) to bf16 [N, heads, D]
     outputs: q and k rotated by positions * inv_freq, v copied.  rotary_dim = 2 * len(inv_freq)."""
-    dev, N = _device(), positions.numel()
+    dev, handle = _launch_on(positions, stream, "positions")
+    N = positions.numel()
     first = q if q is not None else k if k is not None else v
     if first is None or first.dtype not in _TYPES:
         raise TypeError("q, k, v: bf16 or fp32, all the same")
@@ -414,7 +420,7 @@ def adt_rope_qkv(q, k, v, positions, inv_freq, *, H, Hkv, D, layout=ROPE_HALF, m
     va, ldv, vo = _rope_pair(v, v_out, dtype, dev, Hkv, D, N, "v")
     st = lib().adt_rope_qkv(qa, ldq, ka, ldk, va, ldv, _TYPES[dtype], _vec(positions, torch.int32, dev, N, "positions"),
                             _vec(inv_freq, torch.float64, dev, 0, "inv_freq"), magnitude, layout, N, H, Hkv, D,
-                            2 * inv_freq.numel(), qo, ko, vo, _stream(stream))
+                            2 * inv_freq.numel(), qo, ko, vo, handle)
     _check(st, "adt_rope_qkv")
 
 
@@ -435,7 +441,8 @@ def adt_kv_score(q, lse, k_cache, kv_len, node_offsets, path, max_path, accept_l
                  D, num_layers, max_kv, softmax_scale, decay=1.0, stream=None) -> None:
     """q [layers, nodes, H, D] bf16, lse [layers, nodes, H], k_cache [layers, B, Hkv, rows >= max_kv, D] and score
     [layers, B, Hkv, rows >= max_kv] fp32, updated in place unless score_out (the same strides) is given."""
-    dev, f32, i32, bf16 = _device(), torch.float32, torch.int32, torch.bfloat16
+    dev, handle = _launch_on(q, stream, "q")
+    f32, i32, bf16 = torch.float32, torch.int32, torch.bfloat16
     qs, ls, nodes = q.stride(), lse.stride(), q.shape[1]
     if q.shape[2:] != (H, D) or q.shape[0] < num_layers or qs[1:] != (H * D, D, 1):
         raise ValueError(f"q: expected [{num_layers}, nodes, {H}, {D}], each layer contiguous")
@@ -454,7 +461,7 @@ def adt_kv_score(q, lse, k_cache, kv_len, node_offsets, path, max_path, accept_l
                             _vec(kv_len, i32, dev, B, "kv_len"), _vec(node_offsets, i32, dev, B + 1, "node_offsets"),
                             _vec(path, i32, dev, B * max_path, "path"), max_path,
                             _vec(accept_len, i32, dev, B, "accept_len"), B, H, Hkv, D, num_layers, max_kv, qs[0], ls[0], *cs,
-                            softmax_scale, decay, sa, so, *ss, _stream(stream))
+                            softmax_scale, decay, sa, so, *ss, handle)
     _check(st, "adt_kv_score")
 
 
@@ -464,13 +471,14 @@ def adt_kv_evict(k_cache, v_cache, score, kv_len, kv_len_out=None, *, k_out=None
     """Caches [layers, B, Hkv, rows >= max_kv, D] bf16 and score [layers, B, Hkv, rows >= max_kv] fp32 cut down to
     `budget` rows: in place, or into k_out, v_out.  The scores go to score_out, by default to where the rows went (in
     place: the same buffer); with move_scores=False they stay as they are."""
-    dev, f32, i32, bf16 = _device(), torch.float32, torch.int32, torch.bfloat16
     if (k_out is None) != (v_out is None):
         raise ValueError("k_out and v_out: both or neither")
     if score_out is not None and not move_scores:
         raise ValueError("score_out without moving scores")
     if score_out is None and move_scores and k_out is not None:
         raise ValueError("score_out: needed where the rows go to another cache")
+    dev, handle = _launch_on(k_cache, stream, "k_cache")
+    f32, i32, bf16 = torch.float32, torch.int32, torch.bfloat16
     ks = _strides3(k_cache, num_layers, B, Hkv, max_kv, D, "k_cache")
     cs = co = _strides3(score, num_layers, B, Hkv, max_kv, 0, "score")
     same = _strides3(v_cache, num_layers, B, Hkv, max_kv, D, "v_cache") == ks
@@ -490,7 +498,7 @@ def adt_kv_evict(k_cache, v_cache, score, kv_len, kv_len_out=None, *, k_out=None
     st = lib().adt_kv_evict(ka, va, *ks, sa, *cs, _vec(kv_len, i32, dev, B, "kv_len"),
                             _vec(kv_len_out, i32, dev, B, "kv_len_out"), ko, vo, *os, so, *co,
                             _vec(keep_idx, i32, dev, num_layers * B * Hkv * budget, "keep_idx"), B, Hkv, D, num_layers,
-                            max_kv, budget, n_sink, n_recent, _stream(stream))
+                            max_kv, budget, n_sink, n_recent, handle)
     _check(st, "adt_kv_evict")
 
 

@@ -41,6 +41,7 @@ constexpr int kVecs = 2;                // 16-byte vectors of a thread in a chun
 constexpr int kDepth = 4;               // chunks that its slots hold
 constexpr int kAhead = 3;               // chunks that loads run ahead of stores
 constexpr int kSlotBytes = kDepth * kVecs * kThreads * 16;
+constexpr int64_t kMaxStride = int64_t{1} << 40;
 constexpr int kBinBits = 11;
 constexpr int kBins = 1 << kBinBits;
 static_assert(kWindow * 4 <= kSlotBytes, "a window's keys share the slots");
@@ -393,7 +394,7 @@ adt_status adt_kv_evict(const adt_bf16* k_src, const adt_bf16* v_src, int64_t sr
   adt::TraceRange trace_("adt_kv_evict");
   ADT_REQUIRE(k_src && v_src && score && kv_len && k_dst && v_dst);
   ADT_REQUIRE(B >= 1 && B <= 65535 && Hkv >= 1 && Hkv <= 65535 && num_layers >= 1 && num_layers <= 65535);
-  ADT_REQUIRE(max_kv >= 1 && max_kv < (1 << 30) && budget >= 1 && n_sink >= 0 && n_recent >= 0 &&
+  ADT_REQUIRE(max_kv >= 1 && max_kv < (1 << 30) && budget >= 1 && budget < (1 << 30) && n_sink >= 0 && n_recent >= 0 &&
               static_cast<int64_t>(n_sink) + n_recent <= budget);
   ADT_REQUIRE(kv_len_out != kv_len);
   if (D != 64 && D != 128) return ADT_ERR_UNSUPPORTED;
@@ -407,6 +408,7 @@ adt_status adt_kv_evict(const adt_bf16* k_src, const adt_bf16* v_src, int64_t sr
   for (int i = 0; i < 3; ++i) {
     ADT_REQUIRE(ss[i] >= 0 && ds[i] >= 0 && cs[i] >= 0 && ss[i] % 8 == 0 && ds[i] % 8 == 0 &&
                 (!score_out || os[i] >= 0));
+    ADT_REQUIRE(ss[i] <= kMaxStride && ds[i] <= kMaxStride && cs[i] <= kMaxStride && (!score_out || os[i] <= kMaxStride));
     ADT_REQUIRE(counts[i] == 1 || (ss[i] >= static_cast<int64_t>(max_kv) * D && ds[i] >= keep * D && cs[i] >= max_kv &&
                                    (!score_out || os[i] >= keep)));
     src_span += (counts[i] - 1) * ss[i];

@@ -52,7 +52,8 @@ constexpr int kBoxKeys = 32;
 constexpr int kGroupWarps = 4;
 constexpr uint32_t kTmemCols = 512;
 constexpr int kTiles = kTmemCols / kQueries;  // of S^T in tensor memory
-constexpr uint32_t kWaitLimit = 1u << 20;
+constexpr uint32_t kWaitLimit = 1u << 24;  // polls: a round of queries can last as long as a CTA's whole share
+constexpr int64_t kMaxStride = int64_t{1} << 40;
 constexpr float kLog2e = 1.44269504088896340736f;
 
 // Warps of the roles.  Few queries a key: the products' and loads' threads are
@@ -299,13 +300,13 @@ __global__ void __launch_bounds__(Roles<kMany>::kThreads, 1)
       if (hit) {
         if (lane == __ffs(hit) - 1) {
           const int64_t off = x0 - (before + upto - cost), slice = off / slice_cost(t);
-          const int r = static_cast<int>(off - slice * slice_cost(t));
+          const int64_t r = off - slice * slice_cost(t);
           w.b = b0 + lane;
           w.l = static_cast<int>(slice / p.Hkv);
           w.g = static_cast<int>(slice - static_cast<int64_t>(w.l) * p.Hkv);
           // Tile k > 0 starts kRound + k passes into its slice; one past the last is the slice's end.
           if (r > 0) {
-            w.first = min(max(1, (r + t.passes - 1) / t.passes - kRound), t.tiles);
+            w.first = static_cast<int>(min(max(int64_t{1}, (r + t.passes - 1) / t.passes - kRound), int64_t{t.tiles}));
             w.left -= static_cast<int64_t>(w.first + kRound) * t.passes - r;
           }
           w.t = t;
@@ -620,6 +621,7 @@ adt_status adt_kv_score(const adt_bf16* q, const float* lse, const adt_bf16* k_c
   ADT_REQUIRE((Hkv == 1 || (cache_stride_h >= rows && score_stride_h >= max_kv)) &&
               (B == 1 || (cache_stride_b >= rows && score_stride_b >= max_kv)) &&
               (num_layers == 1 || (cache_layer_stride >= rows && score_layer_stride >= max_kv)));
+  ADT_REQUIRE(score_layer_stride <= kMaxStride && score_stride_b <= kMaxStride && score_stride_h <= kMaxStride);
   ADT_REQUIRE(adt::aligned16(q) && adt::aligned16(k_cache));
   ADT_REQUIRE(static_cast<int64_t>(max_path) * (H / Hkv) < (1 << 30));
   const int64_t slices = static_cast<int64_t>(num_layers) * B * Hkv;

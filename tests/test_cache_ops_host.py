@@ -102,6 +102,7 @@ def _score_args():
     (dict(ssh=99), INVALID), (dict(ssb=-1), INVALID), (dict(qls=4), INVALID), (dict(q=ctypes.c_void_p(24)), INVALID),
     (dict(kc=ctypes.c_void_p(8)), INVALID), (dict(D=96), UNSUPPORTED), (dict(D=32), UNSUPPORTED),
     (dict(layers=4000, B=2000, cls=1 << 30, csb=1 << 20, sls=1 << 30, ssb=1 << 20), UNSUPPORTED),
+    (dict(sls=2 ** 41), INVALID), (dict(max_path=1 << 20, H=2048, Hkv=2), INVALID),
     (dict(so=ctypes.c_void_p(P[7].value + 4)), INVALID),  # neither the same buffer nor apart
 ])
 def test_score_refuses(lib, change, status):
@@ -120,7 +121,8 @@ def _evict_args():
     (dict(Hkv=0), INVALID), (dict(layers=0), INVALID), (dict(max_kv=0), INVALID), (dict(budget=0), INVALID),
     (dict(sink=-1), INVALID), (dict(recent=-1), INVALID), (dict(sink=30, recent=21), INVALID),
     (dict(sink=2 ** 31 - 1, recent=2 ** 31 - 1), INVALID), (dict(D=80), UNSUPPORTED),
-    (dict(max_kv=1 << 30, budget=50), INVALID), (dict(ssh=6399), INVALID), (dict(ssh=6300), INVALID),
+    (dict(max_kv=1 << 30, budget=50), INVALID), (dict(budget=1 << 30), INVALID),
+    (dict(cls=2 ** 41), INVALID), (dict(ko=P[6], vo=P[7], dls=2 ** 41), INVALID), (dict(ssh=6399), INVALID), (dict(ssh=6300), INVALID),
     (dict(csh=99), INVALID), (dict(ko=P[6], vo=P[7], dsh=3199), INVALID), (dict(ko=P[6], vo=P[7], osh=49), INVALID),
     (dict(k=ctypes.c_void_p(8)), INVALID),
     (dict(ko=P[6]), INVALID),                              # K elsewhere, V in place

@@ -194,3 +194,68 @@ def test_decode_with_the_librarys_rotation_equals_greedy(rope, dtype):
     for b in range(2):
         _check(out[b], choice[b], margins[b], max_ties=3, near_tie=NEAR_TIE_BF16)
     assert B.adt_get_device_error() == 0
+
+
+def _calls(seed, H=4, Hkv=2, D=64, L=300, rows=360):
+    """Inputs of a score and an eviction of their own, on the device."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+
+    def rnd(*shape):
+        return torch.randn(shape, generator=g, device="cuda")
+
+    q, lse = rnd(2, 6, H, D).bfloat16(), rnd(2, 6, H).abs() + 5
+    kc, vc, score = rnd(2, 2, Hkv, rows, D).bfloat16(), rnd(2, 2, Hkv, rows, D).bfloat16(), rnd(2, 2, Hkv, rows).exp()
+    i = dict(dtype=torch.int32, device="cuda")
+    return dict(q=q, lse=lse, kc=kc, vc=vc, score=score, kv=torch.tensor([L, 40 + seed], **i), offs=torch.tensor([0, 3, 6], **i),
+                path=torch.tensor([[0, 2], [0, 1]], **i), alen=torch.tensor([1, 1], **i), out=torch.tensor([L + 2, 42 + seed], **i))
+
+
+def _turn(c, stream=None, D=64):
+    kw = dict(B=2, Hkv=2, D=D, num_layers=2, max_kv=c["kc"].shape[3], stream=stream)
+    B.adt_kv_score(c["q"], c["lse"], c["kc"], c["kv"], c["offs"], c["path"], 2, c["alen"], c["score"], H=4, softmax_scale=0.125, **kw)
+    B.adt_kv_evict(c["kc"], c["vc"], c["score"], c["out"], budget=100, n_sink=2, n_recent=20, **kw)
+
+
+def test_turns_on_two_streams_at_once():
+    """Neither call keeps a workspace: turns that overlap on the device do not meet."""
+    alone = [_calls(s) for s in range(6)]
+    for c in alone:
+        _turn(c)
+    both = [_calls(s) for s in range(6)]
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    torch.cuda.synchronize()
+    for k, c in enumerate(both):
+        _turn(c, streams[k % 3])
+    torch.cuda.synchronize()
+    for a, c in zip(alone, both):
+        for name in ("kc", "vc", "score"):
+            assert torch.equal(a[name], c[name])
+
+
+def test_offsets_past_32_bits():
+    """Layers, heads and rows of projections that lie more than 2^32 bytes and 2^31 elements apart."""
+    c = _calls(3)
+    want = {k: v.clone() for k, v in c.items()}
+    _turn(want)
+    far = (1 << 31) + 64
+    big = torch.empty(far + (1 << 26), dtype=torch.bfloat16, device="cuda")
+    wide = torch.empty(far + (1 << 20), device="cuda")
+    shape, rows = c["kc"].shape, c["kc"].shape[3]
+    stride = (far, 1 << 18, 1 << 16, 64, 1)
+    kc, vc = big.as_strided(shape, stride), big.as_strided(shape, stride, 1 << 22)
+    score = wide.as_strided(shape[:4], (far, 4 * rows, rows, 1))
+    for t, s in ((kc, "kc"), (vc, "vc"), (score, "score")):
+        t.copy_(c[s])
+    _turn(dict(c, kc=kc, vc=vc, score=score))
+    assert B.adt_get_device_error() == 0
+    for t, s in ((kc, "kc"), (vc, "vc"), (score, "score")):
+        assert torch.equal(t, want[s])
+    x = torch.randn((3, 2 * 64), device="cuda").bfloat16()
+    ld = 1 << 30
+    y = big.as_strided((3, 2 * 64), (ld + 8, 1))
+    y.copy_(x)
+    pos, inv = torch.tensor([3, 4, 5], dtype=torch.int32, device="cuda"), torch.ones(32, dtype=torch.float64, device="cuda")
+    out = [torch.empty((3, 2, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    for src, o in zip((x, y), out):
+        B.adt_rope_qkv(src, None, None, pos, inv, H=2, Hkv=1, D=64, q_out=o)
+    assert torch.equal(*out)

@@ -191,7 +191,7 @@ def test_evict_in_a_graph_on_another_stream():
 
 
 def test_evict_the_longest_cache():
-    """2^20 rows (the most there may be) of one head, nearly all distinct scores: against torch's stable sort."""
+    """2^20 rows of one head, nearly all distinct scores: against torch's stable sort."""
     L, budget = 1 << 20, 300001
     g = torch.Generator(device="cuda").manual_seed(1)
     score = torch.rand((1, 1, 1, L), generator=g, device="cuda")
