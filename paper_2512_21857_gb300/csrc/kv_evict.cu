@@ -34,18 +34,31 @@
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
-constexpr int kWindow = kThreads * 32;  // rows whose kept ones are listed at a time: a word of bits for every thread
-constexpr int kVecs = 2;                // 16-byte vectors of a thread in a chunk
-constexpr int kDepth = 4;               // chunks that its slots hold
-constexpr int kAhead = 3;               // chunks that loads run ahead of stores
-constexpr int kSlotBytes = kDepth * kVecs * kThreads * 16;
+constexpr int kVecs = 2;   // 16-byte vectors of a thread in a chunk
+constexpr int kDepth = 4;  // chunks that its slots hold
+constexpr int kAhead = 3;  // chunks that loads run ahead of stores
 constexpr int64_t kMaxStride = int64_t{1} << 40;
 constexpr int kBinBits = 11;
 constexpr int kBins = 1 << kBinBits;
-static_assert(kWindow * 4 <= kSlotBytes, "a window's keys share the slots");
-static_assert(kBins * 4 <= kWindow * 2, "its bins share the list");
+
+// Sizes of a CTA of T threads.
+template <int T>
+struct Cta {
+  static constexpr int kWarps = T / 32;
+  static constexpr int kWindow = T * 32;  // rows whose kept ones are listed at a time: a word of bits for every thread
+  static constexpr int kSlotBytes = kDepth * kVecs * T * 16;
+  static_assert(kWindow * 4 <= kSlotBytes, "a window's keys share the slots");
+  static_assert(kBins * 4 <= kWindow * 2, "its bins share the list");
+  struct Scratch {
+    union {
+      uint16_t list[kWindow];  // kept rows of a window, relative to its first
+      uint32_t hist[kBins];    // the search's bins
+    };
+    uint32_t warp[2 * kWarps];
+    uint32_t bin, need, count;
+  };
+  static constexpr int kSmem = kSlotBytes + static_cast<int>(sizeof(Scratch));
+};
 
 struct EvictParams {
   const uint8_t* src[2];  // K, V
@@ -76,16 +89,8 @@ __device__ __forceinline__ uint32_t score_key(float s) {
 // key: 0, rows that are not there.)
 constexpr uint32_t kStays = 0xffffffffu;
 
-struct Scratch {
-  union {
-    uint16_t list[kWindow];  // kept rows of a window, relative to its first
-    uint32_t hist[kBins];    // the search's bins
-  };
-  uint32_t warp[2 * kWarps];
-  uint32_t bin, need, count;
-};
-
 // Exclusive prefix sum of one value a thread; *total gets the sum.
+template <int T>
 __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* warp_sums, uint32_t* total) {
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   uint32_t x = v;
@@ -98,7 +103,7 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* warp_sums, 
   __syncthreads();
   uint32_t base = 0, all = 0;
 #pragma unroll
-  for (int i = 0; i < kWarps; ++i) {
+  for (int i = 0; i < Cta<T>::kWarps; ++i) {
     const uint32_t s = warp_sums[i];
     if (i < w) base += s;
     all += s;
@@ -117,11 +122,12 @@ struct Cut {
 
 // Keys of the rows w0 .. of a window, into shared memory; the rows from `hi` on
 // and those before `lo` stay.
+template <int T>
 __device__ __forceinline__ void window_keys(const float* score, int w0, int L, int lo, int hi, uint32_t* keys,
                                             uint32_t* low, uint32_t* high) {
-  const int rows = min(L - w0, kWindow);
+  const int rows = min(L - w0, Cta<T>::kWindow);
 #pragma unroll 8
-  for (int r = threadIdx.x; r < rows; r += kThreads) {
+  for (int r = threadIdx.x; r < rows; r += T) {
     uint32_t k = score_key(score[w0 + r]);
     if (w0 + r >= lo && w0 + r < hi) {
       *low = min(*low, k);
@@ -137,12 +143,14 @@ __device__ __forceinline__ void window_keys(const float* score, int w0, int L, i
 
 // The cut that keeps `want` of the rows [lo, hi).  Of a slice that is one window
 // the keys are left in shared memory.
+template <int T>
 __device__ __forceinline__ Cut find_cut(const float* score, uint32_t* keys, bool small, int L, int lo, int hi, int want,
-                                        Scratch* sc) {
+                                        typename Cta<T>::Scratch* sc) {
+  constexpr int kThreads = T, kWarps = Cta<T>::kWarps, kWindow = Cta<T>::kWindow;
   const int tid = threadIdx.x;
   uint32_t low = 0xffffffffu, high = 0u;
   for (int i = tid; i < kBins; i += kThreads) sc->hist[i] = 0;
-  for (int w0 = 0; w0 < L; w0 += kWindow) window_keys(score, w0, L, lo, hi, keys, &low, &high);
+  for (int w0 = 0; w0 < L; w0 += kWindow) window_keys<T>(score, w0, L, lo, hi, keys, &low, &high);
   low = __reduce_min_sync(adt::kFullMask, low);
   high = __reduce_max_sync(adt::kFullMask, high);
   if ((tid & 31) == 0) {
@@ -181,7 +189,7 @@ __device__ __forceinline__ Cut find_cut(const float* score, uint32_t* keys, bool
     uint32_t c[kOwn], sum = 0, total;
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) sum += c[i] = sc->hist[kBins - 1 - (tid * kOwn + i)];
-    uint32_t above = block_scan(sum, sc->warp, &total);
+    uint32_t above = block_scan<T>(sum, sc->warp, &total);
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) {
       if (above < need && need <= above + c[i]) {
@@ -214,7 +222,8 @@ __device__ __forceinline__ void mover_sync(int id, int threads) {
 // Moves rows first .. rows - 1 of the list: list[r] of src to row r of dst, by
 // `threads` threads of which this is number t.  A row is 2^pitch bytes, of which
 // 2^shift vectors are moved; slots: this thread's first.  (A window's rows are
-// within 2 MB, so that offsets take 32 bits.)
+// within 8 MB, so that offsets take 32 bits.)
+template <int T>
 __device__ __forceinline__ void move_rows(uint8_t* slots, const uint8_t* src, uint8_t* dst, const uint16_t* list, int first,
                                           int rows, int shift, int pitch, int t, int threads, int barrier, bool in_place) {
   const int step = threads >> shift;  // rows that one vector of every thread makes
@@ -229,7 +238,7 @@ __device__ __forceinline__ void move_rows(uint8_t* slots, const uint8_t* src, ui
 #pragma unroll
     for (int v = 0; v < kVecs; ++v)
       if (v * step < to_load)
-        sm100::cp_async16(smem + (slot * kVecs + v) * (kThreads * 16), src + (static_cast<uint32_t>(list[v * step]) << pitch), 16);
+        sm100::cp_async16(smem + (slot * kVecs + v) * (T * 16), src + (static_cast<uint32_t>(list[v * step]) << pitch), 16);
     list += kVecs * step;
     to_load -= kVecs * step;
     asm volatile("cp.async.commit_group;\n" ::: "memory");
@@ -247,7 +256,7 @@ __device__ __forceinline__ void move_rows(uint8_t* slots, const uint8_t* src, ui
         for (int v = 0; v < kVecs; ++v)
           if (v * step < to_store)
             *reinterpret_cast<uint4*>(dst + v * dstep) =
-                *reinterpret_cast<const uint4*>(slots + (u * kVecs + v) * (kThreads * 16));
+                *reinterpret_cast<const uint4*>(slots + (u * kVecs + v) * (T * 16));
         dst += kVecs * dstep;
         to_store -= kVecs * step;
       }
@@ -256,9 +265,11 @@ __device__ __forceinline__ void move_rows(uint8_t* slots, const uint8_t* src, ui
   asm volatile("cp.async.wait_group 0;\n" ::: "memory");
 }
 
-__global__ void __launch_bounds__(kThreads) kv_evict_kernel(const EvictParams p) {
-  extern __shared__ __align__(128) uint8_t smem[];  // the movers' slots
-  __shared__ Scratch sc;
+template <int T>
+__global__ void __launch_bounds__(T) kv_evict_kernel(const EvictParams p) {
+  constexpr int kThreads = T, kWarps = Cta<T>::kWarps, kWindow = Cta<T>::kWindow;
+  extern __shared__ __align__(128) uint8_t smem[];  // the movers' slots, then the scratch
+  typename Cta<T>::Scratch& sc = *reinterpret_cast<typename Cta<T>::Scratch*>(smem + Cta<T>::kSlotBytes);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = p.parts == 1 ? 0 : static_cast<int>(blockIdx.x) % p.parts, slice = blockIdx.x / p.parts;
   const int g = slice % p.Hkv, b = slice / p.Hkv % p.B, l = slice / p.Hkv / p.B;
@@ -277,7 +288,7 @@ __global__ void __launch_bounds__(kThreads) kv_evict_kernel(const EvictParams p)
   const int lo = L > n ? p.n_sink : L, hi = L > n ? L - p.n_recent : L;
   uint32_t* keys = reinterpret_cast<uint32_t*>(smem);  // of a window's rows
   const bool small = L <= kWindow;
-  Cut cut = find_cut(score, keys, small, L, lo, hi, n - lo - (L - hi), &sc);
+  Cut cut = find_cut<T>(score, keys, small, L, lo, hi, n - lo - (L - hi), &sc);
   // K by one half of the threads and V by the other, or one of them by all.
   const int movers = p.parts == 1 ? kThreads / 2 : kThreads;
   const int x = p.parts == 1 ? tid / movers : rank & 1;
@@ -289,7 +300,7 @@ __global__ void __launch_bounds__(kThreads) kv_evict_kernel(const EvictParams p)
   for (int w0 = 0; w0 < L; w0 += kWindow) {
     if (!small) {  // (all movers have left the slots)
       uint32_t low = 0u, high = 0u;
-      window_keys(score, w0, L, lo, hi, keys, &low, &high);
+      window_keys<T>(score, w0, L, lo, hi, keys, &low, &high);
       __syncthreads();
     }
     // Bits of the rows that stay and of those that tie, a word a lane: a warp
@@ -316,7 +327,7 @@ __global__ void __launch_bounds__(kThreads) kv_evict_kernel(const EvictParams p)
       }
     }
     if (by_row) {
-      const int before = static_cast<int>(block_scan(__popc(tie), sc.warp, &total));
+      const int before = static_cast<int>(block_scan<T>(__popc(tie), sc.warp, &total));
       int most = min(max(cut.ties - before, 0), __popc(tie));  // of this word's ties, the lowest rows
       for (; most > 0; --most) {
         stay |= tie & (0u - tie);
@@ -324,7 +335,7 @@ __global__ void __launch_bounds__(kThreads) kv_evict_kernel(const EvictParams p)
       }
       cut.ties -= min(cut.ties, static_cast<int>(total));
     }
-    uint32_t at = block_scan(__popc(stay), sc.warp, &total);
+    uint32_t at = block_scan<T>(__popc(stay), sc.warp, &total);
     const int rows = static_cast<int>(total);
     // Rows before the first that goes are in place.
     const uint32_t gone = lane < here && stay != 0xffffffffu ? (first + lane) * 32 + __ffs(~stay) - 1 : kWindow;
@@ -363,7 +374,7 @@ __global__ void __launch_bounds__(kThreads) kv_evict_kernel(const EvictParams p)
       }
     }
     __syncthreads();  // the slots take the place of the keys
-    move_rows(smem + tid * 16, src + static_cast<int64_t>(w0) * p.row_bytes, dst + static_cast<int64_t>(done) * p.row_bytes,
+    move_rows<T>(smem + tid * 16, src + static_cast<int64_t>(w0) * p.row_bytes, dst + static_cast<int64_t>(done) * p.row_bytes,
               sc.list, lead, rows, shift, __ffs(p.row_bytes) - 1, p.parts == 1 ? tid - x * movers : tid, movers, 1 + x,
               p.in_place != 0);
     __syncthreads();  // the list is read
@@ -377,6 +388,21 @@ __global__ void __launch_bounds__(kThreads) kv_evict_kernel(const EvictParams p)
 bool caches_overlap(const void* a, int64_t na, const void* b, int64_t nb) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
   return x < y + nb && y < x + na;
+}
+
+template <int T>
+adt_status launch(const EvictParams& p, cudaLaunchConfig_t* cfg, int dev) {
+  static unsigned configured[2] = {0u, 0u};  // bit per device (< 64), per instantiation
+  const unsigned bit = 1u << (dev & 31);
+  unsigned& word = configured[(dev >> 5) & 1];
+  if (!(__atomic_load_n(&word, __ATOMIC_ACQUIRE) & bit)) {
+    ADT_CUDA_TRY(cudaFuncSetAttribute(kv_evict_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cta<T>::kSmem));
+    __atomic_fetch_or(&word, bit, __ATOMIC_ACQ_REL);
+  }
+  cfg->blockDim = dim3(T, 1, 1);
+  cfg->dynamicSmemBytes = Cta<T>::kSmem;
+  ADT_CUDA_TRY(cudaLaunchKernelEx(cfg, kv_evict_kernel<T>, p));
+  return adt::launch_status();
 }
 
 }  // namespace
@@ -465,17 +491,8 @@ adt_status adt_kv_evict(const adt_bf16* k_src, const adt_bf16* v_src, int64_t sr
   // 37.4, 36.5; 256 slices 77.2, 77.2, 87.2.
   p.parts = 1;
   while (p.parts < 8 && slices * p.parts < info.sm_count) p.parts *= 2;
-  static unsigned configured[2] = {0u, 0u};  // bit per device (< 64)
-  const unsigned bit = 1u << (info.device & 31);
-  unsigned& word = configured[(info.device >> 5) & 1];
-  if (!(__atomic_load_n(&word, __ATOMIC_ACQUIRE) & bit)) {  // 48.1 KB with the static part
-    ADT_CUDA_TRY(cudaFuncSetAttribute(kv_evict_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSlotBytes));
-    __atomic_fetch_or(&word, bit, __ATOMIC_ACQ_REL);
-  }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(slices * p.parts), 1, 1);
-  cfg.blockDim = dim3(kThreads, 1, 1);
-  cfg.dynamicSmemBytes = kSlotBytes;
   cfg.stream = adt::as_stream(stream);
   cudaLaunchAttribute attr[2];
   attr[0] = adt::pdl_attribute();
@@ -485,8 +502,12 @@ adt_status adt_kv_evict(const adt_bf16* k_src, const adt_bf16* v_src, int64_t sr
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = p.parts > 1 ? 2 : 1;
-  ADT_CUDA_TRY(cudaLaunchKernelEx(&cfg, kv_evict_kernel, p));
-  return adt::launch_status();
+  // One CTA an SM at most and many rows to search: more threads.  us with 256 and
+  // 512 threads, one layer, half the rows kept: 2 heads x 128, 2400 rows 9.0, 9.1,
+  // 4800 13.5, 12.2, 16000 45.5, 27.9, 60000 177, 123; 16 heads, 2400 rows 11.1,
+  // 12.9, 4800 17.5, 17.9, 8000 29.8, 27.9.
+  return slices * p.parts <= info.sm_count && max_kv > 4096 ? launch<512>(p, &cfg, info.device)
+                                                            : launch<256>(p, &cfg, info.device);
 }
 
 }  // extern "C"

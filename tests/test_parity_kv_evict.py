@@ -85,6 +85,7 @@ SHAPES = [
     (40, 5, 64, [130, 60], 64, 1, 16),               # many slices
     (1, 2, 64, [300], 5000, 3, 100),                 # a budget past the capacity
     (3, 1, 128, [257, 1025, 513, 2049], 256, 0, 7),
+    (1, 1, 128, [16500, 16384, 3], 9000, 4, 100),    # around a window of the launches for few long slices
 ]
 
 
