@@ -363,10 +363,13 @@ def _addr(t, dtype, dev, name):
 
 def _vec(t, dtype, dev, count, name):
     """The address of a contiguous tensor of at least `count` elements; None for None."""
-    a = _addr(t, dtype, dev, name)
-    if t is not None and (t.numel() < count or not t.is_contiguous()):
+    if t is None:
+        return None
+    if t.dtype != dtype or t.get_device() != dev:
+        return _addr(t, dtype, dev, name)  # raises
+    if t.numel() < count or not t.is_contiguous():
         raise ValueError(f"{name}: expected {count} elements, contiguous")
-    return a
+    return t.data_ptr()
 
 
 def _launch_on(t, stream, name):
@@ -444,9 +447,10 @@ def adt_kv_score(q, lse, k_cache, kv_len, node_offsets, path, max_path, accept_l
     dev, handle = _launch_on(q, stream, "q")
     f32, i32, bf16 = torch.float32, torch.int32, torch.bfloat16
     qs, ls, nodes = q.stride(), lse.stride(), q.shape[1]
-    if q.shape[2:] != (H, D) or q.shape[0] < num_layers or qs[1:] != (H * D, D, 1):
+    # (Strides of dimensions of one say nothing: torch's own check where they differ.)
+    if q.shape[2:] != (H, D) or q.shape[0] < num_layers or (qs[1:] != (H * D, D, 1) and not q[0].is_contiguous()):
         raise ValueError(f"q: expected [{num_layers}, nodes, {H}, {D}], each layer contiguous")
-    if lse.shape[1:] != (nodes, H) or lse.shape[0] < num_layers or ls[1:] != (H, 1):
+    if lse.shape[1:] != (nodes, H) or lse.shape[0] < num_layers or (ls[1:] != (H, 1) and not lse[0].is_contiguous()):
         raise ValueError(f"lse: expected [{num_layers}, {nodes}, {H}], each layer contiguous")
     cs = _strides3(k_cache, num_layers, B, Hkv, max_kv, D, "k_cache")
     ss = _strides3(score, num_layers, B, Hkv, max_kv, 0, "score")
@@ -483,20 +487,20 @@ def adt_kv_evict(k_cache, v_cache, score, kv_len, kv_len_out=None, *, k_out=None
     cs = co = _strides3(score, num_layers, B, Hkv, max_kv, 0, "score")
     same = _strides3(v_cache, num_layers, B, Hkv, max_kv, D, "v_cache") == ks
     ka, va, sa = _addr(k_cache, bf16, dev, "k_cache"), _addr(v_cache, bf16, dev, "v_cache"), _addr(score, f32, dev, "score")
-    ko, vo, so, os = ka, va, sa if move_scores else None, ks
+    ko, vo, so, to = ka, va, sa if move_scores else None, ks
     rows = min(max_kv, budget)
     if k_out is not None and k_out is not k_cache:
-        os = _strides3(k_out, num_layers, B, Hkv, rows, D, "k_out")
+        to = _strides3(k_out, num_layers, B, Hkv, rows, D, "k_out")
         ko = _addr(k_out, bf16, dev, "k_out")
     if v_out is not None and v_out is not v_cache:
-        same = same and _strides3(v_out, num_layers, B, Hkv, rows, D, "v_out") == os
+        same = same and _strides3(v_out, num_layers, B, Hkv, rows, D, "v_out") == to
         vo = _addr(v_out, bf16, dev, "v_out")
     if not same:
         raise ValueError("K and V must share strides")
     if score_out is not None:
         co, so = _strides3(score_out, num_layers, B, Hkv, rows, 0, "score_out"), _addr(score_out, f32, dev, "score_out")
     st = lib().adt_kv_evict(ka, va, *ks, sa, *cs, _vec(kv_len, i32, dev, B, "kv_len"),
-                            _vec(kv_len_out, i32, dev, B, "kv_len_out"), ko, vo, *os, so, *co,
+                            _vec(kv_len_out, i32, dev, B, "kv_len_out"), ko, vo, *to, so, *co,
                             _vec(keep_idx, i32, dev, num_layers * B * Hkv * budget, "keep_idx"), B, Hkv, D, num_layers,
                             max_kv, budget, n_sink, n_recent, handle)
     _check(st, "adt_kv_evict")

@@ -209,3 +209,25 @@ def test_evict_the_longest_cache():
     assert torch.equal(idx.long(), rows) and torch.equal(score[..., :budget], want)
     for x in (kc, vc):
         assert torch.equal(x.view(torch.int32)[0, 0, 0, :budget], rows.to(torch.int32)[0, 0, 0, :, None].expand(budget, 32))
+
+
+def test_evict_binding_checks_what_it_is_given():
+    c = Case(2, 2, 64, [140, 60], 150, "spread", 10)
+    kc, vc, score, kv = c.tensors()
+    n, idx = c.outputs(64)
+    other = [torch.zeros((2, 2, 2, 64, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    small = torch.zeros((2, 2, 2, 64), device="cuda")
+    for args, more, err in [
+            ((kc.half(), vc, score, kv), {}, TypeError), ((kc, vc[:1], score, kv), {}, ValueError),
+            ((kc, vc, score[..., :149], kv), {}, ValueError), ((kc, vc, score.double(), kv), {}, TypeError),
+            ((kc, vc, score, kv.long()), {}, TypeError), ((kc, vc, score, kv[:1]), {}, ValueError),
+            ((kc, vc, score, kv, kv), {}, B.AdtError), ((kc, vc, score, kv, n), dict(keep_idx=idx[:1]), ValueError),
+            ((kc, vc, score, kv, n), dict(k_out=other[0]), ValueError), ((kc, vc, score, kv, n), dict(k_out=other[0], v_out=other[1]), ValueError),
+            ((kc, vc, score, kv, n), dict(k_out=other[0], v_out=other[0][:, :, :, :63], score_out=small), ValueError),
+            ((kc, vc, score, kv, n), dict(k_out=other[0], v_out=vc, score_out=small), B.AdtError),
+            ((kc, vc, score, kv, n), dict(score_out=small[..., :63]), ValueError),
+            ((kc, vc.transpose(1, 2).contiguous().transpose(1, 2), score, kv, n), {}, ValueError),
+            ((kc, vc, score, kv, n), dict(n_sink=60, n_recent=5), B.AdtError)]:
+        with pytest.raises(err):
+            B.adt_kv_evict(*args, **c.kw(budget=64, **more))
+    assert np.array_equal(bits(kc), bits(c.kc)) and np.array_equal(bits(vc), bits(c.vc))

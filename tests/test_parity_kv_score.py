@@ -240,3 +240,27 @@ def test_score_wait_that_runs_out_is_reported(D, paths):
 def test_score_deals_uneven_trees(kv, paths):
     c = Case(3, 4, 2, 64, kv, paths, 140, seed=18)
     c.check(c.run())
+
+
+def test_score_binding_checks_what_it_is_given():
+    """Dimensions of one may have any stride; wrong shapes, types and strides are refused."""
+    c = Case(1, 1, 1, 64, [70], [[0]], 1, seed=19)
+    args = list(c.args())
+    args[0] = args[0].as_strided((1, 1, 1, 64), (8, 8, 8, 1))
+    args[1] = args[1].as_strided((1, 1, 1), (3, 5, 7))
+    B.adt_kv_score(*args, **c.kw())
+    c.check(args[-1])
+    c = Case(2, 4, 2, 64, [100, 50], [[0, 1], [0, 2]], 5, seed=20)
+    good = list(c.args())
+    for i, bad, err in [(0, good[0].float(), TypeError), (0, good[0][:1], ValueError), (0, good[0].transpose(1, 2), ValueError),
+                        (0, good[0][..., ::2], ValueError), (1, good[1][:, :9], ValueError), (1, good[1].double(), TypeError),
+                        (2, good[2][:, :, :1], ValueError), (2, good[2][:, :, :, :90], ValueError), (2, good[2].half(), TypeError),
+                        (2, good[2].transpose(3, 4).contiguous().transpose(3, 4), ValueError), (3, good[3][:1], ValueError),
+                        (3, good[3].long(), TypeError), (4, good[4][:2], ValueError), (5, good[5][:1], ValueError),
+                        (7, good[7].cpu(), ValueError), (8, good[8][..., ::2], ValueError), (8, good[8].cpu(), ValueError)]:
+        args = list(good)
+        args[i] = bad
+        with pytest.raises(err):
+            B.adt_kv_score(*args, **c.kw())
+    with pytest.raises(ValueError, match="share strides"):
+        B.adt_kv_score(*good, **c.kw(), score_out=torch.zeros((2, 2, 2, c.lmax + 1), device="cuda"))
