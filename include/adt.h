@@ -442,9 +442,9 @@ adt_status adt_kv_compact_inplace(adt_bf16* k_cache, adt_bf16* v_cache, const in
  * q_out [device] bf16 [N][H][D]; k_out, v_out bf16 [N][Hkv][D].  An output may
  *         be its own input (bf16, ld = heads*D); otherwise outputs overlap
  *         neither inputs nor each other (ADT_ERR_INVALID_ARG).
- * Pointers need their type's alignment only; rows and heads that are multiples
- * of 16 bytes on 16-byte boundaries, with rotary_dim a multiple of 16, are
- * moved as vectors.
+ * Pointers need their type's alignment only.  Rows on 16-byte boundaries with D a
+ * multiple of 8 are moved as vectors (fastest with rotary_dim a multiple of 16,
+ * or of 8 side by side), others element by element.
  * ------------------------------------------------------------------------ */
 typedef enum adt_dtype { ADT_TYPE_BF16 = 0, ADT_TYPE_F32 = 1 } adt_dtype;
 typedef enum adt_rope_layout { ADT_ROPE_HALF = 0, ADT_ROPE_INTERLEAVED = 1 } adt_rope_layout;
