@@ -534,11 +534,11 @@ adt_status adt_kv_score(const adt_bf16* q, const float* lse, const adt_bf16* k_c
  *         In place (the same pointers and strides for both caches), or into
  *         caches that overlap neither source (compared as the ranges of memory
  *         that they span).  A destination slice holds
- *         min(max_kv, budget) rows.
+ *         min(max_kv, budget) rows, and k_dst's and v_dst's do not overlap.
  * score   [device] fp32, as adt_kv_score writes it; score_out: a buffer with
  *         strides of its own, the same buffer (with the same strides), or NULL.
  * kv_len  [device] int32 [B], <= max_kv; kv_len_out [device] int32 [B] or NULL
- *         receives n (not the same buffer as kv_len).
+ *         receives n (a buffer that does not overlap kv_len).
  * keep_idx [device] int32 [num_layers][B][Hkv][budget] or NULL: the kept rows,
  *         padded with -1.
  * D in {64, 128}; 1 <= budget < 2^30; n_sink, n_recent >= 0, n_sink + n_recent

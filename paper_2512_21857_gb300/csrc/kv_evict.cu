@@ -422,7 +422,7 @@ adt_status adt_kv_evict(const adt_bf16* k_src, const adt_bf16* v_src, int64_t sr
   ADT_REQUIRE(B >= 1 && B <= 65535 && Hkv >= 1 && Hkv <= 65535 && num_layers >= 1 && num_layers <= 65535);
   ADT_REQUIRE(max_kv >= 1 && max_kv < (1 << 30) && budget >= 1 && budget < (1 << 30) && n_sink >= 0 && n_recent >= 0 &&
               static_cast<int64_t>(n_sink) + n_recent <= budget);
-  ADT_REQUIRE(kv_len_out != kv_len);
+  ADT_REQUIRE(!kv_len_out || !caches_overlap(kv_len, B * 4ll, kv_len_out, B * 4ll));
   if (D != 64 && D != 128) return ADT_ERR_UNSUPPORTED;
   const int64_t keep = max_kv < budget ? max_kv : budget;  // rows that a destination slice holds
   const int64_t counts[3] = {num_layers, B, Hkv};
@@ -453,6 +453,9 @@ adt_status adt_kv_evict(const adt_bf16* k_src, const adt_bf16* v_src, int64_t sr
                 !caches_overlap(v_src, src_span * 2, v_dst, dst_span * 2) &&
                 !caches_overlap(k_src, src_span * 2, v_dst, dst_span * 2) &&
                 !caches_overlap(v_src, src_span * 2, k_dst, dst_span * 2));
+  // K and V may lie in one allocation (slices of both in turn), not in the same rows.
+  const int64_t slice_bytes = (in_place ? max_kv : keep) * D * 2;
+  ADT_REQUIRE(!caches_overlap(k_dst, slice_bytes, v_dst, slice_bytes));
   if (score_out && !(score_out == score && same(cs, os)))
     ADT_REQUIRE(!caches_overlap(score, c_span * 4, score_out, o_span * 4));
   const int64_t slices = counts[0] * counts[1] * counts[2];

@@ -136,6 +136,15 @@ def test_evict_refuses(lib, change, status):
     assert _call(lib.adt_kv_evict, _evict_args(), **change) == status
 
 
+def test_evict_refuses_one_destination_for_both_and_lengths_that_overlap(lib):
+    # K and V onto one another: in place, and from caches of their own
+    assert _call(lib.adt_kv_evict, _evict_args(), k=P[0], v=P[0], ko=P[0], vo=P[0]) == INVALID
+    assert _call(lib.adt_kv_evict, _evict_args(), ko=P[6], vo=P[6]) == INVALID
+    # tree 1's length read where tree 0's new one is written, and the other way round
+    for shift in (4, -4):
+        assert _call(lib.adt_kv_evict, _evict_args(), kvo=ctypes.c_void_p(P[3].value + shift)) == INVALID
+
+
 def test_bindings_refuse_cpu_tensors_and_wrong_types(lib):
     bf, f32, i32 = torch.zeros(2, 64, dtype=torch.bfloat16), torch.zeros(2, 64), torch.zeros(2, dtype=torch.int32)
     inv = torch.zeros(32, dtype=torch.float64)
