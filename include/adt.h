@@ -437,8 +437,8 @@ adt_status adt_kv_compact_inplace(adt_bf16* k_cache, adt_bf16* v_cache, const in
  * positions [device] int32 [N], any value (a negative one turns back).
  * inv_freq  [device] fp64 [rotary_dim/2], radians a position (adt_rope_freqs
  *         makes the usual ones); may be NULL when rotary_dim is 0.
- * N >= 0 (of 0 rows no pointer is read and nothing launched); 1 <= D <= 4096; 0 <= rotary_dim <= D, even, at
- *         most 1024; magnitude finite.
+ * 0 <= N <= 2^30 (of 0 rows no pointer is read and nothing launched), N * ld <= 2^40; 1 <= D <= 4096;
+ *         0 <= rotary_dim <= D, even, at most 1024; magnitude finite.
  * q_out [device] bf16 [N][H][D]; k_out, v_out bf16 [N][Hkv][D].  An output may
  *         be its own input (bf16, ld = heads*D); otherwise outputs overlap
  *         neither inputs nor each other (ADT_ERR_INVALID_ARG).

@@ -21,6 +21,8 @@
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kMaxRows = 1 << 30;               // token numbers, and those of a CTA past the last, take 32 bits
+constexpr int64_t kMaxSpan = int64_t{1} << 40;  // elements of all rows with what lies between: their bytes take 64 bits
 constexpr int kMaxRotary = 1024;  // cosines and sines of a token: 4 KB of shared memory
 constexpr double kTwoPi = 6.283185307179586476925286766559;
 
@@ -348,7 +350,7 @@ adt_status adt_rope_qkv(const void* q, int64_t ld_q, const void* k, int64_t ld_k
   adt::TraceRange trace_("adt_rope_qkv");
   ADT_REQUIRE(in_type == ADT_TYPE_BF16 || in_type == ADT_TYPE_F32);
   ADT_REQUIRE(layout == ADT_ROPE_HALF || layout == ADT_ROPE_INTERLEAVED);
-  ADT_REQUIRE(N >= 0 && D >= 1 && D <= 4096 && rotary_dim >= 0 && rotary_dim % 2 == 0 && rotary_dim <= D);
+  ADT_REQUIRE(N >= 0 && N <= kMaxRows && D >= 1 && D <= 4096 && rotary_dim >= 0 && rotary_dim % 2 == 0 && rotary_dim <= D);
   if (rotary_dim > kMaxRotary) return ADT_ERR_UNSUPPORTED;
   ADT_REQUIRE(isfinite(magnitude));
   if (N == 0) return ADT_OK;
@@ -366,7 +368,7 @@ adt_status adt_rope_qkv(const void* q, int64_t ld_q, const void* k, int64_t ld_k
   for (int x = 0; x < 3; ++x) {
     p.heads[x] = !in[x] ? 0 : x == 0 ? H : Hkv;
     const int64_t width = static_cast<int64_t>(p.heads[x]) * D;
-    ADT_REQUIRE(!in[x] || (ld[x] >= width && ld[x] <= (int64_t{1} << 40)));
+    ADT_REQUIRE(!in[x] || (ld[x] >= width && ld[x] <= kMaxSpan / N));
     ADT_REQUIRE(reinterpret_cast<uintptr_t>(in[x]) % esize == 0 && reinterpret_cast<uintptr_t>(out[x]) % 2 == 0);
     in_bytes[x] = in[x] ? ((N - 1) * ld[x] + width) * esize : 0;
     out_bytes[x] = in[x] ? N * width * 2 : 0;

@@ -82,6 +82,14 @@ def test_rope_refuses(lib, change, status):
     assert _call(lib.adt_rope_qkv, _rope_args(), **change) == status
 
 
+def test_rope_refuses_more_rows_than_its_indexes_take(lib):
+    one = dict(q=P[0], qo=P[5], k=None, ko=None, v=None, vo=None)
+    assert _call(lib.adt_rope_qkv, _rope_args(), **dict(one, D=8, rot=8, ldq=8, qo=ctypes.c_void_p(1 << 50)),
+                 N=2 ** 31 - 1) == INVALID
+    # rows whose bytes pass 64 bits
+    assert _call(lib.adt_rope_qkv, _rope_args(), **dict(one, ldq=2 ** 40, N=2 ** 29, qo=ctypes.c_void_p(1 << 50))) == INVALID
+
+
 def test_rope_of_no_rows_is_done(lib):
     assert _call(lib.adt_rope_qkv, _rope_args(), N=0, q=None, qo=None, pos=None) == 0
 
