@@ -231,3 +231,17 @@ def test_evict_binding_checks_what_it_is_given():
         with pytest.raises(err):
             B.adt_kv_evict(*args, **c.kw(budget=64, **more))
     assert np.array_equal(bits(kc), bits(c.kc)) and np.array_equal(bits(vc), bits(c.vc))
+
+
+@pytest.mark.parametrize("max_more", [0, 5])
+def test_evict_of_caches_in_one_allocation(max_more):
+    # [layers, B, Hkv, K and V, rows, D]: the spans of K and V overlap, their slices do not.
+    c = Case(2, 3, 64, [300, 80], 300, "spread", 17)
+    both = torch.zeros(2, 2, 3, 2, 300 + max_more, 64, dtype=torch.bfloat16, device="cuda")
+    both[:, :, :, 0, :300], both[:, :, :, 1, :300] = c.kc.cuda(), c.vc.cuda()
+    kc, vc = both[:, :, :, 0], both[:, :, :, 1]
+    _, _, score, kv_len = c.tensors()
+    n, idx = c.outputs(100)
+    B.adt_kv_evict(kc, vc, score, kv_len, n, keep_idx=idx, **c.kw(budget=100, n_sink=4, n_recent=16))
+    same((kc[..., :300, :], vc[..., :300, :], score, n, idx), c.oracle(100, 4, 16))
+    assert not both[:, :, :, :, 300:].any()
