@@ -494,7 +494,8 @@ adt_status adt_rope_qkv(const void* q, int64_t ld_q, const void* k, int64_t ld_k
  * q       [device] bf16, element (l, n, h, d) at l*q_layer_stride + (n*H + h)*D + d,
  *         as given to adt_tree_attn.
  * lse     [device] fp32, element (l, n, h) at l*lse_layer_stride + n*H + h, as
- *         adt_tree_attn returned it; a query with lse = -inf adds nothing.
+ *         adt_tree_attn returned it; a query with lse = -inf adds nothing,
+ *         whatever its values and the keys' are (NaN and infinities among them).
  * k_cache [device] bf16, strides as for adt_kv_compact; kv_len [device] int32 [B].
  * node_offsets [device] int32 [B+1]; path [device] int32 [B][max_path];
  *         accept_len [device] int32 [B].
