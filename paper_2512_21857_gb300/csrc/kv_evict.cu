@@ -30,6 +30,7 @@
 #include <math.h>
 
 #include "adt_common.cuh"
+#include "slices.h"
 #include "sm100.cuh"
 
 namespace {
@@ -453,9 +454,11 @@ adt_status adt_kv_evict(const adt_bf16* k_src, const adt_bf16* v_src, int64_t sr
                 !caches_overlap(v_src, src_span * 2, v_dst, dst_span * 2) &&
                 !caches_overlap(k_src, src_span * 2, v_dst, dst_span * 2) &&
                 !caches_overlap(v_src, src_span * 2, k_dst, dst_span * 2));
-  // K and V may lie in one allocation (slices of both in turn), not in the same rows.
-  const int64_t slice_bytes = (in_place ? max_kv : keep) * D * 2;
-  ADT_REQUIRE(!caches_overlap(k_dst, slice_bytes, v_dst, slice_bytes));
+  // No slice of K shares memory with one of V.  (Both may lie in one allocation,
+  // slices of both in turn.)
+  const int64_t slice = (in_place ? max_kv : keep) * D;
+  const int64_t v_off = static_cast<int64_t>(reinterpret_cast<uintptr_t>(v_dst) - reinterpret_cast<uintptr_t>(k_dst)) / 2;
+  ADT_REQUIRE(v_off != 0 && !adt::slices_meet(counts, ds, slice, v_off));
   if (score_out && !(score_out == score && same(cs, os)))
     ADT_REQUIRE(!caches_overlap(score, c_span * 4, score_out, o_span * 4));
   const int64_t slices = counts[0] * counts[1] * counts[2];
