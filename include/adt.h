@@ -535,8 +535,9 @@ adt_status adt_kv_score(const adt_bf16* q, const float* lse, const adt_bf16* k_c
  *         In place (the same pointers and strides for both caches), or into
  *         caches that overlap neither source (compared as the ranges of memory
  *         that they span).  A destination slice holds
- *         min(max_kv, budget) rows (in place max_kv), and no slice of k_dst
- *         overlaps one of v_dst; both may lie in one allocation, in turn.
+ *         min(max_kv, budget) rows (in place max_kv); no two slices of k_dst
+ *         and v_dst overlap (both may lie in one allocation, in turn), nor two
+ *         of score_out.
  * score   [device] fp32, as adt_kv_score writes it; score_out: a buffer with
  *         strides of its own, the same buffer (with the same strides), or NULL.
  * kv_len  [device] int32 [B], <= max_kv; kv_len_out [device] int32 [B] or NULL

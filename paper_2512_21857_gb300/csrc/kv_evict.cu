@@ -454,13 +454,16 @@ adt_status adt_kv_evict(const adt_bf16* k_src, const adt_bf16* v_src, int64_t sr
                 !caches_overlap(v_src, src_span * 2, v_dst, dst_span * 2) &&
                 !caches_overlap(k_src, src_span * 2, v_dst, dst_span * 2) &&
                 !caches_overlap(v_src, src_span * 2, k_dst, dst_span * 2));
-  // No slice of K shares memory with one of V.  (Both may lie in one allocation,
-  // slices of both in turn.)
+  // No two slices that are written share memory, none of K's with one of V's
+  // either.  (Both may lie in one allocation, slices of both in turn.)
   const int64_t slice = (in_place ? max_kv : keep) * D;
   const int64_t v_off = static_cast<int64_t>(reinterpret_cast<uintptr_t>(v_dst) - reinterpret_cast<uintptr_t>(k_dst)) / 2;
-  ADT_REQUIRE(v_off != 0 && !adt::slices_meet(counts, ds, slice, v_off));
-  if (score_out && !(score_out == score && same(cs, os)))
-    ADT_REQUIRE(!caches_overlap(score, c_span * 4, score_out, o_span * 4));
+  ADT_REQUIRE(v_off != 0 && !adt::slices_meet(counts, ds, slice, 0) && !adt::slices_meet(counts, ds, slice, v_off));
+  if (score_out) {
+    const bool scores_in_place = score_out == score && same(cs, os);
+    ADT_REQUIRE(scores_in_place || !caches_overlap(score, c_span * 4, score_out, o_span * 4));
+    ADT_REQUIRE(!adt::slices_meet(counts, os, scores_in_place ? max_kv : keep, 0));
+  }
   const int64_t slices = counts[0] * counts[1] * counts[2];
   if (slices > (1 << 28)) return ADT_ERR_UNSUPPORTED;
   adt::DeviceInfo info;

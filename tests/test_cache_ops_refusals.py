@@ -29,3 +29,24 @@ def test_evict_refuses_v_in_the_gaps_of_k_where_a_slice_does_not_fit(lib):  # no
     wide |= dict(dsh=wide["ssh"], dsb=wide["ssb"], dls=wide["sls"])
     v = _at(P[6], HEAD)
     assert _call(lib.adt_kv_evict, _evict_args(), k=P[6], ko=P[6], v=v, vo=v, **wide) == INVALID
+
+
+ALIASED = [  # (layer, tree, head) strides that pass a slice each and still put two slices on one another
+    (2 * 100, 100, 100), (100, 2 * 100, 100), (200, 200, 100), (200, 100, 300), (399, 200, 100), (300, 100, 600), (250, 100, 150)]
+
+
+@pytest.mark.parametrize("strides", ALIASED)
+def test_evict_refuses_destinations_whose_slices_share_rows(lib, strides):  # noqa: F811
+    k = dict(zip(("sls", "ssb", "ssh"), (64 * s for s in strides))) | dict(zip(("dls", "dsb", "dsh"), (64 * s for s in strides)))
+    assert _call(lib.adt_kv_evict, _evict_args(), **k) == INVALID
+    # into other caches, of slices of 50 rows
+    half = dict(zip(("dls", "dsb", "dsh"), (32 * s for s in strides)))
+    assert _call(lib.adt_kv_evict, _evict_args(), ko=P[6], vo=P[7], **half) == INVALID
+
+
+@pytest.mark.parametrize("strides", ALIASED)
+def test_evict_refuses_scores_whose_slices_share_rows(lib, strides):  # noqa: F811
+    c = dict(zip(("cls", "csb", "csh"), strides)) | dict(zip(("ols", "osb", "osh"), strides))
+    assert _call(lib.adt_kv_evict, _evict_args(), **c) == INVALID
+    half = dict(zip(("ols", "osb", "osh"), (s // 2 for s in strides)))
+    assert _call(lib.adt_kv_evict, _evict_args(), so=P[8], **half) == INVALID
