@@ -500,8 +500,8 @@ adt_status adt_rope_qkv(const void* q, int64_t ld_q, const void* k, int64_t ld_k
  * node_offsets [device] int32 [B+1]; path [device] int32 [B][max_path];
  *         accept_len [device] int32 [B].
  * score_in, score_out [device] fp32, element (l, b, g, j) at l*score_layer_stride
- *         + b*score_stride_b + g*score_stride_h + j (any strides that keep
- *         slices of max_kv apart, up to 2^40).  They may be the same; otherwise
+ *         + b*score_stride_b + g*score_stride_h + j (any strides up to 2^40 that
+ *         keep slices of max_kv apart; others: ADT_ERR_INVALID_ARG).  They may be the same; otherwise
  *         the memory that they span does not overlap.  With decay = 0 score_in is not read.
  * D in {64, 128}; 1 <= max_path <= 2^20; 1 <= max_kv < 2^30; 0 <= decay <= 1;
  * num_layers * B * Hkv <= 2^22.

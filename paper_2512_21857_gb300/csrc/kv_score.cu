@@ -42,6 +42,7 @@
 #include <utility>
 
 #include "adt_common.cuh"
+#include "slices.h"
 #include "sm100.cuh"
 
 namespace {
@@ -659,6 +660,9 @@ adt_status adt_kv_score(const adt_bf16* q, const float* lse, const adt_bf16* k_c
     ADT_REQUIRE(x >= y + span || y >= x + span);
   }
   if (slices > (1 << 22)) return ADT_ERR_UNSUPPORTED;
+  // No two slices of the scores share memory: CTAs of their own add to them.
+  const int64_t counts[3] = {num_layers, B, Hkv}, ss[3] = {score_layer_stride, score_stride_b, score_stride_h};
+  ADT_REQUIRE(!adt::slices_meet(counts, ss, max_kv, 0));
   adt::DeviceInfo info;
   adt_status st = adt::device_info(&info);
   if (st != ADT_OK) return st;

@@ -5,7 +5,7 @@ import ctypes
 
 import pytest
 
-from test_cache_ops_host import INVALID, P, _call, _evict_args, lib  # noqa: F401 (lib: a fixture)
+from test_cache_ops_host import INVALID, P, _call, _evict_args, _score_args, lib  # noqa: F401 (lib: a fixture)
 
 
 def _at(base, elements, size=2):
@@ -50,3 +50,10 @@ def test_evict_refuses_scores_whose_slices_share_rows(lib, strides):  # noqa: F8
     assert _call(lib.adt_kv_evict, _evict_args(), **c) == INVALID
     half = dict(zip(("ols", "osb", "osh"), (s // 2 for s in strides)))
     assert _call(lib.adt_kv_evict, _evict_args(), so=P[8], **half) == INVALID
+
+
+@pytest.mark.parametrize("strides", ALIASED)
+def test_score_refuses_scores_whose_slices_share_rows(lib, strides):  # noqa: F811
+    c = dict(zip(("sls", "ssb", "ssh"), strides))
+    assert _call(lib.adt_kv_score, _score_args(), **c) == INVALID
+    assert _call(lib.adt_kv_score, _score_args(), **c, so=P[8]) == INVALID
