@@ -504,7 +504,8 @@ adt_status adt_rope_qkv(const void* q, int64_t ld_q, const void* k, int64_t ld_k
  *         keep slices of max_kv apart; others: ADT_ERR_INVALID_ARG).  They may be the same; otherwise
  *         the memory that they span does not overlap.  With decay = 0 score_in is not read.
  * D in {64, 128}; 1 <= max_path <= 2^20; 1 <= max_kv < 2^30; 0 <= decay <= 1;
- * num_layers * B * Hkv <= 2^22.
+ * num_layers * B * Hkv <= 2^22 and, times max_kv, <= 2^36; layer strides of q and
+ * lse <= 2^40.
  * accept_len[b] outside [0, max_path) or kv_len[b] + accept_len[b] + 1 > max_kv
  * sets ADT_DEVERR_KV_RANGE and skips tree b; a path entry outside the tree
  * sets ADT_DEVERR_BAD_PATH and adds nothing.

@@ -55,6 +55,7 @@ constexpr uint32_t kTmemCols = 512;
 constexpr int kTiles = kTmemCols / kQueries;  // of S^T in tensor memory
 constexpr uint32_t kWaitLimit = 1u << 24;  // polls: a round of queries can last as long as a CTA's whole share
 constexpr int64_t kMaxStride = int64_t{1} << 40;
+constexpr int64_t kMaxRows = int64_t{1} << 36;  // of all slices (8 TB of keys): what they cost takes 64 bits
 constexpr float kLog2e = 1.44269504088896340736f;
 
 // Warps of the roles.  Few queries a key: the products' and loads' threads are
@@ -649,7 +650,8 @@ adt_status adt_kv_score(const adt_bf16* q, const float* lse, const adt_bf16* k_c
   ADT_REQUIRE((Hkv == 1 || (cache_stride_h >= rows && score_stride_h >= max_kv)) &&
               (B == 1 || (cache_stride_b >= rows && score_stride_b >= max_kv)) &&
               (num_layers == 1 || (cache_layer_stride >= rows && score_layer_stride >= max_kv)));
-  ADT_REQUIRE(score_layer_stride <= kMaxStride && score_stride_b <= kMaxStride && score_stride_h <= kMaxStride);
+  ADT_REQUIRE(score_layer_stride <= kMaxStride && score_stride_b <= kMaxStride && score_stride_h <= kMaxStride &&
+              q_layer_stride <= kMaxStride && lse_layer_stride <= kMaxStride);
   ADT_REQUIRE(adt::aligned16(q) && adt::aligned16(k_cache));
   ADT_REQUIRE(static_cast<int64_t>(max_path) * (H / Hkv) < (1 << 30));
   const int64_t slices = static_cast<int64_t>(num_layers) * B * Hkv;
@@ -659,7 +661,7 @@ adt_status adt_kv_score(const adt_bf16* q, const float* lse, const adt_bf16* k_c
     const uintptr_t x = reinterpret_cast<uintptr_t>(score_in), y = reinterpret_cast<uintptr_t>(score_out);
     ADT_REQUIRE(x >= y + span || y >= x + span);
   }
-  if (slices > (1 << 22)) return ADT_ERR_UNSUPPORTED;
+  if (slices > (1 << 22) || slices * max_kv > kMaxRows) return ADT_ERR_UNSUPPORTED;
   // No two slices of the scores share memory: CTAs of their own add to them.
   const int64_t counts[3] = {num_layers, B, Hkv}, ss[3] = {score_layer_stride, score_stride_b, score_stride_h};
   ADT_REQUIRE(!adt::slices_meet(counts, ss, max_kv, 0));

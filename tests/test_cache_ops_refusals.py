@@ -5,7 +5,7 @@ import ctypes
 
 import pytest
 
-from test_cache_ops_host import INVALID, P, _call, _evict_args, _score_args, lib  # noqa: F401 (lib: a fixture)
+from test_cache_ops_host import INVALID, P, UNSUPPORTED, _call, _evict_args, _score_args, lib  # noqa: F401 (lib: a fixture)
 
 
 def _at(base, elements, size=2):
@@ -57,3 +57,13 @@ def test_score_refuses_scores_whose_slices_share_rows(lib, strides):  # noqa: F8
     c = dict(zip(("sls", "ssb", "ssh"), strides))
     assert _call(lib.adt_kv_score, _score_args(), **c) == INVALID
     assert _call(lib.adt_kv_score, _score_args(), **c, so=P[8]) == INVALID
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(qls=2 ** 41), INVALID), (dict(lls=2 ** 40 + 1), INVALID), (dict(lls=2 ** 62), INVALID),
+    # 2^20 slices of 2^29 rows, 2^22 passes over each tile of 128: 2^64 in all
+    (dict(layers=2 ** 9, B=2 ** 8, H=2 ** 14, Hkv=2 ** 3, max_kv=2 ** 29, max_path=2 ** 18, csh=2 ** 35, csb=2 ** 35, cls=2 ** 35,
+          ssh=2 ** 29, ssb=2 ** 32, sls=2 ** 40), UNSUPPORTED),
+])
+def test_score_refuses_sizes_whose_products_pass_their_types(lib, change, status):  # noqa: F811
+    assert _call(lib.adt_kv_score, _score_args(), **change) == status
