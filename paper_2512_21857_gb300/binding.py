@@ -429,7 +429,7 @@ def adt_rope_qkv(q, k, v, positions, inv_freq, *, H, Hkv, D, layout=ROPE_HALF, m
 
 def _strides3(t, layers, B, Hkv, rows, D, name):
     """Strides of the first three dimensions of [layers, B, Hkv, rows or more, D] (D = 0: of [layers, B, Hkv, rows or
-    more]); the rows are packed."""
+    more]), those of a dimension of one as 0: they say nothing; the rows are packed."""
     shape, strides = t.shape, t.stride()
     want = 5 if D else 4
     if len(shape) != want or shape[0] != layers or shape[1] != B or shape[2] != Hkv or shape[3] < rows or \
@@ -437,7 +437,7 @@ def _strides3(t, layers, B, Hkv, rows, D, name):
         raise ValueError(f"{name}: expected {[layers, B, Hkv, rows, D][:want]} or more rows, got {list(shape)}")
     if (strides[3] != (D or 1) and shape[3] > 1) or (D and strides[4] != 1):
         raise ValueError(f"{name}: expected packed rows")
-    return strides[:3]
+    return strides[0] if layers > 1 else 0, strides[1] if B > 1 else 0, strides[2] if Hkv > 1 else 0
 
 
 def adt_kv_score(q, lse, k_cache, kv_len, node_offsets, path, max_path, accept_len, score, *, score_out=None, B, H, Hkv,
@@ -464,7 +464,8 @@ def adt_kv_score(q, lse, k_cache, kv_len, node_offsets, path, max_path, accept_l
     st = lib().adt_kv_score(_addr(q, bf16, dev, "q"), _addr(lse, f32, dev, "lse"), _addr(k_cache, bf16, dev, "k_cache"),
                             _vec(kv_len, i32, dev, B, "kv_len"), _vec(node_offsets, i32, dev, B + 1, "node_offsets"),
                             _vec(path, i32, dev, B * max_path, "path"), max_path,
-                            _vec(accept_len, i32, dev, B, "accept_len"), B, H, Hkv, D, num_layers, max_kv, qs[0], ls[0], *cs,
+                            _vec(accept_len, i32, dev, B, "accept_len"), B, H, Hkv, D, num_layers, max_kv,
+                            qs[0] if num_layers > 1 else 0, ls[0] if num_layers > 1 else 0, *cs,
                             softmax_scale, decay, sa, so, *ss, handle)
     _check(st, "adt_kv_score")
 
