@@ -246,9 +246,12 @@ class TreeVerifyStep:
 
     def load_inputs(self, inp):
         """Copies a dict of host inputs (see synth.step_inputs) into the step's
-        device buffers."""
+        device buffers.  With a kv_budget, other caches start with scores of
+        zero, or with those given as "score"."""
+        if self.shape.kv_budget and ("k_cache" in inp or "v_cache" in inp):
+            self.score.zero_()
         for name in ("k_cache", "v_cache", "q", "k_tree", "v_tree", "target", "u_accept", "u_sample",
-                     "root_token"):
+                     "root_token", *(("score",) if self.shape.kv_budget else ())):
             if name in inp:
                 getattr(self, name).copy_(torch.as_tensor(inp[name]))
         if "draft_rows" in inp:
