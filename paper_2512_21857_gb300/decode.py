@@ -352,6 +352,8 @@ class Decoder:
         if not 2 <= P <= self.max_nodes + 1:
             raise ValueError("prompt of 2 .. max_nodes + 1 tokens (the prefill is one tree)")
         n = P - 1
+        if self.kv_budget and P > self.prompt_len and n + self.d_most + 1 > self.target.lmax:
+            raise ValueError(f"prompt of {P} tokens: with a kv_budget the cache was made for prompt_len = {self.prompt_len}")
         tok = self._i32(list(prompt[:-1]) * Bn)
         par = torch.cat([_chain(n, dev)] * Bn)
         offs = self._i32([b * n for b in range(Bn + 1)])
