@@ -51,11 +51,12 @@ WORKLOADS = {
 }
 
 # DRAM bytes (read + write) of one tree_attn launch at the 7B shape, from one
-# ncu capture; valid only for the kernel source with this SHA-256 prefix.
+# ncu capture; valid only for the kernel sources with this SHA-256 prefix (see
+# attn_source_sha; profiles/tree_attn_tc_kernel_128_7b_layer.md is the capture).
 HOST_MARKER = b"// ---------------------------------------------------------------- host side"
 NCU_TRAFFIC = {
-    # dram__bytes_read.sum + dram__bytes_write.sum = 41,496,064 + 0
-    "ff8e57f5063e1bca": 41496064,
+    # dram__bytes_read.sum + dram__bytes_write.sum = 41,495,808 + 0
+    "b4a0ff1e401d4199": 41495808,
 }
 
 
@@ -91,12 +92,16 @@ def measured_peaks():
 
 
 def attn_source_sha():
-    """SHA-256 prefix of the attention kernel's device code: tree_attn.cu up to
-    its host-side section (host-only edits do not change the kernel)."""
-    with open(os.path.join(ROOT, "paper_2512_21857_gb300", "csrc", "tree_attn.cu"), "rb") as f:
-        src = f.read()
-    cut = src.find(HOST_MARKER)
-    return hashlib.sha256(src if cut < 0 else src[:cut]).hexdigest()[:16]
+    """SHA-256 prefix of the attention kernels' device code: tree_attn.cu up to
+    its host-side section (host-only edits do not change the kernels) and the
+    headers that it includes, whole."""
+    h = hashlib.sha256()
+    for name in ("tree_attn.cu", "tree_attn_wide.cuh", "sm100.cuh", "adt_common.cuh"):
+        with open(os.path.join(ROOT, "paper_2512_21857_gb300", "csrc", name), "rb") as f:
+            src = f.read()
+        cut = src.find(HOST_MARKER) if name.endswith(".cu") else -1
+        h.update(src if cut < 0 else src[:cut])
+    return h.hexdigest()[:16]
 
 
 # ------------------------------------------------------------------ clocks
