@@ -1,5 +1,6 @@
 """The decode loop's refusals with a bounded cache that need no GPU."""
 import pytest
+import torch
 
 from paper_2512_21857_gb300.decode import Decoder, ModelShape
 
@@ -10,6 +11,10 @@ TINY = ModelShape(layers=1, hidden=128, heads=2, kv_heads=2, head_dim=64, ffn=25
 def _built():
     from paper_2512_21857_gb300 import build
     build.build()
+    threads = torch.get_num_threads()
+    torch.set_num_threads(1)  # (no thread pool: tests that follow fork this process)
+    yield
+    torch.set_num_threads(threads)
 
 
 @pytest.mark.parametrize("length,refused", [(8, False), (17, False), (33, False), (34, True), (60, True)])
