@@ -466,7 +466,9 @@ typedef struct adt_rope_params {
  *   NTK       theta * s^(rotary_dim/(rotary_dim-2)) for theta (rotary_dim > 2);
  *   BY_PARTS  inv_freq * (r + (1 - r)/s), r the pair's turns in orig_len
  *             positions mapped from [turns_lo, turns_hi] to [0, 1], clamped
- *             (the usual bounds are 1 and 32); magnitude 0.1 ln s + 1.
+ *             (the usual bounds are 1 and 32); magnitude 0.1 ln s + 1.  The ramp
+ *             is linear in the turns, as published; models trained with one
+ *             that is linear in p need frequencies of their own.
  * *magnitude is 1 otherwise.  The caller copies inv_freq to the device. */
 adt_status adt_rope_freqs(const adt_rope_params* params, double* inv_freq, float* magnitude);
 

@@ -19,14 +19,14 @@
 // With fewer, nothing hides the search: its chain of passes over a slice's
 // scores takes 4 us at 1700 rows and 8 us at 5120 (a pass is bound by its
 // instructions, so keys are kept, not scores; a tenth of it is instructions
-// fetched cold).  256 slices of 1777 to 6001 rows, 2048 kept, 77 us of 61; 1440
-// slices of 1577 and 1693 rows of 128 bytes, 512 kept, 76 us of 58.  Four CTAs an
-// SM hide loads best with three chunks ahead (six chunks and half the CTAs: 75
-// -> 87 us for the last); 512 threads a CTA cost it 5 us, 128 6 us and the first
-// 38.  Bulk copies a run of rows at a time were as fast for long runs (371 us) but
-// not for short ones (431 against 93 us then for the 256 slices).  Bins over the
-// scores' range spread the counts; those over the top bits of fp32 met 30 bins
-// and cost 4 us at 5120 rows.
+// fetched cold).  256 slices of 1777 to 6001 rows, 2048 kept, 83 us of 61 (76 in a
+// graph of such calls); 1440 of 1577 and 1693 rows of 128 bytes, 512 kept, 76 us
+// of 58.  Four CTAs an SM hide loads best with three chunks ahead (six chunks and
+// half the CTAs: 75 -> 87 us for the last); 512 threads a CTA cost it 5 us, 128
+// 6 us and the first 38.  Bulk copies a run of rows at a time were as fast for long
+// runs (371 us) but not for short ones (431 against 93 us then for the 256
+// slices).  Bins over the scores' range spread the counts; those over the top bits
+// of fp32 met 30 bins and cost 4 us at 5120 rows.
 #include <math.h>
 
 #include "adt_common.cuh"
@@ -497,7 +497,7 @@ adt_status adt_kv_evict(const adt_bf16* k_src, const adt_bf16* v_src, int64_t sr
   // anew, and rows in pieces cost the memory more, so not beyond.  us with this
   // rule, with one CTA a slice, and with a CTA more an SM: 8 heads, 576 rows of
   // 64 6.0, 7.6, 5.9; 8 heads, 2400 rows of 128 9.4, 19.0, 9.4; 128 slices 33.2,
-  // 37.4, 36.5; 256 slices 77.2, 77.2, 87.2.
+  // 37.4, 36.5; 256 slices (in graphs) 77.2, 77.2, 87.2.
   p.parts = 1;
   while (p.parts < 8 && slices * p.parts < info.sm_count) p.parts *= 2;
   cudaLaunchConfig_t cfg = {};

@@ -26,11 +26,13 @@
 //
 // Bound by HBM with few queries: 32 layers of 32 heads x 128, 2400 rows, a path of
 // eight 102 us (96 at the measured copy rate); four trees of 3500 to 6001 rows, 8
-// layers, 32 / 8 heads 54.6 us (48.5).  A call's fixed cost is 4 us (the lengths,
-// the share, the first tile, the last) and a launch.  With many queries by the
-// issue slots of the exponentials (about 5 cycles a warp for each): two prompts
-// of 256 tokens, 36 layers, 20 heads x 64, 82 us (33 for the bytes, 35 for 281
-// million exponentials at 32 a cycle and SM).  What took how much: a score read
+// layers, 32 / 8 heads 54.4 us (48.5).  A call's fixed cost is 4 us (the lengths,
+// the share, the first tile, the last) and a launch.  With many queries by waits:
+// two prompts of 256 tokens, 36 layers, 20 heads x 64, 83 us (33 for the bytes, 30
+// for 281 million exponentials at 32 a cycle and SM and 1.95 GHz).  The unit that
+// makes those is busy 38 % of the time there, issue slots 55 %, the tensor cores
+// 23 %; a warp is stalled longest for loads (tensor memory, the scores so far), of
+// which it has one chunk on the way at a time.  What took how much: a score read
 // when it was needed 5 us of the second; the product's thread polling one
 // barrier after the other (1000 cycles a tile) 3 us of the first, 10 of the
 // prompts; divisions in the walk from slice to slice 2 us; queries masked at

@@ -7,9 +7,11 @@
 // 20 bits before the point, so that in fp32 the cosine would be off by 0.03.
 //
 // Bound by HBM where there are many tokens: 16384 of 32 / 32 heads x 128 124 us
-// for 805 MB (119 at the measured copy rate); 4096 of 32 / 8 heads 20.4 us for 101
-// MB (14.9; the angles' 64-bit chain is a fifth of a CTA's time there), 26.2 with
-// one unit a thread; and by a launch (2 us) up to about 300.
+// for 805 MB (119 at the measured copy rate); 4096 of 32 / 8 heads 19 to 20 us for
+// 101 MB (14.9; the angles' 64-bit chain is a fifth of a CTA's time there), 26.2
+// with one unit a thread; and by a launch (2 us) up to about 300.  Halves spill at
+// the register limits that their CTAs an SM leave them: 48 bytes a thread for bf16
+// rows (64 registers), 32 for fp32 (80).
 //
 // A CTA takes one token or a few (and, where there are few tokens, a share of
 // their heads): one thread a pair makes the cosines and sines once, in shared
@@ -199,7 +201,8 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3)
 // a thread takes two neighbouring elements with their partners, wherever they
 // lie, at a time (4-byte stores of a warp are a row's 128 bytes).  Straight from
 // global memory one element at a time 4096 tokens of 32 / 8 heads x 128 with 50
-// turned took 56 us, so 36.
+// turned took 56 us, so 34 (14.9 at the copy rate: every element passes through
+// shared memory in fp32, and stores are 4 bytes a thread).
 constexpr int kStaged = 4096;  // elements: 16 KB
 
 template <typename T>
@@ -275,7 +278,9 @@ __global__ void __launch_bounds__(kThreads) rope_staged_kernel(const RopeParams 
 }
 
 // One pair or one copied element at a time: any even rotary_dim, any head
-// size, row stride and alignment (the vectors' kernels are 2 to 3 times as fast).
+// size, row stride and alignment.  4096 tokens of 32 / 8 heads x 128 in rows off a
+// 16-byte boundary take 41 us (19 to 20 as vectors, 14.9 at the copy rate): loads
+// and stores of 2 bytes a thread.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) rope_scalar_kernel(const RopeParams p) {
   __shared__ float2 cs[kMaxRotary / 2];

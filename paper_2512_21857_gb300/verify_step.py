@@ -44,7 +44,7 @@ class StepShape:
     lmax: int = 0         # cache capacity per image (default: max kv_len + max_nodes)
     mode: int = B.ACCEPT_GREEDY
     temperature: float = 1.0
-    kv_budget: int = 0    # rows that a cache keeps (0: all); the first kv_sink and the last kv_recent among them
+    kv_budget: int = 0    # rows that a cache keeps (0: all), after every step: the first kv_sink and the last kv_recent among them
     kv_sink: int = 0
     kv_recent: int = 0
 
