@@ -305,8 +305,8 @@ class Decoder:
         self.kv_keep = dict(n_sink=min(kv_sink, kv_budget // 2), n_recent=min(kv_recent, kv_budget // 2))
         target_rows = self.lmax
         if kv_budget:  # the target's cache holds the budget, the slack and one step's path
-            if kv_budget < 1 or kv_slack < 0:
-                raise ValueError("kv_budget >= 1 and kv_slack >= 0")
+            if kv_budget < 1 or min(kv_slack, kv_sink, kv_recent) < 0:
+                raise ValueError("kv_budget >= 1, and kv_slack, kv_sink and kv_recent >= 0")
             self.d_most = max(self.ctrl_params["d_hi"], self.ctrl_params.get("fix_d", 0))
             target_rows = min(self.lmax, max(prompt_len, kv_budget + kv_slack) + self.d_most + 1)
         tw = target if target is not None else DecoderWeights(s, s.layers, seed, device)

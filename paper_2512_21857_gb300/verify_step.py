@@ -70,6 +70,8 @@ class TreeVerifyStep:
     def __init__(self, shape: StepShape, device="cuda", keep_layer_outputs=False, input_slots=1):
         s = self.shape = shape
         self.device = device
+        if s.kv_budget and not (s.kv_budget > 0 <= min(s.kv_sink, s.kv_recent) and s.kv_sink + s.kv_recent <= s.kv_budget):
+            raise ValueError("kv_budget >= 1, kv_sink and kv_recent >= 0, together at most kv_budget")
         Bn = s.batch
         self.n = [s.nodes(b) for b in range(Bn)]
         offs = [0]
