@@ -68,3 +68,19 @@ def test_large_sizes(meet):
     assert not meet([64, 64, 65535], [2 ** 40, 2 ** 38, 2 ** 20], 2 ** 19, 2 ** 19)
     assert meet([64, 64, 65535], [2 ** 40, 2 ** 38, 2 ** 20], 2 ** 19, 2 ** 19 + 1)
     assert meet([64, 64, 65535], [2 ** 40, 2 ** 38, 2 ** 20], 2 ** 19, -(2 ** 38) - 5)
+
+
+def test_every_pair_agrees_of_dimensions_one_within_the_other(meet):
+    """Packed layouts with gaps, and second sets a few strides away."""
+    rng, seen = random.Random(6), [0, 0]
+    for _ in range(20000):
+        count, need = [rng.randint(1, 4) for _ in range(3)], rng.randint(1, 6)
+        stride, step = [0] * 3, need
+        for k in rng.sample(range(3), 3):
+            stride[k] = step + rng.choice([0, 0, need, 2 * need + 1])
+            step = stride[k] * count[k] if count[k] > 1 else step
+        delta = sum(rng.randint(-2, 2) * s for s in stride) + rng.choice([0, need, -need, need - 1, rng.randint(-9, 9)])
+        want = pairs(count, [s if n > 1 else 0 for n, s in zip(count, stride)], need, delta)
+        assert meet(count, stride, need, delta) == want, (count, stride, need, delta)
+        seen[want] += 1
+    assert min(seen) > 2000
