@@ -52,7 +52,7 @@ WORKLOADS = {
 
 # DRAM bytes (read + write) of one tree_attn launch at the 7B shape, from one
 # ncu capture; valid only for the kernel sources with this SHA-256 prefix (see
-# attn_source_sha; profiles/tree_attn_tc_kernel_128_7b_layer.md is the capture).
+# attn_source_sha).
 HOST_MARKER = b"// ---------------------------------------------------------------- host side"
 NCU_TRAFFIC = {
     # dram__bytes_read.sum + dram__bytes_write.sum = 41,495,808 + 0
