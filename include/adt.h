@@ -17,8 +17,11 @@
  *   adt_kv_compact    copy the accepted nodes' K/V into the cache.
  *   adt_rope_qkv      rotate the projections' rows to their positions, as they
  *                     enter attention and cache.
+ *   adt_norm_rope_qkv the same with norms of the query and key heads before it.
  *   adt_kv_score      add up the attention weight that each cached row got.
  *   adt_kv_evict      cut the cache down to the rows with the most of it.
+ *   adt_kv_compact_q8, adt_kv_read_q8, adt_tree_attn_q8  the commit into a cache
+ *                     of 8-bit rows, its rows as bf16, the attention over it.
  *   adt_ctrl_*        host-side depth / width controller (Sec. 4.1, 4.2).
  *
  * Conventions shared by every entry point
@@ -478,6 +481,35 @@ adt_status adt_rope_qkv(const void* q, int64_t ld_q, const void* k, int64_t ld_k
                         adt_bf16* q_out, adt_bf16* k_out, adt_bf16* v_out, void* stream);
 
 /* ------------------------------------------------------------------------
+ * adt_norm_rope_qkv - adt_rope_qkv with a norm of every query and key head
+ * before the rotation, in the same pass (the paper prints no formula; image
+ * models of this kind norm their heads so).
+ *
+ * Head row x of node n (D elements), all of it in fp32:
+ *   ADT_NORM_RMS:   y = x / sqrt(mean x^2 + eps)
+ *   ADT_NORM_LAYER: y = (x - mean x) / sqrt(mean (x - mean x)^2 + eps)
+ * then y w + b element by element, the rotation by positions[n], and one
+ * rounding to bf16.  v is neither normed nor rotated, only copied.
+ *
+ * q_weight, q_bias, k_weight, k_bias [device] of weight_type, each NULL (ones,
+ *         zeros) or D values that all heads share (stride 0) or that head h has
+ *         at h*stride (stride >= D, that of a weight and its bias).
+ * eps finite and not negative.  D <= 4096; all else, what may alias among it, as
+ * for adt_rope_qkv; outputs overlap no weights either.  Squares are summed in
+ * fp32: elements past 2^60 are outside the domain.
+ * Rows and weights on 16-byte boundaries with D (up to 512) and rotary_dim
+ * multiples of 16 are moved as vectors, others element by element.
+ * ------------------------------------------------------------------------ */
+typedef enum adt_norm { ADT_NORM_RMS = 0, ADT_NORM_LAYER = 1 } adt_norm;
+
+adt_status adt_norm_rope_qkv(const void* q, int64_t ld_q, const void* k, int64_t ld_k, const void* v, int64_t ld_v,
+                             adt_dtype in_type, adt_norm norm, float eps, const void* q_weight, const void* q_bias,
+                             int32_t q_weight_stride, const void* k_weight, const void* k_bias, int32_t k_weight_stride,
+                             adt_dtype weight_type, const int32_t* positions, const double* inv_freq, float magnitude,
+                             adt_rope_layout layout, int32_t N, int32_t H, int32_t Hkv, int32_t D, int32_t rotary_dim,
+                             adt_bf16* q_out, adt_bf16* k_out, adt_bf16* v_out, void* stream);
+
+/* ------------------------------------------------------------------------
  * adt_kv_score - the attention weight that every cached row got from the
  * tokens just committed, added to a running score, all layers in one launch
  * (no counterpart in the paper; what adt_kv_evict goes by).
@@ -560,6 +592,65 @@ adt_status adt_kv_evict(const adt_bf16* k_src, const adt_bf16* v_src, int64_t sr
                         int64_t score_out_stride_h, int32_t* keep_idx, int32_t B, int32_t Hkv, int32_t D,
                         int32_t num_layers, int32_t max_kv, int32_t budget, int32_t n_sink, int32_t n_recent,
                         void* stream);
+
+/* ------------------------------------------------------------------------
+ * The 8-bit cache (no counterpart in the paper: half the memory, and half the
+ * bytes that attention reads).  A row, one kv head of one token, is D e4m3
+ * values and one byte s: value = e4m3 * 2^(s - 127), not a number for s = 255.
+ *
+ * k_cache, v_cache [device] e4m3, element (l, b, g, pos, d) at
+ *         l*cache_layer_stride + b*cache_stride_b + g*cache_stride_h + pos*D + d.
+ * k_scale, v_scale [device] uint8, row (l, b, g, pos) at l*scale_layer_stride +
+ *         b*scale_stride_b + g*scale_stride_h + pos.
+ * D in {64, 128}; max_kv < 2^30.  Strides of dimensions of more than one: at
+ * least a slice of max_kv rows, at most 2^40; those of the caches multiples of 16,
+ * the caches 16-byte aligned (scales need no alignment).  Caches do not overlap
+ * scales, nor, where they are written, slices one another (K and V may lie in
+ * one allocation, slices of both in turn).
+ *
+ * adt_kv_compact_q8 - adt_kv_compact into such caches, with its arguments and
+ * errors otherwise.  Of a row x the scale is the least power of two with max |x|
+ * <= 448 * 2^(s - 127), s >= 7; the elements x * 2^(127 - s) are rounded to the
+ * nearest e4m3 value, halves to even.  A row with an infinity or a NaN becomes s =
+ * 255 and zeros.  kv_len_out does not overlap kv_len.
+ *
+ * adt_kv_read_q8 - rows 0 .. kv_len[b]-1 of every layer, tree and kv head as
+ * bf16 (exact for what adt_kv_compact_q8 wrote), where bf16 operators take
+ * them: k_out, v_out with strides of their own (multiples of 8, slices of max_kv
+ * rows apart), that overlap no input.  Rows behind are left as they were.
+ * kv_len[b] outside [0, max_kv] sets ADT_DEVERR_KV_RANGE and skips tree b.
+ *
+ * adt_tree_attn_q8 - adt_tree_attn over such a prefix, one layer (q, the tree's
+ * own k_tree and v_tree, parents, out and lse as there; a plain decoding step
+ * is trees of one node).  Scores, softmax and sums are made from the values the
+ * rows stand for.  Rows behind kv_len[b] are not used, whatever they hold.
+ * 1 <= max_nodes <= 256, any H % Hkv == 0, B * max_nodes * H <= 2^24.
+ * Errors as for adt_tree_attn.
+ * ------------------------------------------------------------------------ */
+adt_status adt_kv_compact_q8(uint8_t* k_cache, uint8_t* v_cache, uint8_t* k_scale, uint8_t* v_scale,
+                             const int32_t* kv_len, int32_t* kv_len_out, const adt_bf16* k_tree, const adt_bf16* v_tree,
+                             const int32_t* node_offsets, const int32_t* path, int32_t max_path,
+                             const int32_t* accept_len, int32_t B, int32_t Hkv, int32_t D, int32_t num_layers,
+                             int32_t max_kv, int64_t cache_layer_stride, int64_t cache_stride_b, int64_t cache_stride_h,
+                             int64_t scale_layer_stride, int64_t scale_stride_b, int64_t scale_stride_h,
+                             int64_t tree_layer_stride, void* stream);
+
+adt_status adt_kv_read_q8(const uint8_t* k_cache, const uint8_t* v_cache, const uint8_t* k_scale, const uint8_t* v_scale,
+                          const int32_t* kv_len, adt_bf16* k_out, adt_bf16* v_out, int32_t B, int32_t Hkv, int32_t D,
+                          int32_t num_layers, int32_t max_kv, int64_t cache_layer_stride, int64_t cache_stride_b,
+                          int64_t cache_stride_h, int64_t scale_layer_stride, int64_t scale_stride_b,
+                          int64_t scale_stride_h, int64_t out_layer_stride, int64_t out_stride_b, int64_t out_stride_h,
+                          void* stream);
+
+size_t adt_tree_attn_q8_workspace_size(int32_t B, int32_t H, int32_t Hkv, int32_t D, int32_t max_nodes, int32_t max_kv);
+
+adt_status adt_tree_attn_q8(const adt_bf16* q, const uint8_t* k_cache, const uint8_t* v_cache, const uint8_t* k_scale,
+                            const uint8_t* v_scale, const int32_t* kv_len, int64_t cache_stride_b,
+                            int64_t cache_stride_h, int64_t scale_stride_b, int64_t scale_stride_h,
+                            const adt_bf16* k_tree, const adt_bf16* v_tree, const int32_t* parents,
+                            const int32_t* node_offsets, int32_t B, int32_t H, int32_t Hkv, int32_t D,
+                            int32_t max_nodes, int32_t max_kv, float softmax_scale, adt_bf16* out, float* lse,
+                            void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
  * Depth / width controller (host only, no GPU).  Sec. 4.1 adjacent

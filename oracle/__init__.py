@@ -9,4 +9,5 @@ from .tree_verify import (ACCEPT_GREEDY, ACCEPT_SPEC, ACCEPT_SPEC_DET, ancestor_
                           softmax64, tree_accept, tree_attention, tree_expand, tree_rerank)
 from .controller import (INIT_HORIZONTAL, INIT_RANDOM, INIT_TOKENFLOCK, INIT_VERTICAL, Controller,  # noqa: F401
                          CtrlParams, anole_params, counter_draw, llamagen_params, splitmix64)
-from .cache_ops import kv_evict, kv_score, rope_freqs, rope_rows  # noqa: F401
+from .cache_ops import (e4m3_values, kv_evict, kv_score, norm_rows, q8_rows, q8_values, rope_freqs,  # noqa: F401
+                        rope_rows)

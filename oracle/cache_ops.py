@@ -1,5 +1,6 @@
-"""Plain CPU oracle of the cache operators: rotary positions, the attention
-weight added up per cached row, and the eviction that goes by it.
+"""Plain CPU oracle of the cache operators: rotary positions (with head norms
+before them), the attention weight added up per cached row, the eviction that
+goes by it, and the 8-bit cache.
 
 TEST INFRASTRUCTURE, like the rest of ``oracle/``: fp64 throughout, one row at
 a time, no code shared with the library.
@@ -103,3 +104,56 @@ def kv_evict(k_cache, v_cache, score, kv_len, budget, n_sink=0, n_recent=0, k_ds
                 for s, d in zip(src, dst):
                     d[l, b, g, :len(rows)] = s[l, b, g, rows]
     return dst[0], dst[1], dst[2], np.minimum(np.asarray(kv_len), budget), idx
+
+
+def norm_rows(x, layer, eps, weight=None, bias=None):
+    """x [N, heads, D] normed head by head; weight and bias [D] or [heads, D].  Returns the result and, for error
+    bounds, the normed rows before weight and bias and each head's mean |x| / sqrt(mean square + eps)."""
+    x = np.asarray(x, np.float64)
+    y = x - x.mean(-1, keepdims=True) if layer else x
+    root = np.sqrt((y * y).mean(-1, keepdims=True) + eps)
+    hat = y / root
+    out = hat if weight is None else hat * np.asarray(weight, np.float64)
+    if bias is not None:
+        out = out + np.asarray(bias, np.float64)
+    return out, hat, np.abs(x).mean(-1, keepdims=True) / root
+
+
+def e4m3_values():
+    """The value of every e4m3 byte, by its bits (NaN for 0x7f and 0xff)."""
+    out = np.empty(256)
+    for b in range(256):
+        e, m = b >> 3 & 15, b & 7
+        v = m * 2.0 ** -9 if e == 0 else (1 + m / 8) * 2.0 ** (e - 7)
+        out[b] = math.nan if b & 127 == 127 else -v if b & 128 else v
+    return out
+
+
+def q8_rows(x):
+    """Rows x [..., D] as (e4m3 bytes [..., D], scale bytes [...]): the least power of two 2^(s - 127), s >= 7, with
+    max |x| <= 448 times it; elements to the nearest value, halves to the even byte."""
+    x = np.asarray(x, np.float64)
+    table = e4m3_values()[:127]  # the values that are not negative, ascending
+    q, s = np.zeros(x.shape, np.uint8), np.zeros(x.shape[:-1], np.uint8)
+    for at in np.ndindex(x.shape[:-1]):
+        row = x[at]
+        if not np.isfinite(row).all():
+            s[at] = 255
+            continue
+        e = -120
+        while np.abs(row).max() > 448 * 2.0 ** e:
+            e += 1
+        y = np.abs(row) / 2.0 ** e
+        hi = np.searchsorted(table, y).clip(1, 126)  # table[hi - 1] <= y <= table[hi]
+        up, down = table[hi] - y, y - table[hi - 1]
+        pick = np.where(up < down, hi, np.where(up > down, hi - 1, np.where(hi % 2 == 0, hi, hi - 1)))
+        q[at] = pick + np.where(np.signbit(row), 128, 0)
+        s[at] = e + 127
+    return q, s
+
+
+def q8_values(q, s):
+    """What rows of an 8-bit cache stand for."""
+    s = np.asarray(s).astype(np.int64)
+    scale = np.where(s == 255, math.nan, np.exp2(np.where(s == 255, 0, s) - 127.0))
+    return e4m3_values()[np.asarray(q)] * scale[..., None]

@@ -1,0 +1,406 @@
+// adt_norm_rope_qkv: norms of the query and key heads, then their rotation, in
+// one pass over a projection's rows.
+//
+// Head row x of D elements: RMS y = x / sqrt(mean x^2 + eps); LAYER the same of
+// x - mean x; then y w + b, the rotation of adt_rope_qkv, and one rounding to
+// bf16.  Everything before it is fp32; the variance is a sum over centred values
+// (E x^2 - (E x)^2 loses what is left of them where a row's mean is large).
+//
+// A head is split over a group of lanes, 16 elements each, which are such that
+// the partner of every rotated element lies in the same lane: two vectors of 8, in
+// a half layout those of a pair's two sides.  So a norm costs two or four rounds of
+// shuffles of one value and the rotation none.
+#include <math.h>
+
+#include "adt_common.cuh"
+#include "rope_common.cuh"
+
+namespace {
+
+using adt::Eight;
+using adt::kMaxRotary;
+using adt::kMaxRows;
+using adt::kMaxSpan;
+using adt::overlap;
+using adt::put;
+using adt::to_f32;
+using adt::token_angles;
+
+constexpr int kThreads = 256;
+constexpr int kUnit = 16;     // elements of a head in a thread
+constexpr int kMaxHead = 4096;
+
+struct NormParams {
+  const void* in[3];        // rows of q, k, v
+  int64_t ld[3];            // row strides in elements
+  __nv_bfloat16* out[3];    // [N][heads][D]
+  int heads[3];
+  const void* weight[2];    // of q and k; NULL: ones
+  const void* bias[2];      // NULL: zeros
+  int wld[2];               // elements from a head's weights to the next one's, 0: shared
+  const int32_t* pos;
+  const double* inv_freq;
+  float magnitude, eps;
+  int D, rot, interleaved, layer;
+};
+
+// Sum over the aligned group of `width` (a power of two) lanes.
+__device__ __forceinline__ float group_sum(float v, int width) {
+  for (int o = width >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(adt::kFullMask, v, o);
+  return v;
+}
+
+// Vectors: 16 | D <= 512, 16 | rot, 16-byte boundaries.  A CTA takes one token or
+// a few (and where there are few, a share of their heads); a thread keeps its place
+// within the heads, so that it reads its cosines and sines once, and its first
+// units are on their way while the angles are made.
+template <typename T, typename W>
+__global__ void __launch_bounds__(kThreads, 3)
+    norm_rope_vec_kernel(const NormParams p, int N, int tokens, int lanes, int width) {
+  extern __shared__ float2 cs[];
+  constexpr int kBatch = 2;
+  adt::pdl_wait_then_release();
+  const int n0 = blockIdx.x * tokens, here = min(tokens, N - n0);
+  const int tok = threadIdx.x / lanes, lane = threadIdx.x - tok * lanes;
+  const bool active = tok < here;
+  const int64_t n = n0 + (active ? tok : 0);
+  const int half = p.rot / 2, units = p.D / kUnit;
+  const int per_pass = lanes / width, hl = lane / width, u = lane - hl * width;
+  const bool turned = u * kUnit < p.rot, split_pair = turned && !p.interleaved;
+  const int e0 = split_pair ? u * 8 : u * kUnit, e1 = split_pair ? e0 + half : e0 + 8;
+  const int heads = p.heads[0] + p.heads[1];
+  const int h0 = static_cast<int>(blockIdx.y) * per_pass + hl, hstep = static_cast<int>(gridDim.y) * per_pass;
+  const int v0 = static_cast<int>(blockIdx.y) * lanes + lane, vstep = static_cast<int>(gridDim.y) * lanes;
+  const int vectors = active ? p.heads[2] * p.D / 8 : 0;
+  const bool mine = active && u < units;  // (lanes past a head's elements add zeros to its sums)
+
+  Eight<T> x[kBatch][2], v[2 * kBatch];
+  auto fetch = [&](int h, int vi) {
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const int hk = h + k * hstep;
+      if (mine && hk < heads) {
+        const bool q = hk < p.heads[0];
+        const T* src = static_cast<const T*>(q ? p.in[0] : p.in[1]) + n * (q ? p.ld[0] : p.ld[1]) +
+                       (q ? hk : hk - p.heads[0]) * p.D;
+        x[k][0].load(src + e0);
+        x[k][1].load(src + e1);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 2 * kBatch; ++k)
+      if (vi + k * vstep < vectors)
+        v[k].load(static_cast<const T*>(p.in[2]) + n * p.ld[2] + static_cast<int64_t>(vi + k * vstep) * 8);
+  };
+  fetch(h0, v0);
+  token_angles(p, n0, here, cs);
+  float c[8], s[8];
+  if (turned && mine) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float2 z = cs[tok * half + u * 8 + i];
+      c[i] = z.x;
+      s[i] = z.y;
+    }
+  }
+  const float inv_d = 1.f / static_cast<float>(p.D);
+  // (Every lane of a warp makes the same rounds: the sums are exchanged by all.)
+  const int first = static_cast<int>(blockIdx.y) * per_pass;
+  int h = h0, vi = v0;
+  for (int base = first, vb = v0 - lane; base < heads || vb < p.heads[2] * p.D / 8;
+       base += kBatch * hstep, vb += 2 * kBatch * vstep) {
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      if (base + k * hstep >= heads) break;  // (uniform)
+      const int hk = h + k * hstep;
+      const bool have = mine && hk < heads;
+      float y[kUnit];
+      {
+        float a[8], b[8];
+        x[k][0].get(a);
+        x[k][1].get(b);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          y[i] = have ? a[i] : 0.f;
+          y[8 + i] = have ? b[i] : 0.f;
+        }
+      }
+      if (p.layer) {
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < kUnit; ++i) sum += y[i];
+        const float mean = group_sum(sum, width) * inv_d;
+#pragma unroll
+        for (int i = 0; i < kUnit; ++i) y[i] = have ? y[i] - mean : 0.f;
+      }
+      float sq = 0.f;
+#pragma unroll
+      for (int i = 0; i < kUnit; ++i) sq = fmaf(y[i], y[i], sq);
+      const float r = rsqrtf(fmaf(group_sum(sq, width), inv_d, p.eps));
+      if (!have) continue;
+      const int which = hk < p.heads[0] ? 0 : 1, hh = which ? hk - p.heads[0] : hk;
+      const W* w = static_cast<const W*>(which ? p.weight[1] : p.weight[0]);
+      const W* bi = static_cast<const W*>(which ? p.bias[1] : p.bias[0]);
+      const int64_t woff = static_cast<int64_t>(hh) * (which ? p.wld[1] : p.wld[0]);
+#pragma unroll
+      for (int i = 0; i < kUnit; ++i) y[i] *= r;
+      if (w) {
+        Eight<W> t[2];
+        float a[8], b[8];
+        t[0].load(w + woff + e0);
+        t[1].load(w + woff + e1);
+        t[0].get(a);
+        t[1].get(b);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          y[i] *= a[i];
+          y[8 + i] *= b[i];
+        }
+      }
+      if (bi) {
+        Eight<W> t[2];
+        float a[8], b[8];
+        t[0].load(bi + woff + e0);
+        t[1].load(bi + woff + e1);
+        t[0].get(a);
+        t[1].get(b);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          y[i] += a[i];
+          y[8 + i] += b[i];
+        }
+      }
+      float z[kUnit];
+      if (!turned) {
+#pragma unroll
+        for (int i = 0; i < kUnit; ++i) z[i] = y[i];
+      } else if (p.interleaved) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          z[2 * i] = y[2 * i] * c[i] - y[2 * i + 1] * s[i];
+          z[2 * i + 1] = y[2 * i + 1] * c[i] + y[2 * i] * s[i];
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          z[i] = y[i] * c[i] - y[8 + i] * s[i];
+          z[8 + i] = y[8 + i] * c[i] + y[i] * s[i];
+        }
+      }
+      __nv_bfloat16* dst = (which ? p.out[1] : p.out[0]) + (n * (which ? p.heads[1] : p.heads[0]) + hh) * p.D;
+      float za[8], zb[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        za[i] = z[i];
+        zb[i] = z[8 + i];
+      }
+      put(dst + e0, za);
+      put(dst + e1, zb);
+    }
+#pragma unroll
+    for (int k = 0; k < 2 * kBatch; ++k) {
+      if (vi + k * vstep < vectors) {
+        float a[8];
+        v[k].get(a);
+        put(p.out[2] + n * p.heads[2] * p.D + static_cast<int64_t>(vi + k * vstep) * 8, a);
+      }
+    }
+    h += kBatch * hstep;
+    vi += 2 * kBatch * vstep;
+    fetch(h, vi);
+  }
+}
+
+// Any head size, even rotary_dim, row stride and alignment: a warp takes a head
+// at a time, in shared memory as fp32, element by element.
+template <typename T, typename W>
+__global__ void __launch_bounds__(kThreads) norm_rope_any_kernel(const NormParams p) {
+  extern __shared__ float2 shared[];
+  float2* cs = shared;
+  adt::pdl_wait_then_release();
+  const int64_t n = blockIdx.x;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  const int half = p.rot / 2, heads = p.heads[0] + p.heads[1];
+  float* row = reinterpret_cast<float*>(shared + half) + warp * p.D;
+  token_angles(p, blockIdx.x, 1, cs);
+  for (int h = blockIdx.y * warps + warp; h < heads; h += gridDim.y * warps) {
+    const int which = h < p.heads[0] ? 0 : 1, hh = which ? h - p.heads[0] : h;
+    const T* src = static_cast<const T*>(p.in[which]) + n * p.ld[which] + static_cast<int64_t>(hh) * p.D;
+    const W* w = static_cast<const W*>(p.weight[which]);
+    const W* bi = static_cast<const W*>(p.bias[which]);
+    const int64_t woff = static_cast<int64_t>(hh) * p.wld[which];
+    float sum = 0.f;
+    for (int e = lane; e < p.D; e += 32) {
+      const float x = to_f32(src[e]);
+      row[e] = x;
+      sum += x;
+    }
+    const float mean = p.layer ? adt::warp_sum(sum) / static_cast<float>(p.D) : 0.f;
+    float sq = 0.f;
+    for (int e = lane; e < p.D; e += 32) {
+      const float x = row[e] - mean;
+      sq = fmaf(x, x, sq);
+    }
+    const float r = rsqrtf(adt::warp_sum(sq) / static_cast<float>(p.D) + p.eps);
+    for (int e = lane; e < p.D; e += 32) {
+      float y = (row[e] - mean) * r;
+      if (w) y *= to_f32(w[woff + e]);
+      if (bi) y += to_f32(bi[woff + e]);
+      row[e] = y;
+    }
+    __syncwarp();
+    __nv_bfloat16* dst = p.out[which] + (n * p.heads[which] + hh) * p.D;
+    for (int e = lane; e < p.D; e += 32) {
+      float y = row[e];
+      if (e < p.rot) {
+        const int pair = p.interleaved ? e >> 1 : e < half ? e : e - half;
+        const bool lead = p.interleaved ? (e & 1) == 0 : e < half;
+        const float2 z = cs[pair];
+        const float other = row[p.interleaved ? e ^ 1 : lead ? e + half : e - half];
+        y = y * z.x + other * (lead ? -z.y : z.y);
+      }
+      dst[e] = __float2bfloat16(y);
+    }
+    __syncwarp();  // before the row is overwritten
+  }
+  const T* in = static_cast<const T*>(p.in[2]) + n * p.ld[2];
+  __nv_bfloat16* out = p.out[2] + n * p.heads[2] * p.D;
+  for (int i = blockIdx.y * blockDim.x + threadIdx.x; i < p.heads[2] * p.D; i += gridDim.y * blockDim.x)
+    out[i] = __float2bfloat16(to_f32(in[i]));
+}
+
+template <typename T, typename W>
+adt_status launch(const NormParams& p, bool vec, int N, const adt::DeviceInfo& info, cudaLaunchConfig_t* cfg) {
+  const int heads = p.heads[0] + p.heads[1];
+  if (vec) {
+    const int units = p.D / kUnit, width = adt::next_pow2(units);
+    // Threads of a token, as adt_rope_qkv chooses them: one unit of its heads and
+    // one pair of vectors of its values each, or with many tokens two of each.
+    const int qk = heads * width, vs = (p.heads[2] * units + 1) / 2, want = qk > vs ? qk : vs;
+    auto lanes_of = [&](int each) {
+      int l = ((want + each - 1) / each + 31) / 32 * 32;
+      return l < kThreads ? l : kThreads;
+    };
+    const bool many = static_cast<int64_t>(N) * lanes_of(2) >= int64_t{4} * kThreads * info.sm_count;
+    const int lanes = lanes_of(many ? 2 : 1);
+    const int tokens = kThreads / lanes;
+    const int passes = (want + lanes - 1) / lanes;
+    const int groups = (N + tokens - 1) / tokens;
+    // Few tokens: their heads over several CTAs, up to two an SM.
+    int split = 2 * info.sm_count / groups;
+    split = split < 1 ? 1 : split > passes ? passes : split;
+    cfg->gridDim = dim3(static_cast<unsigned>(groups), static_cast<unsigned>(split), 1);
+    cfg->blockDim = dim3(static_cast<unsigned>(lanes * tokens), 1, 1);
+    cfg->dynamicSmemBytes = static_cast<size_t>(tokens) * (p.rot / 2) * sizeof(float2);
+    ADT_CUDA_TRY(cudaLaunchKernelEx(cfg, norm_rope_vec_kernel<T, W>, p, N, tokens, lanes, width));
+    return adt::launch_status();
+  }
+  // Rows of shared memory: within the 48 KB that need no opting in.
+  int warps = (48 * 1024 - kMaxRotary * 4) / (p.D * 4);
+  warps = warps > kThreads / 32 ? kThreads / 32 : warps;
+  const int most = heads > 0 ? (heads + warps - 1) / warps : 1;
+  int split = 2 * info.sm_count / N;
+  split = split < 1 ? 1 : split > most ? most : split;
+  cfg->gridDim = dim3(static_cast<unsigned>(N), static_cast<unsigned>(split), 1);
+  cfg->blockDim = dim3(static_cast<unsigned>(warps * 32), 1, 1);
+  cfg->dynamicSmemBytes = p.rot / 2 * sizeof(float2) + static_cast<size_t>(warps) * p.D * 4;
+  ADT_CUDA_TRY(cudaLaunchKernelEx(cfg, norm_rope_any_kernel<T, W>, p));
+  return adt::launch_status();
+}
+
+static_assert((48 * 1024 - kMaxRotary * 4) / (kMaxHead * 4) >= 1, "a warp's row fits");
+
+}  // namespace
+
+extern "C" {
+
+adt_status adt_norm_rope_qkv(const void* q, int64_t ld_q, const void* k, int64_t ld_k, const void* v, int64_t ld_v,
+                             adt_dtype in_type, adt_norm norm, float eps, const void* q_weight, const void* q_bias,
+                             int32_t q_weight_stride, const void* k_weight, const void* k_bias, int32_t k_weight_stride,
+                             adt_dtype weight_type, const int32_t* positions, const double* inv_freq, float magnitude,
+                             adt_rope_layout layout, int32_t N, int32_t H, int32_t Hkv, int32_t D, int32_t rotary_dim,
+                             adt_bf16* q_out, adt_bf16* k_out, adt_bf16* v_out, void* stream) {
+  adt::TraceRange trace_("adt_norm_rope_qkv");
+  ADT_REQUIRE(in_type == ADT_TYPE_BF16 || in_type == ADT_TYPE_F32);
+  ADT_REQUIRE(weight_type == ADT_TYPE_BF16 || weight_type == ADT_TYPE_F32);
+  ADT_REQUIRE(norm == ADT_NORM_RMS || norm == ADT_NORM_LAYER);
+  ADT_REQUIRE(layout == ADT_ROPE_HALF || layout == ADT_ROPE_INTERLEAVED);
+  ADT_REQUIRE(N >= 0 && N <= kMaxRows && D >= 1 && D <= kMaxHead && rotary_dim >= 0 && rotary_dim % 2 == 0 &&
+              rotary_dim <= D);
+  if (rotary_dim > kMaxRotary) return ADT_ERR_UNSUPPORTED;
+  ADT_REQUIRE(isfinite(magnitude) && isfinite(eps) && eps >= 0.f);
+  if (N == 0) return ADT_OK;
+  ADT_REQUIRE((q != nullptr) == (q_out != nullptr) && (k != nullptr) == (k_out != nullptr) &&
+              (v != nullptr) == (v_out != nullptr));
+  ADT_REQUIRE(q || k || v);
+  ADT_REQUIRE((!q || (H >= 1 && H <= 65535)) && ((!k && !v) || (Hkv >= 1 && Hkv <= 65535)));
+  ADT_REQUIRE(positions && (inv_freq || rotary_dim == 0));
+  NormParams p{};
+  const void* in[3] = {q, k, v};
+  adt_bf16* out[3] = {q_out, k_out, v_out};
+  const int64_t ld[3] = {ld_q, ld_k, ld_v};
+  const void* weight[2] = {q_weight, k_weight};
+  const void* bias[2] = {q_bias, k_bias};
+  const int32_t wld[2] = {q_weight_stride, k_weight_stride};
+  const int esize = in_type == ADT_TYPE_BF16 ? 2 : 4, wsize = weight_type == ADT_TYPE_BF16 ? 2 : 4;
+  int64_t in_bytes[3], out_bytes[3];
+  for (int x = 0; x < 3; ++x) {
+    p.heads[x] = !in[x] ? 0 : x == 0 ? H : Hkv;
+    const int64_t width = static_cast<int64_t>(p.heads[x]) * D;
+    ADT_REQUIRE(!in[x] || (ld[x] >= width && ld[x] <= kMaxSpan / N));
+    ADT_REQUIRE(reinterpret_cast<uintptr_t>(in[x]) % esize == 0 && reinterpret_cast<uintptr_t>(out[x]) % 2 == 0);
+    in_bytes[x] = in[x] ? ((N - 1) * ld[x] + width) * esize : 0;
+    out_bytes[x] = in[x] ? N * width * 2 : 0;
+    p.in[x] = in[x];
+    p.ld[x] = ld[x];
+    p.out[x] = reinterpret_cast<__nv_bfloat16*>(out[x]);
+  }
+  bool aligned = D % 8 == 0;
+  for (int x = 0; x < 2; ++x) {
+    const void* params[2] = {weight[x], bias[x]};
+    for (const void* w : params) {
+      if (!w || !in[x]) continue;
+      ADT_REQUIRE(wld[x] == 0 || wld[x] >= D);
+      ADT_REQUIRE(reinterpret_cast<uintptr_t>(w) % wsize == 0);
+      const int64_t bytes = (static_cast<int64_t>(p.heads[x] - 1) * wld[x] + D) * wsize;
+      for (int y = 0; y < 3; ++y) ADT_REQUIRE(!overlap(out[y], out_bytes[y], w, bytes));
+      aligned = aligned && adt::aligned16(w) && static_cast<int64_t>(wld[x]) * wsize % 16 == 0;
+    }
+    p.weight[x] = weight[x];
+    p.bias[x] = bias[x];
+    p.wld[x] = wld[x];
+  }
+  // An output may be its own input (a head is read before it is overwritten);
+  // nothing else may overlap.
+  for (int x = 0; x < 3; ++x) {
+    for (int y = 0; y < 3; ++y) {
+      if (overlap(out[x], out_bytes[x], in[y], in_bytes[y]))
+        ADT_REQUIRE(x == y && out[x] == in[x] && esize == 2 && ld[x] == static_cast<int64_t>(p.heads[x]) * D);
+      ADT_REQUIRE(x == y || !overlap(out[x], out_bytes[x], out[y], out_bytes[y]));
+    }
+    aligned = aligned && (!in[x] || (adt::aligned16(in[x]) && adt::aligned16(out[x]) && ld[x] * esize % 16 == 0));
+  }
+  p.pos = positions;
+  p.inv_freq = inv_freq;
+  p.magnitude = magnitude;
+  p.eps = eps;
+  p.D = D;
+  p.rot = rotary_dim;
+  p.interleaved = layout == ADT_ROPE_INTERLEAVED;
+  p.layer = norm == ADT_NORM_LAYER;
+  adt::DeviceInfo info;
+  adt_status st = adt::device_info(&info);
+  if (st != ADT_OK) return st;
+  cudaLaunchConfig_t cfg = {};
+  cfg.stream = adt::as_stream(stream);
+  cudaLaunchAttribute attr[1] = {adt::pdl_attribute()};
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  const bool vec = aligned && D % kUnit == 0 && rotary_dim % kUnit == 0 && D <= 32 * kUnit;
+  if (esize == 2)
+    return wsize == 2 ? launch<__nv_bfloat16, __nv_bfloat16>(p, vec, N, info, &cfg)
+                      : launch<__nv_bfloat16, float>(p, vec, N, info, &cfg);
+  return wsize == 2 ? launch<float, __nv_bfloat16>(p, vec, N, info, &cfg) : launch<float, float>(p, vec, N, info, &cfg);
+}
+
+}  // extern "C"
