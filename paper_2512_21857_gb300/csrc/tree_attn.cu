@@ -87,6 +87,8 @@ using sm100::pack_f32x2;
 using sm100::pack_u32x2;
 using sm100::sw128_off;
 using sm100::tmem_ld_32;
+using sm100::tmem_st_16;
+using sm100::tmem_st_32;
 using sm100::tmem_wait_ld_into;
 using sm100::unpack_f32x2;
 using sm100::wait_bar;
