@@ -58,12 +58,13 @@ constexpr int kChunk = 128;             // keys of a chunk
 constexpr int kMaxTreeNodes = 256;
 constexpr int64_t kMaxRows = 1 << 24;   // query rows of a call
 constexpr int kItemCost = 2;            // chunks that an item's start and end take the time of
+constexpr int kJoinCost = 6;            // ... and that joining an item's parts takes
 constexpr int kMinShare = 6;            // coordinates (see Walk) of a CTA's share, where there are few
 constexpr int kSoftmaxThreads = 256;
 constexpr int kKWarp = 8, kVWarp = 9, kSWarp = 10, kPvWarp = 11, kConvWarp = 12;
 constexpr int kConvThreads = 128;
 constexpr int kThreads = 512;
-constexpr int kMaxScaleSlots = 16;
+constexpr int kMaxScaleSlots = 10;
 constexpr int kMaxStages = 6;
 constexpr int kMaxGrid = 1024;          // tickets of the workspace
 constexpr uint32_t kTmemCols = 512;
@@ -78,22 +79,37 @@ template <int D>
 struct Cfg {
   static constexpr int kKStages = D == 128 ? 3 : 6;
   static constexpr int kVStages = D == 128 ? 2 : 4;
-  static constexpr int kScaleSlots = D == 128 ? 8 : 16;
+  static constexpr int kScaleSlots = kKStages + 4;
   static constexpr int kTile = kChunk * D;                // 128 rows of e4m3
-  static constexpr int kBlock = kChunk * 128;             // one 64-column block of 128 rows of bf16
-  static constexpr int kWide = D / 64 * kBlock;           // 128 rows of bf16
+  static constexpr int kBlock = kChunk * 128;             // one 64-column block of 128 rows of fp16
+  static constexpr int kWide = D / 64 * kBlock;           // 128 rows of fp16
   static constexpr int kQOff = 0;                         // [2 items][high, low]
   static constexpr int kKOff = kQOff + 4 * kTile;
   static constexpr int kVOff = kKOff + kKStages * kTile;
   static constexpr int kWideOff = kVOff + kVStages * kTile;
   static constexpr int kScaleOff = kWideOff + 2 * kWide;  // [slots][K, V][128] fp32
-  static constexpr int kDynSmem = kScaleOff + kScaleSlots * 2 * kChunk * 4 + 1024;  // + alignment slack
-  static constexpr uint32_t kIdescS = sm100::idesc_e4m3_f32(kRows, kChunk);
-  static constexpr uint32_t kIdescO = sm100::idesc_bf16_f32(kRows, D, 0, 1);
+  static constexpr int kJoinOff = kScaleOff + kScaleSlots * 2 * kChunk * 4;  // D = 64: [2 groups][128][32] fp32
+  static constexpr int kDynSmem = kJoinOff + (D == 128 ? 0 : 2 * kRows * 32 * 4) + 1024;  // + alignment slack
+  static_assert(D != 128 || kWide == 2 * kRows * 32 * 4, "copies are joined in a V tile");
+  static constexpr uint32_t kIdescO = sm100::idesc_f16_f32(kRows, D, 0, 1);
   static_assert(kKStages <= kMaxStages && kVStages <= kMaxStages && kScaleSlots <= kMaxScaleSlots && kOCol + D <= kPCol, "sizes");
 };
 
+// What the first launch makes of the queries and of the trees, as the second one's
+// shared memory takes it.  Blocks of q_rows (<= 128) queries, chunks of t_rows
+// (<= 128) nodes; (b, g) the tree and kv head.
+struct Prepared {
+  uint8_t* q;       // [b, g][block][high, low][q_rows x D]
+  float* q_scale;   // [b, g][block][q_rows], times softmax_scale log2 e
+  uint8_t* k;       // [b, g][chunk][high, low][t_rows x D]
+  uint4* v;         // [b, g][chunk][D / 64][t_rows][8], fp16
+  uint8_t* scale;   // [b, g][chunk][of K, of V, whether V is not finite][t_rows]
+  uint4* seen;      // [b][node][chunk]: the nodes that it sees
+  int q_rows, blocks, t_rows, chunks;
+};
+
 struct AttnParams {
+  Prepared pre;
   const __nv_bfloat16* q;
   const uint8_t* v_cache;
   const uint8_t* scale[2];
@@ -102,13 +118,14 @@ struct AttnParams {
   const int32_t* parents;
   const int32_t* offs;
   int B, H, Hkv, group, max_nodes, max_kv, slot_rows;
+  int copies;          // of a row in a tile: 1, 2 or 4
   int64_t sb, sh, ssb, ssh;
   float scale_log2;
   __nv_bfloat16* out;
   float* lse;
   unsigned* tickets;   // [grid], of the items that start in a CTA's share and end in another's
   float2* part_ml;     // [2 grid][slot_rows]: of a CTA's first and of its last item
-  float* part_o;       // [2 grid][slot_rows][D]
+  float4* part_o;      // [2 grid][D / 4][slot_rows]
   unsigned* err;
   uint32_t wait_limit;
 };
@@ -135,10 +152,13 @@ __device__ __forceinline__ Tree tree_of(const AttnParams& p, int b, unsigned* bi
 // Item by item (tree, kv head, block) a coordinate runs through kItemCost units
 // and then a unit a chunk; a share is a range of coordinates and takes the chunks
 // that lie in it.  Share c of G of a total of X starts at c X / G, rounded down.
+// Where an item a CTA takes no longer than equal shares with their joining would,
+// all items are padded to one width, and a share is an item.
 struct Walk {
   int b, g, blk;
   Tree t;
   int64_t start, end;  // the item's first coordinate; the end of the share
+  int padded;          // every item's width, or 0: its chunks and kItemCost
   int k0, k1;          // the share's chunks of the item
   bool first;          // of the share's items
   __device__ __forceinline__ void clip(int64_t from) {
@@ -148,7 +168,7 @@ struct Walk {
   }
   __device__ __forceinline__ bool some() const { return k1 > k0; }
   __device__ __forceinline__ bool next(const AttnParams& p) {
-    start += kItemCost + t.chunks;
+    start += padded ? padded : kItemCost + t.chunks;
     first = false;
     if (start + kItemCost >= end) return false;
     if (++blk == t.blocks) {
@@ -167,6 +187,26 @@ struct Walk {
   }
 };
 
+// The tree's values that are not finite were left out of the products: adds those
+// that node t sees, of nodes t0 up to before t1, to `cols` columns of its row, as
+// written (final or partial).  tree: the first node's values at the first column.
+__device__ __noinline__ void add_odd(__nv_bfloat16* out, float* part, int part_step, int cols, const __nv_bfloat16* tree,
+                                     const int32_t* parents, int64_t step, int t, int t0, int t1) {
+  for (;;) {
+    for (int i = 0; t >= t0 && t < t1 && i < cols; ++i) {
+      const float f = __bfloat162float(tree[t * step + i]);
+      if (isfinite(f)) continue;
+      if (out)
+        out[i] = __float2bfloat16(__bfloat162float(out[i]) + f);
+      else
+        part[(i / 4) * part_step * 4 + i % 4] += f;
+    }
+    const int up = parents[t];
+    if (up < 0 || up >= t) return;
+    t = up;
+  }
+}
+
 struct Bars {
   uint64_t k_full[kMaxStages], k_free[kMaxStages];
   uint64_t v_full[kMaxStages], v_free[kMaxStages];
@@ -177,6 +217,7 @@ struct Bars {
   uint64_t mu[2][4];         // the running maxima after a chunk are in shared memory, per group and warp
   uint64_t done[4];          // the PV product of chunk j is done (barrier j % 4)
   uint64_t o_free;           // an item's O is read
+  uint64_t join_free[2];     // its copies are joined (even and odd items: a second one may end before the first is asked for)
   uint64_t drain[2];
 };
 
@@ -211,11 +252,21 @@ __device__ __forceinline__ uint64_t tile_desc(uint32_t addr) {
   return D == 128 ? sm100::smem_desc_sw128(addr, 16, 1024) : sm100::smem_desc_sw64(addr);
 }
 
+__device__ __forceinline__ uint32_t e4m3x2_to_f16(uint32_t two) {
+  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(two & 0xffffu), __NV_E4M3);
+  return static_cast<uint32_t>(h.x) | static_cast<uint32_t>(h.y) << 16;
+}
+
+__device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
+  const __half2 v = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+
 // 16 elements of a bf16 row, D / 16 neighbouring lanes to a row (all lanes of the
-// warp take part): cut into two e4m3 rows at `high` and `low`.  Returns the scale, a
-// power of two, that their sum goes with.  A row that is not finite becomes NaN.
+// warp take part): cut into two e4m3 rows, high and low, whose sum goes with the
+// scale 2^(s - 127), s what it returns.  A row that is not finite becomes NaN.
 template <int D>
-__device__ __forceinline__ float cut_row(const uint4 (&x)[2], uint8_t* high, uint8_t* low, bool store) {
+__device__ __forceinline__ uint32_t cut_row(const uint4 (&x)[2], uint4& high, uint4& low) {
   const uint32_t w[8] = {x[0].x, x[0].y, x[0].z, x[0].w, x[1].x, x[1].y, x[1].z, x[1].w};
   uint32_t most = 0u;
 #pragma unroll
@@ -240,11 +291,144 @@ __device__ __forceinline__ float cut_row(const uint4 (&x)[2], uint8_t* high, uin
     }
     if (!finite) h[k] = l[k] = 0x7f7f7f7fu;
   }
-  if (store) {
-    *reinterpret_cast<uint4*>(high) = make_uint4(h[0], h[1], h[2], h[3]);
-    *reinterpret_cast<uint4*>(low) = make_uint4(l[0], l[1], l[2], l[3]);
+  high = make_uint4(h[0], h[1], h[2], h[3]);
+  low = make_uint4(l[0], l[1], l[2], l[3]);
+  return s;
+}
+
+__device__ __forceinline__ void group_sync(int grp) {  // of the four warps of a softmax group
+  if (grp == 0)
+    asm volatile("bar.sync 3, 128;\n" ::: "memory");
+  else
+    asm volatile("bar.sync 4, 128;\n" ::: "memory");
+}
+
+// (The polling apart from its many callers: instructions are what this kernel's
+// roles, each in code of its own, wait for most.)
+__device__ __noinline__ bool wait_on(uint64_t* bar, uint32_t parity, volatile int* abort_flag, unsigned* err, uint32_t limit) {
+  return sm100::wait_bar(bar, parity, abort_flag, err, limit);
+}
+
+// 2^(s - ref + kHeadroom) for a value row's scale s against a reference: what its weights take on.
+constexpr int kHeadroom = 4, kSlack = 3;
+__device__ __forceinline__ float value_factor(int s, int ref) {
+  const int e = s - ref + kHeadroom + 127;
+  return s == 255 ? __uint_as_float(0x7fc00000u) : e > 0 ? __uint_as_float(static_cast<uint32_t>(e) << 23) : 0.f;
+}
+__device__ __forceinline__ float power_of_two(int e) {
+  return e < -126 ? 0.f : __uint_as_float(static_cast<uint32_t>(min(e, 127) + 127) << 23);
+}
+
+// The first launch: a row is D / 16 lanes', 16 elements each.  Of a tree the query
+// rows, then its nodes' rows of every kv head (zeros up to a multiple of 16 nodes).
+// Bound by its launch and two rounds of loads (trees of 64 nodes, 32 / 8 heads x
+// 128, are 2 MB); within the second one, every item and every share of one would do
+// it anew, by warps that have other work.
+constexpr int kPrepThreads = 256;
+
+template <int D>
+__global__ void __launch_bounds__(kPrepThreads) prepare_kernel(const AttnParams p) {
+  constexpr int kLanes = D / 16, kPass = kPrepThreads / kLanes;
+  __shared__ int16_t s_par[kMaxTreeNodes];
+  asm volatile("griddepcontrol.wait;\n" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+  const int b = blockIdx.y, tid = threadIdx.x;
+  unsigned bits = 0u;
+  const Tree t = tree_of(p, b, &bits);
+  if (blockIdx.x == 0 && tid == 0 && bits) adt::raise_error(p.err, bits);
+  if (t.n == 0) return;
+  const Prepared& w = p.pre;
+  const int queries = t.n * p.H, nodes = (t.n + 15) & ~15;
+  const int unit = blockIdx.x * kPass + tid / kLanes, cl = tid % kLanes;
+  if (blockIdx.x == 0) {
+    // What each node sees.  Parents precede their children; anything else marks the
+    // tree malformed.
+    for (int i = tid; i < t.n; i += kPrepThreads) {
+      const int up = p.parents[t.node0 + i];
+      s_par[i] = static_cast<int16_t>(min(max(up, -1), kMaxTreeNodes));
+      if ((i == 0) != (up < 0) || up >= i) adt::raise_error(p.err, ADT_DEVERR_BAD_TREE);
+    }
+    __syncthreads();
+    for (int i = tid; i < t.n * w.chunks; i += kPrepThreads) {
+      uint32_t m[4] = {0u, 0u, 0u, 0u};
+      const int t0 = i % w.chunks * kChunk;
+      for (int x = i / w.chunks;;) {
+        const int at = x - t0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) m[e] |= at >> 5 == e ? 1u << (at & 31) : 0u;
+        const int up = s_par[x];
+        if (up < 0 || up >= x) break;
+        x = up;
+      }
+      w.seen[static_cast<int64_t>(b) * p.max_nodes * w.chunks + i] = make_uint4(m[0], m[1], m[2], m[3]);
+    }
   }
-  return __uint_as_float(s << 23);
+  uint4 x[2] = {}, v[2] = {};
+  const bool is_q = unit < queries;
+  const int rest = unit - queries, node = is_q ? unit / p.H : rest / p.Hkv;
+  const bool is_t = !is_q && node < nodes;
+  const int h = is_q ? unit - node * p.H : 0, g = is_q ? h / p.group : rest - node * p.Hkv;
+  if (is_q) {
+    const uint4* src = reinterpret_cast<const uint4*>(p.q + (static_cast<int64_t>(t.node0) * p.H + unit) * D) + cl * 2;
+    x[0] = src[0];
+    x[1] = src[1];
+  } else if (is_t && node < t.n) {
+    const int64_t at = (static_cast<int64_t>(t.node0 + node) * p.Hkv + g) * D;
+    const uint4* src = reinterpret_cast<const uint4*>(p.tree[0] + at) + cl * 2;
+    x[0] = src[0];
+    x[1] = src[1];
+    src = reinterpret_cast<const uint4*>(p.tree[1] + at) + cl * 2;
+    v[0] = src[0];
+    v[1] = src[1];
+  }
+  uint4 high, low;
+  const uint32_t s = cut_row<D>(x, high, low);
+  const int64_t bg = static_cast<int64_t>(b) * p.Hkv + g;
+  if (is_q) {
+    const int row = node * p.group + h - g * p.group, blk = row / kRows, r = row % kRows;
+    const int64_t at = bg * w.blocks + blk;
+    uint8_t* dst = w.q + at * 2 * w.q_rows * D + tile_off<D>(r, cl);
+    *reinterpret_cast<uint4*>(dst) = high;
+    *reinterpret_cast<uint4*>(dst + w.q_rows * D) = low;
+    if (cl == 0) w.q_scale[at * w.q_rows + r] = __uint_as_float(s << 23) * p.scale_log2;
+  }
+  // Values: those that are not finite as zeros (a weight of 0 times them would
+  // reach rows that do not see them), scaled as their cached rows would be, but in
+  // fp16: below 448, with 2^-24 the least step, 2^-33 of the row's largest.
+  uint32_t y[8] = {v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w}, most = 0u, odd = 0u;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const bool lo = (y[e] & 0x7f80u) == 0x7f80u, hi = (y[e] & 0x7f800000u) == 0x7f800000u;
+    odd |= lo || hi ? 1u : 0u;
+    if (lo) y[e] &= 0xffff0000u;
+    if (hi) y[e] &= 0xffffu;
+    most = max(most, max(y[e] << 16 & 0x7fff0000u, y[e] & 0x7fff0000u));
+  }
+#pragma unroll
+  for (int o = kLanes / 2; o > 0; o >>= 1) {
+    most = max(most, __shfl_xor_sync(adt::kFullMask, most, o));
+    odd |= __shfl_xor_sync(adt::kFullMask, odd, o);
+  }
+  if (!is_t) return;
+  const uint32_t vs = adt::q8_row_scale(__uint_as_float(most));
+  const float inv = __uint_as_float((254u - vs) << 23);
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    y[e] = pack_half2(__uint_as_float(y[e] << 16) * inv, __uint_as_float(y[e] & 0xffff0000u) * inv);
+  const int r = node % kChunk;
+  const int64_t at = bg * w.chunks + node / kChunk;
+  uint8_t* dst = w.k + at * 2 * w.t_rows * D + tile_off<D>(r, cl);
+  *reinterpret_cast<uint4*>(dst) = high;
+  *reinterpret_cast<uint4*>(dst + w.t_rows * D) = low;
+  uint8_t* wide = reinterpret_cast<uint8_t*>(w.v + at * (D / 64) * w.t_rows * 8);
+  *reinterpret_cast<uint4*>(wide + sw128_off(r, 2 * cl, w.t_rows)) = make_uint4(y[0], y[1], y[2], y[3]);
+  *reinterpret_cast<uint4*>(wide + sw128_off(r, 2 * cl + 1, w.t_rows)) = make_uint4(y[4], y[5], y[6], y[7]);
+  if (cl == 0) {
+    uint8_t* sc = w.scale + at * 3 * w.t_rows + r;
+    sc[0] = static_cast<uint8_t>(s);
+    sc[w.t_rows] = static_cast<uint8_t>(vs);
+    sc[2 * w.t_rows] = static_cast<uint8_t>(odd);
+  }
 }
 
 template <int D>
@@ -255,10 +439,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (sm100::smem_addr(smem_raw) & 1023u)) & 1023u);
   __shared__ Bars bars;
-  __shared__ uint4 s_anc[2][kRows];          // the keys of a tree chunk that a row sees
-  __shared__ int16_t s_par[kMaxTreeNodes];
-  __shared__ float s_mu[kRows], s_l[2][2][kRows], s_qscale[4][kRows];
-  __shared__ int s_odd[8];                   // an item's tree has values that are not finite
+  __shared__ float s_mu[kRows], s_m[2][kRows], s_l[2][2][kRows];
+  __shared__ int s_ref[kMaxScaleSlots];      // the reference of a chunk's value scales
+  __shared__ float s_drop[kMaxScaleSlots];   // what O shrinks by where it rose with the chunk
+  __shared__ int s_odd[kMaxScaleSlots];      // whether a tree chunk has values that are not finite
   __shared__ Walk s_walk;
   __shared__ int64_t s_total;
   __shared__ int s_grid, s_last;
@@ -287,10 +471,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     init(bars.mu[0], 8, 1);
     init(bars.done, 4, 1);
     init(&bars.o_free, 1, 8);
+    init(bars.join_free, 2, 8);
     init(bars.drain, 2, 1);
     sm100::fence_mbar_init();
   }
-  if (tid < 8) s_odd[tid] = 0;
   if (warp == kPvWarp) {
     sm100::tmem_alloc(sm100::smem_addr(&tmem_slot), kTmemCols);
     sm100::tmem_relinquish();
@@ -300,19 +484,29 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp == 0) {
     // This CTA's share.
     unsigned bits = 0u;
-    auto cost = [&](const Tree& t) -> int64_t {
-      return t.chunks ? static_cast<int64_t>(t.chunks + kItemCost) * t.blocks * p.Hkv : 0;
-    };
     Tree t{};
     int64_t mine = 0;
+    int items = 0, longest = 0;
     for (int b = lane; b < p.B; b += 32) {
       t = tree_of(p, b, &bits);
-      mine += cost(t);
+      if (!t.chunks) continue;
+      items += t.blocks * p.Hkv;  // (at most 2^24 rows: no more items)
+      longest = max(longest, t.chunks);
+      mine += static_cast<int64_t>(t.chunks + kItemCost) * t.blocks * p.Hkv;
     }
-    if (blockIdx.x == 0 && bits) adt::raise_error(p.err, bits);
-    const int64_t total = adt::warp_sum(mine);
+    int64_t total = adt::warp_sum(mine);
+    items = adt::warp_sum(items);
+    longest = __reduce_max_sync(adt::kFullMask, longest);
     int64_t shares = total / kMinShare;
     shares = shares < 1 ? 1 : shares > gridDim.x ? gridDim.x : shares;
+    int padded = 0;
+    if (items > 0 && items <= static_cast<int>(gridDim.x) && longest + kItemCost <= total / gridDim.x + kJoinCost) {
+      padded = longest + kItemCost;
+      shares = items;
+      total = static_cast<int64_t>(items) * padded;
+    }
+    auto width = [&](const Tree& t) -> int { return padded ? padded : t.chunks + kItemCost; };
+    auto cost = [&](const Tree& t) -> int64_t { return t.chunks ? static_cast<int64_t>(width(t)) * t.blocks * p.Hkv : 0; };
     const int64_t c = blockIdx.x;
     const int64_t x0 = c < shares ? c * total / shares : total, x1 = c < shares ? (c + 1) * total / shares : total;
     Walk w{};
@@ -330,13 +524,14 @@ __global__ void __launch_bounds__(kThreads, 1)
       const unsigned hit = __ballot_sync(adt::kFullMask, before + upto > x0);
       if (hit) {
         if (lane == __ffs(hit) - 1) {
-          const int64_t off = x0 - (before + upto - mine_here), each = t.chunks + kItemCost, item = off / each;
+          const int64_t off = x0 - (before + upto - mine_here), each = width(t), item = off / each;
           w.b = b0 + lane;
           w.g = static_cast<int>(item / t.blocks);
           w.blk = static_cast<int>(item % t.blocks);
           w.t = t;
           w.start = x0 - off + item * each;
           w.end = x1;
+          w.padded = padded;
           w.clip(x0);
           s_walk = w;
         }
@@ -364,7 +559,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint8_t* sK = smem + C::kKOff;
   uint8_t* sV = smem + C::kVOff;
   uint8_t* sWide = smem + C::kWideOff;
-  auto wait = [&](uint64_t* bar, uint32_t phase) { return sm100::wait_bar(bar, phase & 1u, &s_abort, p.err, p.wait_limit); };
+  auto wait = [&](uint64_t* bar, uint32_t phase) {
+    return sm100::mbar_try_wait(sm100::smem_addr(bar), phase & 1u) || wait_on(bar, phase & 1u, &s_abort, p.err, p.wait_limit);
+  };
   auto all_wait = [&](uint64_t* bar, uint32_t phase) { return __all_sync(adt::kFullMask, wait(bar, phase)); };
   auto arrive = [&](uint64_t* bar) { sm100::mbar_arrive(sm100::smem_addr(bar)); };
   // Chunk j (counted over the whole share) has slot j % stages of a ring, its
@@ -374,36 +571,80 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   if (warp == kKWarp) {
     // ------------------------------------------------------------ K tiles, scales
-    uint32_t issued = 0;  // one past the last tile requested
+    uint32_t issued = 0, q_issued = 0;  // one past the last tile, and the last item's queries, requested
     bool ok = true;
-    float pend[8] = {};
-    int pend_slot = -1;
+    uint32_t pend[3] = {};  // scales of four keys and of their values; a tree's values that are not finite
+    int pend_slot = -1, ref = 0;
+    bool pend_first = false;
     auto flush = [&]() {
       if (pend_slot < 0) return;
+      uint32_t most = 0u;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t v = pend[1] >> (8 * i) & 255u;
+        most = max(most, v == 255u ? 0u : v);
+      }
+      most = __reduce_max_sync(adt::kFullMask, most);
+      // The reference is the first chunk's largest scale, and rises where one is
+      // more than kSlack above it.
+      const int before = ref;
+      if (pend_first || static_cast<int>(most) > ref + kSlack) ref = static_cast<int>(most);
+      float f[8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        f[i] = adt::q8_scale(pend[0] >> (8 * i) & 255u);
+        f[4 + i] = value_factor(static_cast<int>(pend[1] >> (8 * i) & 255u), ref);
+      }
       float4* dst = reinterpret_cast<float4*>(s_scale + pend_slot * 2 * kChunk);
-      dst[lane] = make_float4(pend[0], pend[1], pend[2], pend[3]);
-      dst[32 + lane] = make_float4(pend[4], pend[5], pend[6], pend[7]);
+      dst[lane] = make_float4(f[0], f[1], f[2], f[3]);
+      dst[32 + lane] = make_float4(f[4], f[5], f[6], f[7]);
+      const bool odd = __any_sync(adt::kFullMask, pend[2] != 0u);
+      if (lane == 0) {
+        s_odd[pend_slot] = odd;
+        s_ref[pend_slot] = ref;
+        s_drop[pend_slot] = pend_first ? 1.f : power_of_two(before - ref);
+      }
       __syncwarp();
       if (lane == 0) arrive(&bars.scale_full[pend_slot]);
       pend_slot = -1;
     };
-    for (bool more = true; ok && more; more = w.next(p)) {
-      const int64_t s0 = w.b * p.ssb + w.g * p.ssh;
-      for (int k = w.k0; k < w.k1; ++k, ++j) {
-        if (k >= w.t.prefix) {  // (the tree's: warps 12-15)
-          flush();
-          continue;
+    uint32_t item = 0;
+    for (bool more = true; ok && more; more = w.next(p), ++item) {
+      const int64_t s0 = w.b * p.ssb + w.g * p.ssh, bg = static_cast<int64_t>(w.b) * p.Hkv + w.g;
+      // The item's queries, `copies` times.
+      if (lane == 0) ok = item < 2 || wait(&bars.q_free[item & 1], (item >> 1) - 1);
+      ok = __shfl_sync(adt::kFullMask, ok ? 1 : 0, 0) != 0;
+      if (!ok) break;
+      if (lane == 0) {
+        const int rows = (min(w.t.n * p.group - w.blk * kRows, kRows) + 7) & ~7;
+        const uint32_t bar = sm100::smem_addr(&bars.q_full[item & 1]);
+        sm100::mbar_arrive_expect_tx(bar, 2 * p.copies * rows * D);
+        const uint8_t* src = p.pre.q + (bg * p.pre.blocks + w.blk) * 2 * p.pre.q_rows * D;
+        const uint32_t dst = sm100::smem_addr(sQ + (item & 1) * 2 * C::kTile);
+        for (int c = 0; c < p.copies; ++c) {
+          sm100::bulk_load(dst + c * (C::kTile / p.copies), src, rows * D, bar);
+          sm100::bulk_load(dst + C::kTile + c * (C::kTile / p.copies), src + p.pre.q_rows * D, rows * D, bar);
         }
+        q_issued = item + 1;
+      }
+      for (int k = w.k0; k < w.k1; ++k, ++j) {
         const int st = j % KS;
-        // (S products end in order: where tree chunks are left out, a later wait
-        // of this warp covers theirs.)
         if (lane == 0) ok = j < KS || wait(&bars.k_free[st], j / KS - 1);
         ok = __shfl_sync(adt::kFullMask, ok ? 1 : 0, 0) != 0;
         if (!ok) break;
+        const bool tree_k = k >= w.t.prefix;
+        const int64_t chunk = bg * p.pre.chunks + k - w.t.prefix;  // (of the tree's)
+        const int keys = tree_k ? w.t.n - (k - w.t.prefix) * kChunk : w.t.L - k * kChunk;
         if (lane == 0) {
-          const uint32_t bar = sm100::smem_addr(&bars.k_full[st]);
-          sm100::mbar_arrive_expect_tx(bar, C::kTile);
-          sm100::tma_load_4d(sm100::smem_addr(sK + st * C::kTile), &tm_k, 0, k * kChunk, w.g, w.b, bar);
+          const uint32_t bar = sm100::smem_addr(&bars.k_full[st]), dst = sm100::smem_addr(sK + st * C::kTile);
+          if (tree_k) {  // (the low part comes from warp 9 to the same barrier)
+            const int bytes = min(kChunk, (keys + 15) & ~15) * D;
+            sm100::mbar_arrive_expect_tx(bar, 2 * bytes);
+            sm100::bulk_load(dst, p.pre.k + chunk * 2 * p.pre.t_rows * D, bytes, bar);
+          } else {
+            sm100::mbar_arrive_expect_tx(bar, C::kTile);
+            sm100::tma_load_4d(dst, &tm_k, 0, k * kChunk, w.g, w.b, bar);
+          }
         }
         issued = j + 1;
         // The scales, written when the next chunk's are asked for.  Their slot was
@@ -411,28 +652,34 @@ __global__ void __launch_bounds__(kThreads, 1)
         // four chunks on could start, and S(j - KS) is done.
         static_assert(kScaleSlots >= KS + 4, "a slot that is read");
         flush();
-        float now[8];
+        const int left = keys - lane * 4;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int key = k * kChunk + lane * 4 + (i & 3);
-          // (Rows past the prefix: a score times 1 is masked, a weight of 0 stays 0.)
-          now[i] = key < w.t.L ? adt::q8_scale(p.scale[i >> 2][s0 + key]) : 1.f;
+        for (int x = 0; x < 3; ++x) {
+          if (x == 2 && !tree_k) {
+            pend[x] = 0u;
+            break;
+          }
+          const uint8_t* src = (tree_k ? p.pre.scale + (chunk * 3 + x) * p.pre.t_rows : p.scale[x & 1] + s0 + k * kChunk) + lane * 4;
+          uint32_t v = 0u;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v |= (i < left ? static_cast<uint32_t>(src[i]) : x ? 0u : 127u) << (8 * i);
+          pend[x] = v;
         }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) pend[i] = now[i];
+        pend_first = k == w.k0;
         pend_slot = static_cast<int>(j % kScaleSlots);
       }
     }
     flush();
     asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
     // Every copy issued lands before the CTA goes on (also after an abort).
-    if (lane == 0)
-      for (int st = 0; st < KS; ++st) {
-        // the last use of the slot before `issued` (tree chunks among them, which have no copy)
-        if (issued <= static_cast<uint32_t>(st)) continue;
-        const uint32_t use = (issued - 1 - st) / KS;
-        (void)sm100::mbar_wait_bounded(sm100::smem_addr(&bars.k_full[st]), use & 1u, kDrainLimit);
-      }
+    if (lane == 0) {
+      auto landed = [&](uint64_t* bar, uint32_t n, uint32_t slots) {  // the last uses of a ring, of n in all
+        for (uint32_t i = n > slots ? n - slots : 0; i < n; ++i)
+          (void)sm100::mbar_wait_bounded(sm100::smem_addr(bar + i % slots), i / slots & 1u, kDrainLimit);
+      };
+      landed(bars.k_full, issued, KS);
+      landed(bars.q_full, q_issued, 2);
+    }
     __syncwarp();
   } else if (warp == kVWarp) {
     // ------------------------------------------------------------ V tiles
@@ -449,14 +696,21 @@ __global__ void __launch_bounds__(kThreads, 1)
             break;
           }
           if (k >= w.t.prefix) {
-            // Warps 12-15 write the tree's keys to this chunk's slots of both rings.
-            // (S(j - 2 KS) is done: V(j - VS) was widened after PV(j - VS - 2).)
+            // The low part of the tree's keys, once the chunk before in that slot of K
+            // is done with, and its barrier's phase with it.  (S(j - 2 KS) is: V(j - VS)
+            // was widened after PV(j - VS - 2).)
             static_assert(VS + 2 <= 2 * KS, "a phase of k_free that is known complete");
             if (j >= KS && !wait(&bars.k_free[j % KS], j / KS - 1)) {
               ok = false;
               break;
             }
+            const int c = k - w.t.prefix, bytes = min(kChunk, (w.t.n - c * kChunk + 15) & ~15) * D;
+            const int64_t chunk = (static_cast<int64_t>(w.b) * p.Hkv + w.g) * p.pre.chunks + c;
+            // (Warps 12-15 do not wait for this phase: S frees the slot, and the next one
+            // may be complete first.  It is before S can be.)
             sm100::mbar_arrive(bar);
+            sm100::bulk_load(sm100::smem_addr(sV + st * C::kTile), p.pre.k + (chunk * 2 + 1) * p.pre.t_rows * D, bytes,
+                             sm100::smem_addr(&bars.k_full[j % KS]));
           } else {
             const int rows = min(w.t.L - k * kChunk, kChunk);
             sm100::mbar_arrive_expect_tx(bar, rows * D);
@@ -465,6 +719,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           issued = j + 1;
         }
       }
+      if (!ok) __nanosleep(200000);  // (a tree's keys on their way, on another barrier)
       for (int st = 0; st < VS; ++st) {
         if (issued <= static_cast<uint32_t>(st)) continue;
         const uint32_t use = (issued - 1 - st) / VS;
@@ -478,30 +733,26 @@ __global__ void __launch_bounds__(kThreads, 1)
       bool ok = true;
       uint32_t item = 0;
       for (bool more = true; ok && more; more = w.next(p), ++item) {
-        const uint32_t q = sm100::smem_addr(sQ + (item & 1) * 2 * C::kTile);
+        const uint64_t q = tile_desc<D>(sm100::smem_addr(sQ + (item & 1) * 2 * C::kTile));
         ok = wait(&bars.q_full[item & 1], item >> 1);
         for (int k = w.k0; ok && k < w.k1; ++k, ++j) {
           const int grp = j & 1;
           ok = wait(&bars.k_full[j % KS], j / KS) && (j < 2 || wait(&bars.s_free[grp], (j >> 1) - 1));
           if (!ok) break;
           sm100::tc_fence_after();
-          const uint32_t kt = sm100::smem_addr(sK + (j % KS) * C::kTile);
           const uint32_t d = tmem + grp * kChunk;
+          const int keys = k < w.t.prefix ? w.t.L - k * kChunk : w.t.n - (k - w.t.prefix) * kChunk;
+          const uint32_t idesc = sm100::idesc_e4m3_f32(kRows, 0) | static_cast<uint32_t>(min(kChunk, (keys + 15) & ~15) >> 3) << 17;
+          auto product = [&](uint64_t kt, uint32_t first) {
 #pragma unroll
-          for (int part = 0; part < 2; ++part) {
-#pragma unroll
-            for (int kk = 0; kk < D / 32; ++kk)
-              sm100::mma_f8_ss(d, tile_desc<D>(q + part * C::kTile + kk * 32), tile_desc<D>(kt + kk * 32), C::kIdescS,
-                               part > 0 || kk > 0 ? 1u : 0u);
-          }
-          if (k >= w.t.prefix) {  // the low part of the tree's keys
-            const uint32_t lt = sm100::smem_addr(sV + (j % VS) * C::kTile);
-#pragma unroll
-            for (int part = 0; part < 2; ++part) {
-#pragma unroll
-              for (int kk = 0; kk < D / 32; ++kk)
-                sm100::mma_f8_ss(d, tile_desc<D>(q + part * C::kTile + kk * 32), tile_desc<D>(lt + kk * 32), C::kIdescS, 1u);
+            for (int i = 0; i < D / 16; ++i) {  // the queries' high part, then the low one
+              const int part = i / (D / 32), kk = i % (D / 32);
+              sm100::mma_f8_ss(d, q + (part * C::kTile + kk * 32) / 16, kt + kk * 2, idesc, i == 0 ? first : 1u);
             }
+          };
+          product(tile_desc<D>(sm100::smem_addr(sK + (j % KS) * C::kTile)), 0u);
+          if (k >= w.t.prefix) {  // the low part of the tree's keys
+            product(tile_desc<D>(sm100::smem_addr(sV + (j % VS) * C::kTile)), 1u);
             sm100::mma_commit(sm100::smem_addr(&bars.v_free[j % VS]));
           }
           sm100::mma_commit(sm100::smem_addr(&bars.s_full[grp]));
@@ -545,237 +796,147 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     __syncwarp();
   } else if (warp >= kConvWarp) {
-    // ------------------------------------------------------------ operands
+    // ------------------------------------------------------------ V in fp16
     constexpr int kLanes = D / 16, kPass = kConvThreads / kLanes;  // lanes of a row, rows of a pass
     const int ct = tid - kConvWarp * 32, cl = ct % kLanes, cr = ct / kLanes;
-    uint32_t item = 0;
-    // Item `it`'s queries, rows without a node left out.
-    auto queries = [&](const Walk& v, uint32_t it) -> bool {
-      if (it >= 2 && any_of<1, kConvThreads>(!wait(&bars.q_free[it & 1], (it >> 1) - 1))) return false;
-      const int rows = min(v.t.n * p.group - v.blk * kRows, kRows);
-      uint8_t* high = sQ + (it & 1) * 2 * C::kTile;
-#pragma unroll 2
-      for (int r0 = 0; r0 < rows; r0 += kPass) {
-        const int r = r0 + cr, row = v.blk * kRows + r;
-        uint4 x[2] = {};
-        if (r < rows) {
-          const int t = row / p.group, hh = row - t * p.group;
-          const uint4* src = reinterpret_cast<const uint4*>(
-              p.q + (static_cast<int64_t>(v.t.node0 + t) * p.H + v.g * p.group + hh) * D) + cl * 2;
-          x[0] = src[0];
-          x[1] = src[1];
-        }
-        const uint32_t off = tile_off<D>(r, cl);
-        const float s = cut_row<D>(x, high + off, high + C::kTile + off, r < rows);
-        if (r < rows && cl == 0) s_qscale[it & 3][r] = s * p.scale_log2;
-      }
-      sm100::fence_proxy_async_smem();
-      conv_sync();
-      if (ct == 0) arrive(&bars.q_full[it & 1]);
-      return true;
-    };
-    bool ok = queries(w, 0), more = true;
-    while (ok && more) {
-      Walk nw = w;
-      bool has_next = false;
+    // Eight lanes' stores fall on all banks: where they would not, the halves of 16
+    // elements are taken in the other order.  A pass further the place within the
+    // swizzle's eight rows is the same.
+    static_assert(kPass % 8 == 0, "the swizzle repeats");
+    const int swap = cl >> 2 & 1;
+    const uint32_t from = static_cast<uint32_t>(cr * D + cl * 16);
+    const uint32_t to[2] = {sw128_off(cr, 2 * cl + swap, kChunk), sw128_off(cr, 2 * cl + 1 - swap, kChunk)};
+    uint32_t ended = 0, joins = 0;  // ended, bit i: chunk j - 1 - i was its item's last
+    bool ok = true;
+    for (bool more = true; ok && more; more = w.next(p)) {
       for (int k = w.k0; k < w.k1; ++k, ++j) {
         const int st = j % VS;
         uint8_t* wide = sWide + (j & 1) * C::kWide;
-        // PV(j - 2) read this tile.  (Known complete before: PV(j - 3), and so PV(j - 6).)
-        if (any_of<1, kConvThreads>((j >= 2 && !wait(&bars.done[(j - 2) & 3], (j - 2) >> 2)) ||
-                                    !wait(&bars.v_full[st], j / VS))) {
-          ok = false;
-          break;
-        }
-        if (k < w.t.prefix) {
-          const int rows = w.t.L - k * kChunk;
-          const uint8_t* src = sV + st * C::kTile;
-#pragma unroll 4
-          for (int i = 0; i < kChunk / kPass; ++i) {
-            const int r = i * kPass + cr;
-            uint4 v = make_uint4(0u, 0u, 0u, 0u);
-            if (r < rows) v = *reinterpret_cast<const uint4*>(src + r * D + cl * 16);
-            const uint32_t x[4] = {v.x, v.y, v.z, v.w};
-            uint32_t y[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const float2 f = adt::e4m3x2_to_f32(x[e >> 1] >> (16 * (e & 1)) & 0xffffu);
-              y[e] = pack_bf16x2(f.x, f.y);
-            }
-            // (The order of the two halves: eight lanes' stores fall on all banks.)
-            const int swap = cl >> 2 & 1;
-            const uint4 lo = make_uint4(y[0], y[1], y[2], y[3]), hi = make_uint4(y[4], y[5], y[6], y[7]);
-            *reinterpret_cast<uint4*>(wide + sw128_off(r, 2 * cl + swap, kChunk)) = swap ? hi : lo;
-            *reinterpret_cast<uint4*>(wide + sw128_off(r, 2 * cl + 1 - swap, kChunk)) = swap ? lo : hi;
-          }
-          sm100::fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) arrive(&bars.wide_full[j & 1]);
-          conv_sync();  // all have read the e4m3 tile
-          if (ct == 0) arrive(&bars.v_free[st]);
-        } else {
-          // The tree's chunk: its parents and ancestor bits; its keys, cut in two,
-          // and their scales; its values, those that are not finite as zeros
-          // (a weight of 0 times them would reach rows that do not see them).
-          const int t0 = (k - w.t.prefix) * kChunk, n = w.t.n, node0 = w.t.node0;
-          float* ks = s_scale + (j % kScaleSlots) * 2 * kChunk;
-          for (int t = ct; t < n; t += kConvThreads) s_par[t] = static_cast<int16_t>(min(max(p.parents[node0 + t], -1), kMaxTreeNodes));
-          int odd = 0;
-#pragma unroll 2
-          for (int i = 0; i < kChunk / kPass; ++i) {
-            const int r = i * kPass + cr, t = t0 + r;
-            uint4 x[2] = {}, v[2] = {};
-            if (t < n) {
-              const int64_t at = (static_cast<int64_t>(node0 + t) * p.Hkv + w.g) * D;
-              const uint4* src = reinterpret_cast<const uint4*>(p.tree[0] + at) + cl * 2;
-              x[0] = src[0];
-              x[1] = src[1];
-              src = reinterpret_cast<const uint4*>(p.tree[1] + at) + cl * 2;
-              v[0] = src[0];
-              v[1] = src[1];
-            }
-            const uint32_t off = tile_off<D>(r, cl);
-            const float s = cut_row<D>(x, sK + (j % KS) * C::kTile + off, sV + st * C::kTile + off, true);
-            if (cl == 0) {
-              ks[r] = t < n ? s : 1.f;
-              ks[kChunk + r] = 1.f;
-            }
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-              uint32_t y[4] = {v[half].x, v[half].y, v[half].z, v[half].w};
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const bool a = (y[e] & 0x7f80u) == 0x7f80u, b = (y[e] & 0x7f800000u) == 0x7f800000u;
-                odd |= a || b;
-                if (a) y[e] &= 0xffff0000u;
-                if (b) y[e] &= 0xffffu;
-              }
-              *reinterpret_cast<uint4*>(wide + sw128_off(r, 2 * cl + half, kChunk)) = make_uint4(y[0], y[1], y[2], y[3]);
-            }
-          }
-          if (odd) s_odd[item & 7] = 1;
-          conv_sync();
-          for (int t = ct; t < n; t += kConvThreads) {
-            const int up = s_par[t];
-            if ((t == 0) != (up < 0) || up >= t) adt::raise_error(p.err, ADT_DEVERR_BAD_TREE);
-          }
-          {
-            uint32_t m[4] = {0u, 0u, 0u, 0u};
-            const int row = w.blk * kRows + ct;
-            int t = row / p.group;
-            if (t < n) {
-              for (;;) {
-                const int at = t - t0;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) m[e] |= at >> 5 == e ? 1u << (at & 31) : 0u;
-                const int up = s_par[t];
-                if (up < 0 || up >= t) break;
-                t = up;
-              }
-            }
-            s_anc[j & 1][ct] = make_uint4(m[0], m[1], m[2], m[3]);
-          }
-          sm100::fence_proxy_async_smem();
-          conv_sync();
-          if (lane == 0) arrive(&bars.wide_full[j & 1]);
+        // PV(j - 2) read this tile (known complete before: PV(j - 3), and so PV(j - 6)),
+        // and copies of that item's rows are joined in it.  Of V's slot the phase
+        // before is known complete: chunk j - VS's product is.
+        const bool tree_k = k >= w.t.prefix;
+        static_assert(VS >= 2, "V's slot");
+        const bool join = p.copies > 1 && (ended & 2u);
+        ok = !any_of<1, kConvThreads>((j >= 2 && !wait(&bars.done[(j - 2) & 3], (j - 2) >> 2)) ||
+                                      (!tree_k && !wait(&bars.v_full[st], j / VS)) || (join && !wait(&bars.join_free[joins & 1], joins >> 1)));
+        if (!ok) break;
+        joins += join ? 1u : 0u;
+        ended = ended << 1 | (k + 1 == w.k1 ? 1u : 0u);
+        if (tree_k) {  // the tree's are prepared
           if (ct == 0) {
-            arrive(&bars.k_full[j % KS]);
-            arrive(&bars.scale_full[j % kScaleSlots]);
+            const int c = k - w.t.prefix, rows = min(kChunk, (w.t.n - c * kChunk + 15) & ~15);
+            const int64_t chunk = (static_cast<int64_t>(w.b) * p.Hkv + w.g) * p.pre.chunks + c;
+            const uint32_t bar = sm100::smem_addr(&bars.wide_full[j & 1]);
+            sm100::mbar_arrive_expect_tx(bar, rows * D * 2);
+            for (int x = 0; x < D / 64; ++x)
+              sm100::bulk_load(sm100::smem_addr(wide + x * C::kBlock), p.pre.v + (chunk * (D / 64) + x) * p.pre.t_rows * 8,
+                               rows * 128, bar);
+          } else if (lane == 0) {
+            arrive(&bars.wide_full[j & 1]);
+          }
+          continue;
+        }
+        const int rows = w.t.L - k * kChunk - cr;
+        const uint8_t* src = sV + st * C::kTile + from;
+#pragma unroll 1
+        for (int i = 0; i < kChunk / kPass; ++i) {
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            uint2 v = make_uint2(0u, 0u);  // (rows past the prefix: anything in the cache, zeros here)
+            if (i * kPass < rows) v = *reinterpret_cast<const uint2*>(src + i * kPass * D + 8 * (x ^ swap));
+            *reinterpret_cast<uint4*>(wide + to[x] + i * kPass * 128) =
+                make_uint4(e4m3x2_to_f16(v.x), e4m3x2_to_f16(v.x >> 16), e4m3x2_to_f16(v.y), e4m3x2_to_f16(v.y >> 16));
           }
         }
-        if (k == w.k0) {
-          has_next = nw.next(p);
-          if (has_next && !queries(nw, item + 1)) {
-            ok = false;
-            break;
-          }
-        }
+        sm100::fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) arrive(&bars.wide_full[j & 1]);
+        conv_sync();  // all have read the e4m3 tile
+        if (ct == 0) arrive(&bars.v_free[st]);
       }
-      w = nw;
-      more = has_next;
-      ++item;
-      // (Read last seven items back; of the one four back O is read at least.)
-      if (ct == 0) s_odd[(item + 1) & 7] = 0;
     }
+    // (A tree's values on their way: PV, or after an abort the wait here, sees them land.)
+    if (ct == 0 && j > 0)
+      for (uint32_t i = j > 2 ? j - 2 : 0; i < j; ++i)
+        (void)sm100::mbar_wait_bounded(sm100::smem_addr(&bars.wide_full[i & 1]), i >> 1 & 1u, kDrainLimit);
+    __syncwarp();
   } else {
     // ------------------------------------------------------------ softmax
-    const int grp = warp >> 2, w4 = warp & 3, row = w4 * 32 + lane;
+    const int grp = warp >> 2, w4 = warp & 3, lrow = w4 * 32 + lane;
     const uint32_t lanes = static_cast<uint32_t>(w4 * 32) << 16;
     const uint32_t s_col = tmem + lanes + grp * kChunk, o_col = tmem + lanes + kOCol, p_col = tmem + lanes + kPCol + grp * 64;
+    // Copy c of a row takes the quarters [c, c + 1) 4 / copies of every chunk's keys.
+    const int copies = p.copies, span = kRows / copies, row = lrow & (span - 1);
+    const int first_quarter = lrow / span * (4 / copies), end_quarter = first_quarter + 4 / copies;
+    if (copies > 1) {  // the weights of other copies' keys stay zero
+      uint32_t zero[32] = {};
+      tmem_st_32(p_col, zero);
+      tmem_st_32(p_col + 32, zero);
+      sm100::tmem_wait_st();
+    }
     uint32_t item = 0;
     bool ok = true;
     for (bool more = true; ok && more; more = w.next(p), ++item) {
-      const int index = w.blk * kRows + row, node = index / p.group, hh = index - node * p.group;
+      const int index = w.blk * kRows + row, node = index / p.group;
       const bool valid = node < w.t.n, active = __any_sync(adt::kFullMask, valid);
       const uint32_t j0 = j, j1 = j + static_cast<uint32_t>(w.k1 - w.k0);
-      float mu = -INFINITY, l = 0.f, scale = 0.f;
+      float mu = -INFINITY, l = 0.f;
+      const int64_t bg = static_cast<int64_t>(w.b) * p.Hkv + w.g;
+      const float scale = valid ? p.pre.q_scale[(bg * p.pre.blocks + w.blk) * p.pre.q_rows + row] : 0.f;
       if ((j0 & 1) != static_cast<uint32_t>(grp)) ++j;
       for (; j < j1; j += 2) {
         const int k = w.k0 + static_cast<int>(j - j0);
-        if (!all_wait(&bars.s_full[grp], j >> 1) || !all_wait(&bars.scale_full[j % kScaleSlots], j / kScaleSlots)) {
+        const int slot = static_cast<int>(j % kScaleSlots);
+        const bool tree_j = k >= w.t.prefix;
+        uint4 seen = make_uint4(0u, 0u, 0u, 0u);
+        if (tree_j && valid) seen = p.pre.seen[(static_cast<int64_t>(w.b) * p.max_nodes + node) * p.pre.chunks + k - w.t.prefix];
+        if (!all_wait(&bars.s_full[grp], j >> 1) || !all_wait(&bars.scale_full[slot], j / kScaleSlots)) {
           ok = false;
           break;
         }
         sm100::tc_fence_after();
-        if (j <= j0 + 1) scale = s_qscale[item & 3][row];  // (S came of these queries)
-        const bool tree_j = k >= w.t.prefix;
         const int kl = tree_j ? w.t.n - (k - w.t.prefix) * kChunk : w.t.L - k * kChunk;
-        const int quarters = min(4, (kl + 31) / 32);
+        const int quarters = min(end_quarter, (kl + 31) / 32);
+        auto release_s = [&]() {  // S is in registers: its tile may be written again
+          sm100::tc_fence_before();
+          __syncwarp();
+          if (lane == 0) arrive(&bars.s_free[grp]);
+        };
         if (active) {
-          if (tree_j || kl < kChunk) {
-            // -inf where the row does not see the key, in place.
-            const uint32_t* bits = reinterpret_cast<const uint32_t*>(&s_anc[j & 1][row]);
-#pragma unroll 1
-            for (int s = 0; s < quarters; ++s) {
-              const int left = kl - 32 * s;
-              const uint32_t keep = tree_j ? bits[s] : left >= 32 ? ~0u : (1u << left) - 1u;
-              uint32_t r[32];
-              tmem_ld_32(s_col + 32 * s, r);
-              tmem_wait_ld_into(r);
-#pragma unroll
-              for (int e = 0; e < 32; ++e) r[e] = (keep >> e) & 1u ? r[e] : 0xFF800000u;
-              tmem_st_32(s_col + 32 * s, r);
-            }
-            sm100::tmem_wait_st();
-          }
-          const ulonglong2* ks = reinterpret_cast<const ulonglong2*>(s_scale + (j % kScaleSlots) * 2 * kChunk);
+          const ulonglong2* ks = reinterpret_cast<const ulonglong2*>(s_scale + slot * 2 * kChunk);
           const ulonglong2* vf = ks + kChunk / 4;
-          uint32_t x[32], y[32];
+          const bool masked = tree_j || kl < kChunk;
           float mq[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-          auto largest = [&](const uint32_t (&r)[32], int s) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const ulonglong2 f = ks[8 * s + e];
-              float a, b;
-              unpack_f32x2(mul_f32x2(pack_u32x2(r[4 * e], r[4 * e + 1]), f.x), a, b);
-              mq[e & 1] = fmaxf(fmaxf(mq[e & 1], a), b);
-              unpack_f32x2(mul_f32x2(pack_u32x2(r[4 * e + 2], r[4 * e + 3]), f.y), a, b);
-              mq[2 + (e & 1)] = fmaxf(fmaxf(mq[2 + (e & 1)], a), b);
-            }
-          };
-          // The quarters in turn, each loaded while the one before is used; at
-          // the end the first one again, for the exponentials.
-          tmem_ld_32(s_col, x);
-          tmem_wait_ld_into(x);
-          if (quarters == 4) {
-#pragma unroll
-            for (int s = 0; s < 4; s += 2) {
-              tmem_ld_32(s_col + 32 * s + 32, y);
-              largest(x, s);
-              tmem_wait_ld_into(y);
-              tmem_ld_32(s_col + (s == 0 ? 64 : 0), x);
-              largest(y, s + 1);
-              tmem_wait_ld_into(x);
-            }
-          } else {
-            largest(x, 0);
+          // Scores times their keys' scales, back in place.
 #pragma unroll 1
-            for (int s = 1; s < quarters; ++s) {
-              tmem_ld_32(s_col + 32 * s, y);
-              tmem_wait_ld_into(y);
-              largest(y, s);
+          for (int s = 2 * first_quarter; s < 2 * quarters; ++s) {
+            uint32_t x[16];
+            sm100::tmem_ld_16(s_col + 16 * s, x);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const ulonglong2 f = ks[4 * s + e];
+              float a, b, c, d;
+              unpack_f32x2(mul_f32x2(pack_u32x2(x[4 * e], x[4 * e + 1]), f.x), a, b);
+              unpack_f32x2(mul_f32x2(pack_u32x2(x[4 * e + 2], x[4 * e + 3]), f.y), c, d);
+              x[4 * e] = __float_as_uint(a);
+              x[4 * e + 1] = __float_as_uint(b);
+              x[4 * e + 2] = __float_as_uint(c);
+              x[4 * e + 3] = __float_as_uint(d);
             }
+            if (masked) {  // (after the product: -inf whatever a key and its scale are)
+              const int left = kl - 16 * s, q4 = s >> 1;
+              const uint32_t bits = (q4 == 0 ? seen.x : q4 == 1 ? seen.y : q4 == 2 ? seen.z : seen.w) >> (16 * (s & 1));
+              const uint32_t keep = tree_j ? bits : left >= 16 ? ~0u : left > 0 ? (1u << left) - 1u : 0u;
+#pragma unroll
+              for (int e = 0; e < 16; ++e) x[e] = (keep >> e) & 1u ? x[e] : 0xFF800000u;
+            }
+#pragma unroll
+            for (int e = 0; e < 16; e += 2)
+              mq[(e >> 1) & 3] = fmaxf(fmaxf(mq[(e >> 1) & 3], __uint_as_float(x[e])), __uint_as_float(x[e + 1]));
+            tmem_st_16(s_col + 16 * s, x);
           }
+          sm100::tmem_wait_st();
           const float mx = valid ? fmaxf(fmaxf(mq[0], mq[1]), fmaxf(mq[2], mq[3])) * scale : -INFINITY;  // scale > 0
           // The running maximum after the chunk before (the other group's).  (An
           // item's last chunk is done before the next one's: so are its maxima.)
@@ -785,12 +946,12 @@ __global__ void __launch_bounds__(kThreads, 1)
               ok = false;
               break;
             }
-            prev = s_mu[row];
+            prev = s_mu[lrow];
           }
           // Raised only when a row grows by more than 2^8; then O (once the chunks
           // before are in it) is scaled.
           const float nm = mx > prev + kRescaleThreshold ? mx : prev;
-          s_mu[row] = nm;
+          s_mu[lrow] = nm;
           __syncwarp();
           if (lane == 0) arrive(&bars.mu[grp][w4]);
           if (nm != mu) l *= ex2_approx(mu - nm);
@@ -799,13 +960,14 @@ __global__ void __launch_bounds__(kThreads, 1)
             ok = false;
             break;
           }
-          if (j > j0 && __any_sync(adt::kFullMask, nm != prev)) {
+          const float drop = s_drop[slot];
+          if (j > j0 && __any_sync(adt::kFullMask, nm != prev || drop != 1.f)) {
             if (!all_wait(&bars.done[(j - 1) & 3], (j - 1) >> 2)) {
               ok = false;
               break;
             }
             sm100::tc_fence_after();
-            const float alpha = nm == prev ? 1.f : ex2_approx(prev - nm);
+            const float alpha = (nm == prev ? 1.f : ex2_approx(prev - nm)) * drop;
 #pragma unroll 1
             for (int c = 0; c < D; c += 32) {
               uint32_t r[32];
@@ -821,54 +983,27 @@ __global__ void __launch_bounds__(kThreads, 1)
           const float base = mu == -INFINITY ? 0.f : mu;
           const uint64_t scale2 = pack_f32x2(scale, scale), base2 = pack_f32x2(-base, -base);
           uint64_t l2[2] = {0ull, 0ull};
-          // 32 scores -> 16 pairs of weights, in bf16 with their values' scales.
-          auto quarter = [&](const uint32_t (&r)[32], int s) {
-            uint32_t pk[16];
+          // 16 scores at a time -> 8 pairs of weights, in fp16 with their values' scales.
+#pragma unroll 1
+          for (int s = 2 * first_quarter; s < 2 * quarters; ++s) {
+            uint32_t x[16], pk[8];
+            sm100::tmem_ld_16(s_col + 16 * s, x);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const ulonglong2 f = ks[8 * s + e], g = vf[8 * s + e];
+            for (int e = 0; e < 4; ++e) {
+              const ulonglong2 g = vf[4 * s + e];
 #pragma unroll
               for (int h = 0; h < 2; ++h) {
-                const uint64_t z = mul_f32x2(pack_u32x2(r[4 * e + 2 * h], r[4 * e + 2 * h + 1]), h ? f.y : f.x);
                 float a, b;
-                unpack_f32x2(fma_f32x2(z, scale2, base2), a, b);
+                unpack_f32x2(fma_f32x2(pack_u32x2(x[4 * e + 2 * h], x[4 * e + 2 * h + 1]), scale2, base2), a, b);
                 const uint64_t wt = pack_f32x2(ex2_approx(a), ex2_approx(b));
                 l2[h] = add_f32x2(l2[h], wt);
                 unpack_f32x2(mul_f32x2(wt, h ? g.y : g.x), a, b);
-                pk[2 * e + h] = pack_bf16x2(a, b);
+                pk[2 * e + h] = pack_half2(a, b);
               }
             }
-            tmem_st_16(p_col + 16 * s, pk);
-          };
-          auto release_s = [&]() {  // S is in registers: its tile may be written again
-            sm100::tc_fence_before();
-            __syncwarp();
-            if (lane == 0) arrive(&bars.s_free[grp]);
-          };
-          if (quarters == 4) {
-#pragma unroll 1
-            for (int s = 0; s < 4; s += 2) {
-              tmem_ld_32(s_col + 32 * s + 32, y);
-              quarter(x, s);
-              tmem_wait_ld_into(y);
-              if (s == 0)
-                tmem_ld_32(s_col + 64, x);
-              else
-                release_s();
-              quarter(y, s + 1);
-              tmem_wait_ld_into(x);
-            }
-          } else {
-#pragma unroll 1
-            for (int s = 0; s < quarters; ++s) {
-              if (s > 0) {
-                tmem_ld_32(s_col + 32 * s, x);
-                tmem_wait_ld_into(x);
-              }
-              quarter(x, s);
-            }
-            release_s();
+            sm100::tmem_st_8(p_col + 8 * s, pk);
           }
+          release_s();
           float la, lb, lc, ld;
           unpack_f32x2(l2[0], la, lb);
           unpack_f32x2(l2[1], lc, ld);
@@ -897,61 +1032,107 @@ __global__ void __launch_bounds__(kThreads, 1)
       ok = ok && all_wait(&bars.done[(j1 - 1) & 3], (j1 - 1) >> 2);
       sm100::tc_fence_after();
       constexpr int kHalf = D / 2;
-      uint32_t o[kHalf / 32][32];
-#pragma unroll
-      for (int c = 0; c < kHalf / 32; ++c) tmem_ld_32(o_col + grp * kHalf + 32 * c, o[c]);
-#pragma unroll
-      for (int c = 0; c < kHalf / 32; ++c) tmem_wait_ld_into(o[c]);
-      const float m = s_mu[row];
-      s_l[item & 1][grp][row] = mu == m ? l : l * ex2_approx(mu - m);
-      sm100::tc_fence_before();
-      __syncwarp();
-      if (lane == 0) arrive(&bars.o_free);
+      const float m = s_mu[lrow];
+      const int par = item & 1;
+      s_m[par][lrow] = m;  // (both groups write the same)
+      s_l[par][grp][lrow] = mu == m ? l : l * ex2_approx(mu - m);
+      const float unit = power_of_two(s_ref[(j1 - 1) % kScaleSlots] - 127 - kHeadroom);
       ok = !any_of<2, kSoftmaxThreads>(!ok);  // (after a wait that gave up they leave together)
       if (!ok) break;
-      l = s_l[item & 1][0][row] + s_l[item & 1][1][row];
-      const int64_t out_row = static_cast<int64_t>(w.t.node0 + node) * p.H + w.g * p.group + hh;
-      if (s_odd[item & 7] && valid && w.k1 > w.t.prefix) {
-        // Values that are not finite, of the nodes that the row sees.
-        for (int t = node;;) {
-          if (t / kChunk + w.t.prefix >= w.k0 && t / kChunk + w.t.prefix < w.k1) {
-            const __nv_bfloat16* v = p.tree[1] + (static_cast<int64_t>(w.t.node0 + t) * p.Hkv + w.g) * D + grp * kHalf;
+      // A thread writes its own row's columns, or, of rows in copies, parts of row r:
+      // the copies' sums, with weights that bring them to one maximum.
+      const int tg = tid & 127, r = copies == 1 ? row : tg / copies;
+      float M = -INFINITY, lt = 0.f;
+      for (int c = r; c < kRows; c += span) M = fmaxf(M, s_m[par][c]);
+      auto weight = [&](float mc, float Mc) { return mc == Mc ? 1.f : ex2_approx(mc - Mc); };
+      for (int c = r; c < kRows; c += span) lt += (s_l[par][0][c] + s_l[par][1][c]) * weight(s_m[par][c], M);
+      float mine = unit;
+      if (copies > 1) {
+        float Mr = -INFINITY;
+        for (int c = row; c < kRows; c += span) Mr = fmaxf(Mr, s_m[par][c]);
+        mine *= weight(m, Mr);
+      }
+      const bool whole = w.k0 == 0 && w.k1 == w.t.chunks;
+      if (whole) mine = copies == 1 ? mine * __fdividef(1.f, lt) : mine;
+      const float inv = whole && copies > 1 ? __fdividef(1.f, lt) : 1.f;
+      const int64_t slot = 2ll * blockIdx.x + (w.first ? 0 : 1);
+      const int ri = w.blk * kRows + r, rt = ri / p.group;
+      const bool there = rt < w.t.n;
+      const int64_t out_row = static_cast<int64_t>(w.t.node0 + rt) * p.H + w.g * p.group + (ri - rt * p.group);
+      __nv_bfloat16* out = p.out + out_row * D + grp * kHalf;
+      float4* part = p.part_o + (slot * (D / 4) + grp * (kHalf / 4)) * p.slot_rows + r;
+      auto put4 = [&](int c, float4 v) {
+        if (whole) {
+          uint2 y;
+          y.x = pack_bf16x2(v.x * inv, v.y * inv);
+          y.y = pack_bf16x2(v.z * inv, v.w * inv);
+          *reinterpret_cast<uint2*>(out + c) = y;
+        } else {
+          part[c / 4 * p.slot_rows] = v;
+        }
+      };
+#pragma unroll 1
+      for (int c0 = 0; c0 < kHalf; c0 += 32) {
+        uint32_t o[32];
+        tmem_ld_32(o_col + grp * kHalf + c0, o);
+        tmem_wait_ld_into(o);
+        if (c0 + 32 == kHalf) {
+          sm100::tc_fence_before();
+          __syncwarp();
+          if (lane == 0) arrive(&bars.o_free);
+        }
+        auto four = [&](int c) {
+          return make_float4(__uint_as_float(o[c]) * mine, __uint_as_float(o[c + 1]) * mine, __uint_as_float(o[c + 2]) * mine,
+                             __uint_as_float(o[c + 3]) * mine);
+        };
+        if (copies == 1) {
+          if (there) {
 #pragma unroll
-            for (int c = 0; c < kHalf; ++c) {
-              const float f = __bfloat162float(v[c]);
-              if (!isfinite(f)) o[c / 32][c % 32] = __float_as_uint(__uint_as_float(o[c / 32][c % 32]) + f);
-            }
+            for (int c = 0; c < 32; c += 4) put4(c0 + c, four(c));
           }
-          const int up = p.parents[w.t.node0 + t];
-          if (up < 0 || up >= t) break;
-          t = up;
+          continue;
+        }
+        // Through the V tile of the item's last chunk, which warps 12-15 leave alone
+        // until then (D = 64: a buffer).
+        float4* buf = reinterpret_cast<float4*>(D == 128 ? sWide + ((j1 - 1) & 1) * C::kWide : smem + C::kJoinOff) + grp * kRows * 8;
+        if (c0) group_sync(grp);  // the columns before are read
+#pragma unroll
+        for (int c = 0; c < 8; ++c) buf[lrow * 8 + (c ^ (lrow & 7))] = four(4 * c);
+        group_sync(grp);
+        for (int c = tg & (copies - 1); there && c < 8; c += copies) {
+          float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+          for (int x = r; x < kRows; x += span) {
+            const float4 y = buf[x * 8 + (c ^ (x & 7))];
+            v.x += y.x;
+            v.y += y.y;
+            v.z += y.z;
+            v.w += y.w;
+          }
+          put4(c0 + 4 * c, v);
         }
       }
-      if (w.k0 == 0 && w.k1 == w.t.chunks) {
-        if (valid) {
-          const float inv = __fdividef(1.f, l);
-          uint4* dst = reinterpret_cast<uint4*>(p.out + out_row * D + grp * kHalf);
-#pragma unroll
-          for (int c = 0; c < kHalf; c += 8) {
-            uint32_t y[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              y[e] = pack_bf16x2(__uint_as_float(o[c / 32][c % 32 + 2 * e]) * inv,
-                                 __uint_as_float(o[c / 32][c % 32 + 2 * e + 1]) * inv);
-            dst[c / 8] = make_uint4(y[0], y[1], y[2], y[3]);
-          }
-          if (grp == 0 && p.lse) p.lse[out_row] = (m + __log2f(l)) * kLn2;
-        }
-      } else {
-        const int64_t slot = 2ll * blockIdx.x + (w.first ? 0 : 1);
-        if (valid) {
-          float4* dst = reinterpret_cast<float4*>(p.part_o + (slot * p.slot_rows + row) * D + grp * kHalf);
-#pragma unroll
-          for (int c = 0; c < kHalf; c += 4)
-            dst[c / 4] = make_float4(__uint_as_float(o[c / 32][c % 32]), __uint_as_float(o[c / 32][c % 32 + 1]),
-                                     __uint_as_float(o[c / 32][c % 32 + 2]), __uint_as_float(o[c / 32][c % 32 + 3]));
-          if (grp == 0) p.part_ml[slot * p.slot_rows + row] = make_float2(m, l);
-        }
+      if (copies > 1) {
+        __syncwarp();
+        if (lane == 0) arrive(&bars.join_free[item & 1]);
+      }
+      if (there && grp == 0 && (copies == 1 || (tg & (copies - 1)) == 0)) {
+        if (!whole)
+          p.part_ml[slot * p.slot_rows + r] = make_float2(M, lt);
+        else if (p.lse)
+          p.lse[out_row] = (M + __log2f(lt)) * kLn2;
+      }
+      // (The slots of an item's last two chunks, of its tree's two at most, are in
+      // use until the next items' S products are read.)
+      bool odd = false;
+      for (int k = max(w.k0, w.t.prefix); k < w.k1; ++k) odd |= s_odd[(j1 - static_cast<uint32_t>(w.k1 - k)) % kScaleSlots] != 0;
+      if (odd) {
+        group_sync(grp);  // the rows are written
+        if (there && (copies == 1 || (tg & (copies - 1)) == 0))
+          add_odd(whole ? out : nullptr, reinterpret_cast<float*>(part), p.slot_rows, kHalf,
+                  p.tree[1] + (static_cast<int64_t>(w.t.node0) * p.Hkv + w.g) * D + grp * kHalf, p.parents + w.t.node0,
+                  static_cast<int64_t>(p.Hkv) * D, rt, (w.k0 - w.t.prefix) * kChunk, (w.k1 - w.t.prefix) * kChunk);
+      }
+      if (!whole) {
         // The CTAs that the item's first and last chunk lie in: share c starts at
         // the largest coordinate c X / G that is not above.
         const int64_t X = s_total, G = s_grid, a = w.start + kItemCost, z = a + w.t.chunks - 1;
@@ -961,35 +1142,64 @@ __global__ void __launch_bounds__(kThreads, 1)
           s_last = adt::atomic_add_acq_rel_gpu(p.tickets + first, 1u) == static_cast<unsigned>(last - first);
         softmax_sync();
         if (s_last) {
-          // Partial rows joined: weights 2^(m_c - M) over their sum.
+          // Partial rows joined: weights 2^(m_c - M) over their sum.  Neighbouring lanes
+          // take neighbouring rows, a thread 16 columns at a time, of two CTAs' parts.
           const int rows = min(w.t.n * p.group - w.blk * kRows, kRows);
-          const int64_t slot0 = 2ll * first + (first * X / G >= w.start ? 0 : 1);
-          auto slot_of = [&](int c) { return c == first ? slot0 : 2ll * c; };
-          for (int i = tid; i < rows * (D / 4); i += kSoftmaxThreads) {
-            const int r = i / (D / 4), c4 = i % (D / 4);
-            float M = -INFINITY;
-            for (int c = first; c <= last; ++c) M = fmaxf(M, __ldcg(&p.part_ml[slot_of(c) * p.slot_rows + r]).x);
-            float lt = 0.f;
-            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+          const int shift = 32 - __clz(rows - 1), jr = tid & ((1 << shift) - 1);  // (rows rounded up to a power of two)
+          const int slot0 = first * 2 + (first * X / G >= w.start ? 0 : 1);
+          auto slot_of = [&](int c) -> int64_t { return c == first ? slot0 : 2 * c; };
+          if (jr < rows) {
+            float Mj = -INFINITY, lj = 0.f;
+#pragma unroll 4
+            for (int c = first; c <= last; ++c) Mj = fmaxf(Mj, __ldcg(&p.part_ml[slot_of(c) * p.slot_rows + jr]).x);
+#pragma unroll 4
             for (int c = first; c <= last; ++c) {
-              const int64_t at = slot_of(c) * p.slot_rows + r;
-              const float2 ml = __ldcg(&p.part_ml[at]);
-              const float4 v = __ldcg(reinterpret_cast<const float4*>(p.part_o + at * D) + c4);
-              const float wt = ml.x == M ? 1.f : ex2_approx(ml.x - M);
-              lt += wt * ml.y;
-              acc.x += wt * v.x;
-              acc.y += wt * v.y;
-              acc.z += wt * v.z;
-              acc.w += wt * v.w;
+              const float2 ml = __ldcg(&p.part_ml[slot_of(c) * p.slot_rows + jr]);
+              lj += ml.y * weight(ml.x, Mj);
             }
-            const float inv = __fdividef(1.f, lt);
-            const int idx = w.blk * kRows + r, t = idx / p.group;
-            const int64_t dst = static_cast<int64_t>(w.t.node0 + t) * p.H + w.g * p.group + idx - t * p.group;
-            uint2 pk;
-            pk.x = pack_bf16x2(acc.x * inv, acc.y * inv);
-            pk.y = pack_bf16x2(acc.z * inv, acc.w * inv);
-            *reinterpret_cast<uint2*>(p.out + dst * D + c4 * 4) = pk;
-            if (c4 == 0 && p.lse) p.lse[dst] = (M + __log2f(lt)) * kLn2;
+            const float invj = __fdividef(1.f, lj);
+            const int idx = w.blk * kRows + jr, tj = idx / p.group;
+            const int64_t at = static_cast<int64_t>(w.t.node0 + tj) * p.H + w.g * p.group + idx - tj * p.group;
+#pragma unroll 1
+            for (int c16 = tid >> shift; c16 < D / 16; c16 += kSoftmaxThreads >> shift) {
+              float4 acc[4] = {};
+#pragma unroll 1
+              for (int c = first; c <= last; c += 2) {
+                const bool two = c < last;
+                float wt[2] = {0.f, 0.f};
+                float4 v[2][4] = {};
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                  if (x == 1 && !two) continue;
+                  const int64_t sl = slot_of(c + x);
+                  wt[x] = __ldcg(&p.part_ml[sl * p.slot_rows + jr]).x;
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) v[x][e] = __ldcg(p.part_o + (sl * (D / 4) + c16 * 4 + e) * p.slot_rows + jr);
+                }
+                wt[0] = weight(wt[0], Mj);
+                wt[1] = two ? weight(wt[1], Mj) : 0.f;
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) {
+                    acc[e].x += wt[x] * v[x][e].x;
+                    acc[e].y += wt[x] * v[x][e].y;
+                    acc[e].z += wt[x] * v[x][e].z;
+                    acc[e].w += wt[x] * v[x][e].w;
+                  }
+                }
+              }
+              uint32_t y[8];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                y[2 * e] = pack_bf16x2(acc[e].x * invj, acc[e].y * invj);
+                y[2 * e + 1] = pack_bf16x2(acc[e].z * invj, acc[e].w * invj);
+              }
+              uint4* dst = reinterpret_cast<uint4*>(p.out + at * D) + c16 * 2;
+              dst[0] = make_uint4(y[0], y[1], y[2], y[3]);
+              dst[1] = make_uint4(y[4], y[5], y[6], y[7]);
+              if (c16 == 0 && p.lse) p.lse[at] = (Mj + __log2f(lj)) * kLn2;
+            }
           }
           if (tid == 0) p.tickets[first] = 0u;
         }
@@ -1026,13 +1236,40 @@ struct WsLayout {
   size_t part_ml, part_o, total;
 };
 
-// Tickets at the start, for any grid; then two items' partial rows of each CTA.
-WsLayout ws_layout(int grid, int rows, int D) {
-  WsLayout w;
-  w.part_ml = kMaxGrid * sizeof(unsigned);
-  w.part_o = adt::align_up(w.part_ml + static_cast<size_t>(2 * grid) * rows * sizeof(float2), 256);
-  w.total = w.part_o + static_cast<size_t>(2 * grid) * rows * D * sizeof(float);
-  return w;
+int slot_rows_for(int H, int Hkv, int max_nodes) {
+  const int64_t rows = static_cast<int64_t>(max_nodes) * (H / Hkv);
+  return rows < kRows ? static_cast<int>(rows) : kRows;
+}
+
+// Tickets at the start, for any grid; two items' partial rows of each CTA; what is
+// prepared.  (Offsets from `base`, which may be NULL; at most 2^24 query rows, so
+// that all sizes stay below 2^50.)
+size_t ws_layout(uint8_t* base, int grid, int B, int H, int Hkv, int D, int max_nodes, AttnParams* p) {
+  const int rows = slot_rows_for(H, Hkv, max_nodes);
+  size_t at = kMaxGrid * sizeof(unsigned);
+  auto take = [&](size_t bytes) {
+    uint8_t* x = base + at;
+    at = adt::align_up(at + bytes, 256);
+    return x;
+  };
+  Prepared& w = p->pre;
+  w.q_rows = (rows + 7) & ~7;
+  w.blocks = static_cast<int>((static_cast<int64_t>(max_nodes) * (H / Hkv) + kRows - 1) / kRows);
+  w.t_rows = max_nodes < kChunk ? (max_nodes + 15) & ~15 : kChunk;
+  w.chunks = (max_nodes + kChunk - 1) / kChunk;
+  const size_t bg = static_cast<size_t>(B) * Hkv, slots = 2 * static_cast<size_t>(grid) * rows;
+  p->slot_rows = rows;
+  p->copies = rows <= 32 ? 4 : rows <= 64 ? 2 : 1;
+  p->tickets = reinterpret_cast<unsigned*>(base);
+  p->part_ml = reinterpret_cast<float2*>(take(slots * sizeof(float2)));
+  p->part_o = reinterpret_cast<float4*>(take(slots * D * sizeof(float)));
+  w.q = take(bg * w.blocks * 2 * w.q_rows * D);
+  w.q_scale = reinterpret_cast<float*>(take(bg * w.blocks * w.q_rows * sizeof(float)));
+  w.k = take(bg * w.chunks * 2 * w.t_rows * D);
+  w.v = reinterpret_cast<uint4*>(take(bg * w.chunks * w.t_rows * D * 2));
+  w.scale = take(bg * w.chunks * 3 * w.t_rows);
+  w.seen = reinterpret_cast<uint4*>(take(static_cast<size_t>(B) * max_nodes * w.chunks * sizeof(uint4)));
+  return at;
 }
 
 // One CTA an SM, or fewer where no lengths within the limits make as many shares.
@@ -1045,11 +1282,6 @@ int grid_for(int sm_count, int B, int H, int Hkv, int max_nodes, int max_kv) {
   return most < sms ? static_cast<int>(most) : sms;
 }
 
-int slot_rows_for(int H, int Hkv, int max_nodes) {
-  const int64_t rows = static_cast<int64_t>(max_nodes) * (H / Hkv);
-  return rows < kRows ? static_cast<int>(rows) : kRows;
-}
-
 template <int D>
 adt_status launch(const AttnParams& p, const CUtensorMap& tm, int grid, int dev, cudaStream_t st) {
   static unsigned configured[2] = {0u, 0u};  // bit per device (< 64), per instantiation
@@ -1060,13 +1292,18 @@ adt_status launch(const AttnParams& p, const CUtensorMap& tm, int grid, int dev,
     __atomic_fetch_or(&word, bit, __ATOMIC_ACQ_REL);
   }
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(grid), 1, 1);
-  cfg.blockDim = dim3(kThreads, 1, 1);
-  cfg.dynamicSmemBytes = Cfg<D>::kDynSmem;
-  cfg.stream = st;
   cudaLaunchAttribute attr[1] = {adt::pdl_attribute()};
   cfg.attrs = attr;
   cfg.numAttrs = 1;
+  cfg.stream = st;
+  constexpr int kPass = kPrepThreads / (D / 16);
+  const int64_t units = static_cast<int64_t>(p.max_nodes) * p.H + ((p.max_nodes + 15) & ~15) * static_cast<int64_t>(p.Hkv);
+  cfg.gridDim = dim3(static_cast<unsigned>((units + kPass - 1) / kPass), static_cast<unsigned>(p.B), 1);
+  cfg.blockDim = dim3(kPrepThreads, 1, 1);
+  ADT_CUDA_TRY(cudaLaunchKernelEx(&cfg, prepare_kernel<D>, p));
+  cfg.gridDim = dim3(static_cast<unsigned>(grid), 1, 1);
+  cfg.blockDim = dim3(kThreads, 1, 1);
+  cfg.dynamicSmemBytes = Cfg<D>::kDynSmem;
   ADT_CUDA_TRY(cudaLaunchKernelEx(&cfg, tree_attn_q8_kernel<D>, tm, p));
   return adt::launch_status();
 }
@@ -1081,7 +1318,8 @@ size_t adt_tree_attn_q8_workspace_size(int32_t B, int32_t H, int32_t Hkv, int32_
     return 0;
   adt::DeviceInfo info;
   if (adt::device_info(&info) != ADT_OK) return 0;
-  return ws_layout(grid_for(info.sm_count, B, H, Hkv, max_nodes, max_kv), slot_rows_for(H, Hkv, max_nodes), D).total;
+  AttnParams p{};
+  return ws_layout(nullptr, grid_for(info.sm_count, B, H, Hkv, max_nodes, max_kv), B, H, Hkv, D, max_nodes, &p);
 }
 
 adt_status adt_tree_attn_q8(const adt_bf16* q, const uint8_t* k_cache, const uint8_t* v_cache, const uint8_t* k_scale,
@@ -1108,10 +1346,10 @@ adt_status adt_tree_attn_q8(const adt_bf16* q, const uint8_t* k_cache, const uin
   adt::DeviceInfo info;
   st = adt::device_info(&info);
   if (st != ADT_OK) return st;
-  const int grid = grid_for(info.sm_count, B, H, Hkv, max_nodes, max_kv), rows = slot_rows_for(H, Hkv, max_nodes);
-  const WsLayout ws = ws_layout(grid, rows, D);
-  if (!workspace || workspace_bytes < ws.total || !adt::aligned16(workspace)) return ADT_ERR_WORKSPACE;
+  const int grid = grid_for(info.sm_count, B, H, Hkv, max_nodes, max_kv);
   AttnParams p{};
+  const size_t bytes = ws_layout(static_cast<uint8_t*>(workspace), grid, B, H, Hkv, D, max_nodes, &p);
+  if (!workspace || workspace_bytes < bytes || !adt::aligned16(workspace)) return ADT_ERR_WORKSPACE;
   p.q = reinterpret_cast<const __nv_bfloat16*>(q);
   p.v_cache = v_cache;
   p.scale[0] = k_scale, p.scale[1] = v_scale;
@@ -1132,11 +1370,6 @@ adt_status adt_tree_attn_q8(const adt_bf16* q, const uint8_t* k_cache, const uin
   p.out = reinterpret_cast<__nv_bfloat16*>(out);
   p.lse = lse;
   p.err = info.error_word;
-  p.slot_rows = rows;
-  uint8_t* base = static_cast<uint8_t*>(workspace);
-  p.tickets = reinterpret_cast<unsigned*>(base);
-  p.part_ml = reinterpret_cast<float2*>(base + ws.part_ml);
-  p.part_o = reinterpret_cast<float*>(base + ws.part_o);
   p.wait_limit = adt::wait_limit(kWaitLimit);
   CUtensorMap tm;
   st = make_cache_map(&tm, k_cache, D, max_kv, Hkv, B, cache_stride_h, cache_stride_b);
