@@ -9,12 +9,14 @@ missing library raises instead of falling back to anything else.
 from __future__ import annotations
 
 import ctypes
+import importlib.util
 import os
 
 import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libadt.so")
+MARSHAL_PATH = os.path.join(_HERE, "_marshal.so")
 
 ADT_OK = 0
 STATUS_NAMES = {0: "ADT_OK", 1: "ADT_ERR_INVALID_ARG", 2: "ADT_ERR_UNSUPPORTED", 3: "ADT_ERR_CUDA",
@@ -116,6 +118,22 @@ _SIGS = {
 }
 
 _LIB = None
+_MARSHAL = None
+
+
+def _native():
+    """The C++ part that marshals the calls of the later operators (once)."""
+    global _MARSHAL
+    if _MARSHAL is None:
+        lib()
+        if not os.path.exists(MARSHAL_PATH):
+            raise RuntimeError(f"{MARSHAL_PATH} is missing: build it with `python -m paper_2512_21857_gb300.build`")
+        spec = importlib.util.spec_from_file_location("_marshal", MARSHAL_PATH)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        module.load(LIB_PATH)
+        _MARSHAL = module
+    return _MARSHAL
 
 
 def lib() -> ctypes.CDLL:
@@ -515,94 +533,39 @@ def adt_kv_evict(k_cache, v_cache, score, kv_len, kv_len_out=None, *, k_out=None
     _check(st, "adt_kv_evict")
 
 
-def _norm_params(weight, bias, heads, D, dtype, dev, name):
-    """(weight address, bias address, stride from head to head) of [D], or [heads, D], each; None: absent."""
-    each = {t.dim() for t in (weight, bias) if t is not None}
-    if len(each) > 1:
-        raise ValueError(f"{name}_weight and {name}_bias: both [{D}] or both [{heads}, {D}]")
-    for t in (weight, bias):
-        if t is not None and tuple(t.shape) not in ((D,), (heads, D)):
-            raise ValueError(f"{name}_weight, {name}_bias: expected [{D}] or [{heads}, {D}], got {list(t.shape)}")
-    return (_vec(weight, dtype, dev, 0, name + "_weight"), _vec(bias, dtype, dev, 0, name + "_bias"), D if each == {2} else 0)
-
-
 def adt_norm_rope_qkv(q, k, v, positions, inv_freq, *, H, Hkv, D, norm=NORM_RMS, eps=1e-6, q_weight=None, q_bias=None,
                       k_weight=None, k_bias=None, layout=ROPE_HALF, magnitude=1.0, q_out=None, k_out=None, v_out=None,
                       stream=None) -> None:
     """adt_rope_qkv of heads that are normed first.  Weights and biases (fp32 or bf16, all the same): [D] for all heads,
     or a head's own in [heads, D]; None: ones, zeros."""
-    dev, handle = _launch_on(positions, stream, "positions")
-    N = positions.numel()
-    first = q if q is not None else k if k is not None else v
-    if first is None or first.dtype not in _TYPES:
-        raise TypeError("q, k, v: bf16 or fp32, all the same")
-    dtype, wtype = first.dtype, torch.float32
-    for t in (q_weight, q_bias, k_weight, k_bias):
-        if t is not None:
-            wtype = t.dtype
-            break
-    if wtype not in _TYPES:
-        raise TypeError("weights and biases: bf16 or fp32, all the same")
-    qa, ldq, qo = _rope_pair(q, q_out, dtype, dev, H, D, N, "q")
-    ka, ldk, ko = _rope_pair(k, k_out, dtype, dev, Hkv, D, N, "k")
-    va, ldv, vo = _rope_pair(v, v_out, dtype, dev, Hkv, D, N, "v")
-    st = lib().adt_norm_rope_qkv(qa, ldq, ka, ldk, va, ldv, _TYPES[dtype], norm, eps,
-                                 *_norm_params(q_weight, q_bias, H, D, wtype, dev, "q"),
-                                 *_norm_params(k_weight, k_bias, Hkv, D, wtype, dev, "k"), _TYPES[wtype],
-                                 _vec(positions, torch.int32, dev, N, "positions"),
-                                 _vec(inv_freq, torch.float64, dev, 0, "inv_freq"), magnitude, layout, N, H, Hkv, D,
-                                 2 * inv_freq.numel(), qo, ko, vo, handle)
-    _check(st, "adt_norm_rope_qkv")
+    st = (_MARSHAL or _native()).norm_rope_qkv(q, k, v, positions, inv_freq, H, Hkv, D, norm, eps, q_weight, q_bias, k_weight,
+                                               k_bias, layout, magnitude, q_out, k_out, v_out, stream)
+    if st:
+        _check(st, "adt_norm_rope_qkv")
 
 
 # ----------------------------------------------------------------------------- the 8-bit cache
 
-def _q8_cache(k_cache, v_cache, k_scale, v_scale, layers, B, Hkv, rows, D, dev):
-    """(four addresses, strides of the caches, strides of the scales) of [layers, B, Hkv, rows or more, D] e4m3 caches
-    and their [layers, B, Hkv, rows or more] scales."""
-    cs = _strides3(k_cache, layers, B, Hkv, rows, D, "k_cache")
-    ss = _strides3(k_scale, layers, B, Hkv, rows, 0, "k_scale")
-    if _strides3(v_cache, layers, B, Hkv, rows, D, "v_cache") != cs or \
-            _strides3(v_scale, layers, B, Hkv, rows, 0, "v_scale") != ss:
-        raise ValueError("K and V must share strides")
-    e4m3, u8 = torch.float8_e4m3fn, torch.uint8
-    return (_addr(k_cache, e4m3, dev, "k_cache"), _addr(v_cache, e4m3, dev, "v_cache"), _addr(k_scale, u8, dev, "k_scale"),
-            _addr(v_scale, u8, dev, "v_scale")), cs, ss
+# (Their checks of tensors: csrc/marshal.cc.)
 
 
 def adt_kv_compact_q8(k_cache, v_cache, k_scale, v_scale, kv_len, kv_len_out, k_tree, v_tree, node_offsets, path, max_path,
                       accept_len, *, B, Hkv, D, num_layers, max_kv, stream=None) -> None:
     """Caches [layers, B, Hkv, rows >= max_kv, D] float8_e4m3fn, scales [layers, B, Hkv, rows >= max_kv] uint8, k_tree and
     v_tree [layers, nodes, Hkv, D] bf16; kv_len_out may be None."""
-    dev, handle = _launch_on(k_cache, stream, "k_cache")
-    i32, bf16 = torch.int32, torch.bfloat16
-    addr, cs, ss = _q8_cache(k_cache, v_cache, k_scale, v_scale, num_layers, B, Hkv, max_kv, D, dev)
-    for t, name in ((k_tree, "k_tree"), (v_tree, "v_tree")):
-        if t.dim() != 4 or t.shape[0] < num_layers or t.shape[2:] != (Hkv, D) or not t[0].is_contiguous():
-            raise ValueError(f"{name}: expected [{num_layers}, nodes, {Hkv}, {D}], each layer contiguous")
-    if k_tree.shape[1] != v_tree.shape[1] or (num_layers > 1 and k_tree.stride(0) != v_tree.stride(0)):
-        raise ValueError("k_tree and v_tree must share their shape and strides")
-    st = lib().adt_kv_compact_q8(*addr, _vec(kv_len, i32, dev, B, "kv_len"), _vec(kv_len_out, i32, dev, B, "kv_len_out"),
-                                 _addr(k_tree, bf16, dev, "k_tree"), _addr(v_tree, bf16, dev, "v_tree"),
-                                 _vec(node_offsets, i32, dev, B + 1, "node_offsets"),
-                                 _vec(path, i32, dev, B * max_path, "path"), max_path,
-                                 _vec(accept_len, i32, dev, B, "accept_len"), B, Hkv, D, num_layers, max_kv, *cs, *ss,
-                                 k_tree.stride(0) if num_layers > 1 else 0, handle)
-    _check(st, "adt_kv_compact_q8")
+    st = (_MARSHAL or _native()).kv_compact_q8(k_cache, v_cache, k_scale, v_scale, kv_len, kv_len_out, k_tree, v_tree,
+                                               node_offsets, path, max_path, accept_len, B, Hkv, D, num_layers, max_kv, stream)
+    if st:
+        _check(st, "adt_kv_compact_q8")
 
 
 def adt_kv_read_q8(k_cache, v_cache, k_scale, v_scale, kv_len, k_out, v_out, *, B, Hkv, D, num_layers, max_kv,
                    stream=None) -> None:
     """Rows of an 8-bit cache (as for adt_kv_compact_q8) to k_out, v_out [layers, B, Hkv, rows >= max_kv, D] bf16."""
-    dev, handle = _launch_on(k_cache, stream, "k_cache")
-    addr, cs, ss = _q8_cache(k_cache, v_cache, k_scale, v_scale, num_layers, B, Hkv, max_kv, D, dev)
-    os = _strides3(k_out, num_layers, B, Hkv, max_kv, D, "k_out")
-    if _strides3(v_out, num_layers, B, Hkv, max_kv, D, "v_out") != os:
-        raise ValueError("k_out and v_out must share strides")
-    st = lib().adt_kv_read_q8(*addr, _vec(kv_len, torch.int32, dev, B, "kv_len"), _addr(k_out, torch.bfloat16, dev, "k_out"),
-                              _addr(v_out, torch.bfloat16, dev, "v_out"), B, Hkv, D, num_layers, max_kv, *cs, *ss, *os,
-                              handle)
-    _check(st, "adt_kv_read_q8")
+    st = (_MARSHAL or _native()).kv_read_q8(k_cache, v_cache, k_scale, v_scale, kv_len, k_out, v_out, B, Hkv, D, num_layers,
+                                            max_kv, stream)
+    if st:
+        _check(st, "adt_kv_read_q8")
 
 
 def adt_tree_attn_q8_workspace_size(B, H, Hkv, D, max_nodes, max_kv) -> int:
@@ -613,18 +576,11 @@ def adt_tree_attn_q8(q, k_cache, v_cache, k_scale, v_scale, kv_len, k_tree, v_tr
                      max_nodes, max_kv, softmax_scale, out, lse=None, workspace, stream=None) -> None:
     """adt_tree_attn of one layer over caches [B, Hkv, rows >= max_kv, D] float8_e4m3fn with scales
     [B, Hkv, rows >= max_kv] uint8; q, k_tree, v_tree, out bf16 [Ntot, *, D], lse fp32 [Ntot, H] or None."""
-    dev, handle = _launch_on(q, stream, "q")
-    i32, bf16 = torch.int32, torch.bfloat16
-    addr, cs, ss = _q8_cache(k_cache[None], v_cache[None], k_scale[None], v_scale[None], 1, B, Hkv, max_kv, D, dev)
-    N = q.shape[0]
-    st = lib().adt_tree_attn_q8(_vec(q, bf16, dev, N * H * D, "q"), *addr, _vec(kv_len, i32, dev, B, "kv_len"), *cs[1:],
-                                *ss[1:], _vec(k_tree, bf16, dev, N * Hkv * D, "k_tree"),
-                                _vec(v_tree, bf16, dev, N * Hkv * D, "v_tree"), _vec(parents, i32, dev, N, "parents"),
-                                _vec(node_offsets, i32, dev, B + 1, "node_offsets"), B, H, Hkv, D, max_nodes, max_kv,
-                                softmax_scale, _vec(out, bf16, dev, N * H * D, "out"),
-                                _vec(lse, torch.float32, dev, N * H, "lse"), _addr(workspace, torch.uint8, dev, "workspace"),
-                                _nbytes(workspace), handle)
-    _check(st, "adt_tree_attn_q8")
+    st = (_MARSHAL or _native()).tree_attn_q8(q, k_cache, v_cache, k_scale, v_scale, kv_len, k_tree, v_tree, parents,
+                                              node_offsets, B, H, Hkv, D, max_nodes, max_kv, softmax_scale, out, lse, workspace,
+                                              stream)
+    if st:
+        _check(st, "adt_tree_attn_q8")
 
 
 # ----------------------------------------------------------------------------- controller

@@ -1,4 +1,5 @@
-"""Builds libadt.so (CUDA for sm_103a) in-tree, next to this file.
+"""Builds libadt.so (CUDA for sm_103a) in-tree, next to this file, and
+_marshal.so, the binding's C++ part (for the torch that is installed).
 
 Every translation unit is compiled in parallel with nvcc, then linked into a
 shared library with the CUDA runtime linked statically.  Run
@@ -11,6 +12,7 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -18,6 +20,7 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD_DIR = os.path.join(ROOT, "_build")
 LIB_PATH = os.path.join(PKG, "libadt.so")
+MARSHAL_PATH = os.path.join(PKG, "_marshal.so")
 
 ARCH_FLAGS = ["-gencode", "arch=compute_103a,code=sm_103a"]
 COMMON_FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC,-O3", "-I", INCLUDE, "-I", CSRC]
@@ -49,12 +52,40 @@ def _compile(src: str, extra) -> str:
     return obj
 
 
+def _marshal() -> str:
+    """The binding's C++ part: against torch's headers, with the host compiler."""
+    src = os.path.join(CSRC, "marshal.cc")
+    import torch
+    home = os.path.dirname(os.path.abspath(torch.__file__))
+    stamp = os.path.join(BUILD_DIR, "marshal.torch")  # rebuilt for another torch
+    deps = [src, os.path.join(INCLUDE, "adt.h")]
+    if os.path.exists(MARSHAL_PATH) and all(os.path.getmtime(MARSHAL_PATH) >= os.path.getmtime(d) for d in deps) and \
+            os.path.exists(stamp) and open(stamp).read() == torch.__version__:
+        return MARSHAL_PATH
+    tmp = MARSHAL_PATH + ".tmp"
+    cuda = os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(nvcc()))), "include")
+    cmd = [os.environ.get("CXX") or "g++", "-O2", "-std=c++17", "-fPIC", "-shared",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", INCLUDE,
+           "-I", sysconfig.get_paths()["include"], "-I", os.path.join(home, "include"),
+           "-I", os.path.join(home, "include", "torch", "csrc", "api", "include"), "-I", cuda, src, "-o", tmp,
+           "-L", os.path.join(home, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-ldl"]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError(f"the compiler failed for {os.path.basename(src)}:\n{res.stdout}\n{res.stderr}")
+    os.replace(tmp, MARSHAL_PATH)
+    with open(stamp, "w") as f:
+        f.write(torch.__version__)
+    return MARSHAL_PATH
+
+
 def build(verbose: bool = False, extra_flags=()) -> str:
     """Compiles the library if any source is newer than it; returns its path."""
     os.makedirs(BUILD_DIR, exist_ok=True)
     srcs = sources()
-    with cf.ThreadPoolExecutor(max_workers=min(8, len(srcs))) as ex:
+    with cf.ThreadPoolExecutor(max_workers=min(8, len(srcs) + 1)) as ex:
+        marshal = ex.submit(_marshal)
         objs = list(ex.map(lambda s: _compile(s, extra_flags), srcs))
+        marshal.result()
     if not os.path.exists(LIB_PATH) or any(os.path.getmtime(o) > os.path.getmtime(LIB_PATH) for o in objs):
         tmp = LIB_PATH + ".tmp"
         cmd = [nvcc()] + ARCH_FLAGS + ["-shared", "-o", tmp] + objs

@@ -253,8 +253,9 @@ __device__ __forceinline__ uint64_t tile_desc(uint32_t addr) {
 }
 
 __device__ __forceinline__ uint32_t e4m3x2_to_f16(uint32_t two) {
-  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(two & 0xffffu), __NV_E4M3);
-  return static_cast<uint32_t>(h.x) | static_cast<uint32_t>(h.y) << 16;
+  uint32_t r;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;\n" : "=r"(r) : "h"(static_cast<uint16_t>(two)));
+  return r;
 }
 
 __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
@@ -302,6 +303,9 @@ __device__ __forceinline__ void group_sync(int grp) {  // of the four warps of a
   else
     asm volatile("bar.sync 4, 128;\n" ::: "memory");
 }
+
+constexpr int kAhead = 8;  // chunks: as many as a warp's lanes prefetch at once
+__device__ __forceinline__ void prefetch_l2(const void* src) { asm volatile("prefetch.global.L2 [%0];\n" ::"l"(src)); }
 
 // (The polling apart from its many callers: instructions are what this kernel's
 // roles, each in code of its own, wait for most.)
@@ -573,7 +577,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // ------------------------------------------------------------ K tiles, scales
     uint32_t issued = 0, q_issued = 0;  // one past the last tile, and the last item's queries, requested
     bool ok = true;
-    uint32_t pend[3] = {};  // scales of four keys and of their values; a tree's values that are not finite
+    uint32_t pend[3][4] = {};  // scales of four keys and of their values; a tree's values that are not finite
     int pend_slot = -1, ref = 0;
     bool pend_first = false;
     auto flush = [&]() {
@@ -581,7 +585,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       uint32_t most = 0u;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const uint32_t v = pend[1] >> (8 * i) & 255u;
+        const uint32_t v = pend[1][i];
         most = max(most, v == 255u ? 0u : v);
       }
       most = __reduce_max_sync(adt::kFullMask, most);
@@ -592,13 +596,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       float f[8];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        f[i] = adt::q8_scale(pend[0] >> (8 * i) & 255u);
-        f[4 + i] = value_factor(static_cast<int>(pend[1] >> (8 * i) & 255u), ref);
+        f[i] = adt::q8_scale(pend[0][i]);
+        f[4 + i] = value_factor(static_cast<int>(pend[1][i]), ref);
       }
       float4* dst = reinterpret_cast<float4*>(s_scale + pend_slot * 2 * kChunk);
       dst[lane] = make_float4(f[0], f[1], f[2], f[3]);
       dst[32 + lane] = make_float4(f[4], f[5], f[6], f[7]);
-      const bool odd = __any_sync(adt::kFullMask, pend[2] != 0u);
+      const bool odd = __any_sync(adt::kFullMask, (pend[2][0] | pend[2][1] | pend[2][2] | pend[2][3]) != 0u);
       if (lane == 0) {
         s_odd[pend_slot] = odd;
         s_ref[pend_slot] = ref;
@@ -611,6 +615,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint32_t item = 0;
     for (bool more = true; ok && more; more = w.next(p), ++item) {
       const int64_t s0 = w.b * p.ssb + w.g * p.ssh, bg = static_cast<int64_t>(w.b) * p.Hkv + w.g;
+      // Scales come byte by byte (their rows need no alignment), to registers, and are
+      // written a chunk later: without a prefetch this warp waited for memory once a
+      // chunk, 2000 cycles of 2800.
+      auto prefetch_scale = [&](int k, int i) {  // first and last byte of K's and of V's
+        const int row = min(k * kChunk + (i & 1) * (kChunk - 1), w.t.L - 1);
+        if (k * kChunk < w.t.L && k < w.k1) prefetch_l2(p.scale[i >> 1 & 1] + s0 + row);
+      };
+      prefetch_scale(w.k0 + (lane >> 2), lane);
       // The item's queries, `copies` times.
       if (lane == 0) ok = item < 2 || wait(&bars.q_free[item & 1], (item >> 1) - 1);
       ok = __shfl_sync(adt::kFullMask, ok ? 1 : 0, 0) != 0;
@@ -653,18 +665,19 @@ __global__ void __launch_bounds__(kThreads, 1)
         static_assert(kScaleSlots >= KS + 4, "a slot that is read");
         flush();
         const int left = keys - lane * 4;
+        const uint8_t* src = (tree_k ? p.pre.scale + chunk * 3 * p.pre.t_rows : p.scale[0] + s0 + k * kChunk) + lane * 4;
+        const uint8_t* vsrc = tree_k ? src + p.pre.t_rows : p.scale[1] + s0 + k * kChunk + lane * 4;
 #pragma unroll
-        for (int x = 0; x < 3; ++x) {
-          if (x == 2 && !tree_k) {
-            pend[x] = 0u;
-            break;
+        for (int i = 0; i < 4; ++i) {
+          pend[0][i] = 127u;
+          pend[1][i] = pend[2][i] = 0u;
+          if (i < left) {
+            pend[0][i] = src[i];
+            pend[1][i] = vsrc[i];
+            if (tree_k) pend[2][i] = vsrc[p.pre.t_rows + i];
           }
-          const uint8_t* src = (tree_k ? p.pre.scale + (chunk * 3 + x) * p.pre.t_rows : p.scale[x & 1] + s0 + k * kChunk) + lane * 4;
-          uint32_t v = 0u;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) v |= (i < left ? static_cast<uint32_t>(src[i]) : x ? 0u : 127u) << (8 * i);
-          pend[x] = v;
         }
+        if (!tree_k && lane < 4) prefetch_scale(k + kAhead, lane);
         pend_first = k == w.k0;
         pend_slot = static_cast<int>(j % kScaleSlots);
       }
