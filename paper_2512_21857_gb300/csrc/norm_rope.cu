@@ -29,6 +29,7 @@ using adt::token_angles;
 constexpr int kThreads = 256;
 constexpr int kUnit = 16;     // elements of a head in a thread
 constexpr int kMaxHead = 4096;
+constexpr int kMaxTurns = 4, kTurnCtas = 8;
 
 struct NormParams {
   const void* in[3];        // rows of q, k, v
@@ -50,164 +51,154 @@ __device__ __forceinline__ float group_sum(float v, int width) {
   return v;
 }
 
-// Vectors: 16 | D <= 512, 16 | rot, 16-byte boundaries.  A CTA takes one token or
-// a few (and where there are few, a share of their heads); a thread keeps its place
-// within the heads, so that it reads its cosines and sines once, and its first
-// units are on their way while the angles are made.
+// Vectors: 16 | D <= 512, 16 | rot, 16-byte boundaries.  A CTA takes a token or a few
+// at a time, one after the other (and where there are few, a share of their heads);
+// a thread keeps its place within the heads, so that it reads a token's cosines and
+// sines once.  Once a thread's unit is widened, its next one is on its way.
 template <typename T, typename W>
-__global__ void __launch_bounds__(kThreads, 3)
-    norm_rope_vec_kernel(const NormParams p, int N, int tokens, int lanes, int width) {
+__global__ void __launch_bounds__(kThreads, sizeof(T) + sizeof(W) == 4 ? 4 : sizeof(T) + sizeof(W) == 6 ? 3 : 2)
+    norm_rope_vec_kernel(const NormParams p, int N, int tokens, int lanes, int width, int turns) {
   extern __shared__ float2 cs[];
-  constexpr int kBatch = 2;
   adt::pdl_wait_then_release();
-  const int n0 = blockIdx.x * tokens, here = min(tokens, N - n0);
-  const int tok = threadIdx.x / lanes, lane = threadIdx.x - tok * lanes;
-  const bool active = tok < here;
-  const int64_t n = n0 + (active ? tok : 0);
+  const int n0 = blockIdx.x * tokens * turns, here = min(tokens * turns, N - n0);
+  const int tok0 = threadIdx.x / lanes, lane = threadIdx.x - tok0 * lanes;
   const int half = p.rot / 2, units = p.D / kUnit;
   const int per_pass = lanes / width, hl = lane / width, u = lane - hl * width;
   const bool turned = u * kUnit < p.rot, split_pair = turned && !p.interleaved;
   const int e0 = split_pair ? u * 8 : u * kUnit, e1 = split_pair ? e0 + half : e0 + 8;
-  const int heads = p.heads[0] + p.heads[1];
-  const int h0 = static_cast<int>(blockIdx.y) * per_pass + hl, hstep = static_cast<int>(gridDim.y) * per_pass;
-  const int v0 = static_cast<int>(blockIdx.y) * lanes + lane, vstep = static_cast<int>(gridDim.y) * lanes;
-  const int vectors = active ? p.heads[2] * p.D / 8 : 0;
-  const bool mine = active && u < units;  // (lanes past a head's elements add zeros to its sums)
-
-  Eight<T> x[kBatch][2], v[2 * kBatch];
-  auto fetch = [&](int h, int vi) {
-#pragma unroll
-    for (int k = 0; k < kBatch; ++k) {
-      const int hk = h + k * hstep;
-      if (mine && hk < heads) {
-        const bool q = hk < p.heads[0];
-        const T* src = static_cast<const T*>(q ? p.in[0] : p.in[1]) + n * (q ? p.ld[0] : p.ld[1]) +
-                       (q ? hk : hk - p.heads[0]) * p.D;
-        x[k][0].load(src + e0);
-        x[k][1].load(src + e1);
-      }
-    }
-#pragma unroll
-    for (int k = 0; k < 2 * kBatch; ++k)
-      if (vi + k * vstep < vectors)
-        v[k].load(static_cast<const T*>(p.in[2]) + n * p.ld[2] + static_cast<int64_t>(vi + k * vstep) * 8);
-  };
-  fetch(h0, v0);
-  token_angles(p, n0, here, cs);
-  float c[8], s[8];
-  if (turned && mine) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float2 z = cs[tok * half + u * 8 + i];
-      c[i] = z.x;
-      s[i] = z.y;
-    }
-  }
+  const int heads = p.heads[0] + p.heads[1], vectors = p.heads[2] * p.D / 8;
+  const int first = static_cast<int>(blockIdx.y) * per_pass, hstep = static_cast<int>(gridDim.y) * per_pass;
+  const int vfirst = static_cast<int>(blockIdx.y) * lanes, vstep = static_cast<int>(gridDim.y) * lanes;
   const float inv_d = 1.f / static_cast<float>(p.D);
-  // (Every lane of a warp makes the same rounds: the sums are exchanged by all.)
-  const int first = static_cast<int>(blockIdx.y) * per_pass;
-  int h = h0, vi = v0;
-  for (int base = first, vb = v0 - lane; base < heads || vb < p.heads[2] * p.D / 8;
-       base += kBatch * hstep, vb += 2 * kBatch * vstep) {
+
+  // What is on its way: the unit of head base + hl, vectors vb + lane and vstep after
+  // it, of token tok.  (base and vb are the same for a warp: its lanes make the same
+  // rounds, the sums are exchanged by all.  Lanes past a head's elements, or without
+  // a head or a token, add zeros.)
+  int tok = tok0, base = first, vb = vfirst;
+  Eight<T> x[2], v[2];
+  auto have_unit = [&]() { return tok < here && u < units && base + hl < heads; };
+  auto fetch = [&]() {
+    const int64_t n = n0 + tok;
+    if (have_unit()) {
+      const int h = base + hl;
+      const bool q = h < p.heads[0];
+      const T* src = static_cast<const T*>(q ? p.in[0] : p.in[1]) + n * (q ? p.ld[0] : p.ld[1]) + (q ? h : h - p.heads[0]) * p.D;
+      x[0].load(src + e0);
+      x[1].load(src + e1);
+    }
 #pragma unroll
-    for (int k = 0; k < kBatch; ++k) {
-      if (base + k * hstep >= heads) break;  // (uniform)
-      const int hk = h + k * hstep;
-      const bool have = mine && hk < heads;
-      float y[kUnit];
-      {
-        float a[8], b[8];
-        x[k][0].get(a);
-        x[k][1].get(b);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          y[i] = have ? a[i] : 0.f;
-          y[8 + i] = have ? b[i] : 0.f;
-        }
-      }
-      if (p.layer) {
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < kUnit; ++i) sum += y[i];
-        const float mean = group_sum(sum, width) * inv_d;
-#pragma unroll
-        for (int i = 0; i < kUnit; ++i) y[i] = have ? y[i] - mean : 0.f;
-      }
-      float sq = 0.f;
-#pragma unroll
-      for (int i = 0; i < kUnit; ++i) sq = fmaf(y[i], y[i], sq);
-      const float r = rsqrtf(fmaf(group_sum(sq, width), inv_d, p.eps));
-      if (!have) continue;
-      const int which = hk < p.heads[0] ? 0 : 1, hh = which ? hk - p.heads[0] : hk;
-      const W* w = static_cast<const W*>(which ? p.weight[1] : p.weight[0]);
-      const W* bi = static_cast<const W*>(which ? p.bias[1] : p.bias[0]);
-      const int64_t woff = static_cast<int64_t>(hh) * (which ? p.wld[1] : p.wld[0]);
-#pragma unroll
-      for (int i = 0; i < kUnit; ++i) y[i] *= r;
-      if (w) {
-        Eight<W> t[2];
-        float a[8], b[8];
-        t[0].load(w + woff + e0);
-        t[1].load(w + woff + e1);
-        t[0].get(a);
-        t[1].get(b);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          y[i] *= a[i];
-          y[8 + i] *= b[i];
-        }
-      }
-      if (bi) {
-        Eight<W> t[2];
-        float a[8], b[8];
-        t[0].load(bi + woff + e0);
-        t[1].load(bi + woff + e1);
-        t[0].get(a);
-        t[1].get(b);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          y[i] += a[i];
-          y[8 + i] += b[i];
-        }
-      }
-      float z[kUnit];
-      if (!turned) {
-#pragma unroll
-        for (int i = 0; i < kUnit; ++i) z[i] = y[i];
-      } else if (p.interleaved) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          z[2 * i] = y[2 * i] * c[i] - y[2 * i + 1] * s[i];
-          z[2 * i + 1] = y[2 * i + 1] * c[i] + y[2 * i] * s[i];
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          z[i] = y[i] * c[i] - y[8 + i] * s[i];
-          z[8 + i] = y[8 + i] * c[i] + y[i] * s[i];
-        }
-      }
-      __nv_bfloat16* dst = (which ? p.out[1] : p.out[0]) + (n * (which ? p.heads[1] : p.heads[0]) + hh) * p.D;
-      float za[8], zb[8];
+    for (int k = 0; k < 2; ++k)
+      if (tok < here && vb + lane + k * vstep < vectors)
+        v[k].load(static_cast<const T*>(p.in[2]) + n * p.ld[2] + static_cast<int64_t>(vb + lane + k * vstep) * 8);
+  };
+  fetch();
+  token_angles(p, n0, here, cs);
+  for (int turn = 0; turn < turns;) {
+    const bool have = have_unit();
+    const int64_t n = n0 + tok;
+    const int h = base + hl, which = h < p.heads[0] ? 0 : 1, hh = which ? h - p.heads[0] : h, at = tok * half + u * 8;
+    const bool any = base < heads;  // (uniform)
+    float y[kUnit];
+    {
+      float a[8], b[8];
+      x[0].get(a);
+      x[1].get(b);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        za[i] = z[i];
-        zb[i] = z[8 + i];
+        y[i] = have ? a[i] : 0.f;
+        y[8 + i] = have ? b[i] : 0.f;
       }
-      put(dst + e0, za);
-      put(dst + e1, zb);
     }
 #pragma unroll
-    for (int k = 0; k < 2 * kBatch; ++k) {
-      if (vi + k * vstep < vectors) {
+    for (int k = 0; k < 2; ++k) {
+      if (tok < here && vb + lane + k * vstep < vectors) {
         float a[8];
         v[k].get(a);
-        put(p.out[2] + n * p.heads[2] * p.D + static_cast<int64_t>(vi + k * vstep) * 8, a);
+        put(p.out[2] + n * p.heads[2] * p.D + static_cast<int64_t>(vb + lane + k * vstep) * 8, a);
       }
     }
-    h += kBatch * hstep;
-    vi += 2 * kBatch * vstep;
-    fetch(h, vi);
+    base += hstep;
+    vb += 2 * vstep;
+    if (base >= heads && vb >= vectors) {
+      ++turn;
+      tok += tokens;
+      base = first;
+      vb = vfirst;
+    }
+    if (turn < turns) fetch();
+    if (!any) continue;
+    const W* w = static_cast<const W*>(which ? p.weight[1] : p.weight[0]);
+    const W* bi = static_cast<const W*>(which ? p.bias[1] : p.bias[0]);
+    const int64_t woff = static_cast<int64_t>(hh) * (which ? p.wld[1] : p.wld[0]);
+    Eight<W> tw[2], tb[2];
+    if (have && w) {
+      tw[0].load(w + woff + e0);
+      tw[1].load(w + woff + e1);
+    }
+    if (have && bi) {
+      tb[0].load(bi + woff + e0);
+      tb[1].load(bi + woff + e1);
+    }
+    if (p.layer) {
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < kUnit; ++i) sum += y[i];
+      const float mean = group_sum(sum, width) * inv_d;
+#pragma unroll
+      for (int i = 0; i < kUnit; ++i) y[i] = have ? y[i] - mean : 0.f;
+    }
+    float sq = 0.f;
+#pragma unroll
+    for (int i = 0; i < kUnit; ++i) sq = fmaf(y[i], y[i], sq);
+    const float r = rsqrtf(fmaf(group_sum(sq, width), inv_d, p.eps));
+    if (!have) continue;
+#pragma unroll
+    for (int i = 0; i < kUnit; ++i) y[i] *= r;
+    if (w) {
+      float a[8], b[8];
+      tw[0].get(a);
+      tw[1].get(b);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        y[i] *= a[i];
+        y[8 + i] *= b[i];
+      }
+    }
+    if (bi) {
+      float a[8], b[8];
+      tb[0].get(a);
+      tb[1].get(b);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        y[i] += a[i];
+        y[8 + i] += b[i];
+      }
+    }
+    if (turned) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float2 z = cs[at + i];
+        if (!p.interleaved) {
+          const float a = y[i], b = y[8 + i];
+          y[i] = a * z.x - b * z.y;
+          y[8 + i] = b * z.x + a * z.y;
+        } else {
+          const float a = y[2 * i], b = y[2 * i + 1];
+          y[2 * i] = a * z.x - b * z.y;
+          y[2 * i + 1] = b * z.x + a * z.y;
+        }
+      }
+    }
+    __nv_bfloat16* dst = (which ? p.out[1] : p.out[0]) + (n * (which ? p.heads[1] : p.heads[0]) + hh) * p.D;
+    float za[8], zb[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      za[i] = y[i];
+      zb[i] = y[8 + i];
+    }
+    put(dst + e0, za);
+    put(dst + e1, zb);
   }
 }
 
@@ -285,14 +276,16 @@ adt_status launch(const NormParams& p, bool vec, int N, const adt::DeviceInfo& i
     const int lanes = lanes_of(many ? 2 : 1);
     const int tokens = kThreads / lanes;
     const int passes = (want + lanes - 1) / lanes;
-    const int groups = (N + tokens - 1) / tokens;
+    int turns = 1;
+    while (turns < kMaxTurns && static_cast<int64_t>(N) >= int64_t{2} * turns * tokens * kTurnCtas * info.sm_count) turns *= 2;
+    const int groups = (N + tokens * turns - 1) / (tokens * turns);
     // Few tokens: their heads over several CTAs, up to two an SM.
     int split = 2 * info.sm_count / groups;
     split = split < 1 ? 1 : split > passes ? passes : split;
     cfg->gridDim = dim3(static_cast<unsigned>(groups), static_cast<unsigned>(split), 1);
     cfg->blockDim = dim3(static_cast<unsigned>(lanes * tokens), 1, 1);
-    cfg->dynamicSmemBytes = static_cast<size_t>(tokens) * (p.rot / 2) * sizeof(float2);
-    ADT_CUDA_TRY(cudaLaunchKernelEx(cfg, norm_rope_vec_kernel<T, W>, p, N, tokens, lanes, width));
+    cfg->dynamicSmemBytes = static_cast<size_t>(tokens) * turns * (p.rot / 2) * sizeof(float2);
+    ADT_CUDA_TRY(cudaLaunchKernelEx(cfg, norm_rope_vec_kernel<T, W>, p, N, tokens, lanes, width, turns));
     return adt::launch_status();
   }
   // Rows of shared memory: within the 48 KB that need no opting in.
