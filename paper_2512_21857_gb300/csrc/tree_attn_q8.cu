@@ -57,14 +57,14 @@ constexpr int kRows = 128;              // query rows of an item
 constexpr int kChunk = 128;             // keys of a chunk
 constexpr int kMaxTreeNodes = 256;
 constexpr int64_t kMaxRows = 1 << 24;   // query rows of a call
-constexpr int kItemCost = 2;            // chunks that an item's start and end take the time of
+constexpr int kItemCost = 4;            // chunks that an item's start and end take the time of
 constexpr int kJoinCost = 6;            // ... and that joining an item's parts takes
 constexpr int kMinShare = 6;            // coordinates (see Walk) of a CTA's share, where there are few
 constexpr int kSoftmaxThreads = 256;
 constexpr int kKWarp = 8, kVWarp = 9, kSWarp = 10, kPvWarp = 11, kConvWarp = 12;
 constexpr int kConvThreads = 128;
 constexpr int kThreads = 512;
-constexpr int kMaxScaleSlots = 10;
+constexpr int kMaxScaleSlots = 16;
 constexpr int kMaxStages = 6;
 constexpr int kMaxGrid = 1024;          // tickets of the workspace
 constexpr uint32_t kTmemCols = 512;
@@ -79,7 +79,7 @@ template <int D>
 struct Cfg {
   static constexpr int kKStages = D == 128 ? 3 : 6;
   static constexpr int kVStages = D == 128 ? 2 : 4;
-  static constexpr int kScaleSlots = kKStages + 4;
+  static constexpr int kScaleSlots = D == 128 ? 8 : 16;
   static constexpr int kTile = kChunk * D;                // 128 rows of e4m3
   static constexpr int kBlock = kChunk * 128;             // one 64-column block of 128 rows of fp16
   static constexpr int kWide = D / 64 * kBlock;           // 128 rows of fp16
@@ -161,31 +161,40 @@ struct Walk {
   int padded;          // every item's width, or 0: its chunks and kItemCost
   int k0, k1;          // the share's chunks of the item
   bool first;          // of the share's items
+  bool more;
   __device__ __forceinline__ void clip(int64_t from) {
     const int64_t base = start + kItemCost;
     k0 = from > base ? static_cast<int>(from - base) : 0;
     k1 = static_cast<int>(min(static_cast<int64_t>(t.chunks), end - base));
   }
   __device__ __forceinline__ bool some() const { return k1 > k0; }
-  __device__ __forceinline__ bool next(const AttnParams& p) {
-    start += padded ? padded : kItemCost + t.chunks;
-    first = false;
-    if (start + kItemCost >= end) return false;
-    if (++blk == t.blocks) {
-      blk = 0;
-      if (++g == p.Hkv) {
-        g = 0;
-        unsigned bits = 0u;
-        do {
-          if (++b >= p.B) return false;
-          t = tree_of(p, b, &bits);
-        } while (t.chunks == 0);
-      }
-    }
-    clip(start);
-    return some();
-  }
 };
+
+// The share's next item; its `more` says whether there is one.  (One copy of this
+// for all roles: the instruction cache of an SM is smaller than this kernel.)
+__device__ __noinline__ Walk next_item(const AttnParams& p, Walk w) {
+  w.start += w.padded ? w.padded : kItemCost + w.t.chunks;
+  w.first = false;
+  w.more = w.start + kItemCost < w.end;
+  if (!w.more) return w;
+  if (++w.blk == w.t.blocks) {
+    w.blk = 0;
+    if (++w.g == p.Hkv) {
+      w.g = 0;
+      unsigned bits = 0u;
+      do {
+        if (++w.b >= p.B) {
+          w.more = false;
+          return w;
+        }
+        w.t = tree_of(p, w.b, &bits);
+      } while (w.t.chunks == 0);
+    }
+  }
+  w.clip(w.start);
+  w.more = w.some();
+  return w;
+}
 
 // The tree's values that are not finite were left out of the products: adds those
 // that node t sees, of nodes t0 up to before t1, to `cols` columns of its row, as
@@ -307,17 +316,23 @@ __device__ __forceinline__ void group_sync(int grp) {  // of the four warps of a
 constexpr int kAhead = 8;  // chunks: as many as a warp's lanes prefetch at once
 __device__ __forceinline__ void prefetch_l2(const void* src) { asm volatile("prefetch.global.L2 [%0];\n" ::"l"(src)); }
 
-// (The polling apart from its many callers: instructions are what this kernel's
-// roles, each in code of its own, wait for most.)
-__device__ __noinline__ bool wait_on(uint64_t* bar, uint32_t parity, volatile int* abort_flag, unsigned* err, uint32_t limit) {
-  return sm100::wait_bar(bar, parity, abort_flag, err, limit);
+// A bounded wait, as short as it can be (its callers are many, and the instruction
+// cache of an SM is smaller than this kernel): false after `limit` polls, or once
+// another role has given up.
+__device__ __forceinline__ bool poll(uint64_t* bar, uint32_t parity, volatile int* abort_flag, uint32_t limit) {
+  const uint32_t a = sm100::smem_addr(bar);
+#pragma unroll 1
+  while (!sm100::mbar_try_wait(a, parity)) {
+    if (--limit == 0 || ((limit & 255u) == 0 && *abort_flag)) return false;
+  }
+  return true;
 }
 
 // 2^(s - ref + kHeadroom) for a value row's scale s against a reference: what its weights take on.
 constexpr int kHeadroom = 4, kSlack = 3;
 __device__ __forceinline__ float value_factor(int s, int ref) {
-  const int e = s - ref + kHeadroom + 127;
-  return s == 255 ? __uint_as_float(0x7fc00000u) : e > 0 ? __uint_as_float(static_cast<uint32_t>(e) << 23) : 0.f;
+  const int e = max(s - ref + kHeadroom + 127, 0);
+  return __uint_as_float(s == 255 ? 0x7fc00000u : static_cast<uint32_t>(e) << 23);
 }
 __device__ __forceinline__ float power_of_two(int e) {
   return e < -126 ? 0.f : __uint_as_float(static_cast<uint32_t>(min(e, 127) + 127) << 23);
@@ -514,7 +529,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int64_t c = blockIdx.x;
     const int64_t x0 = c < shares ? c * total / shares : total, x1 = c < shares ? (c + 1) * total / shares : total;
     Walk w{};
-    w.first = true;
+    w.first = w.more = true;
     int64_t before = 0;
     for (int b0 = 0; x0 < x1 && b0 < p.B; b0 += 32) {
       if (p.B > 32) t = b0 + lane < p.B ? tree_of(p, b0 + lane, &bits) : Tree{};
@@ -563,8 +578,11 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint8_t* sK = smem + C::kKOff;
   uint8_t* sV = smem + C::kVOff;
   uint8_t* sWide = smem + C::kWideOff;
-  auto wait = [&](uint64_t* bar, uint32_t phase) {
-    return sm100::mbar_try_wait(sm100::smem_addr(bar), phase & 1u) || wait_on(bar, phase & 1u, &s_abort, p.err, p.wait_limit);
+  auto wait = [&](uint64_t* bar, uint32_t phase) { return poll(bar, phase & 1u, &s_abort, p.wait_limit); };
+  // What a role says whose wait gave up: the others' give up too.
+  auto give_up = [&]() {
+    s_abort = 1;
+    adt::raise_error(p.err, ADT_DEVERR_TIMEOUT);
   };
   auto all_wait = [&](uint64_t* bar, uint32_t phase) { return __all_sync(adt::kFullMask, wait(bar, phase)); };
   auto arrive = [&](uint64_t* bar) { sm100::mbar_arrive(sm100::smem_addr(bar)); };
@@ -576,77 +594,48 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp == kKWarp) {
     // ------------------------------------------------------------ K tiles, scales
     uint32_t issued = 0, q_issued = 0;  // one past the last tile, and the last item's queries, requested
-    bool ok = true;
-    uint32_t pend[3][4] = {};  // scales of four keys and of their values; a tree's values that are not finite
-    int pend_slot = -1, ref = 0;
-    bool pend_first = false;
-    auto flush = [&]() {
-      if (pend_slot < 0) return;
-      uint32_t most = 0u;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t v = pend[1][i];
-        most = max(most, v == 255u ? 0u : v);
-      }
-      most = __reduce_max_sync(adt::kFullMask, most);
-      // The reference is the first chunk's largest scale, and rises where one is
-      // more than kSlack above it.
-      const int before = ref;
-      if (pend_first || static_cast<int>(most) > ref + kSlack) ref = static_cast<int>(most);
-      float f[8];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        f[i] = adt::q8_scale(pend[0][i]);
-        f[4 + i] = value_factor(static_cast<int>(pend[1][i]), ref);
-      }
-      float4* dst = reinterpret_cast<float4*>(s_scale + pend_slot * 2 * kChunk);
-      dst[lane] = make_float4(f[0], f[1], f[2], f[3]);
-      dst[32 + lane] = make_float4(f[4], f[5], f[6], f[7]);
-      const bool odd = __any_sync(adt::kFullMask, (pend[2][0] | pend[2][1] | pend[2][2] | pend[2][3]) != 0u);
-      if (lane == 0) {
-        s_odd[pend_slot] = odd;
-        s_ref[pend_slot] = ref;
-        s_drop[pend_slot] = pend_first ? 1.f : power_of_two(before - ref);
-      }
-      __syncwarp();
-      if (lane == 0) arrive(&bars.scale_full[pend_slot]);
-      pend_slot = -1;
-    };
+    // Scales of four keys and of their values, and a tree's values that are not finite,
+    // of the chunk before.  They come byte by byte (their rows need no alignment) and
+    // are written a chunk later.
+    uint32_t pend[3][4] = {};
+    int slot = 0, ref = 0, k = w.k0;
     uint32_t item = 0;
-    for (bool more = true; ok && more; more = w.next(p), ++item) {
+    bool ok = true, first = true, have = false;
+    for (;; ++j) {
       const int64_t s0 = w.b * p.ssb + w.g * p.ssh, bg = static_cast<int64_t>(w.b) * p.Hkv + w.g;
-      // Scales come byte by byte (their rows need no alignment), to registers, and are
-      // written a chunk later: without a prefetch this warp waited for memory once a
-      // chunk, 2000 cycles of 2800.
-      auto prefetch_scale = [&](int k, int i) {  // first and last byte of K's and of V's
-        const int row = min(k * kChunk + (i & 1) * (kChunk - 1), w.t.L - 1);
-        if (k * kChunk < w.t.L && k < w.k1) prefetch_l2(p.scale[i >> 1 & 1] + s0 + row);
+      const bool tree_k = k >= w.t.prefix;
+      const int64_t chunk = bg * p.pre.chunks + k - w.t.prefix;  // (of the tree's)
+      const int keys = tree_k ? w.t.n - (k - w.t.prefix) * kChunk : w.t.L - k * kChunk;
+      auto prefetch_scale = [&](int at, int i) {  // first and last byte of K's and of V's
+        const int row = min(at * kChunk + (i & 1) * (kChunk - 1), w.t.L - 1);
+        if (at * kChunk < w.t.L && at < w.k1) prefetch_l2(p.scale[i >> 1 & 1] + s0 + row);
       };
-      prefetch_scale(w.k0 + (lane >> 2), lane);
-      // The item's queries, `copies` times.
-      if (lane == 0) ok = item < 2 || wait(&bars.q_free[item & 1], (item >> 1) - 1);
-      ok = __shfl_sync(adt::kFullMask, ok ? 1 : 0, 0) != 0;
-      if (!ok) break;
-      if (lane == 0) {
-        const int rows = (min(w.t.n * p.group - w.blk * kRows, kRows) + 7) & ~7;
-        const uint32_t bar = sm100::smem_addr(&bars.q_full[item & 1]);
-        sm100::mbar_arrive_expect_tx(bar, 2 * p.copies * rows * D);
-        const uint8_t* src = p.pre.q + (bg * p.pre.blocks + w.blk) * 2 * p.pre.q_rows * D;
-        const uint32_t dst = sm100::smem_addr(sQ + (item & 1) * 2 * C::kTile);
-        for (int c = 0; c < p.copies; ++c) {
-          sm100::bulk_load(dst + c * (C::kTile / p.copies), src, rows * D, bar);
-          sm100::bulk_load(dst + C::kTile + c * (C::kTile / p.copies), src + p.pre.q_rows * D, rows * D, bar);
-        }
-        q_issued = item + 1;
-      }
-      for (int k = w.k0; k < w.k1; ++k, ++j) {
+      const bool fresh = k == w.k0;
+      if (w.more) {
         const int st = j % KS;
-        if (lane == 0) ok = j < KS || wait(&bars.k_free[st], j / KS - 1);
+        if (lane == 0) {
+          ok = !fresh || item < 2 || wait(&bars.q_free[item & 1], (item >> 1) - 1);
+          ok = ok && (j < KS || wait(&bars.k_free[st], j / KS - 1));
+        }
         ok = __shfl_sync(adt::kFullMask, ok ? 1 : 0, 0) != 0;
         if (!ok) break;
-        const bool tree_k = k >= w.t.prefix;
-        const int64_t chunk = bg * p.pre.chunks + k - w.t.prefix;  // (of the tree's)
-        const int keys = tree_k ? w.t.n - (k - w.t.prefix) * kChunk : w.t.L - k * kChunk;
+        if (fresh) {
+          // Without a prefetch this warp waited for memory once a chunk, 2000 cycles of 2800.
+          prefetch_scale(k + (lane >> 2), lane);
+          if (lane == 0) {  // the item's queries, `copies` times
+            const int rows = (min(w.t.n * p.group - w.blk * kRows, kRows) + 7) & ~7;
+            const uint32_t bar = sm100::smem_addr(&bars.q_full[item & 1]);
+            sm100::mbar_arrive_expect_tx(bar, 2 * p.copies * rows * D);
+            const uint8_t* src = p.pre.q + (bg * p.pre.blocks + w.blk) * 2 * p.pre.q_rows * D;
+            const uint32_t dst = sm100::smem_addr(sQ + (item & 1) * 2 * C::kTile);
+#pragma unroll 1
+            for (int c = 0; c < p.copies; ++c) {
+              sm100::bulk_load(dst + c * (C::kTile / p.copies), src, rows * D, bar);
+              sm100::bulk_load(dst + C::kTile + c * (C::kTile / p.copies), src + p.pre.q_rows * D, rows * D, bar);
+            }
+            q_issued = item + 1;
+          }
+        }
         if (lane == 0) {
           const uint32_t bar = sm100::smem_addr(&bars.k_full[st]), dst = sm100::smem_addr(sK + st * C::kTile);
           if (tree_k) {  // (the low part comes from warp 9 to the same barrier)
@@ -659,30 +648,63 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
         issued = j + 1;
-        // The scales, written when the next chunk's are asked for.  Their slot was
-        // read last for a chunk kScaleSlots before, which was done with before S of
-        // four chunks on could start, and S(j - KS) is done.
+      }
+      if (have) {
+        // The scales of the chunk before.  Their slot was read last for a chunk
+        // kScaleSlots before, which was done with before S of four chunks on could
+        // start, and S(j - KS) is done.
         static_assert(kScaleSlots >= KS + 4, "a slot that is read");
-        flush();
-        const int left = keys - lane * 4;
-        const uint8_t* src = (tree_k ? p.pre.scale + chunk * 3 * p.pre.t_rows : p.scale[0] + s0 + k * kChunk) + lane * 4;
-        const uint8_t* vsrc = tree_k ? src + p.pre.t_rows : p.scale[1] + s0 + k * kChunk + lane * 4;
+        uint32_t most = 0u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) most = max(most, pend[1][i] == 255u ? 0u : pend[1][i]);
+        most = __reduce_max_sync(adt::kFullMask, most);
+        const bool odd = __any_sync(adt::kFullMask, (pend[2][0] | pend[2][1] | pend[2][2] | pend[2][3]) != 0u);
+        // The reference is the first chunk's largest scale, and rises where one is
+        // more than kSlack above it.
+        const int before = ref;
+        if (first || static_cast<int>(most) > ref + kSlack) ref = static_cast<int>(most);
+        float f[8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          pend[0][i] = 127u;
-          pend[1][i] = pend[2][i] = 0u;
-          if (i < left) {
-            pend[0][i] = src[i];
-            pend[1][i] = vsrc[i];
-            if (tree_k) pend[2][i] = vsrc[p.pre.t_rows + i];
-          }
+          f[i] = adt::q8_scale(pend[0][i]);
+          f[4 + i] = value_factor(static_cast<int>(pend[1][i]), ref);
         }
-        if (!tree_k && lane < 4) prefetch_scale(k + kAhead, lane);
-        pend_first = k == w.k0;
-        pend_slot = static_cast<int>(j % kScaleSlots);
+        float4* dst = reinterpret_cast<float4*>(s_scale + slot * 2 * kChunk);
+        dst[lane] = make_float4(f[0], f[1], f[2], f[3]);
+        dst[32 + lane] = make_float4(f[4], f[5], f[6], f[7]);
+        if (lane == 0) {
+          s_odd[slot] = odd;
+          s_ref[slot] = ref;
+          s_drop[slot] = first ? 1.f : power_of_two(before - ref);
+        }
+        __syncwarp();
+        if (lane == 0) arrive(&bars.scale_full[slot]);
+      }
+      if (!w.more) break;
+      const uint8_t* src = (tree_k ? p.pre.scale + chunk * 3 * p.pre.t_rows : p.scale[0] + s0 + k * kChunk) + lane * 4;
+      const uint8_t* vsrc = tree_k ? src + p.pre.t_rows : p.scale[1] + s0 + k * kChunk + lane * 4;
+      const int left = keys - lane * 4;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        pend[0][i] = 127u;
+        pend[1][i] = pend[2][i] = 0u;
+        if (i < left) {
+          pend[0][i] = src[i];
+          pend[1][i] = vsrc[i];
+          if (tree_k) pend[2][i] = vsrc[p.pre.t_rows + i];
+        }
+      }
+      if (!tree_k && lane < 4) prefetch_scale(k + kAhead, lane);
+      slot = static_cast<int>(j % kScaleSlots);
+      first = fresh;
+      have = true;
+      if (++k == w.k1) {
+        w = next_item(p, w);
+        k = w.k0;
+        ++item;
       }
     }
-    flush();
+    if (!ok && lane == 0) give_up();
     asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
     // Every copy issued lands before the CTA goes on (also after an abort).
     if (lane == 0) {
@@ -699,7 +721,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (lane == 0) {
       uint32_t issued = 0;
       bool ok = true;
-      for (bool more = true; ok && more; more = w.next(p)) {
+      for (; ok && w.more; w = next_item(p, w)) {
         const uint8_t* v = p.v_cache + w.b * p.sb + w.g * p.sh;
         for (int k = w.k0; k < w.k1; ++k, ++j) {
           const int st = j % VS;
@@ -732,6 +754,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           issued = j + 1;
         }
       }
+      if (!ok) give_up();
       if (!ok) __nanosleep(200000);  // (a tree's keys on their way, on another barrier)
       for (int st = 0; st < VS; ++st) {
         if (issued <= static_cast<uint32_t>(st)) continue;
@@ -744,35 +767,45 @@ __global__ void __launch_bounds__(kThreads, 1)
     // ------------------------------------------------------------ S = Q K^T
     if (lane == 0) {
       bool ok = true;
-      uint32_t item = 0;
-      for (bool more = true; ok && more; more = w.next(p), ++item) {
-        const uint64_t q = tile_desc<D>(sm100::smem_addr(sQ + (item & 1) * 2 * C::kTile));
+      const uint64_t qd0 = tile_desc<D>(sm100::smem_addr(sQ)), kd0 = tile_desc<D>(sm100::smem_addr(sK)),
+                     vd0 = tile_desc<D>(sm100::smem_addr(sV));
+      uint32_t item = 0, phase = 0;
+      int st = 0;
+      for (; ok && w.more; w = next_item(p, w), ++item) {
+        const uint64_t q = qd0 + (item & 1) * (2 * C::kTile / 16);
         ok = wait(&bars.q_full[item & 1], item >> 1);
         for (int k = w.k0; ok && k < w.k1; ++k, ++j) {
           const int grp = j & 1;
-          ok = wait(&bars.k_full[j % KS], j / KS) && (j < 2 || wait(&bars.s_free[grp], (j >> 1) - 1));
+          ok = wait(&bars.k_full[st], phase) && (j < 2 || wait(&bars.s_free[grp], (j >> 1) - 1));
           if (!ok) break;
           sm100::tc_fence_after();
           const uint32_t d = tmem + grp * kChunk;
           const int keys = k < w.t.prefix ? w.t.L - k * kChunk : w.t.n - (k - w.t.prefix) * kChunk;
           const uint32_t idesc = sm100::idesc_e4m3_f32(kRows, 0) | static_cast<uint32_t>(min(kChunk, (keys + 15) & ~15) >> 3) << 17;
-          auto product = [&](uint64_t kt, uint32_t first) {
+          // The queries' high and low part with the keys, of a tree with their low part too.
+          const int parts = k >= w.t.prefix ? 4 : 2;
+          uint32_t more = 0u;
+#pragma unroll 1
+          for (int part = 0; part < parts; ++part) {
+            const uint64_t qd = q + (part & 1) * (C::kTile / 16);
+            const uint64_t kd = part < 2 ? kd0 + st * (C::kTile / 16) : vd0 + (j % VS) * (C::kTile / 16);
 #pragma unroll
-            for (int i = 0; i < D / 16; ++i) {  // the queries' high part, then the low one
-              const int part = i / (D / 32), kk = i % (D / 32);
-              sm100::mma_f8_ss(d, q + (part * C::kTile + kk * 32) / 16, kt + kk * 2, idesc, i == 0 ? first : 1u);
+            for (int kk = 0; kk < D / 32; ++kk) {
+              sm100::mma_f8_ss(d, qd + kk * 2, kd + kk * 2, idesc, more);
+              more = 1u;
             }
-          };
-          product(tile_desc<D>(sm100::smem_addr(sK + (j % KS) * C::kTile)), 0u);
-          if (k >= w.t.prefix) {  // the low part of the tree's keys
-            product(tile_desc<D>(sm100::smem_addr(sV + (j % VS) * C::kTile)), 1u);
-            sm100::mma_commit(sm100::smem_addr(&bars.v_free[j % VS]));
           }
+          if (k >= w.t.prefix) sm100::mma_commit(sm100::smem_addr(&bars.v_free[j % VS]));
           sm100::mma_commit(sm100::smem_addr(&bars.s_full[grp]));
-          sm100::mma_commit(sm100::smem_addr(&bars.k_free[j % KS]));
+          sm100::mma_commit(sm100::smem_addr(&bars.k_free[st]));
+          if (++st == KS) {
+            st = 0;
+            phase ^= 1u;
+          }
         }
         if (ok) sm100::mma_commit(sm100::smem_addr(&bars.q_free[item & 1]));
       }
+      if (!ok) give_up();
       sm100::mma_commit(sm100::smem_addr(&bars.drain[0]));
       (void)sm100::mbar_wait_bounded(sm100::smem_addr(&bars.drain[0]), 0, kDrainLimit);
     }
@@ -781,29 +814,28 @@ __global__ void __launch_bounds__(kThreads, 1)
     // ------------------------------------------------------------ O += P V
     if (lane == 0) {
       bool ok = true;
+      const uint64_t wd0 = sm100::smem_desc_sw128(sm100::smem_addr(sWide), C::kBlock, 1024);
       uint32_t item = 0;
-      for (bool more = true; ok && more; more = w.next(p), ++item) {
+      for (; ok && w.more; w = next_item(p, w), ++item) {
         for (int k = w.k0; ok && k < w.k1; ++k, ++j) {
           ok = wait(&bars.p_full[j & 1], j >> 1) && wait(&bars.wide_full[j & 1], j >> 1) &&
                (k > w.k0 || item == 0 || wait(&bars.o_free, item - 1));
           if (!ok) break;
           sm100::tc_fence_after();
           const uint32_t a = tmem + kPCol + (j & 1) * 64;
-          const uint64_t vd = sm100::smem_desc_sw128(sm100::smem_addr(sWide + (j & 1) * C::kWide), C::kBlock, 1024);
+          const uint64_t vd = wd0 + (j & 1) * (C::kWide / 16);
           const int keys = k < w.t.prefix ? w.t.L - k * kChunk : w.t.n - (k - w.t.prefix) * kChunk;
           const int steps = min(kChunk / 16, (keys + 15) / 16);
-          sm100::mma_bf16_ts(tmem + kOCol, a, vd, C::kIdescO, k > w.k0 ? 1u : 0u);
-          if (steps == kChunk / 16) {
-#pragma unroll
-            for (int kk = 1; kk < kChunk / 16; ++kk)
-              sm100::mma_bf16_ts(tmem + kOCol, a + kk * 8, vd + kk * 128, C::kIdescO, 1u);
-          } else {
-            for (int kk = 1; kk < steps; ++kk)
-              sm100::mma_bf16_ts(tmem + kOCol, a + kk * 8, vd + kk * 128, C::kIdescO, 1u);
+          uint32_t more = k > w.k0 ? 1u : 0u;
+#pragma unroll 1
+          for (int kk = 0; kk < steps; ++kk) {
+            sm100::mma_bf16_ts(tmem + kOCol, a + kk * 8, vd + kk * 128, C::kIdescO, more);
+            more = 1u;
           }
           sm100::mma_commit(sm100::smem_addr(&bars.done[j & 3]));
         }
       }
+      if (!ok) give_up();
       sm100::mma_commit(sm100::smem_addr(&bars.drain[1]));
       (void)sm100::mbar_wait_bounded(sm100::smem_addr(&bars.drain[1]), 0, kDrainLimit);
     }
@@ -821,7 +853,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t to[2] = {sw128_off(cr, 2 * cl + swap, kChunk), sw128_off(cr, 2 * cl + 1 - swap, kChunk)};
     uint32_t ended = 0, joins = 0;  // ended, bit i: chunk j - 1 - i was its item's last
     bool ok = true;
-    for (bool more = true; ok && more; more = w.next(p)) {
+    for (; ok && w.more; w = next_item(p, w)) {
       for (int k = w.k0; k < w.k1; ++k, ++j) {
         const int st = j % VS;
         uint8_t* wide = sWide + (j & 1) * C::kWide;
@@ -831,8 +863,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         const bool tree_k = k >= w.t.prefix;
         static_assert(VS >= 2, "V's slot");
         const bool join = p.copies > 1 && (ended & 2u);
-        ok = !any_of<1, kConvThreads>((j >= 2 && !wait(&bars.done[(j - 2) & 3], (j - 2) >> 2)) ||
-                                      (!tree_k && !wait(&bars.v_full[st], j / VS)) || (join && !wait(&bars.join_free[joins & 1], joins >> 1)));
+        ok = (j < 2 || wait(&bars.done[(j - 2) & 3], (j - 2) >> 2)) && (tree_k || wait(&bars.v_full[st], j / VS)) &&
+             (!join || wait(&bars.join_free[joins & 1], joins >> 1));
+        if (!ok && lane == 0) give_up();
+        ok = !any_of<1, kConvThreads>(!ok);
         if (!ok) break;
         joins += join ? 1u : 0u;
         ended = ended << 1 | (k + 1 == w.k1 ? 1u : 0u);
@@ -869,6 +903,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (ct == 0) arrive(&bars.v_free[st]);
       }
     }
+    if (!ok && lane == 0) give_up();
     // (A tree's values on their way: PV, or after an abort the wait here, sees them land.)
     if (ct == 0 && j > 0)
       for (uint32_t i = j > 2 ? j - 2 : 0; i < j; ++i)
@@ -890,7 +925,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     uint32_t item = 0;
     bool ok = true;
-    for (bool more = true; ok && more; more = w.next(p), ++item) {
+    for (; ok && w.more; w = next_item(p, w), ++item) {
       const int index = w.blk * kRows + row, node = index / p.group;
       const bool valid = node < w.t.n, active = __any_sync(adt::kFullMask, valid);
       const uint32_t j0 = j, j1 = j + static_cast<uint32_t>(w.k1 - w.k0);
@@ -1050,18 +1085,22 @@ __global__ void __launch_bounds__(kThreads, 1)
       s_m[par][lrow] = m;  // (both groups write the same)
       s_l[par][grp][lrow] = mu == m ? l : l * ex2_approx(mu - m);
       const float unit = power_of_two(s_ref[(j1 - 1) % kScaleSlots] - 127 - kHeadroom);
+      if (!ok && lane == 0) give_up();
       ok = !any_of<2, kSoftmaxThreads>(!ok);  // (after a wait that gave up they leave together)
       if (!ok) break;
       // A thread writes its own row's columns, or, of rows in copies, parts of row r:
       // the copies' sums, with weights that bring them to one maximum.
       const int tg = tid & 127, r = copies == 1 ? row : tg / copies;
       float M = -INFINITY, lt = 0.f;
+#pragma unroll 1
       for (int c = r; c < kRows; c += span) M = fmaxf(M, s_m[par][c]);
       auto weight = [&](float mc, float Mc) { return mc == Mc ? 1.f : ex2_approx(mc - Mc); };
+#pragma unroll 1
       for (int c = r; c < kRows; c += span) lt += (s_l[par][0][c] + s_l[par][1][c]) * weight(s_m[par][c], M);
       float mine = unit;
       if (copies > 1) {
         float Mr = -INFINITY;
+#pragma unroll 1
         for (int c = row; c < kRows; c += span) Mr = fmaxf(Mr, s_m[par][c]);
         mine *= weight(m, Mr);
       }
@@ -1099,9 +1138,20 @@ __global__ void __launch_bounds__(kThreads, 1)
                              __uint_as_float(o[c + 3]) * mine);
         };
         if (copies == 1) {
-          if (there) {
+          if (there && whole) {
+            uint4* dst = reinterpret_cast<uint4*>(out + c0);
 #pragma unroll
-            for (int c = 0; c < 32; c += 4) put4(c0 + c, four(c));
+            for (int c = 0; c < 32; c += 8) {
+              uint32_t y[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                y[e] = pack_bf16x2(__uint_as_float(o[c + 2 * e]) * mine, __uint_as_float(o[c + 2 * e + 1]) * mine);
+              dst[c / 8] = make_uint4(y[0], y[1], y[2], y[3]);
+            }
+          } else if (there) {
+            float4* dst = part + c0 / 4 * p.slot_rows;
+#pragma unroll
+            for (int c = 0; c < 8; ++c) dst[c * p.slot_rows] = four(4 * c);
           }
           continue;
         }
@@ -1112,8 +1162,10 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int c = 0; c < 8; ++c) buf[lrow * 8 + (c ^ (lrow & 7))] = four(4 * c);
         group_sync(grp);
+#pragma unroll 1
         for (int c = tg & (copies - 1); there && c < 8; c += copies) {
           float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
           for (int x = r; x < kRows; x += span) {
             const float4 y = buf[x * 8 + (c ^ (x & 7))];
             v.x += y.x;
@@ -1137,6 +1189,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       // (The slots of an item's last two chunks, of its tree's two at most, are in
       // use until the next items' S products are read.)
       bool odd = false;
+#pragma unroll 1
       for (int k = max(w.k0, w.t.prefix); k < w.k1; ++k) odd |= s_odd[(j1 - static_cast<uint32_t>(w.k1 - k)) % kScaleSlots] != 0;
       if (odd) {
         group_sync(grp);  // the rows are written
@@ -1163,9 +1216,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           auto slot_of = [&](int c) -> int64_t { return c == first ? slot0 : 2 * c; };
           if (jr < rows) {
             float Mj = -INFINITY, lj = 0.f;
-#pragma unroll 4
+#pragma unroll 2
             for (int c = first; c <= last; ++c) Mj = fmaxf(Mj, __ldcg(&p.part_ml[slot_of(c) * p.slot_rows + jr]).x);
-#pragma unroll 4
+#pragma unroll 2
             for (int c = first; c <= last; ++c) {
               const float2 ml = __ldcg(&p.part_ml[slot_of(c) * p.slot_rows + jr]);
               lj += ml.y * weight(ml.x, Mj);
