@@ -258,6 +258,72 @@ def test_equal_calls_give_equal_bits_and_one_workspace_serves_any_shape():
     assert B.adt_get_device_error() == 0
 
 
+@pytest.mark.parametrize("H,Hkv,D", [(8, 8, 64), (8, 2, 128)])
+def test_many_items_of_one_chunk(H, Hkv, D):
+    """Trees without a prefix, or with next to none: a thread block has many items, each one or two chunks."""
+    case = Case([1, 2, 1, 5] * 18, [0, 3, 0, 130] * 18, H, Hkv, D)
+    g = case.dev()
+    ws = case.call(g)
+    case.check(g)
+    first = g["out"].clone()
+    for _ in range(5):
+        case.call(g, ws=ws)
+        assert torch.equal(first, g["out"])
+    assert B.adt_get_device_error() == 0
+
+
+@pytest.mark.parametrize("sizes,kv,H,Hkv,D", [([64, 27, 64, 64], [1300, 900, 1444, 1352], 32, 32, 128),
+                                              ([64, 64, 5], [2001, 777, 1500], 32, 8, 128), ([1] * 9, [3000, 1, 900, 128, 5000, 0, 64, 700, 2049], 16, 4, 64)])
+def test_calls_whose_inputs_come_from_memory(sizes, kv, H, Hkv, D):
+    """The roles of a thread block at other speeds: every call after writes larger than L2, all with equal bits."""
+    case = Case(sizes, kv, H, Hkv, D, max_depth=12)
+    g = case.dev()
+    other = torch.empty(400 << 20, dtype=torch.uint8, device="cuda")
+    ws = case.call(g)
+    first, lse = g["out"].clone(), g["lse"].clone()
+    for i in range(25):
+        other.fill_(i)
+        g["out"].zero_()
+        case.call(g, ws=ws)
+        assert torch.equal(first, g["out"]) and torch.equal(lse, g["lse"]), i
+    assert B.adt_get_device_error() == 0
+    case.check(g)
+
+
+def test_waits_that_run_out_end_the_call_with_an_error():
+    case = Case([64, 9], [900, 300], 8, 4, 128)
+    g = case.dev()
+    ws = case.call(g)
+    case.check(g)
+    B.adt_testing_set_wait_limit(1)
+    try:
+        case.call(g, ws=ws)
+        torch.cuda.synchronize()
+        assert B.adt_get_device_error() & B.DEVERR_TIMEOUT
+    finally:
+        B.adt_testing_set_wait_limit(0)
+    ws.zero_()
+    case.call(g, ws=ws)
+    case.check(g)
+    assert B.adt_get_device_error() == 0
+
+
+@pytest.mark.parametrize("H,Hkv,D", [(4, 2, 64), (4, 4, 128), (128, 1, 64)])
+def test_cached_bytes_that_are_not_numbers(H, Hkv, D):
+    case = Case([3, 1], [200, 77], H, Hkv, D)
+    g = case.dev()
+    case.call(g)
+    clean = g["out"].clone()
+    g["vc"].view(torch.uint8)[0, Hkv - 1, 150, 9] = 0xFF  # a column of the last kv head's heads, tree 0
+    g["kc"].view(torch.uint8)[1, 0, 60, 5] = 0x7F        # all of the first kv head's, tree 1
+    case.call(g)
+    want = torch.zeros_like(clean, dtype=torch.bool)
+    group = H // Hkv
+    want[:3, H - group:, 9] = True
+    want[3, :group] = True
+    assert torch.equal(torch.isnan(g["out"]), want) and torch.equal(g["out"][~want], clean[~want])
+
+
 def test_another_stream_and_two_graphs_with_one_workspace():
     a, b = Case([1, 1], [3000, 700], 8, 2, 128), Case([64, 64], [300, 129], 8, 8, 64)
     ws = B.zeroed_workspace(max(B.adt_tree_attn_q8_workspace_size(**c.shape(max_kv=c.rows)) for c in (a, b)))
