@@ -196,6 +196,73 @@ __device__ __noinline__ Walk next_item(const AttnParams& p, Walk w) {
   return w;
 }
 
+// This CTA's share, by one warp: its first item, the coordinates of all items and
+// the number of shares.
+__device__ __forceinline__ void find_share(const AttnParams& p, int lane, Walk* walk, int64_t* all, int* count, unsigned* err) {
+  unsigned bits = 0u;
+  Tree t{};
+  int64_t mine = 0;
+  int items = 0, longest = 0;
+  for (int b = lane; b < p.B; b += 32) {
+    t = tree_of(p, b, &bits);
+    if (!t.chunks) continue;
+    items += t.blocks * p.Hkv;  // (at most 2^24 rows: no more items)
+    longest = max(longest, t.chunks);
+    mine += static_cast<int64_t>(t.chunks + kItemCost) * t.blocks * p.Hkv;
+  }
+  if (err && bits) adt::raise_error(err, bits);
+  int64_t total = adt::warp_sum(mine);
+  items = adt::warp_sum(items);
+  longest = __reduce_max_sync(adt::kFullMask, longest);
+  int64_t shares = total / kMinShare;
+  shares = shares < 1 ? 1 : shares > gridDim.x ? gridDim.x : shares;
+  int padded = 0;
+  if (items > 0 && items <= static_cast<int>(gridDim.x) && longest + kItemCost <= total / gridDim.x + kJoinCost) {
+    padded = longest + kItemCost;
+    shares = items;
+    total = static_cast<int64_t>(items) * padded;
+  }
+  auto width = [&](const Tree& t) -> int { return padded ? padded : t.chunks + kItemCost; };
+  auto cost = [&](const Tree& t) -> int64_t { return t.chunks ? static_cast<int64_t>(width(t)) * t.blocks * p.Hkv : 0; };
+  const int64_t c = blockIdx.x;
+  const int64_t x0 = c < shares ? c * total / shares : total, x1 = c < shares ? (c + 1) * total / shares : total;
+  Walk w{};
+  w.first = w.more = true;
+  int64_t before = 0;
+  for (int b0 = 0; x0 < x1 && b0 < p.B; b0 += 32) {
+    if (p.B > 32) t = b0 + lane < p.B ? tree_of(p, b0 + lane, &bits) : Tree{};
+    const int64_t mine_here = b0 + lane < p.B ? cost(t) : 0;
+    int64_t upto = mine_here;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t y = __shfl_up_sync(adt::kFullMask, upto, o);
+      if (lane >= o) upto += y;
+    }
+    const unsigned hit = __ballot_sync(adt::kFullMask, before + upto > x0);
+    if (hit) {
+      if (lane == __ffs(hit) - 1) {
+        const int64_t off = x0 - (before + upto - mine_here), each = width(t), item = off / each;
+        w.b = b0 + lane;
+        w.g = static_cast<int>(item / t.blocks);
+        w.blk = static_cast<int>(item % t.blocks);
+        w.t = t;
+        w.start = x0 - off + item * each;
+        w.end = x1;
+        w.padded = padded;
+        w.clip(x0);
+        *walk = w;
+      }
+      break;
+    }
+    before += __shfl_sync(adt::kFullMask, upto, 31);
+  }
+  if (lane == 0) {
+    if (x0 >= x1) *walk = w;  // (no chunks)
+    *all = total;
+    *count = static_cast<int>(shares);
+  }
+}
+
 // The tree's values that are not finite were left out of the products: adds those
 // that node t sees, of nodes t0 up to before t1, to `cols` columns of its row, as
 // written (final or partial).  tree: the first node's values at the first column.
@@ -273,10 +340,11 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
 }
 
 // 16 elements of a bf16 row, D / 16 neighbouring lanes to a row (all lanes of the
-// warp take part): cut into two e4m3 rows, high and low, whose sum goes with the
-// scale 2^(s - 127), s what it returns.  A row that is not finite becomes NaN.
-template <int D>
-__device__ __forceinline__ uint32_t cut_row(const uint4 (&x)[2], uint4& high, uint4& low) {
+// warp take part): cut into e4m3 rows, each of kUp times what the ones before leave,
+// whose sum (a row kUp times smaller than the one before) goes with the scale
+// 2^(s - 127), s what it returns.  A row that is not finite becomes NaN.
+template <int D, int kUp, int kParts>
+__device__ __forceinline__ uint32_t cut_row(const uint4 (&x)[2], uint4 (&parts)[kParts]) {
   const uint32_t w[8] = {x[0].x, x[0].y, x[0].z, x[0].w, x[1].x, x[1].y, x[1].z, x[1].w};
   uint32_t most = 0u;
 #pragma unroll
@@ -286,23 +354,30 @@ __device__ __forceinline__ uint32_t cut_row(const uint4 (&x)[2], uint4& high, ui
   const bool finite = most < 0x7f800000u;
   const uint32_t s = finite ? adt::q8_row_scale(__uint_as_float(most)) : 127u;
   const float inv = __uint_as_float((254u - s) << 23);
-  uint32_t h[4], l[4];
+  uint32_t y[kParts][4];
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    h[k] = l[k] = 0u;
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) y[i][k] = 0u;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       const uint32_t z = w[2 * k + e];
-      const float a = __uint_as_float(z << 16) * inv, b = __uint_as_float(z & 0xffff0000u) * inv;
-      const uint32_t two = adt::f32x2_to_e4m3(a, b);
-      const float2 back = adt::e4m3x2_to_f32(two);
-      h[k] |= two << (16 * e);
-      l[k] |= adt::f32x2_to_e4m3(a - back.x, b - back.y) << (16 * e);
+      float a = __uint_as_float(z << 16) * inv, b = __uint_as_float(z & 0xffff0000u) * inv;
+#pragma unroll
+      for (int i = 0; i < kParts; ++i) {
+        const uint32_t two = adt::f32x2_to_e4m3(a, b);
+        const float2 back = adt::e4m3x2_to_f32(two);
+        y[i][k] |= two << (16 * e);
+        a = (a - back.x) * kUp;
+        b = (b - back.y) * kUp;
+      }
     }
-    if (!finite) h[k] = l[k] = 0x7f7f7f7fu;
+#pragma unroll
+    for (int i = 0; i < kParts; ++i)
+      if (!finite) y[i][k] = 0x7f7f7f7fu;
   }
-  high = make_uint4(h[0], h[1], h[2], h[3]);
-  low = make_uint4(l[0], l[1], l[2], l[3]);
+#pragma unroll
+  for (int i = 0; i < kParts; ++i) parts[i] = make_uint4(y[i][0], y[i][1], y[i][2], y[i][3]);
   return s;
 }
 
@@ -333,6 +408,10 @@ constexpr int kHeadroom = 4, kSlack = 3;
 __device__ __forceinline__ float value_factor(int s, int ref) {
   const int e = max(s - ref + kHeadroom + 127, 0);
   return __uint_as_float(s == 255 ? 0x7fc00000u : static_cast<uint32_t>(e) << 23);
+}
+// A query row's cut scale times softmax_scale log2 e; never 0, which would make NaN of the -inf of a masked key.
+__device__ __forceinline__ float row_factor(uint32_t s, float scale_log2) {
+  return fmaxf(__uint_as_float(s << 23) * scale_log2, 1e-38f);
 }
 __device__ __forceinline__ float power_of_two(int e) {
   return e < -126 ? 0.f : __uint_as_float(static_cast<uint32_t>(min(e, 127) + 127) << 23);
@@ -400,16 +479,16 @@ __global__ void __launch_bounds__(kPrepThreads) prepare_kernel(const AttnParams 
     v[0] = src[0];
     v[1] = src[1];
   }
-  uint4 high, low;
-  const uint32_t s = cut_row<D>(x, high, low);
+  uint4 cut[2];
+  const uint32_t s = cut_row<D, 1>(x, cut);
   const int64_t bg = static_cast<int64_t>(b) * p.Hkv + g;
   if (is_q) {
     const int row = node * p.group + h - g * p.group, blk = row / kRows, r = row % kRows;
     const int64_t at = bg * w.blocks + blk;
     uint8_t* dst = w.q + at * 2 * w.q_rows * D + tile_off<D>(r, cl);
-    *reinterpret_cast<uint4*>(dst) = high;
-    *reinterpret_cast<uint4*>(dst + w.q_rows * D) = low;
-    if (cl == 0) w.q_scale[at * w.q_rows + r] = __uint_as_float(s << 23) * p.scale_log2;
+    *reinterpret_cast<uint4*>(dst) = cut[0];
+    *reinterpret_cast<uint4*>(dst + w.q_rows * D) = cut[1];
+    if (cl == 0) w.q_scale[at * w.q_rows + r] = row_factor(s, p.scale_log2);
   }
   // Values: those that are not finite as zeros (a weight of 0 times them would
   // reach rows that do not see them), scaled as their cached rows would be, but in
@@ -437,8 +516,8 @@ __global__ void __launch_bounds__(kPrepThreads) prepare_kernel(const AttnParams 
   const int r = node % kChunk;
   const int64_t at = bg * w.chunks + node / kChunk;
   uint8_t* dst = w.k + at * 2 * w.t_rows * D + tile_off<D>(r, cl);
-  *reinterpret_cast<uint4*>(dst) = high;
-  *reinterpret_cast<uint4*>(dst + w.t_rows * D) = low;
+  *reinterpret_cast<uint4*>(dst) = cut[0];
+  *reinterpret_cast<uint4*>(dst + w.t_rows * D) = cut[1];
   uint8_t* wide = reinterpret_cast<uint8_t*>(w.v + at * (D / 64) * w.t_rows * 8);
   *reinterpret_cast<uint4*>(wide + sw128_off(r, 2 * cl, w.t_rows)) = make_uint4(y[0], y[1], y[2], y[3]);
   *reinterpret_cast<uint4*>(wide + sw128_off(r, 2 * cl + 1, w.t_rows)) = make_uint4(y[4], y[5], y[6], y[7]);
@@ -500,70 +579,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
   if (warp == kKWarp && lane == 0) sm100::prefetch_tensormap(&tm_k);
   asm volatile("griddepcontrol.wait;\n" ::: "memory");
-  if (warp == 0) {
-    // This CTA's share.
-    unsigned bits = 0u;
-    Tree t{};
-    int64_t mine = 0;
-    int items = 0, longest = 0;
-    for (int b = lane; b < p.B; b += 32) {
-      t = tree_of(p, b, &bits);
-      if (!t.chunks) continue;
-      items += t.blocks * p.Hkv;  // (at most 2^24 rows: no more items)
-      longest = max(longest, t.chunks);
-      mine += static_cast<int64_t>(t.chunks + kItemCost) * t.blocks * p.Hkv;
-    }
-    int64_t total = adt::warp_sum(mine);
-    items = adt::warp_sum(items);
-    longest = __reduce_max_sync(adt::kFullMask, longest);
-    int64_t shares = total / kMinShare;
-    shares = shares < 1 ? 1 : shares > gridDim.x ? gridDim.x : shares;
-    int padded = 0;
-    if (items > 0 && items <= static_cast<int>(gridDim.x) && longest + kItemCost <= total / gridDim.x + kJoinCost) {
-      padded = longest + kItemCost;
-      shares = items;
-      total = static_cast<int64_t>(items) * padded;
-    }
-    auto width = [&](const Tree& t) -> int { return padded ? padded : t.chunks + kItemCost; };
-    auto cost = [&](const Tree& t) -> int64_t { return t.chunks ? static_cast<int64_t>(width(t)) * t.blocks * p.Hkv : 0; };
-    const int64_t c = blockIdx.x;
-    const int64_t x0 = c < shares ? c * total / shares : total, x1 = c < shares ? (c + 1) * total / shares : total;
-    Walk w{};
-    w.first = w.more = true;
-    int64_t before = 0;
-    for (int b0 = 0; x0 < x1 && b0 < p.B; b0 += 32) {
-      if (p.B > 32) t = b0 + lane < p.B ? tree_of(p, b0 + lane, &bits) : Tree{};
-      const int64_t mine_here = b0 + lane < p.B ? cost(t) : 0;
-      int64_t upto = mine_here;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int64_t y = __shfl_up_sync(adt::kFullMask, upto, o);
-        if (lane >= o) upto += y;
-      }
-      const unsigned hit = __ballot_sync(adt::kFullMask, before + upto > x0);
-      if (hit) {
-        if (lane == __ffs(hit) - 1) {
-          const int64_t off = x0 - (before + upto - mine_here), each = width(t), item = off / each;
-          w.b = b0 + lane;
-          w.g = static_cast<int>(item / t.blocks);
-          w.blk = static_cast<int>(item % t.blocks);
-          w.t = t;
-          w.start = x0 - off + item * each;
-          w.end = x1;
-          w.padded = padded;
-          w.clip(x0);
-          s_walk = w;
-        }
-        break;
-      }
-      before += __shfl_sync(adt::kFullMask, upto, 31);
-    }
-    if (lane == 0) {
-      if (x0 >= x1) s_walk = w;  // (no chunks)
-      s_total = total;
-      s_grid = static_cast<int>(shares);
-    }
-  }
+  if (warp == 0) find_share(p, lane, &s_walk, &s_total, &s_grid, nullptr);
   sm100::tc_fence_before();
   __syncthreads();
   sm100::tc_fence_after();
@@ -1278,6 +1294,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp == kPvWarp) sm100::tmem_dealloc(tmem, kTmemCols);
 }
 
+#include "tree_attn_q8_few.cuh"
+
 // ---------------------------------------------------------------- host side
 
 // 4-D map of the K cache (d, pos, kv head, tree), boxes of 128 positions.
@@ -1349,12 +1367,13 @@ int grid_for(int sm_count, int B, int H, int Hkv, int max_nodes, int max_kv) {
 }
 
 template <int D>
-adt_status launch(const AttnParams& p, const CUtensorMap& tm, int grid, int dev, cudaStream_t st) {
+adt_status launch(const AttnParams& p, const CUtensorMap& tm, const CUtensorMap& tm_v, int grid, int dev, cudaStream_t st) {
   static unsigned configured[2] = {0u, 0u};  // bit per device (< 64), per instantiation
   const unsigned bit = 1u << (dev & 31);
   unsigned& word = configured[(dev >> 5) & 1];
   if (!(__atomic_load_n(&word, __ATOMIC_ACQUIRE) & bit)) {
     ADT_CUDA_TRY(cudaFuncSetAttribute(tree_attn_q8_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D>::kDynSmem));
+    ADT_CUDA_TRY(cudaFuncSetAttribute(tree_attn_q8_few_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewCfg<D>::kDynSmem));
     __atomic_fetch_or(&word, bit, __ATOMIC_ACQ_REL);
   }
   cudaLaunchConfig_t cfg = {};
@@ -1362,6 +1381,13 @@ adt_status launch(const AttnParams& p, const CUtensorMap& tm, int grid, int dev,
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   cfg.stream = st;
+  if (p.max_nodes * p.group <= kFewRows) {
+    cfg.gridDim = dim3(static_cast<unsigned>(grid), 1, 1);
+    cfg.blockDim = dim3(kThreads, 1, 1);
+    cfg.dynamicSmemBytes = FewCfg<D>::kDynSmem;
+    ADT_CUDA_TRY(cudaLaunchKernelEx(&cfg, tree_attn_q8_few_kernel<D>, tm, tm_v, p));
+    return adt::launch_status();
+  }
   constexpr int kPass = kPrepThreads / (D / 16);
   const int64_t units = static_cast<int64_t>(p.max_nodes) * p.H + ((p.max_nodes + 15) & ~15) * static_cast<int64_t>(p.Hkv);
   cfg.gridDim = dim3(static_cast<unsigned>((units + kPass - 1) / kPass), static_cast<unsigned>(p.B), 1);
@@ -1437,11 +1463,12 @@ adt_status adt_tree_attn_q8(const adt_bf16* q, const uint8_t* k_cache, const uin
   p.lse = lse;
   p.err = info.error_word;
   p.wait_limit = adt::wait_limit(kWaitLimit);
-  CUtensorMap tm;
+  CUtensorMap tm, tm_v;
   st = make_cache_map(&tm, k_cache, D, max_kv, Hkv, B, cache_stride_h, cache_stride_b);
+  if (st == ADT_OK) st = make_cache_map(&tm_v, v_cache, D, max_kv, Hkv, B, cache_stride_h, cache_stride_b);
   if (st != ADT_OK) return st;
-  return D == 128 ? launch<128>(p, tm, grid, info.device, adt::as_stream(stream))
-                  : launch<64>(p, tm, grid, info.device, adt::as_stream(stream));
+  return D == 128 ? launch<128>(p, tm, tm_v, grid, info.device, adt::as_stream(stream))
+                  : launch<64>(p, tm, tm_v, grid, info.device, adt::as_stream(stream));
 }
 
 }  // extern "C"
