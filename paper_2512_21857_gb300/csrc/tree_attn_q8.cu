@@ -340,11 +340,11 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
 }
 
 // 16 elements of a bf16 row, D / 16 neighbouring lanes to a row (all lanes of the
-// warp take part): cut into e4m3 rows, each of kUp times what the ones before leave,
-// whose sum (a row kUp times smaller than the one before) goes with the scale
+// warp take part): cut into e4m3 rows, each of `up` times what the ones before leave,
+// whose sum (a row `up` times smaller than the one before) goes with the scale
 // 2^(s - 127), s what it returns.  A row that is not finite becomes NaN.
-template <int D, int kUp, int kParts>
-__device__ __forceinline__ uint32_t cut_row(const uint4 (&x)[2], uint4 (&parts)[kParts]) {
+template <int D, int kParts>
+__device__ __forceinline__ uint32_t cut_row(const uint4 (&x)[2], float up, uint4 (&parts)[kParts]) {
   const uint32_t w[8] = {x[0].x, x[0].y, x[0].z, x[0].w, x[1].x, x[1].y, x[1].z, x[1].w};
   uint32_t most = 0u;
 #pragma unroll
@@ -368,8 +368,8 @@ __device__ __forceinline__ uint32_t cut_row(const uint4 (&x)[2], uint4 (&parts)[
         const uint32_t two = adt::f32x2_to_e4m3(a, b);
         const float2 back = adt::e4m3x2_to_f32(two);
         y[i][k] |= two << (16 * e);
-        a = (a - back.x) * kUp;
-        b = (b - back.y) * kUp;
+        a = (a - back.x) * up;
+        b = (b - back.y) * up;
       }
     }
 #pragma unroll
@@ -480,7 +480,7 @@ __global__ void __launch_bounds__(kPrepThreads) prepare_kernel(const AttnParams 
     v[1] = src[1];
   }
   uint4 cut[2];
-  const uint32_t s = cut_row<D, 1>(x, cut);
+  const uint32_t s = cut_row<D>(x, 1.f, cut);
   const int64_t bg = static_cast<int64_t>(b) * p.Hkv + g;
   if (is_q) {
     const int row = node * p.group + h - g * p.group, blk = row / kRows, r = row % kRows;
@@ -1373,7 +1373,8 @@ adt_status launch(const AttnParams& p, const CUtensorMap& tm, const CUtensorMap&
   unsigned& word = configured[(dev >> 5) & 1];
   if (!(__atomic_load_n(&word, __ATOMIC_ACQUIRE) & bit)) {
     ADT_CUDA_TRY(cudaFuncSetAttribute(tree_attn_q8_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D>::kDynSmem));
-    ADT_CUDA_TRY(cudaFuncSetAttribute(tree_attn_q8_few_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewCfg<D>::kDynSmem));
+    ADT_CUDA_TRY(cudaFuncSetAttribute(tree_attn_q8_few_kernel<D, 16>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewCfg<D, 16>::kDynSmem));
+    ADT_CUDA_TRY(cudaFuncSetAttribute(tree_attn_q8_few_kernel<D, 32>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewCfg<D, 32>::kDynSmem));
     __atomic_fetch_or(&word, bit, __ATOMIC_ACQ_REL);
   }
   cudaLaunchConfig_t cfg = {};
@@ -1381,13 +1382,15 @@ adt_status launch(const AttnParams& p, const CUtensorMap& tm, const CUtensorMap&
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   cfg.stream = st;
-  if (p.max_nodes * p.group <= kFewRows) {
+  auto few = [&](auto kernel, int bytes) -> adt_status {
     cfg.gridDim = dim3(static_cast<unsigned>(grid), 1, 1);
     cfg.blockDim = dim3(kThreads, 1, 1);
-    cfg.dynamicSmemBytes = FewCfg<D>::kDynSmem;
-    ADT_CUDA_TRY(cudaLaunchKernelEx(&cfg, tree_attn_q8_few_kernel<D>, tm, tm_v, p));
+    cfg.dynamicSmemBytes = static_cast<size_t>(bytes);
+    ADT_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, tm, tm_v, p));
     return adt::launch_status();
-  }
+  };
+  if (p.max_nodes * p.group <= 16) return few(tree_attn_q8_few_kernel<D, 16>, FewCfg<D, 16>::kDynSmem);
+  if (p.max_nodes * p.group <= 32) return few(tree_attn_q8_few_kernel<D, 32>, FewCfg<D, 32>::kDynSmem);
   constexpr int kPass = kPrepThreads / (D / 16);
   const int64_t units = static_cast<int64_t>(p.max_nodes) * p.H + ((p.max_nodes + 15) & ~15) * static_cast<int64_t>(p.Hkv);
   cfg.gridDim = dim3(static_cast<unsigned>((units + kPass - 1) / kPass), static_cast<unsigned>(p.B), 1);

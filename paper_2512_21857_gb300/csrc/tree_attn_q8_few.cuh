@@ -25,31 +25,38 @@
 // whose sums are to 2^-8 of each element, into three 2^-4 apart.
 
 constexpr int kFewRows = 32;
-constexpr float kFewThreshold = 3.f, kFewHeadroom = 4.f;  // weights up to 2^7: e4m3 ends at 448
+constexpr float kFewThreshold = 4.5f, kFewHeadroom = 4.f;  // weights up to 2^8.5: e4m3 ends at 448
 constexpr float kUnset = -3e38f;  // the base of a row that has seen no key
 constexpr int kNoScale = -1000;   // (scales are 2^-127 and more)
 constexpr int kLeastScale = -127;
 
-template <int D>
+// R: 16 or 32, the most rows of an item.
+template <int D, int R>
 struct FewCfg {
   static constexpr int kStages = D == 128 ? 4 : 8;
   static constexpr int kTile = kChunk * D;
-  static constexpr int kSmall = kFewRows * D;           // 32 rows of e4m3
+  static constexpr int kQ = R * D;                      // queries, high or low part
+  static constexpr int kSmall = kFewRows * D;           // a tree's keys or values, a part
   static constexpr int kQOff = 0;                       // [2 items][high, low]
-  static constexpr int kTreeOff = kQOff + 4 * kSmall;   // [2 items][K high, K low, V in three]
+  static constexpr int kTreeOff = kQOff + 4 * kQ;       // [2 items][K high, K low, V in three]
   static constexpr int kTreeBytes = 5 * kSmall;
-  static constexpr int kPOff = kTreeOff + 2 * kTreeBytes;  // [2 groups][128 keys][p1, p2, p3, unused: 32 rows each]
-  static constexpr int kPBytes = kChunk * 128;
-  static constexpr int kKOff = kPOff + 2 * kPBytes;
+  // Weights [128 keys][p1, p2, p3, unused: R each], the swizzle as wide as a row.
+  // Where they fit, two tiles a group: PV(j) is done 2000 cycles after P(j) is written.
+  static constexpr int kPTiles = R == 16 ? 4 : 2;
+  static constexpr int kPBytes = kChunk * 4 * R;
+  static constexpr int kPOff = kTreeOff + 2 * kTreeBytes;
+  static constexpr int kKOff = kPOff + kPTiles * kPBytes;
   static constexpr int kVOff = kKOff + kStages * kTile;
   static constexpr int kDynSmem = kVOff + kStages * kTile + 1024;  // + alignment slack
-  static constexpr uint32_t kIdescO = sm100::idesc_e4m3_f32(D, 3 * kFewRows) | 1u << 15 | 1u << 16;  // both MN-major
+  static constexpr uint32_t kIdescO = sm100::idesc_e4m3_f32(D, 3 * R) | 1u << 15 | 1u << 16;  // both MN-major
+  static constexpr uint32_t kOAt = 4 * R, kLAt = 7 * R;  // after four S tiles of R columns: O, 3 R; then two row sums of R
+  static constexpr uint32_t kCols = R == 16 ? 256 : 512;
 };
 
 struct FewBars {
   uint64_t k_full[8], k_free[8], v_full[8], v_free[8], v_tail;
   uint64_t prep_full[2], prep_free[2];
-  uint64_t s_full[2], s_free[2], p_full[2], mu[2], done[4];
+  uint64_t s_full[4], s_free[4], p_full[4], done[4], mu[2];
   uint64_t o_free, drain[2];
 };
 
@@ -81,26 +88,33 @@ __device__ __forceinline__ float transposed_sum(float (&v)[16], int lane) {
   return v[0] + __shfl_xor_sync(adt::kFullMask, v[0], 1);
 }
 
-template <int D>
+// The largest of a warp's values; NaN counts as none.
+__device__ __forceinline__ float warp_most(float v) {
+  float r;
+  asm("redux.sync.max.f32 %0, %1, 0xffffffff;\n" : "=f"(r) : "f"(v));
+  return r;
+}
+
+template <int D, int R>
 __global__ void __launch_bounds__(kThreads, 1)
     tree_attn_q8_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                             const __grid_constant__ AttnParams p) {
-  using C = FewCfg<D>;
-  constexpr int NS = C::kStages;
+  using C = FewCfg<D, R>;
+  constexpr int NS = C::kStages, PT = C::kPTiles;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (sm100::smem_addr(smem_raw) & 1023u)) & 1023u);
   __shared__ FewBars bars;
   // Of an item's rows (and its tree's keys), by item: four, so that none is written
   // while the item before the last may still be read.
-  __shared__ __align__(16) float s_c[4][kFewRows], s_base[4][kFewRows];
-  __shared__ float s_tk[4][kFewRows];
-  __shared__ int s_tv[4][kFewRows], s_top[4], s_ver[4], s_odd[4];
-  __shared__ uint32_t s_seen[4][kFewRows];             // of a key: the rows that see it
-  __shared__ __align__(16) float s_gb[2][kFewRows], s_alpha[2][kFewRows];  // of a group: the base its row sums are at
-  __shared__ uint32_t s_most[2][4][kFewRows];
+  __shared__ __align__(16) float s_c[4][R], s_base[4][R];
+  __shared__ float s_tk[4][R];
+  __shared__ int s_tv[4][R], s_top[4], s_ver[4], s_odd[4];
+  __shared__ uint32_t s_seen[4][R];                    // of a key: the rows that see it
+  __shared__ __align__(16) float s_gb[2][R], s_alpha[2][R];  // of a group: the base its row sums are at
+  __shared__ float s_most[2][4][R];
   __shared__ int s_wtop[2][4];
-  __shared__ float s_sum[2][8][kFewRows];
-  __shared__ int16_t s_par[kFewRows];
+  __shared__ float s_sum[2][8][R];
+  __shared__ int16_t s_par[R];
   __shared__ Walk s_walk;
   __shared__ int64_t s_total;
   __shared__ int s_grid, s_last;
@@ -120,23 +134,23 @@ __global__ void __launch_bounds__(kThreads, 1)
     init(&bars.v_tail, 1, 1);
     init(bars.prep_full, 2, 4);
     init(bars.prep_free, 2, 1);
-    init(bars.s_full, 2, 1);
-    init(bars.s_free, 2, 4);
-    init(bars.p_full, 2, 4);
+    init(bars.s_full, 4, 1);
+    init(bars.s_free, 4, 4);
+    init(bars.p_full, 4, 4);
     init(bars.mu, 2, 1);
     init(bars.done, 4, 1);
     init(&bars.o_free, 1, 8);
     init(bars.drain, 2, 1);
     sm100::fence_mbar_init();
   }
-  if (tid < 4 * kFewRows) s_base[tid / kFewRows][tid % kFewRows] = kUnset;
+  if (tid < 4 * R) s_base[tid / R][tid % R] = kUnset;
   if (tid < 4) {
     s_top[tid] = kNoScale;
     s_ver[tid] = 0;
     s_odd[tid] = 0;
   }
   if (warp == kPvWarp) {
-    sm100::tmem_alloc(sm100::smem_addr(&tmem_slot), 256);
+    sm100::tmem_alloc(sm100::smem_addr(&tmem_slot), C::kCols);
     sm100::tmem_relinquish();
   }
   if (warp == kKWarp && lane < 2) sm100::prefetch_tensormap(lane ? &tm_v : &tm_k);
@@ -146,11 +160,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   __syncthreads();
   sm100::tc_fence_after();
   const uint32_t tmem = tmem_slot;
-  constexpr uint32_t kOAt = 64, kLAt = 160;  // after two S tiles of 32 columns: O, 96; then two row sums of 32
   Walk w = s_walk;
   if (!w.some()) {
     __syncthreads();
-    if (warp == kPvWarp) sm100::tmem_dealloc(tmem, 256);
+    if (warp == kPvWarp) sm100::tmem_dealloc(tmem, C::kCols);
     return;
   }
   uint8_t* sQ = smem + C::kQOff;
@@ -165,8 +178,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     s_abort = 1;
     adt::raise_error(p.err, ADT_DEVERR_TIMEOUT);
   };
-  // Chunk j (over the whole share) is softmax group j % 2's; of the prefix's chunks, i
-  // in all, tile i has slot i % NS of both rings.  (A wait on a parity is only
+  // Chunk j (over the whole share) is softmax group j % 2's, its scores in S tile j % 4;
+  // of the prefix's chunks, i in all, tile i has slot i % NS of both rings.  (A wait on a parity is only
   // meaningful to a thread that knows the phase before complete.)
   uint32_t j = 0, i = 0, item = 0;
 
@@ -252,12 +265,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint64_t qd0 = tile_desc<D>(sm100::smem_addr(sQ)), kd0 = tile_desc<D>(sm100::smem_addr(sK)),
                      td0 = tile_desc<D>(sm100::smem_addr(sT));
       for (; ok && w.more; w = next_item(p, w), ++item) {
-        const uint32_t idesc = sm100::idesc_e4m3_f32(kChunk, (w.t.n * p.group + 15) & ~15);
+        const uint32_t idesc = sm100::idesc_e4m3_f32(kChunk, R);
         ok = wait(&bars.prep_full[item & 1], item >> 1);
         for (int k = w.k0; ok && k < w.k1; ++k, ++j) {
           const bool tree_k = k >= w.t.prefix;
           const int st = i % NS;
-          ok = (tree_k || wait(&bars.k_full[st], i / NS)) && (j < 2 || wait(&bars.s_free[j & 1], (j >> 1) - 1));
+          ok = (tree_k || wait(&bars.k_full[st], i / NS)) && (j < 4 || wait(&bars.s_free[j & 3], (j >> 2) - 1));
           if (!ok) break;
           sm100::tc_fence_after();
           // The queries' high and low part with the keys, of a tree with their low part too.
@@ -265,15 +278,15 @@ __global__ void __launch_bounds__(kThreads, 1)
           uint32_t more = 0u;
 #pragma unroll 1
           for (int part = 0; part < parts; ++part) {
-            const uint64_t qd = qd0 + ((item & 1) * 2 + (part & 1)) * (C::kSmall / 16);
+            const uint64_t qd = qd0 + ((item & 1) * 2 + (part & 1)) * (C::kQ / 16);
             const uint64_t kd = tree_k ? td0 + ((item & 1) * C::kTreeBytes + (part >> 1) * C::kSmall) / 16 : kd0 + st * (C::kTile / 16);
 #pragma unroll
             for (int kk = 0; kk < D / 32; ++kk) {
-              sm100::mma_f8_ss(tmem + (j & 1) * kFewRows, kd + kk * 2, qd + kk * 2, idesc, more);
+              sm100::mma_f8_ss(tmem + (j & 3) * R, kd + kk * 2, qd + kk * 2, idesc, more);
               more = 1u;
             }
           }
-          sm100::mma_commit(sm100::smem_addr(&bars.s_full[j & 1]));
+          sm100::mma_commit(sm100::smem_addr(&bars.s_full[j & 3]));
           if (!tree_k) {
             sm100::mma_commit(sm100::smem_addr(&bars.k_free[st]));
             ++i;
@@ -291,16 +304,16 @@ __global__ void __launch_bounds__(kThreads, 1)
       bool ok = true;
       // (MN-major: columns of 8 keys 1024 bytes apart, at D = 64 512.)
       const uint64_t vd0 = tile_desc<D>(sm100::smem_addr(sV)), td0 = tile_desc<D>(sm100::smem_addr(sT)),
-                     pd0 = sm100::smem_desc_sw128(sm100::smem_addr(sP), 16, 1024);
+                     pd0 = tile_desc<4 * R>(sm100::smem_addr(sP));
       for (; ok && w.more; w = next_item(p, w), ++item) {
         for (int k = w.k0; ok && k < w.k1; ++k, ++j) {
           const bool tree_k = k >= w.t.prefix;
           const int st = i % NS;
-          ok = wait(&bars.p_full[j & 1], j >> 1) && (tree_k || wait(&bars.v_full[st], i / NS)) &&
+          ok = wait(&bars.p_full[j & 3], j >> 2) && (tree_k || wait(&bars.v_full[st], i / NS)) &&
                (k > w.k0 || item == 0 || wait(&bars.o_free, item - 1));
           if (!ok) break;
           sm100::tc_fence_after();
-          const uint64_t pd = pd0 + (j & 1) * (C::kPBytes / 16);
+          const uint64_t pd = pd0 + (j % PT) * (C::kPBytes / 16);
           const int steps = tree_k ? 3 : min(4, (w.t.L - k * kChunk + 31) / 32);
           uint32_t more = k > w.k0 ? 1u : 0u;
 #pragma unroll 1
@@ -310,8 +323,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             const uint64_t vd = (tree_k ? td0 + ((item & 1) * C::kTreeBytes + (2 + kk) * C::kSmall) / 16
                                         : vd0 + (st * C::kTile + kk * 32 * D) / 16);
             const int part = tree_k ? kk : 0;
-            sm100::mma_f8_ss(tmem + kOAt + part * kFewRows, vd, pd + (kk - part) * (32 * 128 / 16),
-                             C::kIdescO - (static_cast<uint32_t>(part * kFewRows >> 3) << 17), more);
+            sm100::mma_f8_ss(tmem + C::kOAt + part * R, vd, pd + (kk - part) * (32 * 4 * R / 16),
+                             C::kIdescO - (static_cast<uint32_t>(part * R >> 3) << 17), more);
             more = 1u;
           }
           sm100::mma_commit(sm100::smem_addr(&bars.done[j & 3]));
@@ -329,73 +342,95 @@ __global__ void __launch_bounds__(kThreads, 1)
     __syncwarp();
   } else if (warp >= kConvWarp) {
     // ------------------------------------------------------------ queries and trees
+    // A row is D / 16 lanes', 16 elements each: the item's queries, then the tree's keys
+    // and values.  One copy of the code for all, and what there is to read in flight
+    // before: an item's first product waits for this.
     constexpr int kLanes = D / 16, kPass = kConvThreads / kLanes;
     const int ct = tid - kConvWarp * 32, cl = ct % kLanes, cr = ct / kLanes;
     bool ok = true;
     for (; ok && w.more; w = next_item(p, w), ++item) {
       const int at = item & 3, rows = w.t.n * p.group, n = w.t.n;
-      uint8_t* q = sQ + (item & 1) * 2 * C::kSmall;
+      uint8_t* q = sQ + (item & 1) * 2 * C::kQ;
       uint8_t* t = sT + (item & 1) * C::kTreeBytes;
+      const bool tree = w.k1 > w.t.prefix;
+      const int units = tree ? rows + 2 * n : rows;
+      uint4 x[2];
+      int up = -1;
+      auto fetch = [&](int u) {
+        x[0] = x[1] = make_uint4(0u, 0u, 0u, 0u);
+        if (u >= units) return;
+        const __nv_bfloat16* src;
+        if (u < rows) {
+          const int node = u / p.group;
+          src = p.q + (static_cast<int64_t>(w.t.node0 + node) * p.H + w.g * p.group + (u - node * p.group)) * D;
+        } else {
+          const int v = u - rows >= n;
+          src = p.tree[v] + (static_cast<int64_t>(w.t.node0 + u - rows - v * n) * p.Hkv + w.g) * D;
+        }
+        x[0] = reinterpret_cast<const uint4*>(src)[cl * 2];
+        x[1] = reinterpret_cast<const uint4*>(src)[cl * 2 + 1];
+      };
+      fetch(cr);
+      if (tree && ct < n) up = p.parents[w.t.node0 + ct];
       // The item before the last is done with, its products at least.
       ok = item < 2 || wait(&bars.prep_free[item & 1], (item >> 1) - 1);
       if (!ok && lane == 0) give_up();
       ok = !any_of<1, kConvThreads>(!ok);
       if (!ok) break;
-      const bool tree = w.k1 > w.t.prefix;
       if (tree && ct < n) {
-        const int up = p.parents[w.t.node0 + ct];
         s_par[ct] = static_cast<int16_t>(min(max(up, -1), kMaxTreeNodes));
         if ((ct == 0) != (up < 0) || up >= ct) adt::raise_error(p.err, ADT_DEVERR_BAD_TREE);
       }
       if (ct == 0) s_odd[at] = 0;
       any_of<1, kConvThreads>(false);
 #pragma unroll 1
-      for (int r0 = 0; r0 < kFewRows; r0 += kPass) {
-        const int r = r0 + cr;
-        uint4 x[2] = {}, cut[2], vcut[3];
-        if (r < rows) {
-          const int node = r / p.group;
-          const uint4* src = reinterpret_cast<const uint4*>(
-              p.q + (static_cast<int64_t>(w.t.node0 + node) * p.H + w.g * p.group + (r - node * p.group)) * D) + cl * 2;
-          x[0] = src[0];
-          x[1] = src[1];
-        }
-        uint32_t s = cut_row<D, 1>(x, cut);
-        const uint32_t off = tile_off<D>(r, cl);
-        *reinterpret_cast<uint4*>(q + off) = cut[0];
-        *reinterpret_cast<uint4*>(q + C::kSmall + off) = cut[1];
-        if (cl == 0) s_c[at][r] = row_factor(s, p.scale_log2);
-        if (!tree) continue;
-        uint4 v[2] = {};
-        x[0] = x[1] = make_uint4(0u, 0u, 0u, 0u);
-        if (r < n) {
-          const int64_t o = (static_cast<int64_t>(w.t.node0 + r) * p.Hkv + w.g) * D;
-          const uint4* src = reinterpret_cast<const uint4*>(p.tree[0] + o) + cl * 2;
-          x[0] = src[0];
-          x[1] = src[1];
-          src = reinterpret_cast<const uint4*>(p.tree[1] + o) + cl * 2;
-          v[0] = src[0];
-          v[1] = src[1];
-        }
-        s = cut_row<D, 1>(x, cut);
-        *reinterpret_cast<uint4*>(t + off) = cut[0];
-        *reinterpret_cast<uint4*>(t + C::kSmall + off) = cut[1];
-        if (cl == 0) s_tk[at][r] = __uint_as_float(s << 23);
+      for (int u = cr; u - cr < units; u += kPass) {
+        const bool is_q = u < rows, is_v = u >= rows + n;
         // Values that are not finite as zeros: see add_odd.
-        uint32_t* y = reinterpret_cast<uint32_t*>(v);
-        bool odd = false;
+        if (is_v) {
+          uint32_t y[8] = {x[0].x, x[0].y, x[0].z, x[0].w, x[1].x, x[1].y, x[1].z, x[1].w};
+          bool odd = false;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const bool lo = (y[e] & 0x7f80u) == 0x7f80u, hi = (y[e] & 0x7f800000u) == 0x7f800000u;
-          odd |= lo || hi;
-          if (lo) y[e] &= 0xffff0000u;
-          if (hi) y[e] &= 0xffffu;
+          for (int e = 0; e < 8; ++e) {
+            const bool lo = (y[e] & 0x7f80u) == 0x7f80u, hi = (y[e] & 0x7f800000u) == 0x7f800000u;
+            odd |= lo || hi;
+            if (lo) y[e] &= 0xffff0000u;
+            if (hi) y[e] &= 0xffffu;
+          }
+          if (odd) s_odd[at] = 1;
+          x[0] = make_uint4(y[0], y[1], y[2], y[3]);
+          x[1] = make_uint4(y[4], y[5], y[6], y[7]);
         }
-        if (odd) s_odd[at] = 1;
-        s = cut_row<D, 16>(v, vcut);
-#pragma unroll
-        for (int i = 0; i < 3; ++i) *reinterpret_cast<uint4*>(t + (2 + i) * C::kSmall + off) = vcut[i];
-        if (cl == 0) s_tv[at][r] = static_cast<int>(s) - 127;
+        uint4 cut[3];
+        const uint32_t s = cut_row<D>(x, is_v ? 16.f : 1.f, cut);
+        fetch(u + kPass);
+        if (u >= units) continue;
+        const int r = is_q ? u : u - rows - (is_v ? n : 0);
+        uint8_t* dst = (is_q ? q : t + (is_v ? 2 * C::kSmall : 0)) + tile_off<D>(r, cl);
+        const int step = is_q ? C::kQ : C::kSmall;
+        *reinterpret_cast<uint4*>(dst) = cut[0];
+        *reinterpret_cast<uint4*>(dst + step) = cut[1];
+        if (is_v) *reinterpret_cast<uint4*>(dst + 2 * step) = cut[2];
+        if (cl != 0) continue;
+        if (is_q)
+          s_c[at][r] = row_factor(s, p.scale_log2);
+        else if (is_v)
+          s_tv[at][r] = static_cast<int>(s) - 127;
+        else
+          s_tk[at][r] = __uint_as_float(s << 23);
+      }
+      // Zeros: the queries up to R (their scores are read), values up to the 32 that a product reads.
+#pragma unroll 1
+      for (int i = rows * D / 16 + ct; i < R * D / 16; i += kConvThreads) {
+        reinterpret_cast<uint4*>(q)[i] = reinterpret_cast<uint4*>(q + C::kQ)[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (i % (D / 16) == 0) s_c[at][i / (D / 16)] = 1.f;
+      }
+      if (tree) {
+#pragma unroll 1
+        for (int i = n * D / 16 + ct; i < kFewRows * D / 16; i += kConvThreads) {
+          uint4* v = reinterpret_cast<uint4*>(t + 2 * C::kSmall) + i;
+          v[0] = v[C::kSmall / 16] = v[2 * C::kSmall / 16] = make_uint4(0u, 0u, 0u, 0u);
+        }
       }
       if (tree && warp == kConvWarp) {
         // Row by row the keys seen, then key by key the rows that see it.
@@ -409,11 +444,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
         uint32_t mine = 0u;
-        for (int x = 0; x < kFewRows; ++x) {
+#pragma unroll 1
+        for (int x = 0; x < n; ++x) {
           const uint32_t b = __ballot_sync(adt::kFullMask, m >> x & 1u);
           if (x == lane) mine = b;
         }
-        s_seen[at][lane] = mine;
+        if (lane < n) s_seen[at][lane] = mine;
       }
       sm100::fence_proxy_async_smem();
       __syncwarp();
@@ -423,12 +459,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     // ------------------------------------------------------------ softmax
     const int grp = warp >> 2, w4 = warp & 3, key = w4 * 32 + lane;
     const uint32_t lanes = static_cast<uint32_t>(w4 * 32) << 16;
-    const uint32_t s_col = tmem + lanes + grp * kFewRows, o_col = tmem + lanes + kOAt, l_col = tmem + lanes + kLAt + grp * kFewRows;
-    uint8_t* row_p = sP + grp * C::kPBytes + key * 128;
+    const uint32_t o_col = tmem + lanes + C::kOAt, l_col = tmem + lanes + C::kLAt + grp * R;
+    constexpr int kBlocks = R / 16;
     const int gt = tid & 127;
     bool ok = true;
     for (; ok && w.more; w = next_item(p, w), ++item) {
-      const int at = item & 3, rows = w.t.n * p.group, blocks = (rows + 15) / 16;
+      const int at = item & 3, rows = w.t.n * p.group;
       const uint32_t j0 = j, j1 = j + static_cast<uint32_t>(w.k1 - w.k0);
       ok = all_wait(&bars.prep_full[item & 1], item >> 1);
       const int64_t s0 = w.b * p.ssb + w.g * p.ssh + key;
@@ -454,8 +490,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         // The chunk before has settled its bases.  (An item's last chunk is done before
         // the next one's first.)
         // A warp whose wait gave up goes on to where the group leaves together.
-        ok = ok && all_wait(&bars.s_full[grp], j >> 1) && (j == j0 || all_wait(&bars.mu[grp ^ 1], (j - 1) >> 1));
+        ok = ok && all_wait(&bars.s_full[j & 3], j >> 2) && (j == j0 || all_wait(&bars.mu[grp ^ 1], (j - 1) >> 1));
         sm100::tc_fence_after();
+        const uint32_t s_col = tmem + lanes + (j & 3) * R;
         float ks = adt::q8_scale(kbyte);
         int ev = static_cast<int>(vbyte) - 127;
         const bool nan_v = !tree_k && vbyte == 255u;
@@ -482,7 +519,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         float evf = static_cast<float>(max(ev, top - 60));
         float most = -INFINITY;
 #pragma unroll 1
-        for (int blk = 0; blk < blocks; ++blk) {
+        for (int blk = 0; blk < kBlocks; ++blk) {
           float x[16];
           load(blk, x);
           const float4* c4 = reinterpret_cast<const float4*>(s_c[at] + 16 * blk);
@@ -494,7 +531,6 @@ __global__ void __launch_bounds__(kThreads, 1)
             most = fmaxf(most, fmaxf(fmaf(x[4 * e + 2], c.z, -b.z), fmaf(x[4 * e + 3], c.w, -b.w)));
           }
         }
-        // (The rows up to the next 16 are zeros: they may raise bases of their own.)
         const bool more = !ok || most + evf > kFewThreshold, raise = grp == 0 ? any_of<3, 128>(more) : any_of<4, 128>(more);
         if (raise) {
           // The largest scale, then every row's largest exponent over the chunk.
@@ -504,13 +540,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           top = max(max(max(s_wtop[grp][0], s_wtop[grp][1]), max(s_wtop[grp][2], s_wtop[grp][3])), top);
           evf = static_cast<float>(max(ev, top - 60));
 #pragma unroll 1
-          for (int blk = 0; blk < blocks; ++blk) {
+          for (int blk = 0; blk < kBlocks; ++blk) {
             float x[16];
             load(blk, x);
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-              const float y = fmaf(x[e], s_c[at][16 * blk + e], evf);
-              const uint32_t m = __reduce_max_sync(adt::kFullMask, y > -INFINITY ? adt::float_order_key(y) : 0u);
+              const float m = warp_most(fmaf(x[e], s_c[at][16 * blk + e], evf));
               if (lane == 0) s_most[grp][w4][16 * blk + e] = m;
             }
           }
@@ -520,10 +555,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (!ok && lane == 0) give_up();
           ok = !(grp == 0 ? any_of<3, 128>(!ok) : any_of<4, 128>(!ok));
           if (!ok) break;
-          if (gt < 16 * blocks) {
-            const uint32_t m = max(max(s_most[grp][0][gt], s_most[grp][1][gt]), max(s_most[grp][2][gt], s_most[grp][3][gt]));
-            const float old = s_base[at][gt], y = m ? adt::float_from_order_key(m) : kUnset;
-            const float now = y > old + kFewThreshold ? y : old;
+          if (gt < R) {
+            const float y = fmaxf(fmaxf(s_most[grp][0][gt], s_most[grp][1][gt]), fmaxf(s_most[grp][2][gt], s_most[grp][3][gt]));
+            const float old = s_base[at][gt], now = y > old + kFewThreshold ? y : old;
             s_base[at][gt] = now;
             s_alpha[grp][gt] = now == old ? 1.f : ex2_approx(old - now);
           }
@@ -535,13 +569,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (j > j0) {
             sm100::tc_fence_after();
 #pragma unroll 1
-            for (int c = 0; c < 3 * kFewRows; c += 16) {
-              if ((c & (kFewRows - 1)) >= 16 * blocks) continue;
+            for (int c = 0; c < 3 * R; c += 16) {
               uint32_t r[16];
               sm100::tmem_ld_16(o_col + c, r);
 #pragma unroll
               for (int e = 0; e < 16; ++e)
-                r[e] = __float_as_uint(__uint_as_float(r[e]) * s_alpha[grp][(c & (kFewRows - 1)) + e]);
+                r[e] = __float_as_uint(__uint_as_float(r[e]) * s_alpha[grp][(c & (R - 1)) + e]);
               tmem_st_16(o_col + c, r);
             }
             sm100::tmem_wait_st();
@@ -552,7 +585,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         // The row sums of this group come to the bases' new level.
         if (fresh || now != ver) {
 #pragma unroll 1
-          for (int blk = 0; blk < blocks; ++blk) {
+          for (int blk = 0; blk < kBlocks; ++blk) {
             uint32_t r[16];
             sm100::tmem_ld_16(l_col + 16 * blk, r);
 #pragma unroll
@@ -564,17 +597,17 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           sm100::tmem_wait_st();
           group_sync(grp);
-          if (gt < kFewRows) s_gb[grp][gt] = s_base[at][gt] - top;
+          if (gt < R) s_gb[grp][gt] = s_base[at][gt] - top;
           fresh = false;
           ver = now;
         }
-        // P's tile was last read by PV(j - 2).
-        ok = j < 2 || all_wait(&bars.done[(j - 2) & 3], (j - 2) >> 2);
+        // P's tile was last read by PV(j - PT).
+        ok = j < PT || all_wait(&bars.done[(j - PT) & 3], (j - PT) >> 2);
         if (!ok) continue;
         const float iev = power_of_two(top - static_cast<int>(evf)), shift = evf + kFewHeadroom;
         const uint32_t keep = ev < top - 60 ? 0u : ~0u;
 #pragma unroll 1
-        for (int blk = 0; blk < blocks; ++blk) {
+        for (int blk = 0; blk < kBlocks; ++blk) {
           float x[16];
           load(blk, x);
           uint32_t r[16];
@@ -611,18 +644,18 @@ __global__ void __launch_bounds__(kThreads, 1)
             p3[e] &= keep;
           }
           tmem_st_16(l_col + 16 * blk, r);
-          const int sw = key & 7;
-          *reinterpret_cast<uint4*>(row_p + ((blk ^ sw) << 4)) = make_uint4(p1[0], p1[1], p1[2], p1[3]);
-          *reinterpret_cast<uint4*>(row_p + (((2 + blk) ^ sw) << 4)) = make_uint4(p2[0], p2[1], p2[2], p2[3]);
-          *reinterpret_cast<uint4*>(row_p + (((4 + blk) ^ sw) << 4)) = make_uint4(p3[0], p3[1], p3[2], p3[3]);
+          uint8_t* tile_p = sP + (j % PT) * C::kPBytes;
+          *reinterpret_cast<uint4*>(tile_p + tile_off<4 * R>(key, blk)) = make_uint4(p1[0], p1[1], p1[2], p1[3]);
+          *reinterpret_cast<uint4*>(tile_p + tile_off<4 * R>(key, kBlocks + blk)) = make_uint4(p2[0], p2[1], p2[2], p2[3]);
+          *reinterpret_cast<uint4*>(tile_p + tile_off<4 * R>(key, 2 * kBlocks + blk)) = make_uint4(p3[0], p3[1], p3[2], p3[3]);
         }
         sm100::fence_proxy_async_smem();
         sm100::tmem_wait_st();
         sm100::tc_fence_before();
         __syncwarp();
         if (lane == 0) {
-          arrive(&bars.s_free[grp]);
-          arrive(&bars.p_full[grp]);
+          arrive(&bars.s_free[j & 3]);
+          arrive(&bars.p_full[j & 3]);
         }
       }
       j = j1;
@@ -634,7 +667,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int top = s_top[at];
       if (ok) {
 #pragma unroll 1
-        for (int blk = 0; blk < blocks; ++blk) {
+        for (int blk = 0; blk < kBlocks; ++blk) {
           float v[16];
           uint32_t r[16];
           sm100::tmem_ld_16(l_col + 16 * blk, r);
@@ -648,7 +681,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
       const int next = (item + 1) & 3;
-      if (tid < kFewRows) s_base[next][tid] = kUnset;
+      if (tid < R) s_base[next][tid] = kUnset;
       if (tid == 0) {
         s_top[next] = kNoScale;
         s_ver[next] = 0;
@@ -664,26 +697,25 @@ __global__ void __launch_bounds__(kThreads, 1)
       };
       float* part = reinterpret_cast<float*>(p.part_o) + slot * D;
       const float unit = top < -126 ? 0x1p-127f : power_of_two(top);
-      // O, columns back to rows: group g takes the rows from 16 g on.
-      if (grp < blocks) {
-        uint32_t o[3][16];
+      // O, columns back to rows: a group takes half of the rows.
+      const int e0 = R == 32 ? 0 : 8 * grp;
+      uint32_t o[3][16];
 #pragma unroll
-        for (int x = 0; x < 3; ++x) sm100::tmem_ld_16(o_col + x * kFewRows + 16 * grp, o[x]);
-        if (D == 128 || lane < 16) {
+      for (int x = 0; x < 3; ++x) sm100::tmem_ld_16(o_col + x * R + (R == 32 ? 16 * grp : 0), o[x]);
+      if (D == 128 || lane < 16) {
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const int r = 16 * grp + e;
-            if (r >= rows) break;
-            const float v =
-                fmaf(fmaf(__uint_as_float(o[2][e]), 0.0625f, __uint_as_float(o[1][e])), 0.0625f, __uint_as_float(o[0][e])) * unit;
-            if (whole) {
-              float l = 0.f;
+        for (int e = 0; e < 16; ++e) {
+          const int r = (R == 32 ? 16 * grp : 0) + e;
+          if (r >= rows || (R == 16 && (e < e0 || e >= e0 + 8))) continue;
+          const float v =
+              fmaf(fmaf(__uint_as_float(o[2][e]), 0.0625f, __uint_as_float(o[1][e])), 0.0625f, __uint_as_float(o[0][e])) * unit;
+          if (whole) {
+            float l = 0.f;
 #pragma unroll
-              for (int x = 0; x < 8; ++x) l += s_sum[item & 1][x][r];
-              p.out[out_row_of(r) * D + d] = __float2bfloat16(__fdividef(v, l));
-            } else {
-              part[r * D + d] = v;
-            }
+            for (int x = 0; x < 8; ++x) l += s_sum[item & 1][x][r];
+            p.out[out_row_of(r) * D + d] = __float2bfloat16(__fdividef(v, l));
+          } else {
+            part[r * D + d] = v;
           }
         }
       }
@@ -752,5 +784,5 @@ __global__ void __launch_bounds__(kThreads, 1)
   sm100::tc_fence_before();
   __syncthreads();
   sm100::tc_fence_after();
-  if (warp == kPvWarp) sm100::tmem_dealloc(tmem, 256);
+  if (warp == kPvWarp) sm100::tmem_dealloc(tmem, C::kCols);
 }
