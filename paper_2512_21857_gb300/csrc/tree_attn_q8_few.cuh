@@ -57,6 +57,7 @@ struct FewBars {
   uint64_t k_full[8], k_free[8], v_full[8], v_free[8], v_tail;
   uint64_t prep_full[2], prep_free[2];
   uint64_t s_full[4], s_free[4], p_full[4], done[4], mu[2];
+  uint64_t part_full[2];     // an item's rows, final or partial, are written
   uint64_t o_free, drain[2];
 };
 
@@ -113,11 +114,11 @@ __global__ void __launch_bounds__(kThreads, 1)
   __shared__ __align__(16) float s_gb[2][R], s_alpha[2][R];  // of a group: the base its row sums are at
   __shared__ float s_most[2][4][R];
   __shared__ int s_wtop[2][4];
-  __shared__ float s_sum[2][8][R];
+  __shared__ __align__(16) float s_sum[2][R][8];       // of a row: the warps' parts
   __shared__ int16_t s_par[R];
   __shared__ Walk s_walk;
   __shared__ int64_t s_total;
-  __shared__ int s_grid, s_last;
+  __shared__ int s_grid;
   __shared__ uint32_t tmem_slot;
   __shared__ volatile int s_abort;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -139,6 +140,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     init(bars.p_full, 4, 4);
     init(bars.mu, 2, 1);
     init(bars.done, 4, 1);
+    init(bars.part_full, 2, 8);
     init(&bars.o_free, 1, 8);
     init(bars.drain, 2, 1);
     sm100::fence_mbar_init();
@@ -348,7 +350,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     constexpr int kLanes = D / 16, kPass = kConvThreads / kLanes;
     const int ct = tid - kConvWarp * 32, cl = ct % kLanes, cr = ct / kLanes;
     bool ok = true;
-    for (; ok && w.more; w = next_item(p, w), ++item) {
+    Walk before = w;
+    auto prepare = [&]() {
       const int at = item & 3, rows = w.t.n * p.group, n = w.t.n;
       uint8_t* q = sQ + (item & 1) * 2 * C::kQ;
       uint8_t* t = sT + (item & 1) * C::kTreeBytes;
@@ -376,7 +379,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       ok = item < 2 || wait(&bars.prep_free[item & 1], (item >> 1) - 1);
       if (!ok && lane == 0) give_up();
       ok = !any_of<1, kConvThreads>(!ok);
-      if (!ok) break;
+      if (!ok) return;
       if (tree && ct < n) {
         s_par[ct] = static_cast<int16_t>(min(max(up, -1), kMaxTreeNodes));
         if ((ct == 0) != (up < 0) || up >= ct) adt::raise_error(p.err, ADT_DEVERR_BAD_TREE);
@@ -454,6 +457,56 @@ __global__ void __launch_bounds__(kThreads, 1)
       sm100::fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) arrive(&bars.prep_full[item & 1]);
+    };
+    // The parts of a cut item joined, by the CTA that ends its part last, beside the
+    // next item's chunks: weights 2^(m_c - M) over their sum.
+    auto join = [&](const Walk& w, uint32_t item) {
+      ok = wait(&bars.part_full[item & 1], item >> 1);
+      if (!ok && lane == 0) give_up();
+      ok = !any_of<1, kConvThreads>(!ok);
+      if (!ok || (w.k0 == 0 && w.k1 == w.t.chunks)) return;
+      // (Which CTAs these are: as in the kernel of 128 rows.)
+      const int64_t X = s_total, G = s_grid, a = w.start + kItemCost, z = a + w.t.chunks - 1;
+      const int first = static_cast<int>(((a + 1) * G - 1) / X), last = static_cast<int>(((z + 1) * G - 1) / X);
+      const bool mine = ct == 0 && adt::atomic_add_acq_rel_gpu(p.tickets + first, 1u) == static_cast<unsigned>(last - first);
+      if (!any_of<1, kConvThreads>(mine)) return;
+      const int slot0 = first * 2 + (first * X / G >= w.start ? 0 : 1);
+      auto slot_of = [&](int c) -> int64_t { return static_cast<int64_t>(c == first ? slot0 : 2 * c) * p.slot_rows; };
+      const float* po = reinterpret_cast<const float*>(p.part_o);
+#pragma unroll 1
+      for (int i = ct; i < w.t.n * p.group * (D / 4); i += kConvThreads) {
+        const int r = i / (D / 4), c4 = i % (D / 4), node = r / p.group;
+        const int64_t row = static_cast<int64_t>(w.t.node0 + node) * p.H + w.g * p.group + (r - node * p.group);
+        float M = -INFINITY, l = 0.f;
+#pragma unroll 4
+        for (int c = first; c <= last; ++c) M = fmaxf(M, __ldcg(&p.part_ml[slot_of(c) + r]).x);
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int c = first; c <= last; ++c) {
+          const float2 ml = __ldcg(&p.part_ml[slot_of(c) + r]);
+          const float4 v = __ldcg(reinterpret_cast<const float4*>(po + (slot_of(c) + r) * D) + c4);
+          const float wt = ml.x == M ? 1.f : ex2_approx(ml.x - M);
+          l += wt * ml.y;
+          acc.x += wt * v.x;
+          acc.y += wt * v.y;
+          acc.z += wt * v.z;
+          acc.w += wt * v.w;
+        }
+        const float inv = __fdividef(1.f, l);
+        uint2 y;
+        y.x = pack_bf16x2(acc.x * inv, acc.y * inv);
+        y.y = pack_bf16x2(acc.z * inv, acc.w * inv);
+        *reinterpret_cast<uint2*>(p.out + row * D + c4 * 4) = y;
+        if (c4 == 0 && p.lse) p.lse[row] = (M + __log2f(l)) * kLn2;
+      }
+      if (ct == 0) p.tickets[first] = 0u;
+    };
+    for (;; ++item) {
+      if (w.more) prepare();
+      if (ok && item > 0) join(before, item - 1);
+      if (!ok || !w.more) break;
+      before = w;
+      w = next_item(p, w);
     }
   } else {
     // ------------------------------------------------------------ softmax
@@ -677,7 +730,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             v[e] = fresh ? 0.f : __uint_as_float(r[e]) * ex2_approx(d);
           }
           const float sum = transposed_sum(v, lane);
-          if ((lane & 1) == 0) s_sum[item & 1][warp][16 * blk + (lane >> 1)] = sum;
+          if ((lane & 1) == 0) s_sum[item & 1][16 * blk + (lane >> 1)][warp] = sum;
         }
       }
       const int next = (item + 1) & 3;
@@ -696,36 +749,35 @@ __global__ void __launch_bounds__(kThreads, 1)
         return static_cast<int64_t>(w.t.node0 + node) * p.H + w.g * p.group + (r - node * p.group);
       };
       float* part = reinterpret_cast<float*>(p.part_o) + slot * D;
+      auto row_sum = [&](int r) {
+        const float4 a = *reinterpret_cast<const float4*>(s_sum[item & 1][r]), b = *reinterpret_cast<const float4*>(s_sum[item & 1][r] + 4);
+        return ((a.x + a.y) + (a.z + a.w)) + ((b.x + b.y) + (b.z + b.w));
+      };
       const float unit = top < -126 ? 0x1p-127f : power_of_two(top);
       // O, columns back to rows: a group takes half of the rows.
-      const int e0 = R == 32 ? 0 : 8 * grp;
-      uint32_t o[3][16];
+#pragma unroll 1
+      for (int r0 = grp * (R / 2); r0 < min(rows, (grp + 1) * (R / 2)); r0 += 8) {
+        uint32_t o[3][8];
 #pragma unroll
-      for (int x = 0; x < 3; ++x) sm100::tmem_ld_16(o_col + x * R + (R == 32 ? 16 * grp : 0), o[x]);
-      if (D == 128 || lane < 16) {
+        for (int x = 0; x < 3; ++x) sm100::tmem_ld_8(o_col + x * R + r0, o[x]);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int r = (R == 32 ? 16 * grp : 0) + e;
-          if (r >= rows || (R == 16 && (e < e0 || e >= e0 + 8))) continue;
+        for (int e = 0; e < 8; ++e) {
+          const int r = r0 + e;
+          if (r >= rows || (D == 64 && lane >= 16)) break;
           const float v =
               fmaf(fmaf(__uint_as_float(o[2][e]), 0.0625f, __uint_as_float(o[1][e])), 0.0625f, __uint_as_float(o[0][e])) * unit;
-          if (whole) {
-            float l = 0.f;
-#pragma unroll
-            for (int x = 0; x < 8; ++x) l += s_sum[item & 1][x][r];
-            p.out[out_row_of(r) * D + d] = __float2bfloat16(__fdividef(v, l));
-          } else {
+          if (whole)
+            p.out[out_row_of(r) * D + d] = __float2bfloat16(__fdividef(v, row_sum(r)));
+          else
             part[r * D + d] = v;
-          }
         }
+        __syncwarp();
       }
       sm100::tc_fence_before();
       __syncwarp();
       if (lane == 0) arrive(&bars.o_free);
       if (tid < rows) {
-        float l = 0.f;
-#pragma unroll
-        for (int x = 0; x < 8; ++x) l += s_sum[item & 1][x][tid];
+        const float l = row_sum(tid);
         const float m = s_base[at][tid] - top - kFewHeadroom;
         if (!whole)
           p.part_ml[slot + tid] = make_float2(m, l);
@@ -739,46 +791,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                   p.tree[1] + (static_cast<int64_t>(w.t.node0) * p.Hkv + w.g) * D, p.parents + w.t.node0,
                   static_cast<int64_t>(p.Hkv) * D, tid / p.group, 0, w.t.n);
       }
-      if (!whole) {
-        // (As in the kernel of 128 rows.)
-        const int64_t X = s_total, G = s_grid, a = w.start + kItemCost, z = a + w.t.chunks - 1;
-        const int first = static_cast<int>(((a + 1) * G - 1) / X), last = static_cast<int>(((z + 1) * G - 1) / X);
-        softmax_sync();
-        if (tid == 0)
-          s_last = adt::atomic_add_acq_rel_gpu(p.tickets + first, 1u) == static_cast<unsigned>(last - first);
-        softmax_sync();
-        if (s_last) {
-          const int slot0 = first * 2 + (first * X / G >= w.start ? 0 : 1);
-          auto slot_of = [&](int c) -> int64_t { return static_cast<int64_t>(c == first ? slot0 : 2 * c) * p.slot_rows; };
-          const float* po = reinterpret_cast<const float*>(p.part_o);
-#pragma unroll 1
-          for (int x = tid; x < rows * (D / 4); x += kSoftmaxThreads) {
-            const int r = x / (D / 4), c4 = x % (D / 4);
-            float M = -INFINITY, l = 0.f;
-#pragma unroll 4
-            for (int c = first; c <= last; ++c) M = fmaxf(M, __ldcg(&p.part_ml[slot_of(c) + r]).x);
-            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-            for (int c = first; c <= last; ++c) {
-              const float2 ml = __ldcg(&p.part_ml[slot_of(c) + r]);
-              const float4 v = __ldcg(reinterpret_cast<const float4*>(po + (slot_of(c) + r) * D) + c4);
-              const float wt = ml.x == M ? 1.f : ex2_approx(ml.x - M);
-              l += wt * ml.y;
-              acc.x += wt * v.x;
-              acc.y += wt * v.y;
-              acc.z += wt * v.z;
-              acc.w += wt * v.w;
-            }
-            const float inv = __fdividef(1.f, l);
-            uint2 y;
-            y.x = pack_bf16x2(acc.x * inv, acc.y * inv);
-            y.y = pack_bf16x2(acc.z * inv, acc.w * inv);
-            *reinterpret_cast<uint2*>(p.out + out_row_of(r) * D + c4 * 4) = y;
-            if (c4 == 0 && p.lse) p.lse[out_row_of(r)] = (M + __log2f(l)) * kLn2;
-          }
-          if (tid == 0) p.tickets[first] = 0u;
-        }
-      }
+      __syncwarp();
+      if (lane == 0) arrive(&bars.part_full[item & 1]);
     }
   }
   sm100::tc_fence_before();
