@@ -49,7 +49,8 @@ struct FewCfg {
   static constexpr int kVOff = kKOff + kStages * kTile;
   static constexpr int kDynSmem = kVOff + kStages * kTile + 1024;  // + alignment slack
   static constexpr uint32_t kIdescO = sm100::idesc_e4m3_f32(D, 3 * R) | 1u << 15 | 1u << 16;  // both MN-major
-  static constexpr uint32_t kOAt = 4 * R, kLAt = 7 * R;  // after four S tiles of R columns: O, 3 R; then two row sums of R
+  // Tensor memory: four S tiles of R columns, O of two items (3 R), row sums [2 items][2 groups] of R.
+  static constexpr uint32_t kOAt = 4 * R, kLAt = 10 * R;
   static constexpr uint32_t kCols = R == 16 ? 256 : 512;
 };
 
@@ -57,8 +58,7 @@ struct FewBars {
   uint64_t k_full[8], k_free[8], v_full[8], v_free[8], v_tail;
   uint64_t prep_full[2], prep_free[2];
   uint64_t s_full[4], s_free[4], p_full[4], done[4], mu[2];
-  uint64_t part_full[2];     // an item's rows, final or partial, are written
-  uint64_t o_free, drain[2];
+  uint64_t drain[2];
 };
 
 __device__ __forceinline__ uint16_t f16x2_to_e4m3(uint32_t h) {
@@ -105,16 +105,15 @@ __global__ void __launch_bounds__(kThreads, 1)
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (sm100::smem_addr(smem_raw) & 1023u)) & 1023u);
   __shared__ FewBars bars;
-  // Of an item's rows (and its tree's keys), by item: four, so that none is written
-  // while the item before the last may still be read.
-  __shared__ __align__(16) float s_c[4][R], s_base[4][R];
-  __shared__ float s_tk[4][R];
-  __shared__ int s_tv[4][R], s_top[4], s_ver[4], s_odd[4];
-  __shared__ uint32_t s_seen[4][R];                    // of a key: the rows that see it
-  __shared__ __align__(16) float s_gb[2][R], s_alpha[2][R];  // of a group: the base its row sums are at
+  // Of an item's rows (and its tree's keys), by item.
+  __shared__ __align__(16) float s_c[2][R], s_base[2][R];
+  __shared__ float s_tk[2][R];
+  __shared__ int s_tv[2][R], s_top[2], s_ver[2], s_odd[2];
+  __shared__ uint32_t s_seen[2][R];                    // of a key: the rows that see it
+  __shared__ __align__(16) float s_gb[2][2][R], s_alpha[2][R];  // of a group: the level its row sums are at
   __shared__ float s_most[2][4][R];
   __shared__ int s_wtop[2][4];
-  __shared__ __align__(16) float s_sum[2][R][8];       // of a row: the warps' parts
+  __shared__ __align__(16) float s_sum[R][4];          // of a row: the warps' parts
   __shared__ int16_t s_par[R];
   __shared__ Walk s_walk;
   __shared__ int64_t s_total;
@@ -140,16 +139,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     init(bars.p_full, 4, 4);
     init(bars.mu, 2, 1);
     init(bars.done, 4, 1);
-    init(bars.part_full, 2, 8);
-    init(&bars.o_free, 1, 8);
     init(bars.drain, 2, 1);
     sm100::fence_mbar_init();
-  }
-  if (tid < 4 * R) s_base[tid / R][tid % R] = kUnset;
-  if (tid < 4) {
-    s_top[tid] = kNoScale;
-    s_ver[tid] = 0;
-    s_odd[tid] = 0;
   }
   if (warp == kPvWarp) {
     sm100::tmem_alloc(sm100::smem_addr(&tmem_slot), C::kCols);
@@ -190,19 +181,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (lane == 0) {
       bool ok = true;
       for (; ok && w.more; w = next_item(p, w)) {
-        const int64_t s0 = w.b * p.ssb + w.g * p.ssh;
         const int end = min(w.k1, w.t.prefix);
-        // Scales, a byte a thread, come from L2: asked for there kAhead chunks before.
-        auto prefetch = [&](int k) {
-          const int64_t row = static_cast<int64_t>(k) * kChunk;
-          if (k >= end || row + kChunk > w.t.L) return;
-          for (int x = 0; x < 2; ++x) {
-            prefetch_l2(p.scale[x] + s0 + row);
-            prefetch_l2(p.scale[x] + s0 + row + kChunk - 1);
-          }
-        };
-#pragma unroll 1
-        for (int k = w.k0; k < w.k0 + kAhead; ++k) prefetch(k);
         for (int k = w.k0; k < end; ++k, ++i) {
           const int st = i % NS;
           if (i >= NS && !wait(&bars.k_free[st], i / NS - 1)) {
@@ -212,7 +191,6 @@ __global__ void __launch_bounds__(kThreads, 1)
           const uint32_t bar = sm100::smem_addr(&bars.k_full[st]);
           sm100::mbar_arrive_expect_tx(bar, C::kTile);
           sm100::tma_load_4d(sm100::smem_addr(sK + st * C::kTile), &tm_k, 0, k * kChunk, w.g, w.b, bar);
-          prefetch(k + kAhead);
         }
       }
       if (!ok) give_up();
@@ -311,8 +289,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int k = w.k0; ok && k < w.k1; ++k, ++j) {
           const bool tree_k = k >= w.t.prefix;
           const int st = i % NS;
-          ok = wait(&bars.p_full[j & 3], j >> 2) && (tree_k || wait(&bars.v_full[st], i / NS)) &&
-               (k > w.k0 || item == 0 || wait(&bars.o_free, item - 1));
+          ok = wait(&bars.p_full[j & 3], j >> 2) && (tree_k || wait(&bars.v_full[st], i / NS));
           if (!ok) break;
           sm100::tc_fence_after();
           const uint64_t pd = pd0 + (j % PT) * (C::kPBytes / 16);
@@ -325,7 +302,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const uint64_t vd = (tree_k ? td0 + ((item & 1) * C::kTreeBytes + (2 + kk) * C::kSmall) / 16
                                         : vd0 + (st * C::kTile + kk * 32 * D) / 16);
             const int part = tree_k ? kk : 0;
-            sm100::mma_f8_ss(tmem + C::kOAt + part * R, vd, pd + (kk - part) * (32 * 4 * R / 16),
+            sm100::mma_f8_ss(tmem + C::kOAt + ((item & 1) * 3 + part) * R, vd, pd + (kk - part) * (32 * 4 * R / 16),
                              C::kIdescO - (static_cast<uint32_t>(part * R >> 3) << 17), more);
             more = 1u;
           }
@@ -343,16 +320,16 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     __syncwarp();
   } else if (warp >= kConvWarp) {
-    // ------------------------------------------------------------ queries and trees
+    // ------------------------------------------------------------ an item's start and end
     // A row is D / 16 lanes', 16 elements each: the item's queries, then the tree's keys
     // and values.  One copy of the code for all, and what there is to read in flight
     // before: an item's first product waits for this.
     constexpr int kLanes = D / 16, kPass = kConvThreads / kLanes;
     const int ct = tid - kConvWarp * 32, cl = ct % kLanes, cr = ct / kLanes;
     bool ok = true;
-    Walk before = w;
+    // (All threads are past the end of the item before the last, and so are all others.)
     auto prepare = [&]() {
-      const int at = item & 3, rows = w.t.n * p.group, n = w.t.n;
+      const int at = item & 1, rows = w.t.n * p.group, n = w.t.n;
       uint8_t* q = sQ + (item & 1) * 2 * C::kQ;
       uint8_t* t = sT + (item & 1) * C::kTreeBytes;
       const bool tree = w.k1 > w.t.prefix;
@@ -375,16 +352,16 @@ __global__ void __launch_bounds__(kThreads, 1)
       };
       fetch(cr);
       if (tree && ct < n) up = p.parents[w.t.node0 + ct];
-      // The item before the last is done with, its products at least.
-      ok = item < 2 || wait(&bars.prep_free[item & 1], (item >> 1) - 1);
-      if (!ok && lane == 0) give_up();
-      ok = !any_of<1, kConvThreads>(!ok);
-      if (!ok) return;
+      any_of<1, kConvThreads>(false);
+      if (ct < R) s_base[at][ct] = kUnset;
       if (tree && ct < n) {
         s_par[ct] = static_cast<int16_t>(min(max(up, -1), kMaxTreeNodes));
         if ((ct == 0) != (up < 0) || up >= ct) adt::raise_error(p.err, ADT_DEVERR_BAD_TREE);
       }
-      if (ct == 0) s_odd[at] = 0;
+      if (ct == 0) {
+        s_odd[at] = s_ver[at] = 0;
+        s_top[at] = kNoScale;
+      }
       any_of<1, kConvThreads>(false);
 #pragma unroll 1
       for (int u = cr; u - cr < units; u += kPass) {
@@ -458,13 +435,83 @@ __global__ void __launch_bounds__(kThreads, 1)
       __syncwarp();
       if (lane == 0) arrive(&bars.prep_full[item & 1]);
     };
-    // The parts of a cut item joined, by the CTA that ends its part last, beside the
-    // next item's chunks: weights 2^(m_c - M) over their sum.
-    auto join = [&](const Walk& w, uint32_t item) {
-      ok = wait(&bars.part_full[item & 1], item >> 1);
+    // An item's rows, once its products are done: final ones, or this CTA's part.
+    auto finish = [&](const Walk& w, uint32_t item, uint32_t j0) {
+      ok = wait(&bars.prep_free[item & 1], item >> 1);
       if (!ok && lane == 0) give_up();
       ok = !any_of<1, kConvThreads>(!ok);
-      if (!ok || (w.k0 == 0 && w.k1 == w.t.chunks)) return;
+      if (!ok) return;
+      sm100::tc_fence_after();
+      const int at = item & 1, rows = w.t.n * p.group, w4 = warp & 3, top = s_top[at];
+      const uint32_t lanes = static_cast<uint32_t>(w4 * 32) << 16;
+      // Row sums over the keys' lanes, at the bases' last level; of a group that had a chunk.
+#pragma unroll 1
+      for (int blk = 0; blk < R / 16; ++blk) {
+        float v[16] = {};
+#pragma unroll 1
+        for (int g = 0; g < 2; ++g) {
+          if (w.k1 - w.k0 < 2 && (j0 & 1) != static_cast<uint32_t>(g)) continue;
+          uint32_t r[16];
+          sm100::tmem_ld_16(tmem + lanes + C::kLAt + (at * 2 + g) * R + 16 * blk, r);
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            v[e] = fmaf(__uint_as_float(r[e]), ex2_approx(s_gb[at][g][16 * blk + e] - (s_base[at][16 * blk + e] - top)), v[e]);
+        }
+        const float sum = transposed_sum(v, lane);
+        if ((lane & 1) == 0) s_sum[16 * blk + (lane >> 1)][w4] = sum;
+      }
+      any_of<1, kConvThreads>(false);
+      const bool whole = w.k0 == 0 && w.k1 == w.t.chunks;
+      const int64_t slot = (2ll * blockIdx.x + (w.first ? 0 : 1)) * p.slot_rows;
+      const int d = D == 128 ? ct : w4 * 16 + lane;
+      auto out_row_of = [&](int r) {
+        const int node = r / p.group;
+        return static_cast<int64_t>(w.t.node0 + node) * p.H + w.g * p.group + (r - node * p.group);
+      };
+      float* part = reinterpret_cast<float*>(p.part_o) + slot * D;
+      auto row_sum = [&](int r) {
+        const float4 a = *reinterpret_cast<const float4*>(s_sum[r]);
+        return (a.x + a.y) + (a.z + a.w);
+      };
+      const float unit = top < -126 ? 0x1p-127f : power_of_two(top);
+      // O, columns back to rows.
+#pragma unroll 1
+      for (int r0 = 0; r0 < rows; r0 += 8) {
+        uint32_t o[3][8];
+#pragma unroll
+        for (int x = 0; x < 3; ++x) sm100::tmem_ld_8(tmem + lanes + C::kOAt + (at * 3 + x) * R + r0, o[x]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int r = r0 + e;
+          if (r >= rows || (D == 64 && lane >= 16)) break;
+          const float v =
+              fmaf(fmaf(__uint_as_float(o[2][e]), 0.0625f, __uint_as_float(o[1][e])), 0.0625f, __uint_as_float(o[0][e])) * unit;
+          if (whole)
+            p.out[out_row_of(r) * D + d] = __float2bfloat16(__fdividef(v, row_sum(r)));
+          else
+            part[r * D + d] = v;
+        }
+        __syncwarp();
+      }
+      sm100::tc_fence_before();
+      if (ct < rows) {
+        const float l = row_sum(ct), m = s_base[at][ct] - top - kFewHeadroom;
+        if (!whole)
+          p.part_ml[slot + ct] = make_float2(m, l);
+        else if (p.lse)
+          p.lse[out_row_of(ct)] = (m + __log2f(l)) * kLn2;
+      }
+      if (s_odd[at] != 0 && w.k1 > w.t.prefix) {
+        any_of<1, kConvThreads>(false);  // the rows are written
+        if (ct < rows)
+          add_odd(whole ? p.out + out_row_of(ct) * D : nullptr, part + ct * D, 1, D,
+                  p.tree[1] + (static_cast<int64_t>(w.t.node0) * p.Hkv + w.g) * D, p.parents + w.t.node0,
+                  static_cast<int64_t>(p.Hkv) * D, ct / p.group, 0, w.t.n);
+      }
+      if (whole) return;
+      // The parts joined by the CTA that ends its own last, beside the next item's
+      // chunks: weights 2^(m_c - M) over their sum.
+      any_of<1, kConvThreads>(false);
       // (Which CTAs these are: as in the kernel of 128 rows.)
       const int64_t X = s_total, G = s_grid, a = w.start + kItemCost, z = a + w.t.chunks - 1;
       const int first = static_cast<int>(((a + 1) * G - 1) / X), last = static_cast<int>(((z + 1) * G - 1) / X);
@@ -475,8 +522,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       const float* po = reinterpret_cast<const float*>(p.part_o);
 #pragma unroll 1
       for (int i = ct; i < w.t.n * p.group * (D / 4); i += kConvThreads) {
-        const int r = i / (D / 4), c4 = i % (D / 4), node = r / p.group;
-        const int64_t row = static_cast<int64_t>(w.t.node0 + node) * p.H + w.g * p.group + (r - node * p.group);
+        const int r = i / (D / 4), c4 = i % (D / 4);
+        const int64_t row = out_row_of(r);
         float M = -INFINITY, l = 0.f;
 #pragma unroll 4
         for (int c = first; c <= last; ++c) M = fmaxf(M, __ldcg(&p.part_ml[slot_of(c) + r]).x);
@@ -501,9 +548,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       if (ct == 0) p.tickets[first] = 0u;
     };
+    Walk before = w;
     for (;; ++item) {
       if (w.more) prepare();
-      if (ok && item > 0) join(before, item - 1);
+      if (item > 0) {
+        finish(before, item - 1, j);
+        j += static_cast<uint32_t>(before.k1 - before.k0);
+      }
       if (!ok || !w.more) break;
       before = w;
       w = next_item(p, w);
@@ -512,14 +563,17 @@ __global__ void __launch_bounds__(kThreads, 1)
     // ------------------------------------------------------------ softmax
     const int grp = warp >> 2, w4 = warp & 3, key = w4 * 32 + lane;
     const uint32_t lanes = static_cast<uint32_t>(w4 * 32) << 16;
-    const uint32_t o_col = tmem + lanes + C::kOAt, l_col = tmem + lanes + C::kLAt + grp * R;
     constexpr int kBlocks = R / 16;
     const int gt = tid & 127;
-    bool ok = true;
-    for (; ok && w.more; w = next_item(p, w), ++item) {
-      const int at = item & 3, rows = w.t.n * p.group;
+    // A warp whose wait gave up goes on, without further waits, to where its group
+    // leaves together.
+    bool ok = true, left = false;
+    for (; !left && w.more; w = next_item(p, w), ++item) {
+      const int at = item & 1;
+      const uint32_t o_col = tmem + lanes + C::kOAt + at * 3 * R, l_col = tmem + lanes + C::kLAt + (at * 2 + grp) * R;
       const uint32_t j0 = j, j1 = j + static_cast<uint32_t>(w.k1 - w.k0);
-      ok = all_wait(&bars.prep_full[item & 1], item >> 1);
+      // (Then the item before the last is read from tensor and shared memory, too.)
+      ok = ok && all_wait(&bars.prep_full[item & 1], item >> 1);
       const int64_t s0 = w.b * p.ssb + w.g * p.ssh + key;
       const uint8_t *ksrc = p.scale[0] + s0, *vsrc = p.scale[1] + s0;
       if ((j0 & 1) != static_cast<uint32_t>(grp)) ++j;
@@ -540,10 +594,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         const bool tree_k = k >= w.t.prefix;
         const uint32_t kbyte = kb, vbyte = vb;
         fetch(k + 2);
-        // The chunk before has settled its bases.  (An item's last chunk is done before
-        // the next one's first.)
-        // A warp whose wait gave up goes on to where the group leaves together.
-        ok = ok && all_wait(&bars.s_full[j & 3], j >> 2) && (j == j0 || all_wait(&bars.mu[grp ^ 1], (j - 1) >> 1));
+        // The chunk before has settled its bases (another item's too: no phase of a
+        // barrier is passed over).
+        ok = ok && all_wait(&bars.s_full[j & 3], j >> 2) && (j == 0 || all_wait(&bars.mu[grp ^ 1], (j - 1) >> 1));
         sm100::tc_fence_after();
         const uint32_t s_col = tmem + lanes + (j & 3) * R;
         float ks = adt::q8_scale(kbyte);
@@ -570,21 +623,25 @@ __global__ void __launch_bounds__(kThreads, 1)
         };
         int top = s_top[at];
         float evf = static_cast<float>(max(ev, top - 60));
-        float most = -INFINITY;
+        bool raise = j == j0;
+        if (!raise) {
+          float most = -INFINITY;
 #pragma unroll 1
-        for (int blk = 0; blk < kBlocks; ++blk) {
-          float x[16];
-          load(blk, x);
-          const float4* c4 = reinterpret_cast<const float4*>(s_c[at] + 16 * blk);
-          const float4* b4 = reinterpret_cast<const float4*>(s_base[at] + 16 * blk);
+          for (int blk = 0; blk < kBlocks; ++blk) {
+            float x[16];
+            load(blk, x);
+            const float4* c4 = reinterpret_cast<const float4*>(s_c[at] + 16 * blk);
+            const float4* b4 = reinterpret_cast<const float4*>(s_base[at] + 16 * blk);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float4 c = c4[e], b = b4[e];
-            most = fmaxf(most, fmaxf(fmaf(x[4 * e], c.x, -b.x), fmaf(x[4 * e + 1], c.y, -b.y)));
-            most = fmaxf(most, fmaxf(fmaf(x[4 * e + 2], c.z, -b.z), fmaf(x[4 * e + 3], c.w, -b.w)));
+            for (int e = 0; e < 4; ++e) {
+              const float4 c = c4[e], b = b4[e];
+              most = fmaxf(most, fmaxf(fmaf(x[4 * e], c.x, -b.x), fmaf(x[4 * e + 1], c.y, -b.y)));
+              most = fmaxf(most, fmaxf(fmaf(x[4 * e + 2], c.z, -b.z), fmaf(x[4 * e + 3], c.w, -b.w)));
+            }
           }
+          const bool more = !ok || most + evf > kFewThreshold;
+          raise = grp == 0 ? any_of<3, 128>(more) : any_of<4, 128>(more);
         }
-        const bool more = !ok || most + evf > kFewThreshold, raise = grp == 0 ? any_of<3, 128>(more) : any_of<4, 128>(more);
         if (raise) {
           // The largest scale, then every row's largest exponent over the chunk.
           const int wtop = __reduce_max_sync(adt::kFullMask, ev);
@@ -604,10 +661,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           // O is scaled once the chunks before are in it; then nothing reads the bases of
           // the chunk before either.
-          if (ok && j > j0) ok = all_wait(&bars.done[(j - 1) & 3], (j - 1) >> 2);
+          // (That PV(j - 5) is, whose phase comes before, PV(j - 4) says.)
+          if (ok && j > j0)
+            ok = (j < 4 || all_wait(&bars.done[j & 3], (j - 4) >> 2)) && all_wait(&bars.done[(j - 1) & 3], (j - 1) >> 2);
           if (!ok && lane == 0) give_up();
-          ok = !(grp == 0 ? any_of<3, 128>(!ok) : any_of<4, 128>(!ok));
-          if (!ok) break;
+          left = grp == 0 ? any_of<3, 128>(!ok) : any_of<4, 128>(!ok);
+          if (left) break;
           if (gt < R) {
             const float y = fmaxf(fmaxf(s_most[grp][0][gt], s_most[grp][1][gt]), fmaxf(s_most[grp][2][gt], s_most[grp][3][gt]));
             const float old = s_base[at][gt], now = y > old + kFewThreshold ? y : old;
@@ -643,14 +702,14 @@ __global__ void __launch_bounds__(kThreads, 1)
             sm100::tmem_ld_16(l_col + 16 * blk, r);
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-              const float d = s_gb[grp][16 * blk + e] - (s_base[at][16 * blk + e] - top);
+              const float d = s_gb[at][grp][16 * blk + e] - (s_base[at][16 * blk + e] - top);
               r[e] = fresh ? 0u : __float_as_uint(__uint_as_float(r[e]) * ex2_approx(d));
             }
             tmem_st_16(l_col + 16 * blk, r);
           }
           sm100::tmem_wait_st();
           group_sync(grp);
-          if (gt < R) s_gb[grp][gt] = s_base[at][gt] - top;
+          if (gt < R) s_gb[at][grp][gt] = s_base[at][gt] - top;
           fresh = false;
           ver = now;
         }
@@ -712,88 +771,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
       j = j1;
-      ok = ok && all_wait(&bars.done[(j1 - 1) & 3], (j1 - 1) >> 2);
-      if (!ok && lane == 0) give_up();
-      sm100::tc_fence_after();
-      // Row sums over the keys' lanes, at the bases' last level.  (A group without a
-      // chunk of the item has none.)
-      const int top = s_top[at];
-      if (ok) {
-#pragma unroll 1
-        for (int blk = 0; blk < kBlocks; ++blk) {
-          float v[16];
-          uint32_t r[16];
-          sm100::tmem_ld_16(l_col + 16 * blk, r);
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const float d = s_gb[grp][16 * blk + e] - (s_base[at][16 * blk + e] - top);
-            v[e] = fresh ? 0.f : __uint_as_float(r[e]) * ex2_approx(d);
-          }
-          const float sum = transposed_sum(v, lane);
-          if ((lane & 1) == 0) s_sum[item & 1][16 * blk + (lane >> 1)][warp] = sum;
-        }
-      }
-      const int next = (item + 1) & 3;
-      if (tid < R) s_base[next][tid] = kUnset;
-      if (tid == 0) {
-        s_top[next] = kNoScale;
-        s_ver[next] = 0;
-      }
-      ok = !any_of<2, kSoftmaxThreads>(!ok);  // (after a wait that gave up they leave together)
-      if (!ok) break;
-      const bool whole = w.k0 == 0 && w.k1 == w.t.chunks;
-      const int64_t slot = (2ll * blockIdx.x + (w.first ? 0 : 1)) * p.slot_rows;
-      const int d = D == 128 ? key : w4 * 16 + lane;
-      auto out_row_of = [&](int r) {
-        const int node = r / p.group;
-        return static_cast<int64_t>(w.t.node0 + node) * p.H + w.g * p.group + (r - node * p.group);
-      };
-      float* part = reinterpret_cast<float*>(p.part_o) + slot * D;
-      auto row_sum = [&](int r) {
-        const float4 a = *reinterpret_cast<const float4*>(s_sum[item & 1][r]), b = *reinterpret_cast<const float4*>(s_sum[item & 1][r] + 4);
-        return ((a.x + a.y) + (a.z + a.w)) + ((b.x + b.y) + (b.z + b.w));
-      };
-      const float unit = top < -126 ? 0x1p-127f : power_of_two(top);
-      // O, columns back to rows: a group takes half of the rows.
-#pragma unroll 1
-      for (int r0 = grp * (R / 2); r0 < min(rows, (grp + 1) * (R / 2)); r0 += 8) {
-        uint32_t o[3][8];
-#pragma unroll
-        for (int x = 0; x < 3; ++x) sm100::tmem_ld_8(o_col + x * R + r0, o[x]);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int r = r0 + e;
-          if (r >= rows || (D == 64 && lane >= 16)) break;
-          const float v =
-              fmaf(fmaf(__uint_as_float(o[2][e]), 0.0625f, __uint_as_float(o[1][e])), 0.0625f, __uint_as_float(o[0][e])) * unit;
-          if (whole)
-            p.out[out_row_of(r) * D + d] = __float2bfloat16(__fdividef(v, row_sum(r)));
-          else
-            part[r * D + d] = v;
-        }
-        __syncwarp();
-      }
-      sm100::tc_fence_before();
-      __syncwarp();
-      if (lane == 0) arrive(&bars.o_free);
-      if (tid < rows) {
-        const float l = row_sum(tid);
-        const float m = s_base[at][tid] - top - kFewHeadroom;
-        if (!whole)
-          p.part_ml[slot + tid] = make_float2(m, l);
-        else if (p.lse)
-          p.lse[out_row_of(tid)] = (m + __log2f(l)) * kLn2;
-      }
-      if (s_odd[at] != 0 && w.k1 > w.t.prefix) {
-        softmax_sync();  // the rows are written
-        if (tid < rows)
-          add_odd(whole ? p.out + out_row_of(tid) * D : nullptr, part + tid * D, 1, D,
-                  p.tree[1] + (static_cast<int64_t>(w.t.node0) * p.Hkv + w.g) * D, p.parents + w.t.node0,
-                  static_cast<int64_t>(p.Hkv) * D, tid / p.group, 0, w.t.n);
-      }
-      __syncwarp();
-      if (lane == 0) arrive(&bars.part_full[item & 1]);
     }
+    if (!ok && lane == 0) give_up();
   }
   sm100::tc_fence_before();
   __syncthreads();
