@@ -8,28 +8,41 @@
 // CTA an SM in equal contiguous shares, so ragged batches and few long sequences
 // fill the device alike; an item that a share's end cuts is joined from partial
 // rows (O, maximum, sum) in the workspace by the CTA that ends its part last.
+// Two kernels share this: of up to 32 rows tree_attn_q8_few.cuh, of more this one.
 //
 // S = Q K^T is made of e4m3 products, K as it lies in the cache: a query row,
 // scaled by a power of two to at most 448, is cut into an e4m3 row and another of
 // what that leaves, and both products add up in one accumulator (as many
-// instructions as one product of bf16 has).  What the two leave is below 2^-17 of the row's
-// largest magnitude.  The tree's own keys are cut the same way (four products).
-// The key's scale meets the score in fp32.  A weight takes on its value row's
-// scale before it is rounded to bf16, and V is widened to bf16 in shared memory:
-// e4m3 weights, even two of them, would lose keys of 2^-18 of the largest one's
-// weight, of which a long cache can have enough to matter.
+// instructions as one product of bf16 has).  What the two leave is below 2^-17 of
+// the row's largest magnitude.  The tree's own keys are cut the same way (four
+// products).  The key's scale meets the score in fp32.  A weight takes on its
+// value row's scale, against a reference of the share's (2^4 above the largest
+// seen: s_ref), before it is rounded to fp16, and V is widened to fp16 in shared
+// memory, exactly: bf16 weights are three bits worse, and two e4m3 ones a weight
+// would lose keys of 2^-18 of the largest one's, of which a long cache can have
+// enough to matter.
+//
+// Queries, trees and ancestors are prepared by a launch before (prepare_kernel).
+//
+// Of up to 64 rows the tile holds each twice, a copy for each half of a chunk's
+// keys: a thread's softmax is half as long, and the copies are joined at the end.
 //
 // Warp roles (16 warps):
 //   0-3, 4-7  two softmax groups that take the chunks in turn, a thread a row;
 //             the running maximum passes from group to group through shared
 //             memory, P goes to tensor memory;
-//   8         K tiles by TMA into a ring, and the scales of both, eight chunks deep;
+//   8         K tiles by TMA into a ring, the queries, and the scales of both,
+//             written a chunk after their bytes were asked for;
 //   9         V tiles (packed rows: plain bulk copies) into a ring;
 //   10        S products;
 //   11        PV products;
-//   12-15     V from e4m3 to bf16 (the rows past the prefix zeroed), the queries
-//             of the next item, a tree's keys, values and ancestor bits.
+//   12-15     V from e4m3 to fp16 (the rows past the prefix zeroed).
 // Every wait is bounded; a timeout sets ADT_DEVERR_TIMEOUT.
+//
+// Bound by the instructions of a chunk, about 1500 of the softmax groups and the
+// widening warps each at 10 cycles an instruction of a warp (the roles' code
+// together is larger than the SM's instruction cache), 2900 cycles a chunk; the
+// tensor cores are busy a quarter of that.
 #include <math.h>
 
 #include <cuda.h>
@@ -118,7 +131,7 @@ struct AttnParams {
   const int32_t* parents;
   const int32_t* offs;
   int B, H, Hkv, group, max_nodes, max_kv, slot_rows;
-  int copies;          // of a row in a tile: 1, 2 or 4
+  int copies;          // of a row in a tile: 1 or 2
   int64_t sb, sh, ssb, ssh;
   float scale_log2;
   __nv_bfloat16* out;
@@ -930,7 +943,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int grp = warp >> 2, w4 = warp & 3, lrow = w4 * 32 + lane;
     const uint32_t lanes = static_cast<uint32_t>(w4 * 32) << 16;
     const uint32_t s_col = tmem + lanes + grp * kChunk, o_col = tmem + lanes + kOCol, p_col = tmem + lanes + kPCol + grp * 64;
-    // Copy c of a row takes the quarters [c, c + 1) 4 / copies of every chunk's keys.
+    // Copy c of a row takes the quarters [c, c + 1) 4 / copies of every chunk's keys, of four.
     const int copies = p.copies, span = kRows / copies, row = lrow & (span - 1);
     const int first_quarter = lrow / span * (4 / copies), end_quarter = first_quarter + 4 / copies;
     if (copies > 1) {  // the weights of other copies' keys stay zero
@@ -1326,7 +1339,7 @@ int slot_rows_for(int H, int Hkv, int max_nodes) {
 }
 
 // Tickets at the start, for any grid; two items' partial rows of each CTA; what is
-// prepared.  (Offsets from `base`, which may be NULL; at most 2^24 query rows, so
+// prepared where the items have more than 32 rows.  (Offsets from `base`, which may be NULL; at most 2^24 query rows, so
 // that all sizes stay below 2^50.)
 size_t ws_layout(uint8_t* base, int grid, int B, int H, int Hkv, int D, int max_nodes, AttnParams* p) {
   const int rows = slot_rows_for(H, Hkv, max_nodes);
@@ -1343,10 +1356,11 @@ size_t ws_layout(uint8_t* base, int grid, int B, int H, int Hkv, int D, int max_
   w.chunks = (max_nodes + kChunk - 1) / kChunk;
   const size_t bg = static_cast<size_t>(B) * Hkv, slots = 2 * static_cast<size_t>(grid) * rows;
   p->slot_rows = rows;
-  p->copies = rows <= 32 ? 4 : rows <= 64 ? 2 : 1;
+  p->copies = rows <= 64 ? 2 : 1;
   p->tickets = reinterpret_cast<unsigned*>(base);
   p->part_ml = reinterpret_cast<float2*>(take(slots * sizeof(float2)));
   p->part_o = reinterpret_cast<float4*>(take(slots * D * sizeof(float)));
+  if (rows <= kFewRows) return at;
   w.q = take(bg * w.blocks * 2 * w.q_rows * D);
   w.q_scale = reinterpret_cast<float*>(take(bg * w.blocks * w.q_rows * sizeof(float)));
   w.k = take(bg * w.chunks * 2 * w.t_rows * D);
@@ -1390,7 +1404,7 @@ adt_status launch(const AttnParams& p, const CUtensorMap& tm, const CUtensorMap&
     return adt::launch_status();
   };
   if (p.max_nodes * p.group <= 16) return few(tree_attn_q8_few_kernel<D, 16>, FewCfg<D, 16>::kDynSmem);
-  if (p.max_nodes * p.group <= 32) return few(tree_attn_q8_few_kernel<D, 32>, FewCfg<D, 32>::kDynSmem);
+  if (p.max_nodes * p.group <= kFewRows) return few(tree_attn_q8_few_kernel<D, 32>, FewCfg<D, 32>::kDynSmem);
   constexpr int kPass = kPrepThreads / (D / 16);
   const int64_t units = static_cast<int64_t>(p.max_nodes) * p.H + ((p.max_nodes + 15) & ~15) * static_cast<int64_t>(p.Hkv);
   cfg.gridDim = dim3(static_cast<unsigned>((units + kPass - 1) / kPass), static_cast<unsigned>(p.B), 1);

@@ -324,6 +324,59 @@ def test_cached_bytes_that_are_not_numbers(H, Hkv, D):
     assert torch.equal(torch.isnan(g["out"]), want) and torch.equal(g["out"][~want], clean[~want])
 
 
+@pytest.mark.parametrize("sizes,kv,H,Hkv,D", [([1, 1, 1], [700, 1000, 300], 8, 2, 128), ([1, 4, 2], [700, 1000, 300], 8, 2, 64),
+                                              ([8, 1, 5], [700, 1000, 300], 8, 2, 128), ([40, 9, 64], [700, 1000, 300], 4, 2, 64)])
+def test_value_scales_far_apart(sizes, kv, H, Hkv, D):
+    """Tree 0: two of three rows next to nothing, or zeros.  Tree 1: scales that rise along the cache.  Tree 2: no value
+    but zeros, whose scale is the least there is."""
+    case = Case(sizes, kv, H, Hkv, D)
+    at = torch.arange(case.rows)
+    case.vs[0, :, at % 3 == 0] = 20
+    case.vs[0, :, at % 3 == 1] = 7
+    case.vc.view(torch.uint8)[0, :, at % 3 == 1] = 0
+    case.vs[1] = (30 + at // 130 * 21).clamp(max=200).to(torch.uint8)
+    case.vc.view(torch.uint8)[2], case.vs[2] = 0, 7
+    case.vt[case.tb.node_offsets[2]:] = 0
+    case.vval = oracle.q8_values(case.vc.view(torch.uint8).numpy(), case.vs.numpy())
+    g = case.dev()
+    case.call(g)
+    case.check(g)
+    assert (g["out"][case.tb.node_offsets[2]:] == 0).all()
+    # A value that is not a number takes its rows' outputs, and leaves the weights' sum.
+    want = g["lse"].clone()
+    g["vs"][2, 0, 200] = 255
+    case.call(g)
+    n, group = case.tb.node_offsets[2], H // Hkv
+    assert torch.isnan(g["out"][n:, :group]).all() and (g["out"][n:, group:] == 0).all()
+    # (Exponents of up to 256, in fp32: 2^-17 of a weight each time, and of the sum's exponent.)
+    assert ((g["lse"] - want).abs() <= 2.0 ** -15).all() and B.adt_get_device_error() == 0
+
+
+@pytest.mark.parametrize("sizes,H,Hkv,D", [([1], 4, 1, 128), ([2], 8, 1, 64), ([8], 4, 1, 128), ([64], 1, 1, 64)])
+@pytest.mark.parametrize("step", [5.0, 0.5])
+def test_scores_that_grow_along_the_cache(sizes, H, Hkv, D, step):
+    """Every chunk's largest score is above all before, by more than what is let pass without scaling O, or less."""
+    case = Case(sizes, [2500], H, Hkv, D)
+    r = synth.rng(7, "grow")
+    base = r.standard_normal(D)
+    case.q = torch.from_numpy(np.tile(base, (case.n, H, 1))).to(torch.bfloat16)
+    scores = np.arange(case.rows) * (step / 128) + r.standard_normal(case.rows) * 0.3 - step * 19
+    keys = scores[:, None] * base / ((base ** 2).sum() * case.scale)
+    kc, ks = oracle.q8_rows(keys)
+    case.kc[0, 0], case.ks[0, 0] = torch.from_numpy(kc).view(torch.float8_e4m3fn), torch.from_numpy(ks)
+    case.kval = oracle.q8_values(case.kc.view(torch.uint8).numpy(), case.ks.numpy())
+    g = case.dev()
+    ws = case.call(g)
+    case.check(g)
+    first = g["out"].clone()
+    other = torch.empty(400 << 20, dtype=torch.uint8, device="cuda")
+    for i in range(10):
+        other.fill_(i)
+        case.call(g, ws=ws)
+        assert torch.equal(first, g["out"])
+    assert B.adt_get_device_error() == 0
+
+
 def test_another_stream_and_two_graphs_with_one_workspace():
     a, b = Case([1, 1], [3000, 700], 8, 2, 128), Case([64, 64], [300, 129], 8, 8, 64)
     ws = B.zeroed_workspace(max(B.adt_tree_attn_q8_workspace_size(**c.shape(max_kv=c.rows)) for c in (a, b)))
