@@ -878,6 +878,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // swizzle's eight rows is the same.
     static_assert(kPass % 8 == 0, "the swizzle repeats");
     const int swap = cl >> 2 & 1;
+    constexpr int kAtOnce = 4;
     const uint32_t from = static_cast<uint32_t>(cr * D + cl * 16);
     const uint32_t to[2] = {sw128_off(cr, 2 * cl + swap, kChunk), sw128_off(cr, 2 * cl + 1 - swap, kChunk)};
     uint32_t ended = 0, joins = 0;  // ended, bit i: chunk j - 1 - i was its item's last
@@ -916,13 +917,23 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int rows = w.t.L - k * kChunk - cr;
         const uint8_t* src = sV + st * C::kTile + from;
 #pragma unroll 1
-        for (int i = 0; i < kChunk / kPass; ++i) {
+        for (int i = 0; i < kChunk / kPass; i += kAtOnce) {
+          uint2 v[kAtOnce][2];
 #pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            uint2 v = make_uint2(0u, 0u);  // (rows past the prefix: anything in the cache, zeros here)
-            if (i * kPass < rows) v = *reinterpret_cast<const uint2*>(src + i * kPass * D + 8 * (x ^ swap));
-            *reinterpret_cast<uint4*>(wide + to[x] + i * kPass * 128) =
-                make_uint4(e4m3x2_to_f16(v.x), e4m3x2_to_f16(v.x >> 16), e4m3x2_to_f16(v.y), e4m3x2_to_f16(v.y >> 16));
+          for (int y = 0; y < kAtOnce; ++y) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              v[y][x] = make_uint2(0u, 0u);  // (rows past the prefix: anything in the cache, zeros here)
+              if ((i + y) * kPass < rows) v[y][x] = *reinterpret_cast<const uint2*>(src + (i + y) * kPass * D + 8 * (x ^ swap));
+            }
+          }
+#pragma unroll
+          for (int y = 0; y < kAtOnce; ++y) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+              *reinterpret_cast<uint4*>(wide + to[x] + (i + y) * kPass * 128) =
+                  make_uint4(e4m3x2_to_f16(v[y][x].x), e4m3x2_to_f16(v[y][x].x >> 16), e4m3x2_to_f16(v[y][x].y),
+                             e4m3x2_to_f16(v[y][x].y >> 16));
           }
         }
         sm100::fence_proxy_async_smem();
