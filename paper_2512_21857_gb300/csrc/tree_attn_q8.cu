@@ -878,7 +878,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // swizzle's eight rows is the same.
     static_assert(kPass % 8 == 0, "the swizzle repeats");
     const int swap = cl >> 2 & 1;
-    constexpr int kAtOnce = 4;
+    constexpr int kAtOnce = 2;
     const uint32_t from = static_cast<uint32_t>(cr * D + cl * 16);
     const uint32_t to[2] = {sw128_off(cr, 2 * cl + swap, kChunk), sw128_off(cr, 2 * cl + 1 - swap, kChunk)};
     uint32_t ended = 0, joins = 0;  // ended, bit i: chunk j - 1 - i was its item's last
