@@ -81,7 +81,7 @@ constexpr int kMaxScaleSlots = 16;
 constexpr int kMaxStages = 6;
 constexpr int kMaxGrid = 1024;          // tickets of the workspace
 constexpr uint32_t kTmemCols = 512;
-constexpr uint32_t kOCol = 256, kPCol = 384;  // after two S tiles of 128 columns; two P tiles of 64
+constexpr uint32_t kTiles = 3, kOCol = kTiles * kChunk;  // S tiles of 128 columns, whose first 64 P takes as it is made; O
 constexpr uint32_t kWaitLimit = 1u << 22;
 constexpr uint32_t kDrainLimit = 1u << 20;  // of the waits for what is in flight
 constexpr float kLog2e = 1.44269504088896340736f;
@@ -105,7 +105,7 @@ struct Cfg {
   static constexpr int kDynSmem = kJoinOff + (D == 128 ? 0 : 2 * kRows * 32 * 4) + 1024;  // + alignment slack
   static_assert(D != 128 || kWide == 2 * kRows * 32 * 4, "copies are joined in a V tile");
   static constexpr uint32_t kIdescO = sm100::idesc_f16_f32(kRows, D, 0, 1);
-  static_assert(kKStages <= kMaxStages && kVStages <= kMaxStages && kScaleSlots <= kMaxScaleSlots && kOCol + D <= kPCol, "sizes");
+  static_assert(kKStages <= kMaxStages && kVStages <= kMaxStages && kScaleSlots <= kMaxScaleSlots && kOCol + D <= kTmemCols, "sizes");
 };
 
 // What the first launch makes of the queries and of the trees, as the second one's
@@ -302,7 +302,7 @@ struct Bars {
   uint64_t scale_full[kMaxScaleSlots];
   uint64_t wide_full[2];     // a V tile in bf16
   uint64_t q_full[2], q_free[2];
-  uint64_t s_full[2], s_free[2], p_full[2];
+  uint64_t s_full[4], p_full[4];
   uint64_t mu[2][4];         // the running maxima after a chunk are in shared memory, per group and warp
   uint64_t done[4];          // the PV product of chunk j is done (barrier j % 4)
   uint64_t o_free;           // an item's O is read
@@ -576,9 +576,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     init(bars.wide_full, 2, 4);
     init(bars.q_full, 2, 1);
     init(bars.q_free, 2, 1);
-    init(bars.s_full, 2, 1);
-    init(bars.s_free, 2, 4);
-    init(bars.p_full, 2, 4);
+    init(bars.s_full, 4, 1);
+    init(bars.p_full, 4, 4);
     init(bars.mu[0], 8, 1);
     init(bars.done, 4, 1);
     init(&bars.o_free, 1, 8);
@@ -680,7 +679,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       if (have) {
         // The scales of the chunk before.  Their slot was read last for a chunk
-        // kScaleSlots before, which was done with before S of four chunks on could
+        // kScaleSlots before, which was done with before S of three chunks on could
         // start, and S(j - KS) is done.
         static_assert(kScaleSlots >= KS + 4, "a slot that is read");
         uint32_t most = 0u;
@@ -804,11 +803,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint64_t q = qd0 + (item & 1) * (2 * C::kTile / 16);
         ok = wait(&bars.q_full[item & 1], item >> 1);
         for (int k = w.k0; ok && k < w.k1; ++k, ++j) {
-          const int grp = j & 1;
-          ok = wait(&bars.k_full[st], phase) && (j < 2 || wait(&bars.s_free[grp], (j >> 1) - 1));
+          // The tile was S(j - 3)'s and then P's.
+          ok = wait(&bars.k_full[st], phase) && (j < kTiles || wait(&bars.done[(j - kTiles) & 3], (j - kTiles) >> 2));
           if (!ok) break;
           sm100::tc_fence_after();
-          const uint32_t d = tmem + grp * kChunk;
+          const uint32_t d = tmem + j % kTiles * kChunk;
           const int keys = k < w.t.prefix ? w.t.L - k * kChunk : w.t.n - (k - w.t.prefix) * kChunk;
           const uint32_t idesc = sm100::idesc_e4m3_f32(kRows, 0) | static_cast<uint32_t>(min(kChunk, (keys + 15) & ~15) >> 3) << 17;
           // The queries' high and low part with the keys, of a tree with their low part too.
@@ -825,7 +824,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
           }
           if (k >= w.t.prefix) sm100::mma_commit(sm100::smem_addr(&bars.v_free[j % VS]));
-          sm100::mma_commit(sm100::smem_addr(&bars.s_full[grp]));
+          sm100::mma_commit(sm100::smem_addr(&bars.s_full[j & 3]));
           sm100::mma_commit(sm100::smem_addr(&bars.k_free[st]));
           if (++st == KS) {
             st = 0;
@@ -847,11 +846,11 @@ __global__ void __launch_bounds__(kThreads, 1)
       uint32_t item = 0;
       for (; ok && w.more; w = next_item(p, w), ++item) {
         for (int k = w.k0; ok && k < w.k1; ++k, ++j) {
-          ok = wait(&bars.p_full[j & 1], j >> 1) && wait(&bars.wide_full[j & 1], j >> 1) &&
+          ok = wait(&bars.p_full[j & 3], j >> 2) && wait(&bars.wide_full[j & 1], j >> 1) &&
                (k > w.k0 || item == 0 || wait(&bars.o_free, item - 1));
           if (!ok) break;
           sm100::tc_fence_after();
-          const uint32_t a = tmem + kPCol + (j & 1) * 64;
+          const uint32_t a = tmem + j % kTiles * kChunk;
           const uint64_t vd = wd0 + (j & 1) * (C::kWide / 16);
           const int keys = k < w.t.prefix ? w.t.L - k * kChunk : w.t.n - (k - w.t.prefix) * kChunk;
           const int steps = min(kChunk / 16, (keys + 15) / 16);
@@ -953,16 +952,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     // ------------------------------------------------------------ softmax
     const int grp = warp >> 2, w4 = warp & 3, lrow = w4 * 32 + lane;
     const uint32_t lanes = static_cast<uint32_t>(w4 * 32) << 16;
-    const uint32_t s_col = tmem + lanes + grp * kChunk, o_col = tmem + lanes + kOCol, p_col = tmem + lanes + kPCol + grp * 64;
+    const uint32_t o_col = tmem + lanes + kOCol;
     // Copy c of a row takes the quarters [c, c + 1) 4 / copies of every chunk's keys, of four.
     const int copies = p.copies, span = kRows / copies, row = lrow & (span - 1);
     const int first_quarter = lrow / span * (4 / copies), end_quarter = first_quarter + 4 / copies;
-    if (copies > 1) {  // the weights of other copies' keys stay zero
-      uint32_t zero[32] = {};
-      tmem_st_32(p_col, zero);
-      tmem_st_32(p_col + 32, zero);
-      sm100::tmem_wait_st();
-    }
     uint32_t item = 0;
     bool ok = true;
     for (; ok && w.more; w = next_item(p, w), ++item) {
@@ -979,18 +972,14 @@ __global__ void __launch_bounds__(kThreads, 1)
         const bool tree_j = k >= w.t.prefix;
         uint4 seen = make_uint4(0u, 0u, 0u, 0u);
         if (tree_j && valid) seen = p.pre.seen[(static_cast<int64_t>(w.b) * p.max_nodes + node) * p.pre.chunks + k - w.t.prefix];
-        if (!all_wait(&bars.s_full[grp], j >> 1) || !all_wait(&bars.scale_full[slot], j / kScaleSlots)) {
+        if (!all_wait(&bars.s_full[j & 3], j >> 2) || !all_wait(&bars.scale_full[slot], j / kScaleSlots)) {
           ok = false;
           break;
         }
         sm100::tc_fence_after();
         const int kl = tree_j ? w.t.n - (k - w.t.prefix) * kChunk : w.t.L - k * kChunk;
         const int quarters = min(end_quarter, (kl + 31) / 32);
-        auto release_s = [&]() {  // S is in registers: its tile may be written again
-          sm100::tc_fence_before();
-          __syncwarp();
-          if (lane == 0) arrive(&bars.s_free[grp]);
-        };
+        const uint32_t s_col = tmem + lanes + j % kTiles * kChunk;
         if (active) {
           const ulonglong2* ks = reinterpret_cast<const ulonglong2*>(s_scale + slot * 2 * kChunk);
           const ulonglong2* vf = ks + kChunk / 4;
@@ -1043,13 +1032,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           __syncwarp();
           if (lane == 0) arrive(&bars.mu[grp][w4]);
           if (nm != mu) l *= ex2_approx(mu - nm);
-          // P's tile was last read by PV(j - 2).
-          if (j >= 2 && !all_wait(&bars.done[(j - 2) & 3], (j - 2) >> 2)) {
-            ok = false;
-            break;
-          }
           const float drop = s_drop[slot];
           if (j > j0 && __any_sync(adt::kFullMask, nm != prev || drop != 1.f)) {
+            // (PV(j - 5), whose phase comes before, is done: S(j) is, after PV(j - 3).)
             if (!all_wait(&bars.done[(j - 1) & 3], (j - 1) >> 2)) {
               ok = false;
               break;
@@ -1089,34 +1074,30 @@ __global__ void __launch_bounds__(kThreads, 1)
                 pk[2 * e + h] = pack_half2(a, b);
               }
             }
-            sm100::tmem_st_8(p_col + 8 * s, pk);
+            sm100::tmem_st_8(s_col + 8 * s, pk);  // over scores that have been read
           }
-          release_s();
+          if (copies > 1) {  // the weights of the other copy's keys
+            const uint32_t zero[16] = {};
+            tmem_st_16(s_col + (first_quarter ? 0 : 32), zero);
+            tmem_st_16(s_col + (first_quarter ? 16 : 48), zero);
+          }
           float la, lb, lc, ld;
           unpack_f32x2(l2[0], la, lb);
           unpack_f32x2(l2[1], lc, ld);
           l += (la + lb) + (lc + ld);
           sm100::tmem_wait_st();
         } else {
-          // A warp without rows only keeps the barriers moving, within the chunk as
-          // the others: its arrival for P(j) must not fall into the phase of P(j - 2).
-          if (lane == 0) {
-            arrive(&bars.mu[grp][w4]);
-            arrive(&bars.s_free[grp]);
-          }
-          if (j >= 2 && !all_wait(&bars.done[(j - 2) & 3], (j - 2) >> 2)) {
-            ok = false;
-            break;
-          }
+          // A warp without rows only keeps the barriers moving.
+          if (lane == 0) arrive(&bars.mu[grp][w4]);
         }
         sm100::tc_fence_before();
         __syncwarp();
-        if (lane == 0) arrive(&bars.p_full[grp]);
+        if (lane == 0) arrive(&bars.p_full[j & 3]);
       }
       j = j1;
       // The item's O, unnormalised: group 0 takes the first half of its columns,
-      // group 1 the second.  (PV(j1 - 5) is known done: this group's or the other's
-      // last P waited for PV(j1 - 4) at least.)
+      // group 1 the second.  (PV(j1 - 5) is known done: this group's last S, of chunk
+      // j1 - 2 at least, came after it, or the item before ended later.)
       ok = ok && all_wait(&bars.done[(j1 - 1) & 3], (j1 - 1) >> 2);
       sm100::tc_fence_after();
       constexpr int kHalf = D / 2;
