@@ -112,14 +112,14 @@ const char* adt_status_string(adt_status s);
 
 /* Testing hook, not for production use.  Every wait of adt_tree_attn's
  * pipeline (a CTA waiting for its loads, products or softmax stages), of
- * adt_kv_score's, and of adt_tree_accept's sampling walks (a CTA waiting for its
- * cluster's values) is bounded: after `polls` unsuccessful polls it gives up, sets
- * ADT_DEVERR_TIMEOUT in the device error word and the kernel leaves cleanly
- * (the copies and tensor-core products it already issued, and the stores to
- * it that are on their way, are waited for first, so the device stays usable;
- * the outputs of that call are unspecified).  This sets the bound for the
- * launches that follow in this process; 0 restores the defaults (2^20, 2^24 and
- * 2^22 polls), 1 makes every wait of a sampling walk give up.  It lets a
+ * adt_tree_attn_q8's and adt_kv_score's, and of adt_tree_accept's sampling walks (a
+ * CTA waiting for its cluster's values) is bounded: after `polls` unsuccessful polls
+ * it gives up, sets ADT_DEVERR_TIMEOUT in the device error word and the kernel
+ * leaves cleanly (the copies and tensor-core products it already issued, and the
+ * stores to it that are on their way, are waited for first, so the device stays
+ * usable; the outputs of that call are unspecified).  This sets the bound for the
+ * launches that follow in this process; 0 restores the defaults (2^20, 2^22, 2^24
+ * and 2^22 polls), 1 makes every wait of a sampling walk give up.  It lets a
  * test make a bounded wait run out without any fault; it is not synchronised
  * with calls on other threads. */
 adt_status adt_testing_set_wait_limit(uint32_t polls);
@@ -624,6 +624,9 @@ adt_status adt_kv_evict(const adt_bf16* k_src, const adt_bf16* v_src, int64_t sr
  * own k_tree and v_tree, parents, out and lse as there; a plain decoding step
  * is trees of one node).  Scores, softmax and sums are made from the values the
  * rows stand for.  Rows behind kv_len[b] are not used, whatever they hold.
+ * A row of q that is not finite, or of k_tree for those who see it, makes its
+ * outputs NaN; an element of v_tree that is not finite reaches its column for those
+ * who see it.
  * 1 <= max_nodes <= 256, any H % Hkv == 0, B * max_nodes * H <= 2^24.
  * Errors as for adt_tree_attn.
  * ------------------------------------------------------------------------ */

@@ -10,6 +10,11 @@
 // the partner of every rotated element lies in the same lane: two vectors of 8, in
 // a half layout those of a pair's two sides.  So a norm costs two or four rounds of
 // shuffles of one value and the rotation none.
+//
+// Bound by HBM, each element is read and written once: 16384 tokens of 32 / 32 heads
+// x 128 in bf16 (805 MB) 146 us, 82 % of a copy's rate; between a unit's load and
+// its store lie the sums' shuffles, which the next unit's load hides in part.  501
+// tokens of 32 / 8 heads in fp32 with a LayerNorm 9.4 us, one token 4.1 us (its launch).
 #include <math.h>
 
 #include "adt_common.cuh"
@@ -265,8 +270,8 @@ adt_status launch(const NormParams& p, bool vec, int N, const adt::DeviceInfo& i
   const int heads = p.heads[0] + p.heads[1];
   if (vec) {
     const int units = p.D / kUnit, width = adt::next_pow2(units);
-    // Threads of a token, as adt_rope_qkv chooses them: one unit of its heads and
-    // one pair of vectors of its values each, or with many tokens two of each.
+    // Threads of a token: one unit of its heads and one pair of vectors of its values
+    // each, or with many tokens two of each.
     const int qk = heads * width, vs = (p.heads[2] * units + 1) / 2, want = qk > vs ? qk : vs;
     auto lanes_of = [&](int each) {
       int l = ((want + each - 1) / each + 31) / 32 * 32;
@@ -276,6 +281,9 @@ adt_status launch(const NormParams& p, bool vec, int N, const adt::DeviceInfo& i
     const int lanes = lanes_of(many ? 2 : 1);
     const int tokens = kThreads / lanes;
     const int passes = (want + lanes - 1) / lanes;
+    // With many tokens up to four of them a CTA, so that the next one's rows are on their
+    // way while one is normed (16384 tokens 146 us; 175 with one a CTA and each unit
+    // loaded when it is normed), but not all in a few CTAs an SM (152 to 162).
     int turns = 1;
     while (turns < kMaxTurns && static_cast<int64_t>(N) >= int64_t{2} * turns * tokens * kTurnCtas * info.sm_count) turns *= 2;
     const int groups = (N + tokens * turns - 1) / (tokens * turns);
