@@ -542,6 +542,10 @@ __global__ void __launch_bounds__(kPrepThreads) prepare_kernel(const AttnParams 
   }
 }
 
+// What was prepared may be read after this.  (The launch before lets this one start
+// once all work before it is done, so the caller's tensors may be read at any time.)
+__device__ __forceinline__ void await_prepared() { asm volatile("griddepcontrol.wait;\n" ::: "memory"); }
+
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
     tree_attn_q8_kernel(const __grid_constant__ CUtensorMap tm_k, const AttnParams p) {
@@ -590,7 +594,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     sm100::tmem_relinquish();
   }
   if (warp == kKWarp && lane == 0) sm100::prefetch_tensormap(&tm_k);
-  asm volatile("griddepcontrol.wait;\n" ::: "memory");
   if (warp == 0) find_share(p, lane, &s_walk, &s_total, &s_grid, nullptr);
   sm100::tc_fence_before();
   __syncthreads();
@@ -598,6 +601,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t tmem = tmem_slot;
   Walk w = s_walk;
   if (!w.some()) {  // (all threads alike)
+    await_prepared();
     __syncthreads();
     if (warp == kPvWarp) sm100::tmem_dealloc(tmem, kTmemCols);
     return;
@@ -647,9 +651,22 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         ok = __shfl_sync(adt::kFullMask, ok ? 1 : 0, 0) != 0;
         if (!ok) break;
+        if (tree_k && j == 0) await_prepared();
+        if (lane == 0) {
+          const uint32_t bar = sm100::smem_addr(&bars.k_full[st]), dst = sm100::smem_addr(sK + st * C::kTile);
+          if (tree_k) {  // (the low part comes from warp 9 to the same barrier)
+            const int bytes = min(kChunk, (keys + 15) & ~15) * D;
+            sm100::mbar_arrive_expect_tx(bar, 2 * bytes);
+            sm100::bulk_load(dst, p.pre.k + chunk * 2 * p.pre.t_rows * D, bytes, bar);
+          } else {
+            sm100::mbar_arrive_expect_tx(bar, C::kTile);
+            sm100::tma_load_4d(dst, &tm_k, 0, k * kChunk, w.g, w.b, bar);
+          }
+        }
         if (fresh) {
           // Without a prefetch this warp waited for memory once a chunk, 2000 cycles of 2800.
           prefetch_scale(k + (lane >> 2), lane);
+          if (j == 0) await_prepared();
           if (lane == 0) {  // the item's queries, `copies` times
             const int rows = (min(w.t.n * p.group - w.blk * kRows, kRows) + 7) & ~7;
             const uint32_t bar = sm100::smem_addr(&bars.q_full[item & 1]);
@@ -662,17 +679,6 @@ __global__ void __launch_bounds__(kThreads, 1)
               sm100::bulk_load(dst + C::kTile + c * (C::kTile / p.copies), src + p.pre.q_rows * D, rows * D, bar);
             }
             q_issued = item + 1;
-          }
-        }
-        if (lane == 0) {
-          const uint32_t bar = sm100::smem_addr(&bars.k_full[st]), dst = sm100::smem_addr(sK + st * C::kTile);
-          if (tree_k) {  // (the low part comes from warp 9 to the same barrier)
-            const int bytes = min(kChunk, (keys + 15) & ~15) * D;
-            sm100::mbar_arrive_expect_tx(bar, 2 * bytes);
-            sm100::bulk_load(dst, p.pre.k + chunk * 2 * p.pre.t_rows * D, bytes, bar);
-          } else {
-            sm100::mbar_arrive_expect_tx(bar, C::kTile);
-            sm100::tma_load_4d(dst, &tm_k, 0, k * kChunk, w.g, w.b, bar);
           }
         }
         issued = j + 1;
@@ -759,6 +765,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             break;
           }
           if (k >= w.t.prefix) {
+            await_prepared();
             // The low part of the tree's keys, once the chunk before in that slot of K
             // is done with, and its barrier's phase with it.  (S(j - 2 KS) is: V(j - VS)
             // was widened after PV(j - VS - 2).)
@@ -901,6 +908,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         ended = ended << 1 | (k + 1 == w.k1 ? 1u : 0u);
         if (tree_k) {  // the tree's are prepared
           if (ct == 0) {
+            await_prepared();
             const int c = k - w.t.prefix, rows = min(kChunk, (w.t.n - c * kChunk + 15) & ~15);
             const int64_t chunk = (static_cast<int64_t>(w.b) * p.Hkv + w.g) * p.pre.chunks + c;
             const uint32_t bar = sm100::smem_addr(&bars.wide_full[j & 1]);
@@ -956,6 +964,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // Copy c of a row takes the quarters [c, c + 1) 4 / copies of every chunk's keys, of four.
     const int copies = p.copies, span = kRows / copies, row = lrow & (span - 1);
     const int first_quarter = lrow / span * (4 / copies), end_quarter = first_quarter + 4 / copies;
+    await_prepared();
     uint32_t item = 0;
     bool ok = true;
     for (; ok && w.more; w = next_item(p, w), ++item) {
