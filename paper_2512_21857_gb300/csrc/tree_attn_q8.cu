@@ -1239,52 +1239,48 @@ __global__ void __launch_bounds__(kThreads, 1)
         softmax_sync();
         if (s_last) {
           // Partial rows joined: weights 2^(m_c - M) over their sum.  Neighbouring lanes
-          // take neighbouring rows, a thread 16 columns at a time, of two CTAs' parts.
+          // take neighbouring rows, a thread 16 columns at a time, of four CTAs' parts.
+          constexpr int kAtOnce = 4;
           const int rows = min(w.t.n * p.group - w.blk * kRows, kRows);
           const int shift = 32 - __clz(rows - 1), jr = tid & ((1 << shift) - 1);  // (rows rounded up to a power of two)
           const int slot0 = first * 2 + (first * X / G >= w.start ? 0 : 1);
           auto slot_of = [&](int c) -> int64_t { return c == first ? slot0 : 2 * c; };
           if (jr < rows) {
-            float Mj = -INFINITY, lj = 0.f;
-#pragma unroll 2
+            float Mj = -INFINITY;
+#pragma unroll 4
             for (int c = first; c <= last; ++c) Mj = fmaxf(Mj, __ldcg(&p.part_ml[slot_of(c) * p.slot_rows + jr]).x);
-#pragma unroll 2
-            for (int c = first; c <= last; ++c) {
-              const float2 ml = __ldcg(&p.part_ml[slot_of(c) * p.slot_rows + jr]);
-              lj += ml.y * weight(ml.x, Mj);
-            }
-            const float invj = __fdividef(1.f, lj);
             const int idx = w.blk * kRows + jr, tj = idx / p.group;
             const int64_t at = static_cast<int64_t>(w.t.node0 + tj) * p.H + w.g * p.group + idx - tj * p.group;
 #pragma unroll 1
             for (int c16 = tid >> shift; c16 < D / 16; c16 += kSoftmaxThreads >> shift) {
+              float lj = 0.f;
               float4 acc[4] = {};
 #pragma unroll 1
-              for (int c = first; c <= last; c += 2) {
-                const bool two = c < last;
-                float wt[2] = {0.f, 0.f};
-                float4 v[2][4] = {};
+              for (int c = first; c <= last; c += kAtOnce) {
+                float2 ml[kAtOnce];
+                float4 v[kAtOnce][4];
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                  if (x == 1 && !two) continue;
-                  const int64_t sl = slot_of(c + x);
-                  wt[x] = __ldcg(&p.part_ml[sl * p.slot_rows + jr]).x;
+                for (int x = 0; x < kAtOnce; ++x) {
+                  const int64_t sl = slot_of(min(c + x, last));
+                  ml[x] = __ldcg(&p.part_ml[sl * p.slot_rows + jr]);
 #pragma unroll
                   for (int e = 0; e < 4; ++e) v[x][e] = __ldcg(p.part_o + (sl * (D / 4) + c16 * 4 + e) * p.slot_rows + jr);
                 }
-                wt[0] = weight(wt[0], Mj);
-                wt[1] = two ? weight(wt[1], Mj) : 0.f;
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
+                for (int x = 0; x < kAtOnce; ++x) {
+                  if (c + x > last) break;
+                  const float wt = weight(ml[x].x, Mj);
+                  lj += wt * ml[x].y;
 #pragma unroll
                   for (int e = 0; e < 4; ++e) {
-                    acc[e].x += wt[x] * v[x][e].x;
-                    acc[e].y += wt[x] * v[x][e].y;
-                    acc[e].z += wt[x] * v[x][e].z;
-                    acc[e].w += wt[x] * v[x][e].w;
+                    acc[e].x += wt * v[x][e].x;
+                    acc[e].y += wt * v[x][e].y;
+                    acc[e].z += wt * v[x][e].z;
+                    acc[e].w += wt * v[x][e].w;
                   }
                 }
               }
+              const float invj = __fdividef(1.f, lj);
               uint32_t y[8];
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
