@@ -39,10 +39,14 @@
 //   12-15     V from e4m3 to fp16 (the rows past the prefix zeroed).
 // Every wait is bounded; a timeout sets ADT_DEVERR_TIMEOUT.
 //
-// Bound by the instructions of a chunk, about 1500 of the softmax groups and the
-// widening warps each at 10 cycles an instruction of a warp (the roles' code
-// together is larger than the SM's instruction cache), 2900 cycles a chunk; the
-// tensor cores are busy a quarter of that.
+// Bound by the turns of the softmax groups: of a chunk a group takes 2900 cycles with
+// 64 rows (each twice) and 4500 with 128, of which waits for tensor memory, shared
+// memory and the other group are more than half (issue slots 41 % busy, tensor cores
+// 23 %), and two groups take chunks in turn; V's widening keeps up.  Measured: four
+// trees of 64, 64, 27 and 64 nodes over 1444 to 2400 rows, 32 / 32 heads x 128, 40 us
+// (11 at HBM's rate), 5 of them the launch before; trees of 64 nodes over 3500 to
+// 6001 rows, 32 / 8 heads x 128, 48 us (11 at the tensor cores' bf16 rate), 5 of them
+// the joining of cut items.
 #include <math.h>
 
 #include <cuda.h>
@@ -70,7 +74,8 @@ constexpr int kRows = 128;              // query rows of an item
 constexpr int kChunk = 128;             // keys of a chunk
 constexpr int kMaxTreeNodes = 256;
 constexpr int64_t kMaxRows = 1 << 24;   // query rows of a call
-constexpr int kItemCost = 4;            // chunks that an item's start and end take the time of
+constexpr int kItemCost = 4;            // chunks that an item's start and end take the time of (decode over ragged caches:
+                                        // 85 us with 3 to 6 of them, 101 with 1)
 constexpr int kJoinCost = 6;            // ... and that joining an item's parts takes
 constexpr int kMinShare = 6;            // coordinates (see Walk) of a CTA's share, where there are few
 constexpr int kSoftmaxThreads = 256;
@@ -401,7 +406,7 @@ __device__ __forceinline__ void group_sync(int grp) {  // of the four warps of a
     asm volatile("bar.sync 4, 128;\n" ::: "memory");
 }
 
-constexpr int kAhead = 8;  // chunks: as many as a warp's lanes prefetch at once
+constexpr int kAhead = 8;  // chunks whose scales are asked for ahead: as many as a warp's lanes prefetch at once
 __device__ __forceinline__ void prefetch_l2(const void* src) { asm volatile("prefetch.global.L2 [%0];\n" ::"l"(src)); }
 
 // A bounded wait, as short as it can be (its callers are many, and the instruction
@@ -432,8 +437,8 @@ __device__ __forceinline__ float power_of_two(int e) {
 
 // The first launch: a row is D / 16 lanes', 16 elements each.  Of a tree the query
 // rows, then its nodes' rows of every kv head (zeros up to a multiple of 16 nodes).
-// Bound by its launch and two rounds of loads (trees of 64 nodes, 32 / 8 heads x
-// 128, are 2 MB); within the second one, every item and every share of one would do
+// Bound by its launch and two rounds of loads (four trees of 64 nodes, 32 / 32 heads x
+// 128: 5 us more for a call); within the second one, every item and every share of one would do
 // it anew, by warps that have other work.
 constexpr int kPrepThreads = 256;
 

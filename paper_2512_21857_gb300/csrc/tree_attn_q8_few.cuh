@@ -20,10 +20,18 @@
 // 2^-60 there, so that its part of the row sum is neither lost nor too large.
 //
 // Warp roles: 0-3, 4-7 two softmax groups that take the chunks in turn; 8 K tiles, 9 V
-// tiles; 10 S products; 11 PV products; 12-15 the next item's queries and, with the
-// tree's chunk, its rows cut into e4m3 rows: keys into two as the queries, values,
-// whose sums are to 2^-8 of each element, into three 2^-4 apart.
-
+// tiles; 10 S products; 11 PV products; 12-15 an item's start and end beside the
+// chunks of the items around it: queries and, with the tree's chunk, its rows cut
+// into e4m3 rows (keys into two as the queries; values, whose sums are to 2^-8 of
+// each element, into three 2^-4 apart), and O, which has a place for two items, read
+// out and joined.
+//
+// Bound by HBM where caches are long: 16 sequences of 1 to 30011 rows, 32 / 8 heads x
+// 128 (353 MB) 74 us, 70 % of a copy's rate.  Within an item the tiles come at 5.5
+// TB/s, which is what a plain kernel that only reads them gets with cold caches too;
+// about 15 us are the shares' calculation, the first tiles' way and the last one's.
+// Short ones are a chain of waits: one sequence of 512 rows, 8 heads x 64, 11.4 us.
+// (The kernel of 128 rows took 115 and 13.)
 constexpr int kFewRows = 32;
 constexpr float kFewThreshold = 4.5f, kFewHeadroom = 4.f;  // weights up to 2^8.5: e4m3 ends at 448
 constexpr float kUnset = -3e38f;  // the base of a row that has seen no key
@@ -254,6 +262,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (!ok) break;
           sm100::tc_fence_after();
           // The queries' high and low part with the keys, of a tree with their low part too.
+          // (A tree's tile is 128 rows from its 32 on, up to the weights at most: scores of
+          // keys that there are not, which no row sees.)
           const int parts = tree_k ? 4 : 2;
           uint32_t more = 0u;
 #pragma unroll 1
