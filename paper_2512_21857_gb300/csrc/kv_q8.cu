@@ -47,7 +47,7 @@ __global__ void __launch_bounds__(kThreads) kv_compact_q8_kernel(const CompactQ8
   int bad = 0;
   for (int j = tid; fits && j <= a; j += kThreads) {
     const int node = path[j];
-    bad |= node < 0 || node >= n || (j == 0 && node != 0);
+    bad |= node < 0 || node >= n || node0 < 0 || (j == 0 && node != 0);
   }
   bad = __syncthreads_or(bad);
   const bool ok = fits && !bad;

@@ -155,9 +155,9 @@ struct Tree {
 // Tree b; one that is malformed or out of range has no items.
 __device__ __forceinline__ Tree tree_of(const AttnParams& p, int b, unsigned* bits) {
   Tree t;
-  t.node0 = p.offs[b];
-  t.n = p.offs[b + 1] - t.node0;
-  t.L = p.kv_len[b];
+  t.node0 = __ldcg(p.offs + b);
+  t.n = __ldcg(p.offs + b + 1) - t.node0;
+  t.L = __ldcg(p.kv_len + b);
   const bool bad_tree = t.n < 1 || t.n > p.max_nodes || t.node0 < 0, bad_kv = t.L < 0 || t.L > p.max_kv;
   *bits |= bad_tree ? ADT_DEVERR_BAD_TREE : bad_kv ? ADT_DEVERR_KV_RANGE : 0u;
   if (bad_tree || bad_kv) t.n = t.L = 0;
@@ -548,7 +548,8 @@ __global__ void __launch_bounds__(kPrepThreads) prepare_kernel(const AttnParams 
 }
 
 // What was prepared may be read after this.  (The launch before lets this one start
-// once all work before it is done, so the caller's tensors may be read at any time.)
+// once all work before it is done, so the caller's tensors may be read at any time:
+// past L1, which may hold what an earlier launch read.)
 __device__ __forceinline__ void await_prepared() { asm volatile("griddepcontrol.wait;\n" ::: "memory"); }
 
 template <int D>
@@ -728,8 +729,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         pend[0][i] = 127u;
         pend[1][i] = pend[2][i] = 0u;
         if (i < left) {
-          pend[0][i] = src[i];
-          pend[1][i] = vsrc[i];
+          pend[0][i] = __ldcg(src + i);
+          pend[1][i] = __ldcg(vsrc + i);
           if (tree_k) pend[2][i] = vsrc[p.pre.t_rows + i];
         }
       }

@@ -110,6 +110,17 @@ def test_matches_oracle(sizes, kv, H, Hkv, D):
     assert B.adt_get_device_error() == 0
 
 
+@pytest.mark.parametrize("n,H,Hkv", [(16, 2, 2), (17, 2, 2), (32, 3, 3), (33, 2, 2), (4, 8, 2), (5, 6, 2), (8, 4, 1), (9, 8, 2),
+                                     (1, 16, 1), (1, 17, 1), (1, 32, 1), (1, 33, 1), (64, 1, 1), (13, 5, 1)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_numbers_of_rows_at_which_another_kernel_begins(n, H, Hkv, D):
+    case = Case([n, max(n - 1, 1)], [389, 95], H, Hkv, D)
+    g = case.dev()
+    case.call(g)
+    case.check(g)
+    assert B.adt_get_device_error() == 0
+
+
 @pytest.mark.parametrize("sizes,kv,H,Hkv,D", [([64, 9], [512, 100], 8, 4, 64), ([1, 1], [1000, 30], 16, 4, 128)])
 def test_longer_caches_and_larger_trees_than_there_are(sizes, kv, H, Hkv, D):
     case = Case(sizes, kv, H, Hkv, D, spare=5000)
@@ -461,3 +472,39 @@ def test_norm_commit_and_attention_together():
                     max_nodes=1, max_kv=rows, softmax_scale=nxt.scale, out=out,
                     workspace=B.zeroed_workspace(B.adt_tree_attn_workspace_size(1, H, D, 1, rows)))
     assert (out.double() - g["out"].double()).abs().max() < 2e-2
+
+
+@pytest.mark.parametrize("n,H,Hkv,D", [(64, 4, 4, 128), (40, 8, 2, 64), (8, 4, 2, 128), (1, 8, 8, 64)])
+def test_steps_one_after_the_other_read_what_the_commits_before_wrote(n, H, Hkv, D):
+    """Attention, commit, attention, ..., never waited for, equal the same with the device idle before every call."""
+    steps, L, take = 30, 200, min(n, 3)
+    rows = L + steps * take
+    case = Case([n], [L], H, Hkv, D, spare=steps * take, chain=True)
+    shape = dict(B=1, Hkv=Hkv, D=D, num_layers=1, max_kv=rows)
+    other = torch.empty(300 << 20, dtype=torch.uint8, device="cuda")
+
+    def run(idle):
+        g = case.dev()
+        ws = B.zeroed_workspace(B.adt_tree_attn_q8_workspace_size(**case.shape(max_kv=rows)))
+        kv = [i32([L]) for _ in range(steps + 1)]
+        kt, vt = g["kt"].clone(), g["vt"].clone()
+        outs = [torch.empty_like(g["out"]) for _ in range(steps)]
+        path, alen = i32([list(range(take))]), i32([take - 1])
+        for i in range(steps):
+            if idle:
+                torch.cuda.synchronize()
+                other.fill_(i)
+                torch.cuda.synchronize()
+            g["out"], g["kv"] = outs[i], kv[i]
+            case.call(g, ws=ws, lse=False, max_kv=rows)
+            if idle:
+                torch.cuda.synchronize()
+            B.adt_kv_compact_q8(g["kc"][None], g["vc"][None], g["ks"][None], g["vs"][None], kv[i], kv[i + 1], kt[None], vt[None],
+                                g["offs"], path, take, alen, **shape)
+        assert kv[steps].item() == rows
+        return torch.stack(outs)
+
+    want = run(True)
+    for _ in range(5):
+        assert torch.equal(run(False), want)
+    assert B.adt_get_device_error() == 0
