@@ -35,6 +35,7 @@ constexpr int kThreads = 256;
 constexpr int kUnit = 16;     // elements of a head in a thread
 constexpr int kMaxHead = 4096;
 constexpr int kMaxTurns = 4, kTurnCtas = 8;
+constexpr int kAngleBytes = 32 * 1024;  // of a CTA's tokens: with all else within the 48 KB that need no opting in
 
 struct NormParams {
   const void* in[3];        // rows of q, k, v
@@ -285,7 +286,9 @@ adt_status launch(const NormParams& p, bool vec, int N, const adt::DeviceInfo& i
     // way while one is normed (16384 tokens 146 us; 175 with one a CTA and each unit
     // loaded when it is normed), but not all in a few CTAs an SM (152 to 162).
     int turns = 1;
-    while (turns < kMaxTurns && static_cast<int64_t>(N) >= int64_t{2} * turns * tokens * kTurnCtas * info.sm_count) turns *= 2;
+    while (turns < kMaxTurns && static_cast<int64_t>(N) >= int64_t{2} * turns * tokens * kTurnCtas * info.sm_count &&
+           2 * turns * tokens * (p.rot / 2) * static_cast<int>(sizeof(float2)) <= kAngleBytes)
+      turns *= 2;
     const int groups = (N + tokens * turns - 1) / (tokens * turns);
     // Few tokens: their heads over several CTAs, up to two an SM.
     int split = 2 * info.sm_count / groups;

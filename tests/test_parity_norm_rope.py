@@ -105,6 +105,16 @@ def test_large_means_small_rows_and_absent_weights(D, R, layer):
     assert not out[2].any()
 
 
+def test_many_tokens_of_one_large_head():
+    """A thread block's tokens are as many as the angles leave room for."""
+    N, D = 40000, 512
+    q = rows_of(N, D, torch.bfloat16, 4, "q")
+    pos, inv = np.arange(N, dtype=np.int32), oracle.rope_freqs(D)[0]
+    out = torch.empty((N, 1, D), dtype=torch.bfloat16, device="cuda")
+    B.adt_norm_rope_qkv(q, None, None, torch.from_numpy(pos).cuda(), torch.from_numpy(inv).cuda(), H=1, Hkv=1, D=D, q_out=out)
+    check(out, q, False, 1e-6, None, None, pos, inv, 1.0, False)
+
+
 def test_far_and_negative_positions():
     pos = np.array([0, 1, -1, 99999, 1 << 20, (1 << 20) + 1, 2 ** 31 - 1, -2 ** 31, 123456789], np.int32)
     q = rows_of(len(pos), 2 * 128, torch.float32, 5, "q")
