@@ -9,12 +9,13 @@
 // A head is split over a group of lanes, 16 elements each, which are such that
 // the partner of every rotated element lies in the same lane: two vectors of 8, in
 // a half layout those of a pair's two sides.  So a norm costs two or four rounds of
-// shuffles of one value and the rotation none.
+// shuffles of one value and the rotation none.  (Where the sides of a half layout do
+// not begin at a vector, partners meet in shared memory.)
 //
 // Bound by HBM, each element is read and written once: 16384 tokens of 32 / 32 heads
-// x 128 in bf16 (805 MB) 146 us, 82 % of a copy's rate; between a unit's load and
+// x 128 in bf16 (805 MB) 127 us, 94 % of a copy's rate; between a unit's load and
 // its store lie the sums' shuffles, which the next unit's load hides in part.  501
-// tokens of 32 / 8 heads in fp32 with a LayerNorm 9.4 us, one token 4.1 us (its launch).
+// tokens of 32 / 8 heads in fp32 with a LayerNorm 9.4 us, one token 4.0 us (its launch).
 #include <math.h>
 
 #include "adt_common.cuh"
@@ -35,7 +36,7 @@ constexpr int kThreads = 256;
 constexpr int kUnit = 16;     // elements of a head in a thread
 constexpr int kMaxHead = 4096;
 constexpr int kMaxTurns = 4, kTurnCtas = 8;
-constexpr int kAngleBytes = 32 * 1024;  // of a CTA's tokens: with all else within the 48 KB that need no opting in
+constexpr int kAngleBytes = 30 * 1024;  // of a CTA's tokens: with all else within the 48 KB that need no opting in
 
 struct NormParams {
   const void* in[3];        // rows of q, k, v
@@ -57,20 +58,30 @@ __device__ __forceinline__ float group_sum(float v, int width) {
   return v;
 }
 
-// Vectors: 16 | D <= 512, 16 | rot, 16-byte boundaries.  A CTA takes a token or a few
+constexpr int kPadded = kUnit + 1;  // of a thread's elements in shared memory: 16 lanes' lie in 16 banks
+
+// Vectors: 16 | D <= 512, 16-byte boundaries.  Where rot is not a multiple of 16:
+// kPairs, pairs side by side, of which a lane may turn some only; kMeet, a half
+// layout, whose partners lie in different lanes.  A CTA takes a token or a few
 // at a time, one after the other (and where there are few, a share of their heads);
 // a thread keeps its place within the heads, so that it reads a token's cosines and
 // sines once.  Once a thread's unit is widened, its next one is on its way.
-template <typename T, typename W>
-__global__ void __launch_bounds__(kThreads, sizeof(T) + sizeof(W) == 4 ? 4 : sizeof(T) + sizeof(W) == 6 ? 3 : 2)
+enum Rotation { kVectors, kPairs, kMeet };
+
+template <typename T, typename W, int kRot, bool kEarly>
+__global__ void __launch_bounds__(kThreads, !kEarly ? (sizeof(T) == 2 ? 4 : 3)
+                                            : sizeof(T) + sizeof(W) == 4 ? 4
+                                            : sizeof(T) + sizeof(W) == 6 ? 3
+                                                                         : 2)
     norm_rope_vec_kernel(const NormParams p, int N, int tokens, int lanes, int width, int turns) {
   extern __shared__ float2 cs[];
   adt::pdl_wait_then_release();
   const int n0 = blockIdx.x * tokens * turns, here = min(tokens * turns, N - n0);
   const int tok0 = threadIdx.x / lanes, lane = threadIdx.x - tok0 * lanes;
   const int half = p.rot / 2, units = p.D / kUnit;
+  const int row = kRot == kPairs ? (half + 7) & ~7 : half;  // angles of a token
   const int per_pass = lanes / width, hl = lane / width, u = lane - hl * width;
-  const bool turned = u * kUnit < p.rot, split_pair = turned && !p.interleaved;
+  const bool turned = kRot != kMeet && u * kUnit < p.rot, split_pair = turned && !p.interleaved;
   const int e0 = split_pair ? u * 8 : u * kUnit, e1 = split_pair ? e0 + half : e0 + 8;
   const int heads = p.heads[0] + p.heads[1], vectors = p.heads[2] * p.D / 8;
   const int first = static_cast<int>(blockIdx.y) * per_pass, hstep = static_cast<int>(gridDim.y) * per_pass;
@@ -99,11 +110,11 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) + sizeof(W) == 4 ? 4 : siz
         v[k].load(static_cast<const T*>(p.in[2]) + n * p.ld[2] + static_cast<int64_t>(vb + lane + k * vstep) * 8);
   };
   fetch();
-  token_angles(p, n0, here, cs);
+  token_angles(p, n0, here, cs, row);
   for (int turn = 0; turn < turns;) {
     const bool have = have_unit();
     const int64_t n = n0 + tok;
-    const int h = base + hl, which = h < p.heads[0] ? 0 : 1, hh = which ? h - p.heads[0] : h, at = tok * half + u * 8;
+    const int h = base + hl, which = h < p.heads[0] ? 0 : 1, hh = which ? h - p.heads[0] : h, tok_now = tok, at = tok * row + u * 8;
     const bool any = base < heads;  // (uniform)
     float y[kUnit];
     {
@@ -137,12 +148,16 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) + sizeof(W) == 4 ? 4 : siz
     const W* w = static_cast<const W*>(which ? p.weight[1] : p.weight[0]);
     const W* bi = static_cast<const W*>(which ? p.bias[1] : p.bias[0]);
     const int64_t woff = static_cast<int64_t>(hh) * (which ? p.wld[1] : p.wld[0]);
+    // Weights: early, beside the rows' sums, where a call is a chain of a few loads (501
+    // tokens 9.5 us, late 10.4); else where they are used, from L1, and the registers
+    // that they would lie in hold more CTAs (16384 tokens 127 us, early 145; 4096 of 32 / 8
+    // heads 24, early 32).
     Eight<W> tw[2], tb[2];
-    if (have && w) {
+    if (kEarly && have && w) {
       tw[0].load(w + woff + e0);
       tw[1].load(w + woff + e1);
     }
-    if (have && bi) {
+    if (kEarly && have && bi) {
       tb[0].load(bi + woff + e0);
       tb[1].load(bi + woff + e1);
     }
@@ -158,11 +173,15 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) + sizeof(W) == 4 ? 4 : siz
 #pragma unroll
     for (int i = 0; i < kUnit; ++i) sq = fmaf(y[i], y[i], sq);
     const float r = rsqrtf(fmaf(group_sum(sq, width), inv_d, p.eps));
-    if (!have) continue;
+    if (kRot != kMeet && !have) continue;
 #pragma unroll
     for (int i = 0; i < kUnit; ++i) y[i] *= r;
-    if (w) {
+    if (w && have) {
       float a[8], b[8];
+      if (!kEarly) {
+        tw[0].load(w + woff + e0);
+        tw[1].load(w + woff + e1);
+      }
       tw[0].get(a);
       tw[1].get(b);
 #pragma unroll
@@ -171,8 +190,12 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) + sizeof(W) == 4 ? 4 : siz
         y[8 + i] *= b[i];
       }
     }
-    if (bi) {
+    if (bi && have) {
       float a[8], b[8];
+      if (!kEarly) {
+        tb[0].load(bi + woff + e0);
+        tb[1].load(bi + woff + e1);
+      }
       tb[0].get(a);
       tb[1].get(b);
 #pragma unroll
@@ -196,6 +219,24 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) + sizeof(W) == 4 ? 4 : siz
         }
       }
     }
+    if (kRot == kMeet) {  // (by all lanes of the warp)
+      float* head = reinterpret_cast<float*>(cs + tokens * turns * row) + (threadIdx.x - u) * kPadded;
+#pragma unroll
+      for (int i = 0; i < kUnit; ++i) head[u * kPadded + i] = y[i];
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < kUnit; ++i) {
+        const int e = u * kUnit + i;
+        if (!have || e >= p.rot) continue;
+        const bool lead = e < half;
+        const int other = lead ? e + half : e - half;
+        const float2 z = cs[tok_now * row + (lead ? e : other)];
+        const float x = head[other + other / kUnit];
+        y[i] = y[i] * z.x + x * (lead ? -z.y : z.y);
+      }
+      __syncwarp();  // before they are overwritten
+      if (!have) continue;
+    }
     __nv_bfloat16* dst = (which ? p.out[1] : p.out[0]) + (n * (which ? p.heads[1] : p.heads[0]) + hh) * p.D;
     float za[8], zb[8];
 #pragma unroll
@@ -208,7 +249,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) + sizeof(W) == 4 ? 4 : siz
   }
 }
 
-// Any head size, even rotary_dim, row stride and alignment: a warp takes a head
+// Any head size, row stride and alignment: a warp takes a head
 // at a time, in shared memory as fp32, element by element.
 template <typename T, typename W>
 __global__ void __launch_bounds__(kThreads) norm_rope_any_kernel(const NormParams p) {
@@ -270,7 +311,7 @@ template <typename T, typename W>
 adt_status launch(const NormParams& p, bool vec, int N, const adt::DeviceInfo& info, cudaLaunchConfig_t* cfg) {
   const int heads = p.heads[0] + p.heads[1];
   if (vec) {
-    const int units = p.D / kUnit, width = adt::next_pow2(units);
+    const int units = p.D / kUnit, width = adt::next_pow2(units), row = (p.rot / 2 + 7) & ~7;
     // Threads of a token: one unit of its heads and one pair of vectors of its values
     // each, or with many tokens two of each.
     const int qk = heads * width, vs = (p.heads[2] * units + 1) / 2, want = qk > vs ? qk : vs;
@@ -283,11 +324,12 @@ adt_status launch(const NormParams& p, bool vec, int N, const adt::DeviceInfo& i
     const int tokens = kThreads / lanes;
     const int passes = (want + lanes - 1) / lanes;
     // With many tokens up to four of them a CTA, so that the next one's rows are on their
-    // way while one is normed (16384 tokens 146 us; 175 with one a CTA and each unit
-    // loaded when it is normed), but not all in a few CTAs an SM (152 to 162).
+    // way while one is normed (16384 tokens 150 us, with one a CTA and each unit loaded when
+    // it is normed 175; both before weights were loaded late), but not all in a few CTAs
+    // an SM (152 to 162).
     int turns = 1;
     while (turns < kMaxTurns && static_cast<int64_t>(N) >= int64_t{2} * turns * tokens * kTurnCtas * info.sm_count &&
-           2 * turns * tokens * (p.rot / 2) * static_cast<int>(sizeof(float2)) <= kAngleBytes)
+           2 * turns * tokens * row * static_cast<int>(sizeof(float2)) <= kAngleBytes)
       turns *= 2;
     const int groups = (N + tokens * turns - 1) / (tokens * turns);
     // Few tokens: their heads over several CTAs, up to two an SM.
@@ -295,8 +337,12 @@ adt_status launch(const NormParams& p, bool vec, int N, const adt::DeviceInfo& i
     split = split < 1 ? 1 : split > passes ? passes : split;
     cfg->gridDim = dim3(static_cast<unsigned>(groups), static_cast<unsigned>(split), 1);
     cfg->blockDim = dim3(static_cast<unsigned>(lanes * tokens), 1, 1);
-    cfg->dynamicSmemBytes = static_cast<size_t>(tokens) * turns * (p.rot / 2) * sizeof(float2);
-    ADT_CUDA_TRY(cudaLaunchKernelEx(cfg, norm_rope_vec_kernel<T, W>, p, N, tokens, lanes, width, turns));
+    const int rot = p.rot % kUnit == 0 ? kVectors : p.interleaved ? kPairs : kMeet;
+    cfg->dynamicSmemBytes = static_cast<size_t>(tokens) * turns * row * sizeof(float2) + (rot == kMeet ? kThreads * kPadded * 4 : 0);
+    const auto kernel = rot == kVectors ? (many ? norm_rope_vec_kernel<T, W, kVectors, false> : norm_rope_vec_kernel<T, W, kVectors, true>)
+                        : rot == kPairs ? norm_rope_vec_kernel<T, W, kPairs, false>
+                                        : norm_rope_vec_kernel<T, W, kMeet, false>;
+    ADT_CUDA_TRY(cudaLaunchKernelEx(cfg, kernel, p, N, tokens, lanes, width, turns));
     return adt::launch_status();
   }
   // Rows of shared memory: within the 48 KB that need no opting in.
@@ -400,7 +446,7 @@ adt_status adt_norm_rope_qkv(const void* q, int64_t ld_q, const void* k, int64_t
   cudaLaunchAttribute attr[1] = {adt::pdl_attribute()};
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  const bool vec = aligned && D % kUnit == 0 && rotary_dim % kUnit == 0 && D <= 32 * kUnit;
+  const bool vec = aligned && D % kUnit == 0 && D <= 32 * kUnit;
   if (esize == 2)
     return wsize == 2 ? launch<__nv_bfloat16, __nv_bfloat16>(p, vec, N, info, &cfg)
                       : launch<__nv_bfloat16, float>(p, vec, N, info, &cfg);

@@ -15,18 +15,26 @@ __device__ __forceinline__ float to_f32(float x) { return x; }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
 
 // Cosines and sines of `tokens` tokens from n0 on, m included (of p: rot, pos, inv_freq, magnitude).
+// row: entries of a token, those from rot / 2 on turn nothing.
 template <class Params>
-__device__ __forceinline__ void token_angles(const Params& p, int n0, int tokens, float2* cs) {
-  const int half = p.rot / 2;
-  for (int i = threadIdx.x; i < half * tokens; i += blockDim.x) {
-    const int t = tokens == 1 ? 0 : i / half;
-    double turns = static_cast<double>(p.pos[n0 + t]) * (1.0 / kTwoPi) * p.inv_freq[i - t * half];
+__device__ __forceinline__ void token_angles(const Params& p, int n0, int tokens, float2* cs, int row) {
+  for (int i = threadIdx.x; i < row * tokens; i += blockDim.x) {
+    const int t = tokens == 1 ? 0 : i / row, pair = i - t * row;
+    if (pair >= p.rot / 2) {
+      cs[i] = make_float2(1.f, 0.f);
+      continue;
+    }
+    double turns = static_cast<double>(p.pos[n0 + t]) * (1.0 / kTwoPi) * p.inv_freq[pair];
     turns -= rint(turns);
     float s, c;
     sincospif(2.f * static_cast<float>(turns), &s, &c);
     cs[i] = make_float2(c * p.magnitude, s * p.magnitude);
   }
   __syncthreads();
+}
+template <class Params>
+__device__ __forceinline__ void token_angles(const Params& p, int n0, int tokens, float2* cs) {
+  token_angles(p, n0, tokens, cs, p.rot / 2);
 }
 
 // Eight consecutive elements of a row.

@@ -61,7 +61,8 @@ def check(got, x, layer, eps, w, b, pos, inv, magnitude, interleaved):
     (1, 32, 32, 128, 128), (1, 1, 1, 64, 64), (64, 32, 8, 128, 64), (5, 20, 20, 64, 64), (333, 8, 2, 128, 128),
     (3, 7, 1, 80, 80), (3, 5, 5, 80, 48), (2, 3, 3, 6, 2), (9, 4, 2, 64, 16), (4, 4, 4, 128, 0), (2, 2, 1, 33, 20),
     (3, 3, 2, 96, 90), (2, 2, 2, 256, 256), (6, 3, 1, 512, 32), (1, 2, 1, 1500, 1024), (2, 1, 1, 4096, 64), (700, 40, 10, 128, 32),
-    (3, 2, 2, 1, 0), (2000, 8, 8, 64, 64), (1500, 5, 1, 72, 30)])
+    (3, 2, 2, 1, 0), (2000, 8, 8, 64, 64), (1500, 5, 1, 72, 30), (1100, 40, 10, 128, 36), (9, 4, 2, 64, 10),
+    (3, 2, 2, 256, 250), (6, 3, 1, 512, 30), (1300, 1, 1, 48, 2)])
 @pytest.mark.parametrize("layer,interleaved", [(False, False), (True, True), (False, True), (True, False)])
 @pytest.mark.parametrize("dtype,wtype", [(torch.bfloat16, torch.float32), (torch.float32, torch.bfloat16),
                                          (torch.bfloat16, torch.bfloat16), (torch.float32, torch.float32)])
