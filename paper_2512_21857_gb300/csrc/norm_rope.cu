@@ -60,9 +60,9 @@ __device__ __forceinline__ float group_sum(float v, int width) {
 
 constexpr int kPadded = kUnit + 1;  // of a thread's elements in shared memory: 16 lanes' lie in 16 banks
 
-// Vectors: 16 | D <= 512, 16-byte boundaries.  Where rot is not a multiple of 16:
-// kPairs, pairs side by side, of which a lane may turn some only; kMeet, a half
-// layout, whose partners lie in different lanes.  A CTA takes a token or a few
+// Vectors: 16 | D <= 512, 16-byte boundaries.  Where rot is not a multiple of a vector
+// (in a half layout of two): kPairs, pairs side by side, of which a lane may turn some
+// only; kMeet, a half layout, whose partners lie in different lanes.  A CTA takes a token or a few
 // at a time, one after the other (and where there are few, a share of their heads);
 // a thread keeps its place within the heads, so that it reads a token's cosines and
 // sines once.  Once a thread's unit is widened, its next one is on its way.
@@ -81,8 +81,12 @@ __global__ void __launch_bounds__(kThreads, !kEarly ? (sizeof(T) == 2 ? 4 : 3)
   const int half = p.rot / 2, units = p.D / kUnit;
   const int row = kRot == kPairs ? (half + 7) & ~7 : half;  // angles of a token
   const int per_pass = lanes / width, hl = lane / width, u = lane - hl * width;
-  const bool turned = kRot != kMeet && u * kUnit < p.rot, split_pair = turned && !p.interleaved;
-  const int e0 = split_pair ? u * 8 : u * kUnit, e1 = split_pair ? e0 + half : e0 + 8;
+  // Two vectors of 8, of each half of what a group of lanes covers, so that a warp's
+  // loads and stores take whole lines: a half layout's turned elements, then the rest;
+  // else the head.
+  const bool split_pair = kRot == kVectors && !p.interleaved && u * kUnit < p.rot;
+  const int covered = kRot == kVectors && !p.interleaved ? (split_pair ? p.rot : p.D - p.rot) : p.D;
+  const int e0 = covered == p.D || split_pair ? u * 8 : p.rot + (u - p.rot / kUnit) * 8, e1 = e0 + covered / 2;
   const int heads = p.heads[0] + p.heads[1], vectors = p.heads[2] * p.D / 8;
   const int first = static_cast<int>(blockIdx.y) * per_pass, hstep = static_cast<int>(gridDim.y) * per_pass;
   const int vfirst = static_cast<int>(blockIdx.y) * lanes, vstep = static_cast<int>(gridDim.y) * lanes;
@@ -114,7 +118,7 @@ __global__ void __launch_bounds__(kThreads, !kEarly ? (sizeof(T) == 2 ? 4 : 3)
   for (int turn = 0; turn < turns;) {
     const bool have = have_unit();
     const int64_t n = n0 + tok;
-    const int h = base + hl, which = h < p.heads[0] ? 0 : 1, hh = which ? h - p.heads[0] : h, tok_now = tok, at = tok * row + u * 8;
+    const int h = base + hl, which = h < p.heads[0] ? 0 : 1, hh = which ? h - p.heads[0] : h, at = tok * row;
     const bool any = base < heads;  // (uniform)
     float y[kUnit];
     {
@@ -204,33 +208,42 @@ __global__ void __launch_bounds__(kThreads, !kEarly ? (sizeof(T) == 2 ? 4 : 3)
         y[8 + i] += b[i];
       }
     }
-    if (turned) {
+    if (split_pair) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float2 z = cs[at + i];
-        if (!p.interleaved) {
-          const float a = y[i], b = y[8 + i];
-          y[i] = a * z.x - b * z.y;
-          y[8 + i] = b * z.x + a * z.y;
-        } else {
-          const float a = y[2 * i], b = y[2 * i + 1];
-          y[2 * i] = a * z.x - b * z.y;
-          y[2 * i + 1] = b * z.x + a * z.y;
+        const float2 z = cs[at + e0 + i];
+        const float a = y[i], b = y[8 + i];
+        y[i] = a * z.x - b * z.y;
+        y[8 + i] = b * z.x + a * z.y;
+      }
+    } else if (kRot != kMeet && p.interleaved) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        if ((k ? e1 : e0) >= p.rot) continue;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float2 z = cs[at + (k ? e1 : e0) / 2 + i];
+          const float a = y[8 * k + 2 * i], b = y[8 * k + 2 * i + 1];
+          y[8 * k + 2 * i] = a * z.x - b * z.y;
+          y[8 * k + 2 * i + 1] = b * z.x + a * z.y;
         }
       }
     }
     if (kRot == kMeet) {  // (by all lanes of the warp)
       float* head = reinterpret_cast<float*>(cs + tokens * turns * row) + (threadIdx.x - u) * kPadded;
 #pragma unroll
-      for (int i = 0; i < kUnit; ++i) head[u * kPadded + i] = y[i];
+      for (int i = 0; i < kUnit; ++i) {
+        const int e = (i < 8 ? e0 : e1 - 8) + i;
+        if (u < units) head[e + e / kUnit] = y[i];
+      }
       __syncwarp();
 #pragma unroll
       for (int i = 0; i < kUnit; ++i) {
-        const int e = u * kUnit + i;
+        const int e = (i < 8 ? e0 : e1 - 8) + i;
         if (!have || e >= p.rot) continue;
         const bool lead = e < half;
         const int other = lead ? e + half : e - half;
-        const float2 z = cs[tok_now * row + (lead ? e : other)];
+        const float2 z = cs[at + (lead ? e : other)];
         const float x = head[other + other / kUnit];
         y[i] = y[i] * z.x + x * (lead ? -z.y : z.y);
       }
@@ -337,7 +350,7 @@ adt_status launch(const NormParams& p, bool vec, int N, const adt::DeviceInfo& i
     split = split < 1 ? 1 : split > passes ? passes : split;
     cfg->gridDim = dim3(static_cast<unsigned>(groups), static_cast<unsigned>(split), 1);
     cfg->blockDim = dim3(static_cast<unsigned>(lanes * tokens), 1, 1);
-    const int rot = p.rot % kUnit == 0 ? kVectors : p.interleaved ? kPairs : kMeet;
+    const int rot = p.rot % (p.interleaved ? 8 : kUnit) == 0 ? kVectors : p.interleaved ? kPairs : kMeet;
     cfg->dynamicSmemBytes = static_cast<size_t>(tokens) * turns * row * sizeof(float2) + (rot == kMeet ? kThreads * kPadded * 4 : 0);
     const auto kernel = rot == kVectors ? (many ? norm_rope_vec_kernel<T, W, kVectors, false> : norm_rope_vec_kernel<T, W, kVectors, true>)
                         : rot == kPairs ? norm_rope_vec_kernel<T, W, kPairs, false>
