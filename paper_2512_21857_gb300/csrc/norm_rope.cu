@@ -13,9 +13,11 @@
 // not begin at a vector, partners meet in shared memory.)
 //
 // Bound by HBM, each element is read and written once: 16384 tokens of 32 / 32 heads
-// x 128 in bf16 (805 MB) 127 us, 94 % of a copy's rate; between a unit's load and
+// x 128 in bf16 (805 MB) 126 us, 94 % of a copy's rate; between a unit's load and
 // its store lie the sums' shuffles, which the next unit's load hides in part.  501
-// tokens of 32 / 8 heads in fp32 with a LayerNorm 9.4 us, one token 4.0 us (its launch).
+// tokens of 32 / 8 heads in fp32 with a LayerNorm 7.8 us, one token 4.0 us (its launch).
+// 4096 tokens of 32 / 8 heads (14.8 at the copy rate): 22 us with pairs side by side,
+// 24.5 as halves, 42 with 50 elements turned as halves, through shared memory.
 #include <math.h>
 
 #include "adt_common.cuh"
@@ -83,7 +85,7 @@ __global__ void __launch_bounds__(kThreads, !kEarly ? (sizeof(T) == 2 ? 4 : 3)
   const int per_pass = lanes / width, hl = lane / width, u = lane - hl * width;
   // Two vectors of 8, of each half of what a group of lanes covers, so that a warp's
   // loads and stores take whole lines: a half layout's turned elements, then the rest;
-  // else the head.
+  // else the head.  (As one run of 16: 30 us for the 22 above, 9.5 for the 7.8.)
   const bool split_pair = kRot == kVectors && !p.interleaved && u * kUnit < p.rot;
   const int covered = kRot == kVectors && !p.interleaved ? (split_pair ? p.rot : p.D - p.rot) : p.D;
   const int e0 = covered == p.D || split_pair ? u * 8 : p.rot + (u - p.rot / kUnit) * 8, e1 = e0 + covered / 2;
@@ -153,7 +155,7 @@ __global__ void __launch_bounds__(kThreads, !kEarly ? (sizeof(T) == 2 ? 4 : 3)
     const W* bi = static_cast<const W*>(which ? p.bias[1] : p.bias[0]);
     const int64_t woff = static_cast<int64_t>(hh) * (which ? p.wld[1] : p.wld[0]);
     // Weights: early, beside the rows' sums, where a call is a chain of a few loads (501
-    // tokens 9.5 us, late 10.4); else where they are used, from L1, and the registers
+    // tokens 9.5 us, late 10.4, both with vectors side by side); else where they are used, from L1, and the registers
     // that they would lie in hold more CTAs (16384 tokens 127 us, early 145; 4096 of 32 / 8
     // heads 24, early 32).
     Eight<W> tw[2], tb[2];
