@@ -43,9 +43,9 @@
 // 64 rows (each twice) and 4500 with 128, of which waits for tensor memory, shared
 // memory and the other group are more than half (issue slots 41 % busy, tensor cores
 // 23 %), and two groups take chunks in turn; V's widening keeps up.  Measured: four
-// trees of 64, 64, 27 and 64 nodes over 1444 to 2400 rows, 32 / 32 heads x 128, 40 us
+// trees of 64, 64, 27 and 64 nodes over 1444 to 2400 rows, 32 / 32 heads x 128, 39 us
 // (11 at HBM's rate), 5 of them the launch before; trees of 64 nodes over 3500 to
-// 6001 rows, 32 / 8 heads x 128, 48 us (11 at the tensor cores' bf16 rate), 5 of them
+// 6001 rows, 32 / 8 heads x 128, 47 us (11 at the tensor cores' bf16 rate), 5 of them
 // the joining of cut items.
 #include <math.h>
 
