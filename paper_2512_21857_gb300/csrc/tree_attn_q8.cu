@@ -7,7 +7,8 @@
 // items, with kItemCost more for each item's start, are dealt to one persistent
 // CTA an SM in equal contiguous shares, so ragged batches and few long sequences
 // fill the device alike; an item that a share's end cuts is joined from partial
-// rows (O, maximum, sum) in the workspace by the CTA that ends its part last.
+// rows (outputs of its parts, and their sums) in the workspace by the CTA that ends its
+// part last.
 // Two kernels share this: of up to 32 rows tree_attn_q8_few.cuh, of more this one.
 //
 // S = Q K^T is made of e4m3 products, K as it lies in the cache: a query row,
@@ -15,12 +16,19 @@
 // what that leaves, and both products add up in one accumulator (as many
 // instructions as one product of bf16 has).  What the two leave is below 2^-17 of
 // the row's largest magnitude.  The tree's own keys are cut the same way (four
-// products).  The key's scale meets the score in fp32.  A weight takes on its
-// value row's scale, against a reference of the share's (2^4 above the largest
-// seen: s_ref), before it is rounded to fp16, and V is widened to fp16 in shared
-// memory, exactly: bf16 weights are three bits worse, and two e4m3 ones a weight
-// would lose keys of 2^-18 of the largest one's, of which a long cache can have
-// enough to matter.
+// products).  The key's scale meets the score in fp32.
+//
+// With z = score (in powers of two) + e, 2^e the key's value scale, a row's weights are
+// P = 2^(z + kHeadroom - base), base the largest z that it has seen, rounded up (raised
+// only when a row grows by more than 2^kRescaleThreshold), so that what a weight is
+// rounded to goes by what it adds to O, whatever the scales of values that the row does
+// not see or gives no weight.  P is rounded to fp16 and V widened to fp16 in shared
+// memory, exactly: bf16 weights are three bits worse, and two e4m3 ones a weight would
+// lose keys of 2^-18 of the largest one's, of which a long cache can have enough to
+// matter; fp16 ends at 2^-31 of it.  Scores take e relative to `top`, the largest so far
+// (a number within a chunk), and the row sum adds P 2^(top - e - kShift), against a
+// level of its own for each thread.  (Values whose scale is below 2^-kSpan of the top's,
+// which are zeros in earnest, are taken to be 2^-kSpan there.)
 //
 // Queries, trees and ancestors are prepared by a launch before (prepare_kernel).
 //
@@ -29,7 +37,7 @@
 //
 // Warp roles (16 warps):
 //   0-3, 4-7  two softmax groups that take the chunks in turn, a thread a row;
-//             the running maximum passes from group to group through shared
+//             the running base passes from group to group through shared
 //             memory, P goes to tensor memory;
 //   8         K tiles by TMA into a ring, the queries, and the scales of both,
 //             written a chunk after their bytes were asked for;
@@ -92,6 +100,8 @@ constexpr uint32_t kDrainLimit = 1u << 20;  // of the waits for what is in fligh
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 constexpr float kRescaleThreshold = 8.0f;  // log2 units
+constexpr float kHeadroom = 7.0f;          // weights up to 2^15: fp16 ends below 2^16
+constexpr int kSpan = 96, kShift = kSpan / 2;  // (a weight 2^-24 of the largest is a normal number 2^-96 further down)
 
 template <int D>
 struct Cfg {
@@ -105,10 +115,11 @@ struct Cfg {
   static constexpr int kKOff = kQOff + 4 * kTile;
   static constexpr int kVOff = kKOff + kKStages * kTile;
   static constexpr int kWideOff = kVOff + kVStages * kTile;
-  static constexpr int kScaleOff = kWideOff + 2 * kWide;  // [slots][K, V][128] fp32
-  static constexpr int kJoinOff = kScaleOff + kScaleSlots * 2 * kChunk * 4;  // D = 64: [2 groups][128][32] fp32
+  static constexpr int kScaleOff = kWideOff + 2 * kWide;  // [slots][K's scale, e - top, 2^(top - e - kShift)][128] fp32
+  static constexpr int kJoinOff = kScaleOff + kScaleSlots * 3 * kChunk * 4;  // D = 64: [2 groups][128][32] fp32
   static constexpr int kDynSmem = kJoinOff + (D == 128 ? 0 : 2 * kRows * 32 * 4) + 1024;  // + alignment slack
   static_assert(D != 128 || kWide == 2 * kRows * 32 * 4, "copies are joined in a V tile");
+  static_assert(kDynSmem <= 221 * 1024, "with 6 KB of the kernel's own within the 227 of an SM");
   static constexpr uint32_t kIdescO = sm100::idesc_f16_f32(kRows, D, 0, 1);
   static_assert(kKStages <= kMaxStages && kVStages <= kMaxStages && kScaleSlots <= kMaxScaleSlots && kOCol + D <= kTmemCols, "sizes");
 };
@@ -142,8 +153,8 @@ struct AttnParams {
   __nv_bfloat16* out;
   float* lse;
   unsigned* tickets;   // [grid], of the items that start in a CTA's share and end in another's
-  float2* part_ml;     // [2 grid][slot_rows]: of a CTA's first and of its last item
-  float4* part_o;      // [2 grid][D / 4][slot_rows]
+  float2* part_ml;     // [2 grid][slot_rows]: row sums of a CTA's first and of its last item (part_sum)
+  float4* part_o;      // [2 grid][D / 4][slot_rows]: O over the row sum
   unsigned* err;
   uint32_t wait_limit;
 };
@@ -305,7 +316,7 @@ struct Bars {
   uint64_t k_full[kMaxStages], k_free[kMaxStages];
   uint64_t v_full[kMaxStages], v_free[kMaxStages];
   uint64_t scale_full[kMaxScaleSlots];
-  uint64_t wide_full[2];     // a V tile in bf16
+  uint64_t wide_full[2];     // a V tile in fp16
   uint64_t q_full[2], q_free[2];
   uint64_t s_full[4], p_full[4];
   uint64_t mu[2][4];         // the running maxima after a chunk are in shared memory, per group and warp
@@ -421,12 +432,6 @@ __device__ __forceinline__ bool poll(uint64_t* bar, uint32_t parity, volatile in
   return true;
 }
 
-// 2^(s - ref + kHeadroom) for a value row's scale s against a reference: what its weights take on.
-constexpr int kHeadroom = 4, kSlack = 3;
-__device__ __forceinline__ float value_factor(int s, int ref) {
-  const int e = max(s - ref + kHeadroom + 127, 0);
-  return __uint_as_float(s == 255 ? 0x7fc00000u : static_cast<uint32_t>(e) << 23);
-}
 // A query row's cut scale times softmax_scale log2 e; never 0, which would make NaN of the -inf of a masked key.
 __device__ __forceinline__ float row_factor(uint32_t s, float scale_log2) {
   return fmaxf(__uint_as_float(s << 23) * scale_log2, 1e-38f);
@@ -434,6 +439,22 @@ __device__ __forceinline__ float row_factor(uint32_t s, float scale_log2) {
 __device__ __forceinline__ float power_of_two(int e) {
   return e < -126 ? 0.f : __uint_as_float(static_cast<uint32_t>(min(e, 127) + 127) << 23);
 }
+
+// 2^(a - b) for what a level's sums (or O) take on at another one's, where both may be -inf.
+__device__ __forceinline__ float level_factor(float a, float b) { return a == b ? 1.f : ex2_approx(a - b); }
+// O over the row sum l is O reciprocal(l), 0 of a part whose rows see none of its keys, times
+// 2^e of their levels: half_power(e) twice, which stays within fp32 where 2^e may not.
+__device__ __forceinline__ float half_power(float e) { return ex2_approx(0.5f * e); }
+__device__ __forceinline__ float reciprocal(float l) { return l == 0.f ? 0.f : __fdividef(1.f, l); }
+// A part's row sum, l 2^level, as it is stored: a level and a factor in [1, 2), or 0, or what is not finite.
+__device__ __forceinline__ float2 part_sum(float level, float l) {
+  const uint32_t bits = __float_as_uint(l);
+  if (l == 0.f) return make_float2(-INFINITY, 0.f);
+  if ((bits & 0x7f800000u) == 0x7f800000u) return make_float2(level, l);
+  return make_float2(level + static_cast<float>(static_cast<int>(bits >> 23) - 127), __uint_as_float((bits & 0x7fffffu) | 0x3f800000u));
+}
+constexpr float kJoinScale = 0x1p-9f;  // of weights that add parts up: within fp32 whatever the values
+constexpr float kJoinLevel = 9.f;
 
 // The first launch: a row is D / 16 lanes', 16 elements each.  Of a tree the query
 // rows, then its nodes' rows of every kv head (zeros up to a multiple of 16 nodes).
@@ -560,10 +581,11 @@ __global__ void __launch_bounds__(kThreads, 1)
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (sm100::smem_addr(smem_raw) & 1023u)) & 1023u);
   __shared__ Bars bars;
-  __shared__ float s_mu[kRows], s_m[2][kRows], s_l[2][2][kRows];
-  __shared__ int s_ref[kMaxScaleSlots];      // the reference of a chunk's value scales
-  __shared__ float s_drop[kMaxScaleSlots];   // what O shrinks by where it rose with the chunk
-  __shared__ int s_odd[kMaxScaleSlots];      // whether a tree chunk has values that are not finite
+  // Of an item, even or odd (one may begin before all have left the one before): the rows' bases, a group's row sums (level, sum).
+  __shared__ float s_mu[2][kRows];
+  __shared__ float2 s_l[2][2][kRows];
+  __shared__ float s_top[kScaleSlots];    // the largest value scale up to a chunk, as a power of two
+  __shared__ int s_odd[kScaleSlots];      // 1: a tree chunk has values that are not finite; 2: the item has had rows that are not
   __shared__ Walk s_walk;
   __shared__ int64_t s_total;
   __shared__ int s_grid, s_last;
@@ -636,9 +658,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     // of the chunk before.  They come byte by byte (their rows need no alignment) and
     // are written a chunk later.
     uint32_t pend[3][4] = {};
-    int slot = 0, ref = 0, k = w.k0;
+    int slot = 0, top = 0, k = w.k0;
     uint32_t item = 0;
-    bool ok = true, first = true, have = false;
+    bool ok = true, first = true, have = false, lost = false;
     for (;; ++j) {
       const int64_t s0 = w.b * p.ssb + w.g * p.ssh, bg = static_cast<int64_t>(w.b) * p.Hkv + w.g;
       const bool tree_k = k >= w.t.prefix;
@@ -697,25 +719,25 @@ __global__ void __launch_bounds__(kThreads, 1)
         uint32_t most = 0u;
 #pragma unroll
         for (int i = 0; i < 4; ++i) most = max(most, pend[1][i] == 255u ? 0u : pend[1][i]);
+        // A value that is not a number takes the outputs of all rows, which all see it, and leaves the row sums.
+        lost = (lost && !first) || __any_sync(adt::kFullMask, pend[1][0] == 255u || pend[1][1] == 255u || pend[1][2] == 255u || pend[1][3] == 255u);
         most = __reduce_max_sync(adt::kFullMask, most);
         const bool odd = __any_sync(adt::kFullMask, (pend[2][0] | pend[2][1] | pend[2][2] | pend[2][3]) != 0u);
-        // The reference is the first chunk's largest scale, and rises where one is
-        // more than kSlack above it.
-        const int before = ref;
-        if (first || static_cast<int>(most) > ref + kSlack) ref = static_cast<int>(most);
-        float f[8];
+        top = first ? static_cast<int>(most) : max(top, static_cast<int>(most));
+        float f[12];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
+          const int e = max((pend[1][i] == 255u ? 0 : static_cast<int>(pend[1][i])) - top, -kSpan);
           f[i] = adt::q8_scale(pend[0][i]);
-          f[4 + i] = value_factor(static_cast<int>(pend[1][i]), ref);
+          f[4 + i] = static_cast<float>(e);
+          f[8 + i] = power_of_two(-e - kShift);
         }
-        float4* dst = reinterpret_cast<float4*>(s_scale + slot * 2 * kChunk);
-        dst[lane] = make_float4(f[0], f[1], f[2], f[3]);
-        dst[32 + lane] = make_float4(f[4], f[5], f[6], f[7]);
+        float4* dst = reinterpret_cast<float4*>(s_scale + slot * 3 * kChunk);
+#pragma unroll
+        for (int i = 0; i < 3; ++i) dst[32 * i + lane] = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
         if (lane == 0) {
-          s_odd[slot] = odd;
-          s_ref[slot] = ref;
-          s_drop[slot] = first ? 1.f : power_of_two(before - ref);
+          s_odd[slot] = (odd ? 1 : 0) | (lost ? 2 : 0);
+          s_top[slot] = static_cast<float>(top - 127);
         }
         __syncwarp();
         if (lane == 0) arrive(&bars.scale_full[slot]);
@@ -974,10 +996,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint32_t item = 0;
     bool ok = true;
     for (; ok && w.more; w = next_item(p, w), ++item) {
+      const int par = item & 1;
       const int index = w.blk * kRows + row, node = index / p.group;
       const bool valid = node < w.t.n, active = __any_sync(adt::kFullMask, valid);
       const uint32_t j0 = j, j1 = j + static_cast<uint32_t>(w.k1 - w.k0);
-      float mu = -INFINITY, l = 0.f;
+      float l = 0.f, level = -INFINITY;  // sum of weights at the scores' own size: l 2^(level + kShift - kHeadroom)
       const int64_t bg = static_cast<int64_t>(w.b) * p.Hkv + w.g;
       const float scale = valid ? p.pre.q_scale[(bg * p.pre.blocks + w.blk) * p.pre.q_rows + row] : 0.f;
       if ((j0 & 1) != static_cast<uint32_t>(grp)) ++j;
@@ -996,21 +1019,23 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int quarters = min(end_quarter, (kl + 31) / 32);
         const uint32_t s_col = tmem + lanes + j % kTiles * kChunk;
         if (active) {
-          const ulonglong2* ks = reinterpret_cast<const ulonglong2*>(s_scale + slot * 2 * kChunk);
-          const ulonglong2* vf = ks + kChunk / 4;
+          const ulonglong2* ks = reinterpret_cast<const ulonglong2*>(s_scale + slot * 3 * kChunk);
+          const ulonglong2 *ze = ks + kChunk / 4, *iv = ze + kChunk / 4;
+          const float top = s_top[slot];
           const bool masked = tree_j || kl < kChunk;
+          const uint64_t scale2 = pack_f32x2(scale, scale);
           float mq[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-          // Scores times their keys' scales, back in place.
+          // Scores times their keys' scales, with their values' exponents (z - top), back in place.
 #pragma unroll 1
           for (int s = 2 * first_quarter; s < 2 * quarters; ++s) {
             uint32_t x[16];
             sm100::tmem_ld_16(s_col + 16 * s, x);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const ulonglong2 f = ks[4 * s + e];
+              const ulonglong2 f = ks[4 * s + e], z = ze[4 * s + e];
               float a, b, c, d;
-              unpack_f32x2(mul_f32x2(pack_u32x2(x[4 * e], x[4 * e + 1]), f.x), a, b);
-              unpack_f32x2(mul_f32x2(pack_u32x2(x[4 * e + 2], x[4 * e + 3]), f.y), c, d);
+              unpack_f32x2(fma_f32x2(mul_f32x2(pack_u32x2(x[4 * e], x[4 * e + 1]), f.x), scale2, z.x), a, b);
+              unpack_f32x2(fma_f32x2(mul_f32x2(pack_u32x2(x[4 * e + 2], x[4 * e + 3]), f.y), scale2, z.y), c, d);
               x[4 * e] = __float_as_uint(a);
               x[4 * e + 1] = __float_as_uint(b);
               x[4 * e + 2] = __float_as_uint(c);
@@ -1029,8 +1054,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             tmem_st_16(s_col + 16 * s, x);
           }
           sm100::tmem_wait_st();
-          const float mx = valid ? fmaxf(fmaxf(mq[0], mq[1]), fmaxf(mq[2], mq[3])) * scale : -INFINITY;  // scale > 0
-          // The running maximum after the chunk before (the other group's).  (An
+          const float mx = valid ? fmaxf(fmaxf(mq[0], mq[1]), fmaxf(mq[2], mq[3])) + top : -INFINITY;
+          // The running base after the chunk before (the other group's).  (An
           // item's last chunk is done before the next one's: so are its maxima.)
           float prev = -INFINITY;
           if (j > j0) {
@@ -1038,24 +1063,22 @@ __global__ void __launch_bounds__(kThreads, 1)
               ok = false;
               break;
             }
-            prev = s_mu[lrow];
+            prev = s_mu[par][lrow];
           }
-          // Raised only when a row grows by more than 2^8; then O (once the chunks
-          // before are in it) is scaled.
-          const float nm = mx > prev + kRescaleThreshold ? mx : prev;
-          s_mu[lrow] = nm;
+          // Raised only when a row grows by more than 2^8, to a whole number, which takes
+          // `top` without a rounding; then O (once the chunks before are in it) is scaled.
+          const float nm = mx > prev + kRescaleThreshold ? ceilf(mx) : prev;
+          s_mu[par][lrow] = nm;
           __syncwarp();
           if (lane == 0) arrive(&bars.mu[grp][w4]);
-          if (nm != mu) l *= ex2_approx(mu - nm);
-          const float drop = s_drop[slot];
-          if (j > j0 && __any_sync(adt::kFullMask, nm != prev || drop != 1.f)) {
+          if (j > j0 && __any_sync(adt::kFullMask, nm != prev)) {
             // (PV(j - 5), whose phase comes before, is done: S(j) is, after PV(j - 3).)
             if (!all_wait(&bars.done[(j - 1) & 3], (j - 1) >> 2)) {
               ok = false;
               break;
             }
             sm100::tc_fence_after();
-            const float alpha = (nm == prev ? 1.f : ex2_approx(prev - nm)) * drop;
+            const float alpha = level_factor(prev, nm);
 #pragma unroll 1
             for (int c = 0; c < D; c += 32) {
               uint32_t r[32];
@@ -1066,26 +1089,25 @@ __global__ void __launch_bounds__(kThreads, 1)
               tmem_st_32(o_col + c, r);
             }
           }
-          mu = nm;
           sm100::tc_fence_after();
-          const float base = mu == -INFINITY ? 0.f : mu;
-          const uint64_t scale2 = pack_f32x2(scale, scale), base2 = pack_f32x2(-base, -base);
+          const float shift = nm == -INFINITY ? 0.f : top - nm + kHeadroom;
+          const uint64_t shift2 = pack_f32x2(shift, shift);
           uint64_t l2[2] = {0ull, 0ull};
-          // 16 scores at a time -> 8 pairs of weights, in fp16 with their values' scales.
+          // 16 scores at a time -> 8 pairs of weights in fp16.
 #pragma unroll 1
           for (int s = 2 * first_quarter; s < 2 * quarters; ++s) {
             uint32_t x[16], pk[8];
             sm100::tmem_ld_16(s_col + 16 * s, x);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const ulonglong2 g = vf[4 * s + e];
+              const ulonglong2 g = iv[4 * s + e];
 #pragma unroll
               for (int h = 0; h < 2; ++h) {
                 float a, b;
-                unpack_f32x2(fma_f32x2(pack_u32x2(x[4 * e + 2 * h], x[4 * e + 2 * h + 1]), scale2, base2), a, b);
-                const uint64_t wt = pack_f32x2(ex2_approx(a), ex2_approx(b));
-                l2[h] = add_f32x2(l2[h], wt);
-                unpack_f32x2(mul_f32x2(wt, h ? g.y : g.x), a, b);
+                unpack_f32x2(add_f32x2(pack_u32x2(x[4 * e + 2 * h], x[4 * e + 2 * h + 1]), shift2), a, b);
+                a = ex2_approx(a);
+                b = ex2_approx(b);
+                l2[h] = fma_f32x2(pack_f32x2(a, b), h ? g.y : g.x, l2[h]);
                 pk[2 * e + h] = pack_half2(a, b);
               }
             }
@@ -1099,7 +1121,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           float la, lb, lc, ld;
           unpack_f32x2(l2[0], la, lb);
           unpack_f32x2(l2[1], lc, ld);
-          l += (la + lb) + (lc + ld);
+          // (At the larger of both levels: the base may stay while the top rises.)
+          const float at = nm - top, to = fmaxf(at, level);
+          l = l * level_factor(level, to) + ((la + lb) + (lc + ld)) * level_factor(at, to);
+          level = to;
           sm100::tmem_wait_st();
         } else {
           // A warp without rows only keeps the barriers moving.
@@ -1116,33 +1141,37 @@ __global__ void __launch_bounds__(kThreads, 1)
       ok = ok && all_wait(&bars.done[(j1 - 1) & 3], (j1 - 1) >> 2);
       sm100::tc_fence_after();
       constexpr int kHalf = D / 2;
-      const float m = s_mu[lrow];
-      const int par = item & 1;
-      s_m[par][lrow] = m;  // (both groups write the same)
-      s_l[par][grp][lrow] = mu == m ? l : l * ex2_approx(mu - m);
-      const float unit = power_of_two(s_ref[(j1 - 1) % kScaleSlots] - 127 - kHeadroom);
+      const float m = s_mu[par][lrow];
+      s_l[par][grp][lrow] = make_float2(level, l);
       if (!ok && lane == 0) give_up();
       ok = !any_of<2, kSoftmaxThreads>(!ok);  // (after a wait that gave up they leave together)
       if (!ok) break;
       // A thread writes its own row's columns, or, of rows in copies, parts of row r:
       // the copies' sums, with weights that bring them to one maximum.
       const int tg = tid & 127, r = copies == 1 ? row : tg / copies;
-      float M = -INFINITY, lt = 0.f;
+      float M = -INFINITY, G = -INFINITY, lt = 0.f;
 #pragma unroll 1
-      for (int c = r; c < kRows; c += span) M = fmaxf(M, s_m[par][c]);
-      auto weight = [&](float mc, float Mc) { return mc == Mc ? 1.f : ex2_approx(mc - Mc); };
+      for (int c = r; c < kRows; c += span) {
+        M = fmaxf(M, s_mu[par][c]);
+        G = fmaxf(G, fmaxf(s_l[par][0][c].x, s_l[par][1][c].x));
+      }
 #pragma unroll 1
-      for (int c = r; c < kRows; c += span) lt += (s_l[par][0][c] + s_l[par][1][c]) * weight(s_m[par][c], M);
-      float mine = unit;
+      for (int c = r; c < kRows; c += span) {
+        const float2 a = s_l[par][0][c], b = s_l[par][1][c];
+        lt += a.y * level_factor(a.x, G) + b.y * level_factor(b.x, G);
+      }
+      float mine = 1.f;
       if (copies > 1) {
         float Mr = -INFINITY;
 #pragma unroll 1
-        for (int c = row; c < kRows; c += span) Mr = fmaxf(Mr, s_m[par][c]);
-        mine *= weight(m, Mr);
+        for (int c = row; c < kRows; c += span) Mr = fmaxf(Mr, s_mu[par][c]);
+        mine = level_factor(m, Mr);
       }
+      // O 2^M over lt 2^(G + kShift), in two steps that stay within fp32.
       const bool whole = w.k0 == 0 && w.k1 == w.t.chunks;
-      if (whole) mine = copies == 1 ? mine * __fdividef(1.f, lt) : mine;
-      const float inv = whole && copies > 1 ? __fdividef(1.f, lt) : 1.f;
+      const bool lost = (s_odd[(j1 - 1) % kScaleSlots] & 2) != 0;
+      const float inv = lost ? NAN : reciprocal(lt), unit = M == -INFINITY ? 1.f : half_power(M - G - kShift);
+      if (copies == 1) mine = inv;
       const int64_t slot = 2ll * blockIdx.x + (w.first ? 0 : 1);
       const int ri = w.blk * kRows + r, rt = ri / p.group;
       const bool there = rt < w.t.n;
@@ -1150,10 +1179,11 @@ __global__ void __launch_bounds__(kThreads, 1)
       __nv_bfloat16* out = p.out + out_row * D + grp * kHalf;
       float4* part = p.part_o + (slot * (D / 4) + grp * (kHalf / 4)) * p.slot_rows + r;
       auto put4 = [&](int c, float4 v) {
+        v = make_float4(v.x * inv * unit * unit, v.y * inv * unit * unit, v.z * inv * unit * unit, v.w * inv * unit * unit);
         if (whole) {
           uint2 y;
-          y.x = pack_bf16x2(v.x * inv, v.y * inv);
-          y.y = pack_bf16x2(v.z * inv, v.w * inv);
+          y.x = pack_bf16x2(v.x, v.y);
+          y.y = pack_bf16x2(v.z, v.w);
           *reinterpret_cast<uint2*>(out + c) = y;
         } else {
           part[c / 4 * p.slot_rows] = v;
@@ -1169,9 +1199,11 @@ __global__ void __launch_bounds__(kThreads, 1)
           __syncwarp();
           if (lane == 0) arrive(&bars.o_free);
         }
+        const float once = copies == 1 ? unit : 1.f;
+#pragma unroll
+        for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * mine * once * once);
         auto four = [&](int c) {
-          return make_float4(__uint_as_float(o[c]) * mine, __uint_as_float(o[c + 1]) * mine, __uint_as_float(o[c + 2]) * mine,
-                             __uint_as_float(o[c + 3]) * mine);
+          return make_float4(__uint_as_float(o[c]), __uint_as_float(o[c + 1]), __uint_as_float(o[c + 2]), __uint_as_float(o[c + 3]));
         };
         if (copies == 1) {
           if (there && whole) {
@@ -1181,7 +1213,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               uint32_t y[4];
 #pragma unroll
               for (int e = 0; e < 4; ++e)
-                y[e] = pack_bf16x2(__uint_as_float(o[c + 2 * e]) * mine, __uint_as_float(o[c + 2 * e + 1]) * mine);
+                y[e] = pack_bf16x2(__uint_as_float(o[c + 2 * e]), __uint_as_float(o[c + 2 * e + 1]));
               dst[c / 8] = make_uint4(y[0], y[1], y[2], y[3]);
             }
           } else if (there) {
@@ -1217,16 +1249,17 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (lane == 0) arrive(&bars.join_free[item & 1]);
       }
       if (there && grp == 0 && (copies == 1 || (tg & (copies - 1)) == 0)) {
+        const float at = G + (kShift - kHeadroom);
         if (!whole)
-          p.part_ml[slot * p.slot_rows + r] = make_float2(M, lt);
+          p.part_ml[slot * p.slot_rows + r] = part_sum(at, lt);
         else if (p.lse)
-          p.lse[out_row] = (M + __log2f(lt)) * kLn2;
+          p.lse[out_row] = (at + __log2f(lt)) * kLn2;
       }
       // (The slots of an item's last two chunks, of its tree's two at most, are in
       // use until the next items' S products are read.)
       bool odd = false;
 #pragma unroll 1
-      for (int k = max(w.k0, w.t.prefix); k < w.k1; ++k) odd |= s_odd[(j1 - static_cast<uint32_t>(w.k1 - k)) % kScaleSlots] != 0;
+      for (int k = max(w.k0, w.t.prefix); k < w.k1; ++k) odd |= s_odd[(j1 - static_cast<uint32_t>(w.k1 - k)) % kScaleSlots] & 1;
       if (odd) {
         group_sync(grp);  // the rows are written
         if (there && (copies == 1 || (tg & (copies - 1)) == 0))
@@ -1244,7 +1277,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           s_last = adt::atomic_add_acq_rel_gpu(p.tickets + first, 1u) == static_cast<unsigned>(last - first);
         softmax_sync();
         if (s_last) {
-          // Partial rows joined: weights 2^(m_c - M) over their sum.  Neighbouring lanes
+          // Partial rows joined by their sums.  Neighbouring lanes
           // take neighbouring rows, a thread 16 columns at a time, of four CTAs' parts.
           constexpr int kAtOnce = 4;
           const int rows = min(w.t.n * p.group - w.blk * kRows, kRows);
@@ -1275,8 +1308,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                 for (int x = 0; x < kAtOnce; ++x) {
                   if (c + x > last) break;
-                  const float wt = weight(ml[x].x, Mj);
-                  lj += wt * ml[x].y;
+                  const float wt = level_factor(ml[x].x, Mj) * ml[x].y * kJoinScale;
+                  lj += wt;
 #pragma unroll
                   for (int e = 0; e < 4; ++e) {
                     acc[e].x += wt * v[x][e].x;
@@ -1296,7 +1329,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               uint4* dst = reinterpret_cast<uint4*>(p.out + at * D) + c16 * 2;
               dst[0] = make_uint4(y[0], y[1], y[2], y[3]);
               dst[1] = make_uint4(y[4], y[5], y[6], y[7]);
-              if (c16 == 0 && p.lse) p.lse[at] = (Mj + __log2f(lj)) * kLn2;
+              if (c16 == 0 && p.lse) p.lse[at] = (Mj + kJoinLevel + __log2f(lj)) * kLn2;
             }
           }
           if (tid == 0) p.tickets[first] = 0u;
