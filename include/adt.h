@@ -626,7 +626,9 @@ adt_status adt_kv_evict(const adt_bf16* k_src, const adt_bf16* v_src, int64_t sr
  * rows stand for.  Rows behind kv_len[b] are not used, whatever they hold.
  * A row of q that is not finite, or of k_tree for those who see it, makes its
  * outputs NaN; an element of v_tree that is not finite reaches its column for those
- * who see it.
+ * who see it.  Value rows that a tree's nodes see under one kv head lie within 2^96 of
+ * one another in scale, rows of zeros aside: smaller ones are counted, but their
+ * values not exact.
  * 1 <= max_nodes <= 256, any H % Hkv == 0, B * max_nodes * H <= 2^24.
  * Errors as for adt_tree_attn.
  * ------------------------------------------------------------------------ */

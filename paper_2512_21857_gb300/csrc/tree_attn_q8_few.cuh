@@ -14,10 +14,12 @@
 //
 // A weight takes on its value's scale 2^ev in the exponent: 2^(x c + ev - base), x c
 // the score, base the largest such exponent so far (raised only when a row grows by
-// more than 2^kFewThreshold).  The row sum adds it without 2^ev, against 2^top, the
-// largest scale so far.  A value whose scale is below 2^-60 of that (a row of zeros
-// has the least there is) adds nothing to O, and its weight is made as if it were
-// 2^-60 there, so that its part of the row sum is neither lost nor too large.
+// more than 2^kFewThreshold).  A value whose scale is below 2^-kSpan of the largest so
+// far, 2^top (a row of zeros has the least there is), adds nothing to O, and its weight is
+// made as if it were 2^-kSpan there, so that its part of the row sum is neither lost nor
+// too large.  The row sum adds weights times 2^(from - ev - kFewShift): `from` is the first
+// chunk's top, and follows the top 2^kFewLag below (where the top rises for a key that
+// means nothing to a row, the row's base stays, and its sum grows by what `from` does).
 //
 // Warp roles: 0-3, 4-7 two softmax groups that take the chunks in turn; 8 K tiles, 9 V
 // tiles; 10 S products; 11 PV products; 12-15 an item's start and end beside the
@@ -34,6 +36,7 @@
 // (The kernel of 128 rows took 115 and 13.)
 constexpr int kFewRows = 32;
 constexpr float kFewThreshold = 4.5f, kFewHeadroom = 4.f;  // weights up to 2^8.5: e4m3 ends at 448
+constexpr int kFewShift = 8, kFewLag = 80;  // row sums from 2^-84 to 2^97 a key: within fp32, their least parts too
 constexpr float kUnset = -3e38f;  // the base of a row that has seen no key
 constexpr int kNoScale = -1000;   // (scales are 2^-127 and more)
 constexpr int kLeastScale = -127;
@@ -116,7 +119,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   // Of an item's rows (and its tree's keys), by item.
   __shared__ __align__(16) float s_c[2][R], s_base[2][R];
   __shared__ float s_tk[2][R];
-  __shared__ int s_tv[2][R], s_top[2], s_ver[2], s_odd[2];
+  __shared__ int s_tv[2][R], s_top[2], s_from[2], s_ver[2], s_odd[2];
   __shared__ uint32_t s_seen[2][R];                    // of a key: the rows that see it
   __shared__ __align__(16) float s_gb[2][2][R], s_alpha[2][R];  // of a group: the level its row sums are at
   __shared__ float s_most[2][4][R];
@@ -452,7 +455,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       ok = !any_of<1, kConvThreads>(!ok);
       if (!ok) return;
       sm100::tc_fence_after();
-      const int at = item & 1, rows = w.t.n * p.group, w4 = warp & 3, top = s_top[at];
+      const int at = item & 1, rows = w.t.n * p.group, w4 = warp & 3, from = s_from[at];
       const uint32_t lanes = static_cast<uint32_t>(w4 * 32) << 16;
       // Row sums over the keys' lanes, at the bases' last level; of a group that had a chunk.
 #pragma unroll 1
@@ -465,7 +468,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           sm100::tmem_ld_16(tmem + lanes + C::kLAt + (at * 2 + g) * R + 16 * blk, r);
 #pragma unroll
           for (int e = 0; e < 16; ++e)
-            v[e] = fmaf(__uint_as_float(r[e]), ex2_approx(s_gb[at][g][16 * blk + e] - (s_base[at][16 * blk + e] - top)), v[e]);
+            v[e] = fmaf(__uint_as_float(r[e]), ex2_approx(s_gb[at][g][16 * blk + e] - (s_base[at][16 * blk + e] - from)), v[e]);
         }
         const float sum = transposed_sum(v, lane);
         if ((lane & 1) == 0) s_sum[16 * blk + (lane >> 1)][w4] = sum;
@@ -483,8 +486,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         const float4 a = *reinterpret_cast<const float4*>(s_sum[r]);
         return (a.x + a.y) + (a.z + a.w);
       };
-      const float unit = top < -126 ? 0x1p-127f : power_of_two(top);
-      // O, columns back to rows.
+      // O, columns back to rows, over the row sum and at its size, in two steps that stay within fp32.
+      const float unit = half_power(from - kFewShift);
 #pragma unroll 1
       for (int r0 = 0; r0 < rows; r0 += 8) {
         uint32_t o[3][8];
@@ -494,10 +497,12 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int e = 0; e < 8; ++e) {
           const int r = r0 + e;
           if (r >= rows || (D == 64 && lane >= 16)) break;
-          const float v =
-              fmaf(fmaf(__uint_as_float(o[2][e]), 0.0625f, __uint_as_float(o[1][e])), 0.0625f, __uint_as_float(o[0][e])) * unit;
+          float v = __uint_as_float(o[2][e]);
+#pragma unroll
+          for (int x = 1; x >= 0; --x) v = fmaf(v, 0.0625f, __uint_as_float(o[x][e]));
+          v = v * reciprocal(row_sum(r)) * unit * unit;
           if (whole)
-            p.out[out_row_of(r) * D + d] = __float2bfloat16(__fdividef(v, row_sum(r)));
+            p.out[out_row_of(r) * D + d] = __float2bfloat16(v);
           else
             part[r * D + d] = v;
         }
@@ -505,9 +510,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       sm100::tc_fence_before();
       if (ct < rows) {
-        const float l = row_sum(ct), m = s_base[at][ct] - top - kFewHeadroom;
+        const float l = row_sum(ct), m = s_base[at][ct] - from + (kFewShift - kFewHeadroom);
         if (!whole)
-          p.part_ml[slot + ct] = make_float2(m, l);
+          p.part_ml[slot + ct] = part_sum(m, l);
         else if (p.lse)
           p.lse[out_row_of(ct)] = (m + __log2f(l)) * kLn2;
       }
@@ -520,7 +525,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       if (whole) return;
       // The parts joined by the CTA that ends its own last, beside the next item's
-      // chunks: weights 2^(m_c - M) over their sum.
+      // chunks, by their sums.
       any_of<1, kConvThreads>(false);
       // (Which CTAs these are: as in the kernel of 128 rows.)
       const int64_t X = s_total, G = s_grid, a = w.start + kItemCost, z = a + w.t.chunks - 1;
@@ -542,8 +547,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int c = first; c <= last; ++c) {
           const float2 ml = __ldcg(&p.part_ml[slot_of(c) + r]);
           const float4 v = __ldcg(reinterpret_cast<const float4*>(po + (slot_of(c) + r) * D) + c4);
-          const float wt = ml.x == M ? 1.f : ex2_approx(ml.x - M);
-          l += wt * ml.y;
+          const float wt = level_factor(ml.x, M) * ml.y * kJoinScale;
+          l += wt;
           acc.x += wt * v.x;
           acc.y += wt * v.y;
           acc.z += wt * v.z;
@@ -554,7 +559,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         y.x = pack_bf16x2(acc.x * inv, acc.y * inv);
         y.y = pack_bf16x2(acc.z * inv, acc.w * inv);
         *reinterpret_cast<uint2*>(p.out + row * D + c4 * 4) = y;
-        if (c4 == 0 && p.lse) p.lse[row] = (M + __log2f(l)) * kLn2;
+        if (c4 == 0 && p.lse) p.lse[row] = (M + kJoinLevel + __log2f(l)) * kLn2;
       }
       if (ct == 0) p.tickets[first] = 0u;
     };
@@ -632,7 +637,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         };
         int top = s_top[at];
-        float evf = static_cast<float>(max(ev, top - 60));
+        float evf = static_cast<float>(max(ev, top - kSpan));
         bool raise = j == j0;
         if (!raise) {
           float most = -INFINITY;
@@ -658,7 +663,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (lane == 0) s_wtop[grp][w4] = wtop;
           group_sync(grp);
           top = max(max(max(s_wtop[grp][0], s_wtop[grp][1]), max(s_wtop[grp][2], s_wtop[grp][3])), top);
-          evf = static_cast<float>(max(ev, top - 60));
+          evf = static_cast<float>(max(ev, top - kSpan));
 #pragma unroll 1
           for (int blk = 0; blk < kBlocks; ++blk) {
             float x[16];
@@ -684,6 +689,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             s_alpha[grp][gt] = now == old ? 1.f : ex2_approx(old - now);
           }
           if (gt == 0) {
+            s_from[at] = s_top[at] == kNoScale ? top : max(s_from[at], top - kFewLag);
             s_top[at] = top;
             ++s_ver[at];
           }
@@ -704,6 +710,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (gt == 0) arrive(&bars.mu[grp]);
         const int now = s_ver[at];
+        const int from = s_from[at];
         // The row sums of this group come to the bases' new level.
         if (fresh || now != ver) {
 #pragma unroll 1
@@ -712,22 +719,22 @@ __global__ void __launch_bounds__(kThreads, 1)
             sm100::tmem_ld_16(l_col + 16 * blk, r);
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-              const float d = s_gb[at][grp][16 * blk + e] - (s_base[at][16 * blk + e] - top);
+              const float d = s_gb[at][grp][16 * blk + e] - (s_base[at][16 * blk + e] - from);
               r[e] = fresh ? 0u : __float_as_uint(__uint_as_float(r[e]) * ex2_approx(d));
             }
             tmem_st_16(l_col + 16 * blk, r);
           }
           sm100::tmem_wait_st();
           group_sync(grp);
-          if (gt < R) s_gb[at][grp][gt] = s_base[at][gt] - top;
+          if (gt < R) s_gb[at][grp][gt] = s_base[at][gt] - from;
           fresh = false;
           ver = now;
         }
         // P's tile was last read by PV(j - PT).
         ok = j < PT || all_wait(&bars.done[(j - PT) & 3], (j - PT) >> 2);
         if (!ok) continue;
-        const float iev = power_of_two(top - static_cast<int>(evf)), shift = evf + kFewHeadroom;
-        const uint32_t keep = ev < top - 60 ? 0u : ~0u;
+        const float iev = power_of_two(from - static_cast<int>(evf) - kFewShift), shift = evf + kFewHeadroom;
+        const uint32_t keep = ev < top - kSpan ? 0u : ~0u;
 #pragma unroll 1
         for (int blk = 0; blk < kBlocks; ++blk) {
           float x[16];

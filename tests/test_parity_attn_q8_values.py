@@ -21,9 +21,10 @@ def _built():
     ensure_built()
 
 
-# Items of up to 64 and 128 rows; whole ones and ones that several thread blocks share.
+# Items of up to 16, 32, 64 and 128 rows; whole ones and ones that several thread blocks share.
 MANY = [([40], [300], 2, 2, 64), ([40], [300], 2, 2, 128), ([100], [300], 2, 1, 128), ([33], [5000], 1, 1, 128),
         ([200], [2000], 1, 1, 64)]
+FEW = [([3], [300], 2, 2, 64), ([8], [300], 4, 1, 128), ([4], [5000], 4, 1, 128), ([31], [2000], 1, 1, 64)]
 
 
 def star(case):
@@ -109,4 +110,21 @@ def rows_of_zeros(sizes, kv, H, Hkv, D, up):
 @pytest.mark.parametrize("up", [0, 60])
 @pytest.mark.parametrize("sizes,kv,H,Hkv,D", MANY)
 def test_rows_of_zeros_beside_others(sizes, kv, H, Hkv, D, up):
+    rows_of_zeros(sizes, kv, H, Hkv, D, up)
+
+
+@pytest.mark.parametrize("apart", [18, 26, 40, 60, 80])
+@pytest.mark.parametrize("sizes,kv,H,Hkv,D", FEW)
+def test_values_far_above_those_that_count_of_few_rows(sizes, kv, H, Hkv, D, apart):
+    far_apart(sizes, kv, H, Hkv, D, apart)
+
+
+@pytest.mark.parametrize("sizes,kv,H,Hkv,D", FEW)
+def test_values_near_the_largest_of_few_rows(sizes, kv, H, Hkv, D):
+    larger_than_all(sizes, kv, H, Hkv, D)
+
+
+@pytest.mark.parametrize("up", [0, 60])
+@pytest.mark.parametrize("sizes,kv,H,Hkv,D", FEW)
+def test_rows_of_zeros_beside_others_of_few_rows(sizes, kv, H, Hkv, D, up):
     rows_of_zeros(sizes, kv, H, Hkv, D, up)
