@@ -7,10 +7,10 @@
 // few queries would leave empty, and no copy of V in a wider type.  A thread owns a
 // key: its scales are its own registers' and its weights a row of P^T.
 //
-// Weights meet V in three e4m3 numbers, 2^-4 apart: p = p1 + p2 / 16 + p3 / 256, each
-// what the ones before leave, with an accumulator each (columns of one product).
-// Two would lose keys of 2^-18 of the largest one's weight, of which a long cache can
-// have enough to matter; three end at 2^-22.
+// Weights meet V in four e4m3 numbers, 2^-4 apart: p = p1 + p2 / 16 + p3 / 256 + p4 / 4096,
+// each what the ones before leave, with an accumulator each (columns of one product).
+// Three hold all of a weight's bits, but end at 2^-22 of the largest one (times value
+// scale), and a cache of 30000 rows can have 0.7 % of its sum below; four end at 2^-26.
 //
 // A weight takes on its value's scale 2^ev in the exponent: 2^(x c + ev - base), x c
 // the score, base the largest such exponent so far (raised only when a row grows by
@@ -51,7 +51,7 @@ struct FewCfg {
   static constexpr int kQOff = 0;                       // [2 items][high, low]
   static constexpr int kTreeOff = kQOff + 4 * kQ;       // [2 items][K high, K low, V in three]
   static constexpr int kTreeBytes = 5 * kSmall;
-  // Weights [128 keys][p1, p2, p3, unused: R each], the swizzle as wide as a row.
+  // Weights [128 keys][p1, p2, p3, p4: R each], the swizzle as wide as a row.
   // Where they fit, two tiles a group: PV(j) is done 2000 cycles after P(j) is written.
   static constexpr int kPTiles = R == 16 ? 4 : 2;
   static constexpr int kPBytes = kChunk * 4 * R;
@@ -59,9 +59,9 @@ struct FewCfg {
   static constexpr int kKOff = kPOff + kPTiles * kPBytes;
   static constexpr int kVOff = kKOff + kStages * kTile;
   static constexpr int kDynSmem = kVOff + kStages * kTile + 1024;  // + alignment slack
-  static constexpr uint32_t kIdescO = sm100::idesc_e4m3_f32(D, 3 * R) | 1u << 15 | 1u << 16;  // both MN-major
-  // Tensor memory: four S tiles of R columns, O of two items (3 R), row sums [2 items][2 groups] of R.
-  static constexpr uint32_t kOAt = 4 * R, kLAt = 10 * R;
+  static constexpr uint32_t kIdescO = sm100::idesc_e4m3_f32(D, 4 * R) | 1u << 15 | 1u << 16;  // both MN-major
+  // Tensor memory: four S tiles of R columns, O of two items (4 R), row sums [2 items][2 groups] of R.
+  static constexpr uint32_t kOAt = 4 * R, kLAt = 12 * R;
   static constexpr uint32_t kCols = R == 16 ? 256 : 512;
 };
 
@@ -315,7 +315,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const uint64_t vd = (tree_k ? td0 + ((item & 1) * C::kTreeBytes + (2 + kk) * C::kSmall) / 16
                                         : vd0 + (st * C::kTile + kk * 32 * D) / 16);
             const int part = tree_k ? kk : 0;
-            sm100::mma_f8_ss(tmem + C::kOAt + ((item & 1) * 3 + part) * R, vd, pd + (kk - part) * (32 * 4 * R / 16),
+            sm100::mma_f8_ss(tmem + C::kOAt + ((item & 1) * 4 + part) * R, vd, pd + (kk - part) * (32 * 4 * R / 16),
                              C::kIdescO - (static_cast<uint32_t>(part * R >> 3) << 17), more);
             more = 1u;
           }
@@ -490,16 +490,16 @@ __global__ void __launch_bounds__(kThreads, 1)
       const float unit = half_power(from - kFewShift);
 #pragma unroll 1
       for (int r0 = 0; r0 < rows; r0 += 8) {
-        uint32_t o[3][8];
+        uint32_t o[4][8];
 #pragma unroll
-        for (int x = 0; x < 3; ++x) sm100::tmem_ld_8(tmem + lanes + C::kOAt + (at * 3 + x) * R + r0, o[x]);
+        for (int x = 0; x < 4; ++x) sm100::tmem_ld_8(tmem + lanes + C::kOAt + (at * 4 + x) * R + r0, o[x]);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const int r = r0 + e;
           if (r >= rows || (D == 64 && lane >= 16)) break;
-          float v = __uint_as_float(o[2][e]);
+          float v = __uint_as_float(o[3][e]);
 #pragma unroll
-          for (int x = 1; x >= 0; --x) v = fmaf(v, 0.0625f, __uint_as_float(o[x][e]));
+          for (int x = 2; x >= 0; --x) v = fmaf(v, 0.0625f, __uint_as_float(o[x][e]));
           v = v * reciprocal(row_sum(r)) * unit * unit;
           if (whole)
             p.out[out_row_of(r) * D + d] = __float2bfloat16(v);
@@ -585,7 +585,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     bool ok = true, left = false;
     for (; !left && w.more; w = next_item(p, w), ++item) {
       const int at = item & 1;
-      const uint32_t o_col = tmem + lanes + C::kOAt + at * 3 * R, l_col = tmem + lanes + C::kLAt + (at * 2 + grp) * R;
+      const uint32_t o_col = tmem + lanes + C::kOAt + at * 4 * R, l_col = tmem + lanes + C::kLAt + (at * 2 + grp) * R;
       const uint32_t j0 = j, j1 = j + static_cast<uint32_t>(w.k1 - w.k0);
       // (Then the item before the last is read from tensor and shared memory, too.)
       ok = ok && all_wait(&bars.prep_full[item & 1], item >> 1);
@@ -697,7 +697,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (j > j0) {
             sm100::tc_fence_after();
 #pragma unroll 1
-            for (int c = 0; c < 3 * R; c += 16) {
+            for (int c = 0; c < 4 * R; c += 16) {
               uint32_t r[16];
               sm100::tmem_ld_16(o_col + c, r);
 #pragma unroll
@@ -743,7 +743,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           sm100::tmem_ld_16(l_col + 16 * blk, r);
           const float4* c4 = reinterpret_cast<const float4*>(s_c[at] + 16 * blk);
           const float4* b4 = reinterpret_cast<const float4*>(s_base[at] + 16 * blk);
-          uint32_t p1[4], p2[4], p3[4];
+          uint32_t p1[4], p2[4], p3[4], p4[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const float4 c = c4[e], b = b4[e];
@@ -757,26 +757,31 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
 #pragma unroll
             for (int f = 0; f < 2; ++f) h[f] = pack_half2(x[4 * e + 2 * f], x[4 * e + 2 * f + 1]);
-            p1[e] = p2[e] = p3[e] = 0u;
+            p1[e] = p2[e] = p3[e] = p4[e] = 0u;
 #pragma unroll
             for (int f = 0; f < 2; ++f) {
               const uint16_t a1 = f16x2_to_e4m3(h[f]);
               const uint32_t r1 = rest16(h[f], a1);
               const uint16_t a2 = f16x2_to_e4m3(r1);
-              const uint16_t a3 = f16x2_to_e4m3(rest16(r1, a2));
+              const uint32_t r2 = rest16(r1, a2);
+              const uint16_t a3 = f16x2_to_e4m3(r2);
+              const uint16_t a4 = f16x2_to_e4m3(rest16(r2, a3));
               p1[e] |= static_cast<uint32_t>(a1) << (16 * f);
               p2[e] |= static_cast<uint32_t>(a2) << (16 * f);
               p3[e] |= static_cast<uint32_t>(a3) << (16 * f);
+              p4[e] |= static_cast<uint32_t>(a4) << (16 * f);
             }
             p1[e] = nan_v ? 0x7f7f7f7fu : p1[e] & keep;
             p2[e] &= keep;
             p3[e] &= keep;
+            p4[e] &= keep;
           }
           tmem_st_16(l_col + 16 * blk, r);
           uint8_t* tile_p = sP + (j % PT) * C::kPBytes;
           *reinterpret_cast<uint4*>(tile_p + tile_off<4 * R>(key, blk)) = make_uint4(p1[0], p1[1], p1[2], p1[3]);
           *reinterpret_cast<uint4*>(tile_p + tile_off<4 * R>(key, kBlocks + blk)) = make_uint4(p2[0], p2[1], p2[2], p2[3]);
           *reinterpret_cast<uint4*>(tile_p + tile_off<4 * R>(key, 2 * kBlocks + blk)) = make_uint4(p3[0], p3[1], p3[2], p3[3]);
+          *reinterpret_cast<uint4*>(tile_p + tile_off<4 * R>(key, 3 * kBlocks + blk)) = make_uint4(p4[0], p4[1], p4[2], p4[3]);
         }
         sm100::fence_proxy_async_smem();
         sm100::tmem_wait_st();
