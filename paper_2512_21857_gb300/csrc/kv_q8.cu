@@ -275,6 +275,7 @@ adt_status adt_kv_read_q8(const uint8_t* k_cache, const uint8_t* v_cache, const 
   for (int i = 0; i < 4; ++i)
     ADT_REQUIRE(!adt::spans_overlap(in[i], i < 2 ? cache_span : scale_span, k_out, out_span * 2) &&
                 !adt::spans_overlap(in[i], i < 2 ? cache_span : scale_span, v_out, out_span * 2));
+  ADT_REQUIRE(!adt::spans_overlap(kv_len, B * 4ll, k_out, out_span * 2) && !adt::spans_overlap(kv_len, B * 4ll, v_out, out_span * 2));
   const int64_t v_off = static_cast<int64_t>(reinterpret_cast<uintptr_t>(v_out) - reinterpret_cast<uintptr_t>(k_out)) / 2;
   ADT_REQUIRE(v_off != 0 && !adt::slices_meet(counts, os, slice, 0) && !adt::slices_meet(counts, os, slice, v_off));
   ReadQ8Params p{};
