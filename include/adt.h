@@ -612,7 +612,8 @@ adt_status adt_kv_evict(const adt_bf16* k_src, const adt_bf16* v_src, int64_t sr
  * errors otherwise.  Of a row x the scale is the least power of two with max |x|
  * <= 448 * 2^(s - 127), s >= 7; the elements x * 2^(127 - s) are rounded to the
  * nearest e4m3 value, halves to even.  A row with an infinity or a NaN becomes s =
- * 255 and zeros.  kv_len_out does not overlap kv_len.
+ * 255 and zeros.  kv_len_out overlaps none of the lengths, paths, offsets, caches and
+ * scales.
  *
  * adt_kv_read_q8 - rows 0 .. kv_len[b]-1 of every layer, tree and kv head as
  * bf16 (exact for what adt_kv_compact_q8 wrote), where bf16 operators take

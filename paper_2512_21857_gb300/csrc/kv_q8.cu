@@ -191,7 +191,6 @@ adt_status adt_kv_compact_q8(uint8_t* k_cache, uint8_t* v_cache, uint8_t* k_scal
   ADT_REQUIRE(k_cache && v_cache && k_scale && v_scale && kv_len && k_tree && v_tree && node_offsets && path && accept_len);
   ADT_REQUIRE(B >= 1 && B <= 65535 && Hkv >= 1 && Hkv <= 65535 && num_layers >= 1 && num_layers <= 65535);
   ADT_REQUIRE(max_path >= 1 && max_path <= (1 << 20) && max_kv >= 1 && max_kv < (1 << 30));
-  ADT_REQUIRE(!kv_len_out || !adt::spans_overlap(kv_len, B * 4ll, kv_len_out, B * 4ll));
   if (D != 64 && D != 128) return ADT_ERR_UNSUPPORTED;
   const adt::Q8Strides s = {{cache_layer_stride, cache_stride_b, cache_stride_h},
                             {scale_layer_stride, scale_stride_b, scale_stride_h}};
@@ -199,6 +198,11 @@ adt_status adt_kv_compact_q8(uint8_t* k_cache, uint8_t* v_cache, uint8_t* k_scal
   adt_status st = adt::check_q8_cache(k_cache, v_cache, k_scale, v_scale, s, num_layers, B, Hkv, D, max_kv, true,
                                       &cache_span, &scale_span);
   if (st != ADT_OK) return st;
+  // (Every layer's CTAs read what one of the first layer's would write over.)
+  const struct { const void* p; int64_t bytes; } others[] = {
+      {kv_len, B * 4ll}, {accept_len, B * 4ll}, {node_offsets, (B + 1) * 4ll}, {path, B * 4ll * max_path},
+      {k_cache, cache_span}, {v_cache, cache_span}, {k_scale, scale_span}, {v_scale, scale_span}};
+  for (const auto& x : others) ADT_REQUIRE(!kv_len_out || !adt::spans_overlap(x.p, x.bytes, kv_len_out, B * 4ll));
   ADT_REQUIRE(num_layers == 1 || (tree_layer_stride >= 0 && tree_layer_stride % 8 == 0 &&
                                   tree_layer_stride <= adt::kMaxCacheStride));
   ADT_REQUIRE(adt::aligned16(k_tree) && adt::aligned16(v_tree));
