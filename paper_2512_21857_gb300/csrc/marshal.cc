@@ -340,7 +340,7 @@ adt_status tree_attn_q8(Args& a) {
       as<adt_bf16>(vec(&vt, at::kBFloat16, p.dev, tn, "v_tree")), as<int32_t>(vec(&par, at::kInt, p.dev, N, "parents")),
       as<int32_t>(vec(&offs, at::kInt, p.dev, B + int64_t{1}, "node_offsets")), B, H, Hkv, D, max_nodes, max_kv, scale,
       as<adt_bf16>(vec(&out, at::kBFloat16, p.dev, qn, "out")), as<float>(vec(lse, at::kFloat, p.dev, N * H, "lse")),
-      addr(&ws, at::kByte, p.dev, "workspace"), ws.nbytes(), p.stream);
+      vec(&ws, at::kByte, p.dev, 0, "workspace"), ws.nbytes(), p.stream);
 }
 
 template <adt_status (*F)(Args&)>
