@@ -131,6 +131,16 @@ void* vec(const Tensor* t, ScalarType type, int dev, int64_t count, const char* 
   return p;
 }
 
+// A call of the library, without the interpreter's lock: a launch waits where the
+// device's queue is full, which may be for another thread's sake.
+template <class F, class... A>
+adt_status unlocked(F f, A... a) {
+  PyThreadState* state = PyEval_SaveThread();
+  const adt_status st = f(a...);
+  PyEval_RestoreThread(state);
+  return st;
+}
+
 template <class T>
 T* as(void* p) {
   return static_cast<T*>(p);
@@ -261,7 +271,8 @@ adt_status norm_rope_qkv(Args& a) {
   const int32_t* positions = as<int32_t>(vec(&pos, at::kInt, p.dev, N, "positions"));
   const double* freq = as<double>(vec(&inv, at::kDouble, p.dev, 0, "inv_freq"));
   if (inv.numel() > (1 << 20)) bad_value("inv_freq: too many");
-  return g_lib.norm_rope_qkv(rq.in, rq.ld, rk.in, rk.ld, rv.in, rv.ld, static_cast<adt_dtype>(in_type), static_cast<adt_norm>(norm),
+  return unlocked(
+      g_lib.norm_rope_qkv, rq.in, rq.ld, rk.in, rk.ld, rv.in, rv.ld, static_cast<adt_dtype>(in_type), static_cast<adt_norm>(norm),
                            eps, aq.weight, aq.bias, aq.stride, ak.weight, ak.bias, ak.stride,
                            static_cast<adt_dtype>(weight_type), positions, freq, magnitude, static_cast<adt_rope_layout>(layout),
                            static_cast<int32_t>(N), H, Hkv, D, static_cast<int32_t>(2 * inv.numel()), as<adt_bf16>(rq.out),
@@ -295,7 +306,8 @@ adt_status kv_compact_q8(Args& a) {
   a.done();
   const Cache c = cache_of(kc, vc, ks, vs, layers, B, Hkv, max_kv, D, false, p.dev);
   const int64_t tls = tree_stride(kt, vt, layers, Hkv, D);
-  return g_lib.kv_compact_q8(
+  return unlocked(
+      g_lib.kv_compact_q8,
       c.k, c.v, c.ks, c.vs, as<int32_t>(vec(&kv, at::kInt, p.dev, B, "kv_len")), as<int32_t>(vec(kvo, at::kInt, p.dev, B, "kv_len_out")),
       as<adt_bf16>(addr(&kt, at::kBFloat16, p.dev, "k_tree")), as<adt_bf16>(addr(&vt, at::kBFloat16, p.dev, "v_tree")),
       as<int32_t>(vec(&offs, at::kInt, p.dev, B + int64_t{1}, "node_offsets")),
@@ -313,7 +325,8 @@ adt_status kv_read_q8(Args& a) {
   const Cache c = cache_of(kc, vc, ks, vs, layers, B, Hkv, max_kv, D, false, p.dev);
   const Strides os = strides_of(ko, layers, B, Hkv, max_kv, D, false, "k_out");
   if (!(strides_of(vo, layers, B, Hkv, max_kv, D, false, "v_out") == os)) bad_value("k_out and v_out must share strides");
-  return g_lib.kv_read_q8(c.k, c.v, c.ks, c.vs, as<int32_t>(vec(&kv, at::kInt, p.dev, B, "kv_len")),
+  return unlocked(
+      g_lib.kv_read_q8, c.k, c.v, c.ks, c.vs, as<int32_t>(vec(&kv, at::kInt, p.dev, B, "kv_len")),
                         as<adt_bf16>(addr(&ko, at::kBFloat16, p.dev, "k_out")), as<adt_bf16>(addr(&vo, at::kBFloat16, p.dev, "v_out")),
                         B, Hkv, D, layers, max_kv, c.cs.s[0], c.cs.s[1], c.cs.s[2], c.ss.s[0], c.ss.s[1], c.ss.s[2], os.s[0],
                         os.s[1], os.s[2], p.stream);
@@ -334,7 +347,8 @@ adt_status tree_attn_q8(Args& a) {
   if (q.dim() < 1) bad_value("q: expected [Ntot, H, D]");
   const int64_t N = q.size(0), qn = N * H * D, tn = N * Hkv * D;
   const Cache c = cache_of(kc, vc, ks, vs, 1, B, Hkv, max_kv, D, true, p.dev);
-  return g_lib.tree_attn_q8(
+  return unlocked(
+      g_lib.tree_attn_q8,
       as<adt_bf16>(vec(&q, at::kBFloat16, p.dev, qn, "q")), c.k, c.v, c.ks, c.vs, as<int32_t>(vec(&kv, at::kInt, p.dev, B, "kv_len")),
       c.cs.s[1], c.cs.s[2], c.ss.s[1], c.ss.s[2], as<adt_bf16>(vec(&kt, at::kBFloat16, p.dev, tn, "k_tree")),
       as<adt_bf16>(vec(&vt, at::kBFloat16, p.dev, tn, "v_tree")), as<int32_t>(vec(&par, at::kInt, p.dev, N, "parents")),
