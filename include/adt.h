@@ -631,7 +631,7 @@ adt_status adt_kv_evict(const adt_bf16* k_src, const adt_bf16* v_src, int64_t sr
  * one another in scale, rows of zeros aside: smaller ones are counted, but their
  * values not exact.
  * A weight is rounded to 11 bits, and ends at 2^-26 of the row's largest (each
- * times its value's scale; of more than 32 rows of a tree and kv head at 2^-31): n
+ * times its value's scale; of more than 16 rows of a tree and kv head at 2^-31): n
  * keys of less can be off by n times as much of the output, and lse has them all.
  * 1 <= max_nodes <= 256, any H % Hkv == 0, B * max_nodes * H <= 2^24.
  * Errors as for adt_tree_attn.

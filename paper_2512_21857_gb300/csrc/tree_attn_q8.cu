@@ -9,7 +9,7 @@
 // fill the device alike; an item that a share's end cuts is joined from partial
 // rows (outputs of its parts, and their sums) in the workspace by the CTA that ends its
 // part last.
-// Two kernels share this: of up to 32 rows tree_attn_q8_few.cuh, of more this one.
+// Two kernels share this: of up to 16 rows tree_attn_q8_few.cuh, of more this one.
 //
 // S = Q K^T is made of e4m3 products, K as it lies in the cache: a query row,
 // scaled by a power of two to at most 448, is cut into an e4m3 row and another of
@@ -1375,7 +1375,7 @@ int slot_rows_for(int H, int Hkv, int max_nodes) {
 }
 
 // Tickets at the start, for any grid; two items' partial rows of each CTA; what is
-// prepared where the items have more than 32 rows.  (Offsets from `base`, which may be NULL; at most 2^24 query rows, so
+// prepared where the items have more than 16 rows.  (Offsets from `base`, which may be NULL; at most 2^24 query rows, so
 // that all sizes stay below 2^50.)
 size_t ws_layout(uint8_t* base, int grid, int B, int H, int Hkv, int D, int max_nodes, AttnParams* p) {
   const int rows = slot_rows_for(H, Hkv, max_nodes);
@@ -1423,8 +1423,7 @@ adt_status launch(const AttnParams& p, const CUtensorMap& tm, const CUtensorMap&
   unsigned& word = configured[(dev >> 5) & 1];
   if (!(__atomic_load_n(&word, __ATOMIC_ACQUIRE) & bit)) {
     ADT_CUDA_TRY(cudaFuncSetAttribute(tree_attn_q8_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D>::kDynSmem));
-    ADT_CUDA_TRY(cudaFuncSetAttribute(tree_attn_q8_few_kernel<D, 16>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewCfg<D, 16>::kDynSmem));
-    ADT_CUDA_TRY(cudaFuncSetAttribute(tree_attn_q8_few_kernel<D, 32>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewCfg<D, 32>::kDynSmem));
+    ADT_CUDA_TRY(cudaFuncSetAttribute(tree_attn_q8_few_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewCfg<D>::kDynSmem));
     __atomic_fetch_or(&word, bit, __ATOMIC_ACQ_REL);
   }
   cudaLaunchConfig_t cfg = {};
@@ -1432,15 +1431,13 @@ adt_status launch(const AttnParams& p, const CUtensorMap& tm, const CUtensorMap&
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   cfg.stream = st;
-  auto few = [&](auto kernel, int bytes) -> adt_status {
+  if (p.max_nodes * p.group <= kFewRows) {
     cfg.gridDim = dim3(static_cast<unsigned>(grid), 1, 1);
     cfg.blockDim = dim3(kThreads, 1, 1);
-    cfg.dynamicSmemBytes = static_cast<size_t>(bytes);
-    ADT_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, tm, tm_v, p));
+    cfg.dynamicSmemBytes = FewCfg<D>::kDynSmem;
+    ADT_CUDA_TRY(cudaLaunchKernelEx(&cfg, tree_attn_q8_few_kernel<D>, tm, tm_v, p));
     return adt::launch_status();
-  };
-  if (p.max_nodes * p.group <= 16) return few(tree_attn_q8_few_kernel<D, 16>, FewCfg<D, 16>::kDynSmem);
-  if (p.max_nodes * p.group <= kFewRows) return few(tree_attn_q8_few_kernel<D, 32>, FewCfg<D, 32>::kDynSmem);
+  }
   constexpr int kPass = kPrepThreads / (D / 16);
   const int64_t units = static_cast<int64_t>(p.max_nodes) * p.H + ((p.max_nodes + 15) & ~15) * static_cast<int64_t>(p.Hkv);
   cfg.gridDim = dim3(static_cast<unsigned>((units + kPass - 1) / kPass), static_cast<unsigned>(p.B), 1);

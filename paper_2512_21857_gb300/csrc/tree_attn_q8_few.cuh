@@ -1,9 +1,9 @@
-// adt_tree_attn_q8 of few query rows (up to 32 of a tree and kv head: single tokens
+// adt_tree_attn_q8 of few query rows (up to 16 of a tree and kv head: single tokens
 // with grouped heads, small trees).  Included by tree_attn_q8.cu, which holds the
 // kernel of 128 rows and what both share.
 //
 // Products with the keys as the 128 rows of a tile: S^T = K Q^T, O^T = V^T P^T,
-// both of e4m3 operands as they lie in the cache; 32 columns instead of 128 rows that
+// both of e4m3 operands as they lie in the cache; 16 columns instead of 128 rows that
 // few queries would leave empty, and no copy of V in a wider type.  A thread owns a
 // key: its scales are its own registers' and its weights a row of P^T.
 //
@@ -29,40 +29,45 @@
 // out and joined.
 //
 // Bound by HBM where caches are long: 16 sequences of 1 to 30011 rows, 32 / 8 heads x
-// 128 (353 MB) 74 us, 70 % of a copy's rate.  Within an item the tiles come at 5.5
-// TB/s, which is what a plain kernel that only reads them gets with cold caches too;
-// about 15 us are the shares' calculation, the first tiles' way and the last one's.
-// Short ones are a chain of waits: one sequence of 512 rows, 8 heads x 64, 11.4 us.
-// (The kernel of 128 rows took 115 and 13.)
-constexpr int kFewRows = 32;
+// 128 (353 MB) 75 us, 70 % of a copy's rate; about 15 us are the shares' calculation, the
+// first tiles' way and the last one's.  Short ones are a chain of waits: one sequence of
+// 512 rows, 8 heads x 64, 11.5 us.
+//
+// The rule, 16 rows: this kernel against that of 128 rows, us, D = 64 and 128.  Four trees
+// over 2400 rows, 16 / 16 heads: of 1 node 19.8 and 20.8 (27 and 29), of 16 nodes 24.2 and
+// 28.8 (27.3 and 30.3).  Eight tokens over 8000 rows, 16 query heads to each of 8 kv heads:
+// 36.6 and 41.5 (49.4 and 51.6).  With 32 columns it takes for trees of 17 nodes 28.9 and
+// 33.7 (28.0 and 31.4), of 32 nodes 33.5 and 41.5 (28.0 and 31.7), one of 26 nodes over 512
+// rows, 8 heads x 64, 19.2 (12.9); of 20 heads to a kv head 47.1 and 51.6 (49.4 and 51.9).
+constexpr int kFewRows = 16;
+constexpr int kTreeRows = 32;  // of a tree's tiles: keys of a product
 constexpr float kFewThreshold = 4.5f, kFewHeadroom = 4.f;  // weights up to 2^8.5: e4m3 ends at 448
 constexpr int kFewShift = 8, kFewLag = 80;  // row sums from 2^-84 to 2^97 a key: within fp32, their least parts too
 constexpr float kUnset = -3e38f;  // the base of a row that has seen no key
 constexpr int kNoScale = -1000;   // (scales are 2^-127 and more)
 constexpr int kLeastScale = -127;
 
-// R: 16 or 32, the most rows of an item.
-template <int D, int R>
+template <int D>
 struct FewCfg {
   static constexpr int kStages = D == 128 ? 4 : 8;
   static constexpr int kTile = kChunk * D;
-  static constexpr int kQ = R * D;                      // queries, high or low part
-  static constexpr int kSmall = kFewRows * D;           // a tree's keys or values, a part
+  static constexpr int kQ = kFewRows * D;                      // queries, high or low part
+  static constexpr int kSmall = kTreeRows * D;          // a tree's keys or values, a part
   static constexpr int kQOff = 0;                       // [2 items][high, low]
   static constexpr int kTreeOff = kQOff + 4 * kQ;       // [2 items][K high, K low, V in three]
   static constexpr int kTreeBytes = 5 * kSmall;
-  // Weights [128 keys][p1, p2, p3, p4: R each], the swizzle as wide as a row.
-  // Where they fit, two tiles a group: PV(j) is done 2000 cycles after P(j) is written.
-  static constexpr int kPTiles = R == 16 ? 4 : 2;
-  static constexpr int kPBytes = kChunk * 4 * R;
+  // Weights [128 keys][p1, p2, p3, p4: kFewRows each], the swizzle as wide as a row.
+  // Two tiles a group: PV(j) is done 2000 cycles after P(j) is written.
+  static constexpr int kPTiles = 4;
+  static constexpr int kPBytes = kChunk * 4 * kFewRows;
   static constexpr int kPOff = kTreeOff + 2 * kTreeBytes;
   static constexpr int kKOff = kPOff + kPTiles * kPBytes;
   static constexpr int kVOff = kKOff + kStages * kTile;
   static constexpr int kDynSmem = kVOff + kStages * kTile + 1024;  // + alignment slack
-  static constexpr uint32_t kIdescO = sm100::idesc_e4m3_f32(D, 4 * R) | 1u << 15 | 1u << 16;  // both MN-major
-  // Tensor memory: four S tiles of R columns, O of two items (4 R), row sums [2 items][2 groups] of R.
-  static constexpr uint32_t kOAt = 4 * R, kLAt = 12 * R;
-  static constexpr uint32_t kCols = R == 16 ? 256 : 512;
+  static constexpr uint32_t kIdescO = sm100::idesc_e4m3_f32(D, 4 * kFewRows) | 1u << 15 | 1u << 16;  // both MN-major
+  // Tensor memory: four S tiles of kFewRows columns, O of two items (4 kFewRows), row sums [2 items][2 groups] of kFewRows.
+  static constexpr uint32_t kOAt = 4 * kFewRows, kLAt = 12 * kFewRows;
+  static constexpr uint32_t kCols = 16 * kFewRows;
 };
 
 struct FewBars {
@@ -107,25 +112,25 @@ __device__ __forceinline__ float warp_most(float v) {
   return r;
 }
 
-template <int D, int R>
+template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
     tree_attn_q8_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                             const __grid_constant__ AttnParams p) {
-  using C = FewCfg<D, R>;
+  using C = FewCfg<D>;
   constexpr int NS = C::kStages, PT = C::kPTiles;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (sm100::smem_addr(smem_raw) & 1023u)) & 1023u);
   __shared__ FewBars bars;
   // Of an item's rows (and its tree's keys), by item.
-  __shared__ __align__(16) float s_c[2][R], s_base[2][R];
-  __shared__ float s_tk[2][R];
-  __shared__ int s_tv[2][R], s_top[2], s_from[2], s_ver[2], s_odd[2];
-  __shared__ uint32_t s_seen[2][R];                    // of a key: the rows that see it
-  __shared__ __align__(16) float s_gb[2][2][R], s_alpha[2][R];  // of a group: the level its row sums are at
-  __shared__ float s_most[2][4][R];
+  __shared__ __align__(16) float s_c[2][kFewRows], s_base[2][kFewRows];
+  __shared__ float s_tk[2][kFewRows];
+  __shared__ int s_tv[2][kFewRows], s_top[2], s_from[2], s_ver[2], s_odd[2];
+  __shared__ uint32_t s_seen[2][kFewRows];                    // of a key: the rows that see it
+  __shared__ __align__(16) float s_gb[2][2][kFewRows], s_alpha[2][kFewRows];  // of a group: the level its row sums are at
+  __shared__ float s_most[2][4][kFewRows];
   __shared__ int s_wtop[2][4];
-  __shared__ __align__(16) float s_sum[R][4];          // of a row: the warps' parts
-  __shared__ int16_t s_par[R];
+  __shared__ __align__(16) float s_sum[kFewRows][4];          // of a row: the warps' parts
+  __shared__ int16_t s_par[kFewRows];
   __shared__ Walk s_walk;
   __shared__ int64_t s_total;
   __shared__ int s_grid;
@@ -256,7 +261,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint64_t qd0 = tile_desc<D>(sm100::smem_addr(sQ)), kd0 = tile_desc<D>(sm100::smem_addr(sK)),
                      td0 = tile_desc<D>(sm100::smem_addr(sT));
       for (; ok && w.more; w = next_item(p, w), ++item) {
-        const uint32_t idesc = sm100::idesc_e4m3_f32(kChunk, R);
+        const uint32_t idesc = sm100::idesc_e4m3_f32(kChunk, kFewRows);
         ok = wait(&bars.prep_full[item & 1], item >> 1);
         for (int k = w.k0; ok && k < w.k1; ++k, ++j) {
           const bool tree_k = k >= w.t.prefix;
@@ -275,7 +280,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const uint64_t kd = tree_k ? td0 + ((item & 1) * C::kTreeBytes + (part >> 1) * C::kSmall) / 16 : kd0 + st * (C::kTile / 16);
 #pragma unroll
             for (int kk = 0; kk < D / 32; ++kk) {
-              sm100::mma_f8_ss(tmem + (j & 3) * R, kd + kk * 2, qd + kk * 2, idesc, more);
+              sm100::mma_f8_ss(tmem + (j & 3) * kFewRows, kd + kk * 2, qd + kk * 2, idesc, more);
               more = 1u;
             }
           }
@@ -297,7 +302,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       bool ok = true;
       // (MN-major: columns of 8 keys 1024 bytes apart, at D = 64 512.)
       const uint64_t vd0 = tile_desc<D>(sm100::smem_addr(sV)), td0 = tile_desc<D>(sm100::smem_addr(sT)),
-                     pd0 = tile_desc<4 * R>(sm100::smem_addr(sP));
+                     pd0 = tile_desc<4 * kFewRows>(sm100::smem_addr(sP));
       for (; ok && w.more; w = next_item(p, w), ++item) {
         for (int k = w.k0; ok && k < w.k1; ++k, ++j) {
           const bool tree_k = k >= w.t.prefix;
@@ -315,8 +320,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             const uint64_t vd = (tree_k ? td0 + ((item & 1) * C::kTreeBytes + (2 + kk) * C::kSmall) / 16
                                         : vd0 + (st * C::kTile + kk * 32 * D) / 16);
             const int part = tree_k ? kk : 0;
-            sm100::mma_f8_ss(tmem + C::kOAt + ((item & 1) * 4 + part) * R, vd, pd + (kk - part) * (32 * 4 * R / 16),
-                             C::kIdescO - (static_cast<uint32_t>(part * R >> 3) << 17), more);
+            sm100::mma_f8_ss(tmem + C::kOAt + ((item & 1) * 4 + part) * kFewRows, vd, pd + (kk - part) * (32 * 4 * kFewRows / 16),
+                             C::kIdescO - (static_cast<uint32_t>(part * kFewRows >> 3) << 17), more);
             more = 1u;
           }
           sm100::mma_commit(sm100::smem_addr(&bars.done[j & 3]));
@@ -366,7 +371,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       fetch(cr);
       if (tree && ct < n) up = p.parents[w.t.node0 + ct];
       any_of<1, kConvThreads>(false);
-      if (ct < R) s_base[at][ct] = kUnset;
+      if (ct < kFewRows) s_base[at][ct] = kUnset;
       if (tree && ct < n) {
         s_par[ct] = static_cast<int16_t>(min(max(up, -1), kMaxTreeNodes));
         if ((ct == 0) != (up < 0) || up >= ct) adt::raise_error(p.err, ADT_DEVERR_BAD_TREE);
@@ -412,15 +417,15 @@ __global__ void __launch_bounds__(kThreads, 1)
         else
           s_tk[at][r] = __uint_as_float(s << 23);
       }
-      // Zeros: the queries up to R (their scores are read), values up to the 32 that a product reads.
+      // Zeros: the queries up to kFewRows (their scores are read), values up to the 32 that a product reads.
 #pragma unroll 1
-      for (int i = rows * D / 16 + ct; i < R * D / 16; i += kConvThreads) {
+      for (int i = rows * D / 16 + ct; i < kFewRows * D / 16; i += kConvThreads) {
         reinterpret_cast<uint4*>(q)[i] = reinterpret_cast<uint4*>(q + C::kQ)[i] = make_uint4(0u, 0u, 0u, 0u);
         if (i % (D / 16) == 0) s_c[at][i / (D / 16)] = 1.f;
       }
       if (tree) {
 #pragma unroll 1
-        for (int i = n * D / 16 + ct; i < kFewRows * D / 16; i += kConvThreads) {
+        for (int i = n * D / 16 + ct; i < kTreeRows * D / 16; i += kConvThreads) {
           uint4* v = reinterpret_cast<uint4*>(t + 2 * C::kSmall) + i;
           v[0] = v[C::kSmall / 16] = v[2 * C::kSmall / 16] = make_uint4(0u, 0u, 0u, 0u);
         }
@@ -459,13 +464,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint32_t lanes = static_cast<uint32_t>(w4 * 32) << 16;
       // Row sums over the keys' lanes, at the bases' last level; of a group that had a chunk.
 #pragma unroll 1
-      for (int blk = 0; blk < R / 16; ++blk) {
+      for (int blk = 0; blk < kFewRows / 16; ++blk) {
         float v[16] = {};
 #pragma unroll 1
         for (int g = 0; g < 2; ++g) {
           if (w.k1 - w.k0 < 2 && (j0 & 1) != static_cast<uint32_t>(g)) continue;
           uint32_t r[16];
-          sm100::tmem_ld_16(tmem + lanes + C::kLAt + (at * 2 + g) * R + 16 * blk, r);
+          sm100::tmem_ld_16(tmem + lanes + C::kLAt + (at * 2 + g) * kFewRows + 16 * blk, r);
 #pragma unroll
           for (int e = 0; e < 16; ++e)
             v[e] = fmaf(__uint_as_float(r[e]), ex2_approx(s_gb[at][g][16 * blk + e] - (s_base[at][16 * blk + e] - from)), v[e]);
@@ -492,7 +497,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       for (int r0 = 0; r0 < rows; r0 += 8) {
         uint32_t o[4][8];
 #pragma unroll
-        for (int x = 0; x < 4; ++x) sm100::tmem_ld_8(tmem + lanes + C::kOAt + (at * 4 + x) * R + r0, o[x]);
+        for (int x = 0; x < 4; ++x) sm100::tmem_ld_8(tmem + lanes + C::kOAt + (at * 4 + x) * kFewRows + r0, o[x]);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const int r = r0 + e;
@@ -578,14 +583,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     // ------------------------------------------------------------ softmax
     const int grp = warp >> 2, w4 = warp & 3, key = w4 * 32 + lane;
     const uint32_t lanes = static_cast<uint32_t>(w4 * 32) << 16;
-    constexpr int kBlocks = R / 16;
+    constexpr int kBlocks = kFewRows / 16;
     const int gt = tid & 127;
     // A warp whose wait gave up goes on, without further waits, to where its group
     // leaves together.
     bool ok = true, left = false;
     for (; !left && w.more; w = next_item(p, w), ++item) {
       const int at = item & 1;
-      const uint32_t o_col = tmem + lanes + C::kOAt + at * 4 * R, l_col = tmem + lanes + C::kLAt + (at * 2 + grp) * R;
+      const uint32_t o_col = tmem + lanes + C::kOAt + at * 4 * kFewRows, l_col = tmem + lanes + C::kLAt + (at * 2 + grp) * kFewRows;
       const uint32_t j0 = j, j1 = j + static_cast<uint32_t>(w.k1 - w.k0);
       // (Then the item before the last is read from tensor and shared memory, too.)
       ok = ok && all_wait(&bars.prep_full[item & 1], item >> 1);
@@ -613,7 +618,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         // barrier is passed over).
         ok = ok && all_wait(&bars.s_full[j & 3], j >> 2) && (j == 0 || all_wait(&bars.mu[grp ^ 1], (j - 1) >> 1));
         sm100::tc_fence_after();
-        const uint32_t s_col = tmem + lanes + (j & 3) * R;
+        const uint32_t s_col = tmem + lanes + (j & 3) * kFewRows;
         float ks = adt::q8_scale(kbyte);
         int ev = static_cast<int>(vbyte) - 127;
         const bool nan_v = !tree_k && vbyte == 255u;
@@ -682,7 +687,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (!ok && lane == 0) give_up();
           left = grp == 0 ? any_of<3, 128>(!ok) : any_of<4, 128>(!ok);
           if (left) break;
-          if (gt < R) {
+          if (gt < kFewRows) {
             const float y = fmaxf(fmaxf(s_most[grp][0][gt], s_most[grp][1][gt]), fmaxf(s_most[grp][2][gt], s_most[grp][3][gt]));
             const float old = s_base[at][gt], now = y > old + kFewThreshold ? y : old;
             s_base[at][gt] = now;
@@ -697,12 +702,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (j > j0) {
             sm100::tc_fence_after();
 #pragma unroll 1
-            for (int c = 0; c < 4 * R; c += 16) {
+            for (int c = 0; c < 4 * kFewRows; c += 16) {
               uint32_t r[16];
               sm100::tmem_ld_16(o_col + c, r);
 #pragma unroll
               for (int e = 0; e < 16; ++e)
-                r[e] = __float_as_uint(__uint_as_float(r[e]) * s_alpha[grp][(c & (R - 1)) + e]);
+                r[e] = __float_as_uint(__uint_as_float(r[e]) * s_alpha[grp][(c & (kFewRows - 1)) + e]);
               tmem_st_16(o_col + c, r);
             }
             sm100::tmem_wait_st();
@@ -726,7 +731,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           sm100::tmem_wait_st();
           group_sync(grp);
-          if (gt < R) s_gb[at][grp][gt] = s_base[at][gt] - from;
+          if (gt < kFewRows) s_gb[at][grp][gt] = s_base[at][gt] - from;
           fresh = false;
           ver = now;
         }
@@ -778,10 +783,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           tmem_st_16(l_col + 16 * blk, r);
           uint8_t* tile_p = sP + (j % PT) * C::kPBytes;
-          *reinterpret_cast<uint4*>(tile_p + tile_off<4 * R>(key, blk)) = make_uint4(p1[0], p1[1], p1[2], p1[3]);
-          *reinterpret_cast<uint4*>(tile_p + tile_off<4 * R>(key, kBlocks + blk)) = make_uint4(p2[0], p2[1], p2[2], p2[3]);
-          *reinterpret_cast<uint4*>(tile_p + tile_off<4 * R>(key, 2 * kBlocks + blk)) = make_uint4(p3[0], p3[1], p3[2], p3[3]);
-          *reinterpret_cast<uint4*>(tile_p + tile_off<4 * R>(key, 3 * kBlocks + blk)) = make_uint4(p4[0], p4[1], p4[2], p4[3]);
+          *reinterpret_cast<uint4*>(tile_p + tile_off<4 * kFewRows>(key, blk)) = make_uint4(p1[0], p1[1], p1[2], p1[3]);
+          *reinterpret_cast<uint4*>(tile_p + tile_off<4 * kFewRows>(key, kBlocks + blk)) = make_uint4(p2[0], p2[1], p2[2], p2[3]);
+          *reinterpret_cast<uint4*>(tile_p + tile_off<4 * kFewRows>(key, 2 * kBlocks + blk)) = make_uint4(p3[0], p3[1], p3[2], p3[3]);
+          *reinterpret_cast<uint4*>(tile_p + tile_off<4 * kFewRows>(key, 3 * kBlocks + blk)) = make_uint4(p4[0], p4[1], p4[2], p4[3]);
         }
         sm100::fence_proxy_async_smem();
         sm100::tmem_wait_st();

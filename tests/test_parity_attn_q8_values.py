@@ -21,10 +21,10 @@ def _built():
     ensure_built()
 
 
-# Items of up to 16, 32, 64 and 128 rows; whole ones and ones that several thread blocks share.
+# Items of up to 64 and 128 rows, and small ones; whole ones and ones that several thread blocks share.
 MANY = [([40], [300], 2, 2, 64), ([40], [300], 2, 2, 128), ([100], [300], 2, 1, 128), ([33], [5000], 1, 1, 128),
         ([200], [2000], 1, 1, 64)]
-FEW = [([3], [300], 2, 2, 64), ([8], [300], 4, 1, 128), ([4], [5000], 4, 1, 128), ([31], [2000], 1, 1, 64)]
+FEW = [([3], [300], 2, 2, 64), ([16], [300], 1, 1, 128), ([4], [3000], 4, 1, 64), ([8], [300], 4, 1, 128), ([4], [5000], 4, 1, 128), ([31], [2000], 1, 1, 64)]
 
 
 def star(case):
