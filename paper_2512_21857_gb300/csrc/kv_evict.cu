@@ -385,12 +385,6 @@ __global__ void __launch_bounds__(T) kv_evict_kernel(const EvictParams p) {
     for (int r = n + tid; r < p.budget; r += kThreads) idx[r] = -1;
 }
 
-// Whether the byte ranges that two caches of the same shape span overlap.
-bool caches_overlap(const void* a, int64_t na, const void* b, int64_t nb) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return x < y + nb && y < x + na;
-}
-
 template <int T>
 adt_status launch(const EvictParams& p, cudaLaunchConfig_t* cfg, int dev) {
   static unsigned configured[2] = {0u, 0u};  // bit per device (< 64), per instantiation
@@ -423,7 +417,7 @@ adt_status adt_kv_evict(const adt_bf16* k_src, const adt_bf16* v_src, int64_t sr
   ADT_REQUIRE(B >= 1 && B <= 65535 && Hkv >= 1 && Hkv <= 65535 && num_layers >= 1 && num_layers <= 65535);
   ADT_REQUIRE(max_kv >= 1 && max_kv < (1 << 30) && budget >= 1 && budget < (1 << 30) && n_sink >= 0 && n_recent >= 0 &&
               static_cast<int64_t>(n_sink) + n_recent <= budget);
-  ADT_REQUIRE(!kv_len_out || !caches_overlap(kv_len, B * 4ll, kv_len_out, B * 4ll));
+  ADT_REQUIRE(!kv_len_out || !adt::spans_overlap(kv_len, B * 4ll, kv_len_out, B * 4ll));
   if (D != 64 && D != 128) return ADT_ERR_UNSUPPORTED;
   const int64_t keep = max_kv < budget ? max_kv : budget;  // rows that a destination slice holds
   const int64_t counts[3] = {num_layers, B, Hkv};
@@ -450,10 +444,10 @@ adt_status adt_kv_evict(const adt_bf16* k_src, const adt_bf16* v_src, int64_t sr
   };
   const bool in_place = k_src == k_dst && v_src == v_dst && same(ss, ds);
   if (!in_place)
-    ADT_REQUIRE(!caches_overlap(k_src, src_span * 2, k_dst, dst_span * 2) &&
-                !caches_overlap(v_src, src_span * 2, v_dst, dst_span * 2) &&
-                !caches_overlap(k_src, src_span * 2, v_dst, dst_span * 2) &&
-                !caches_overlap(v_src, src_span * 2, k_dst, dst_span * 2));
+    ADT_REQUIRE(!adt::spans_overlap(k_src, src_span * 2, k_dst, dst_span * 2) &&
+                !adt::spans_overlap(v_src, src_span * 2, v_dst, dst_span * 2) &&
+                !adt::spans_overlap(k_src, src_span * 2, v_dst, dst_span * 2) &&
+                !adt::spans_overlap(v_src, src_span * 2, k_dst, dst_span * 2));
   // No two slices that are written share memory, none of K's with one of V's
   // either.  (Both may lie in one allocation, slices of both in turn.)
   const int64_t slice = (in_place ? max_kv : keep) * D;
@@ -461,7 +455,7 @@ adt_status adt_kv_evict(const adt_bf16* k_src, const adt_bf16* v_src, int64_t sr
   ADT_REQUIRE(v_off != 0 && !adt::slices_meet(counts, ds, slice, 0) && !adt::slices_meet(counts, ds, slice, v_off));
   if (score_out) {
     const bool scores_in_place = score_out == score && same(cs, os);
-    ADT_REQUIRE(scores_in_place || !caches_overlap(score, c_span * 4, score_out, o_span * 4));
+    ADT_REQUIRE(scores_in_place || !adt::spans_overlap(score, c_span * 4, score_out, o_span * 4));
     ADT_REQUIRE(!adt::slices_meet(counts, os, scores_in_place ? max_kv : keep, 0));
   }
   const int64_t slices = counts[0] * counts[1] * counts[2];

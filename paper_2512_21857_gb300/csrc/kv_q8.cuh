@@ -21,12 +21,6 @@ struct Q8Strides {
   int64_t cache[3], scale[3];
 };
 
-// Whether the memory that a and b span overlaps.
-inline bool spans_overlap(const void* a, int64_t na, const void* b, int64_t nb) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return x < y + nb && y < x + na;
-}
-
 // Host checks of a pair of 8-bit caches with `rows` rows a slice.  Where `written`
 // no two slices may share memory.  *cache_span and *scale_span: bytes from the
 // first to the last.

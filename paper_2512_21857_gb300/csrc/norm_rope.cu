@@ -29,8 +29,8 @@ using adt::Eight;
 using adt::kMaxRotary;
 using adt::kMaxRows;
 using adt::kMaxSpan;
-using adt::overlap;
 using adt::put;
+using adt::spans_overlap;
 using adt::to_f32;
 using adt::token_angles;
 
@@ -428,7 +428,7 @@ adt_status adt_norm_rope_qkv(const void* q, int64_t ld_q, const void* k, int64_t
       ADT_REQUIRE(wld[x] == 0 || wld[x] >= D);
       ADT_REQUIRE(reinterpret_cast<uintptr_t>(w) % wsize == 0);
       const int64_t bytes = (static_cast<int64_t>(p.heads[x] - 1) * wld[x] + D) * wsize;
-      for (int y = 0; y < 3; ++y) ADT_REQUIRE(!overlap(out[y], out_bytes[y], w, bytes));
+      for (int y = 0; y < 3; ++y) ADT_REQUIRE(!spans_overlap(out[y], out_bytes[y], w, bytes));
       aligned = aligned && adt::aligned16(w) && static_cast<int64_t>(wld[x]) * wsize % 16 == 0;
     }
     p.weight[x] = weight[x];
@@ -439,9 +439,9 @@ adt_status adt_norm_rope_qkv(const void* q, int64_t ld_q, const void* k, int64_t
   // nothing else may overlap.
   for (int x = 0; x < 3; ++x) {
     for (int y = 0; y < 3; ++y) {
-      if (overlap(out[x], out_bytes[x], in[y], in_bytes[y]))
+      if (spans_overlap(out[x], out_bytes[x], in[y], in_bytes[y]))
         ADT_REQUIRE(x == y && out[x] == in[x] && esize == 2 && ld[x] == static_cast<int64_t>(p.heads[x]) * D);
-      ADT_REQUIRE(x == y || !overlap(out[x], out_bytes[x], out[y], out_bytes[y]));
+      ADT_REQUIRE(x == y || !spans_overlap(out[x], out_bytes[x], out[y], out_bytes[y]));
     }
     aligned = aligned && (!in[x] || (adt::aligned16(in[x]) && adt::aligned16(out[x]) && ld[x] * esize % 16 == 0));
   }

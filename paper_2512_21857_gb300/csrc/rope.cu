@@ -28,8 +28,8 @@ using adt::kMaxRotary;
 using adt::kMaxRows;
 using adt::kMaxSpan;
 using adt::kTwoPi;
-using adt::overlap;
 using adt::put;
+using adt::spans_overlap;
 using adt::to_f32;
 using adt::token_angles;
 
@@ -332,9 +332,9 @@ adt_status adt_rope_qkv(const void* q, int64_t ld_q, const void* k, int64_t ld_k
   // first); nothing else may overlap.
   for (int x = 0; x < 3; ++x) {
     for (int y = 0; y < 3; ++y) {
-      if (overlap(out[x], out_bytes[x], in[y], in_bytes[y]))
+      if (spans_overlap(out[x], out_bytes[x], in[y], in_bytes[y]))
         ADT_REQUIRE(x == y && out[x] == in[x] && esize == 2 && ld[x] == static_cast<int64_t>(p.heads[x]) * D);
-      ADT_REQUIRE(x == y || !overlap(out[x], out_bytes[x], out[y], out_bytes[y]));
+      ADT_REQUIRE(x == y || !spans_overlap(out[x], out_bytes[x], out[y], out_bytes[y]));
     }
   }
   p.pos = positions;

@@ -3,6 +3,7 @@
 #pragma once
 
 #include "adt_common.cuh"
+#include "slices.h"
 
 namespace adt {
 
@@ -73,11 +74,6 @@ __device__ __forceinline__ void put(__nv_bfloat16* dst, const float (&x)[8]) {
     w[i] = *reinterpret_cast<const uint32_t*>(&b);
   }
   *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
-}
-
-inline bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return x < y + nb && y < x + na;
 }
 
 }  // namespace adt

@@ -1,10 +1,16 @@
-// Host check of strided outputs (internal, not part of the ABI): whether slices
-// that different CTAs write share memory.
+// Host checks of what calls write (internal, not part of the ABI): whether spans of
+// memory overlap, and whether slices that different CTAs write share memory.
 #pragma once
 
 #include <stdint.h>
 
 namespace adt {
+
+// Whether the memory that a and b span (na and nb bytes) overlaps.
+inline bool spans_overlap(const void* a, int64_t na, const void* b, int64_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + nb && y < x + na;
+}
 
 // Indices differ by less than n[k] in dimension k: whether some differences sum
 // up to a distance within `need` of -x.  For dimensions one within the other, the
