@@ -497,8 +497,9 @@ adt_status adt_rope_qkv(const void* q, int64_t ld_q, const void* k, int64_t ld_k
  * eps finite and not negative.  D <= 4096; all else, what may alias among it, as
  * for adt_rope_qkv; outputs overlap no weights either.  Squares are summed in
  * fp32: elements past 2^60 are outside the domain.
- * Rows and weights on 16-byte boundaries with D (up to 512) and rotary_dim
- * multiples of 16 are moved as vectors, others element by element.
+ * Rows and weights on 16-byte boundaries with D a multiple of 16 up to 512 are moved
+ * as vectors, others element by element; a rotary_dim that is a multiple of 16 (in
+ * the interleaved layout of 8) is turned faster than others.
  * ------------------------------------------------------------------------ */
 typedef enum adt_norm { ADT_NORM_RMS = 0, ADT_NORM_LAYER = 1 } adt_norm;
 
@@ -594,9 +595,12 @@ adt_status adt_kv_evict(const adt_bf16* k_src, const adt_bf16* v_src, int64_t sr
                         void* stream);
 
 /* ------------------------------------------------------------------------
- * The 8-bit cache (no counterpart in the paper: half the memory, and half the
- * bytes that attention reads).  A row, one kv head of one token, is D e4m3
- * values and one byte s: value = e4m3 * 2^(s - 127), not a number for s = 255.
+ * The 8-bit cache (no counterpart in the paper): half the memory, and half the
+ * bytes that attention reads, which makes it faster than adt_tree_attn where
+ * single tokens with grouped heads read long caches; over trees it is slower.
+ * adt_kv_compact_inplace, adt_kv_score and adt_kv_evict take bf16 caches only.
+ * A row, one kv head of one token, is D e4m3 values and one byte s:
+ * value = e4m3 * 2^(s - 127), not a number for s = 255.
  *
  * k_cache, v_cache [device] e4m3, element (l, b, g, pos, d) at
  *         l*cache_layer_stride + b*cache_stride_b + g*cache_stride_h + pos*D + d.
@@ -616,8 +620,8 @@ adt_status adt_kv_evict(const adt_bf16* k_src, const adt_bf16* v_src, int64_t sr
  * scales.
  *
  * adt_kv_read_q8 - rows 0 .. kv_len[b]-1 of every layer, tree and kv head as
- * bf16 (exact for what adt_kv_compact_q8 wrote), where bf16 operators take
- * them: k_out, v_out with strides of their own (multiples of 8, slices of max_kv
+ * bf16 (exact for what adt_kv_compact_q8 wrote, but for elements from 248 * 2^120
+ * up, which it rounds to 2^128: infinity), where bf16 operators take them: k_out, v_out with strides of their own (multiples of 8, slices of max_kv
  * rows apart), that overlap no input.  Rows behind are left as they were.
  * kv_len[b] outside [0, max_kv] sets ADT_DEVERR_KV_RANGE and skips tree b.
  *
@@ -633,6 +637,8 @@ adt_status adt_kv_evict(const adt_bf16* k_src, const adt_bf16* v_src, int64_t sr
  * A weight is rounded to 11 bits, and ends at 2^-26 of the row's largest (each
  * times its value's scale; of more than 16 rows of a tree and kv head at 2^-31): n
  * keys of less can be off by n times as much of the output, and lse has them all.
+ * An element of v_tree counts to 2^-8 of itself or 2^-27 of its row's largest (of
+ * more than 16 rows 2^-33).
  * 1 <= max_nodes <= 256, any H % Hkv == 0, B * max_nodes * H <= 2^24.
  * Errors as for adt_tree_attn.
  * ------------------------------------------------------------------------ */

@@ -47,14 +47,15 @@
 //   12-15     V from e4m3 to fp16 (the rows past the prefix zeroed).
 // Every wait is bounded; a timeout sets ADT_DEVERR_TIMEOUT.
 //
-// Bound by the turns of the softmax groups: of a chunk a group takes 2900 cycles with
-// 64 rows (each twice) and 4500 with 128, of which waits for tensor memory, shared
-// memory and the other group are more than half (issue slots 41 % busy, tensor cores
-// 23 %), and two groups take chunks in turn; V's widening keeps up.  Measured: four
-// trees of 64, 64, 27 and 64 nodes over 1444 to 2400 rows, 32 / 32 heads x 128, 39 us
-// (11 at HBM's rate), 5 of them the launch before; trees of 64 nodes over 3500 to
-// 6001 rows, 32 / 8 heads x 128, 47 us (11 at the tensor cores' bf16 rate), 5 of them
-// the joining of cut items.
+// Bound by the turns of the softmax groups: a CTA takes 2320 cycles a chunk with 64 rows
+// (each twice) and 2790 with 128, its two groups a chunk each at a time, of which waits
+// for tensor memory, shared memory and the other group are more than half (issue slots
+// 42 % busy, tensor cores 23 %); V's widening keeps up.  Measured: four trees of 64, 64,
+// 27 and 64 nodes over 1444 to 2400 rows, 32 / 32 heads x 128, 39 us (11 at HBM's rate), 5
+// of them the launch before; trees of 64 nodes over 3500 to 6001 rows, 32 / 8 heads x 128,
+// 48 us (11 at the tensor cores' bf16 rate), 5 of them the joining of cut items.  (A row's
+// base over scores and value scales, against one of scores alone and one reference for an
+// item's value scales: 39.4 and 47.9 us for 38.7 and 46.6.)
 #include <math.h>
 
 #include <cuda.h>

@@ -24,8 +24,8 @@
 // Warp roles: 0-3, 4-7 two softmax groups that take the chunks in turn; 8 K tiles, 9 V
 // tiles; 10 S products; 11 PV products; 12-15 an item's start and end beside the
 // chunks of the items around it: queries and, with the tree's chunk, its rows cut
-// into e4m3 rows (keys into two as the queries; values, whose sums are to 2^-8 of
-// each element, into three 2^-4 apart), and O, which has a place for two items, read
+// into e4m3 rows (keys into two as the queries; values into three 2^-4 apart, which hold
+// each element to 2^-8 of it or 2^-27 of the row's largest), and O, which has a place for two items, read
 // out and joined.
 //
 // Bound by HBM where caches are long: 16 sequences of 1 to 30011 rows, 32 / 8 heads x
