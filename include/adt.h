@@ -621,8 +621,9 @@ adt_status adt_kv_evict(const adt_bf16* k_src, const adt_bf16* v_src, int64_t sr
  *
  * adt_kv_read_q8 - rows 0 .. kv_len[b]-1 of every layer, tree and kv head as
  * bf16 (exact for what adt_kv_compact_q8 wrote, but for elements from 248 * 2^120
- * up, which it rounds to 2^128: infinity), where bf16 operators take them: k_out, v_out with strides of their own (multiples of 8, slices of max_kv
- * rows apart), that overlap no input.  Rows behind are left as they were.
+ * up, which it rounds to 2^128: infinity), where bf16 operators take them: k_out,
+ * v_out with strides of their own (multiples of 8, slices of max_kv rows apart),
+ * that overlap no input.  Rows behind are left as they were.
  * kv_len[b] outside [0, max_kv] sets ADT_DEVERR_KV_RANGE and skips tree b.
  *
  * adt_tree_attn_q8 - adt_tree_attn over such a prefix, one layer (q, the tree's
